@@ -29,7 +29,10 @@
  * configuration-keyed mask cache, Sec. 4.3), grid_forced_span (jump-forward,
  * Sec. 6.1 step 6), grid_reserve (the token-denominated termination reserve,
  * Sec. 5 Prop. 9) and grid_configs_enable_audit / grid_audit_* (the audit
- * chain, Sec. 6.4).
+ * chain, Sec. 6.4).  The model's side of a step that brings several tokens a
+ * row: grid_kv_append and grid_kv_attend (a chunk through attention over a
+ * paged cache) and grid_draft_verify (drafted tokens against the masked
+ * target distribution).
  *
  * Conventions
  *   - Every call returns 0 (GRID_OK) or a negative GRID_E_* code; the message of
@@ -98,16 +101,22 @@ extern "C" {
                                     /* not byte-complete; impossible with, Prop. 8)   */
 #define GRID_ST_BOUND 5             /* a per-token overlay or reduce-chain bound hit  */
 #define GRID_ST_COMPLETE 6          /* the row accepted EOS; its mask is all zero     */
+#define GRID_ST_PAGES 7             /* a row's chunk does not fit its pages or its    */
+                                    /* positions' table, or a page id is outside the  */
+                                    /* cache                                          */
 
-/* ---- logits dtypes for grid_apply_mask ---- */
+/* ---- dtypes of logits (F32, BF16) and of heads and caches (BF16, F16) ---- */
 #define GRID_DTYPE_F32 0
 #define GRID_DTYPE_BF16 1
+#define GRID_DTYPE_F16 2
 
 typedef struct grid_grammar grid_grammar;
 typedef struct grid_vocab grid_vocab;
 typedef struct grid_spec grid_spec;
 typedef struct grid_configs grid_configs;
 typedef struct grid_cache grid_cache;
+typedef struct grid_kv grid_kv;
+typedef struct grid_drafts grid_drafts;
 
 /* One L3 lexicon: the allowed words W_c of category terminal `category`
  * (Sec. 2, L3).  Word i is words[offsets[i] .. offsets[i+1]); host memory,
@@ -487,6 +496,156 @@ int grid_apply_mask(const uint32_t* d_mask, void* d_logits, int32_t dtype, int32
  * lexicon-trie node of the pending lexeme, and flags (bit 0 = complete). */
 int grid_configs_export(const grid_configs* c, int32_t row, int32_t* stack, int32_t cap,
                         int32_t* depth, int32_t* dfa_state, int32_t* lex_node, int32_t* flags);
+
+/* ---- a chunk of tokens through a model's attention ----
+ * A forced span, a draft, a prompt or one sampled token per row enters the
+ * model as a chunk: B rows of a ragged batch with n_tokens new tokens in all.
+ * Row b's tokens are d_start[b] .. d_start[b+1]-1 of the packed arrays
+ * (d_start[0] = 0, non-decreasing, d_start[B] <= n_tokens; d_start NULL: every
+ * row has n_tokens / B tokens), and its first new token is at position
+ * d_len[b], the number of tokens cached before the chunk (the caller adds the
+ * chunk's lengths after the layers ran).  The paged cache is the caller's
+ * memory: position p of row b is token p % page_size of page
+ * d_table[b * table_stride + p / page_size].  grid_kv_append stores the chunk's
+ * keys and values, grid_kv_attend (same chunk, after the append) attends to
+ * them and to what was cached before.
+ *
+ * Checked on the device, per row: 0 <= d_len, tokens in order and within
+ * n_tokens, chunk within max_pages pages, page ids within the cache (and, in an
+ * append, positions within the rotation's table).  A row that fails gets
+ * GRID_ST_PAGES; an append leaves out its tokens whose own place fails, an
+ * attend writes zeros for the whole row (lse -inf).  Entries of d_table that
+ * no token of the row lies in are not read. */
+typedef struct grid_kv_pages {
+  void *d_k, *d_v;       /* pools of n_pages pages, 16-byte aligned                      */
+  int32_t dtype;         /* GRID_DTYPE_BF16 or GRID_DTYPE_F16, of every head vector here */
+  int32_t head_dim;      /* D = 64 or 128, contiguous                                    */
+  int32_t n_heads;       /* query heads H, a multiple of n_kv_heads: query head h reads  */
+  int32_t n_kv_heads;    /* key head h / (n_heads / n_kv_heads)                          */
+  int32_t page_size;     /* tokens of a page: a power of two in 8 .. 1024                */
+  int32_t n_pages;
+  int64_t k_stride[3];   /* elements from page to page, token to token, head to head:    */
+  int64_t v_stride[3];   /* positive multiples of 8                                      */
+} grid_kv_pages;
+
+typedef struct grid_kv_chunk {
+  const int32_t* d_table; /* [B][table_stride], max_pages entries of a row used          */
+  int64_t table_stride;
+  const int32_t* d_len;   /* [B]                                                         */
+  const int32_t* d_start; /* [B + 1] or NULL                                             */
+  int32_t max_pages, B, n_tokens, reserved;
+} grid_kv_chunk;
+
+/* Head vectors of the chunk: token i, head h at d + i * token_stride + h * head_stride
+ * (elements, multiples of 8; d 16-byte aligned), D contiguous values.  A slice of a
+ * projection's output is one. */
+typedef struct grid_heads {
+  void* d;
+  int64_t token_stride, head_stride;
+} grid_heads;
+
+/* Rotation by position and norm per head, both optional (NULL).  Position p
+ * turns the pair of values (x_i, x_j) to (x_i c - x_j s, x_j c + x_i s) with
+ * c = d_cos[p * rot/2 + m], s = d_sin[...] for m < rot/2, where (i, j) is
+ * (m, m + rot/2), or (2m, 2m + 1) with `pairs`; values from rot on stay.
+ * Tables: fp32, 16-byte aligned, positions 0 .. n_pos-1. */
+typedef struct grid_rotation {
+  const float *d_cos, *d_sin;
+  int32_t n_pos, rot, pairs, reserved; /* rot: a multiple of 16, <= D */
+} grid_rotation;
+
+/* x_d <- x_d w_d / sqrt(mean(x^2) + eps) before the rotation, with the weights
+ * (dtype of the cache, D values, 16-byte aligned) of queries and keys; either
+ * may be NULL. */
+typedef struct grid_head_norm {
+  const void *d_q, *d_k;
+  float eps;
+  int32_t reserved;
+} grid_head_norm;
+
+/* A paged cache and the scratch that attending to it needs (allocates about
+ * 40 MB of device memory and synchronizes).  The pools stay the caller's and
+ * must outlive the handle.  Free with grid_kv_free. */
+int grid_kv_create(const grid_kv_pages* pages, grid_kv** out);
+void grid_kv_free(grid_kv* kv);
+
+/* Store the chunk's keys and values, k normed and rotated on the way; with `q`
+ * (or NULL) its H query heads are normed and rotated into q_out (which may be
+ * q).  Everything is computed in fp32 and rounded once.  k and v must not lie
+ * in the pools.  d_status[b]: GRID_ST_OK or GRID_ST_PAGES.  1 <= B <= 65535;
+ * n_tokens may be 0.  Enqueue only. */
+int grid_kv_append(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_heads* k, const grid_heads* v,
+                   const grid_heads* q, const grid_heads* q_out, const grid_rotation* rot, const grid_head_norm* norm,
+                   int32_t* d_status, void* stream);
+
+typedef struct grid_kv_query {
+  grid_heads q, out;  /* the chunk's n_tokens x H query heads and what they get */
+  float* d_lse;       /* fp32 [n_tokens][H] or NULL                             */
+  float scale;        /* > 0, finite                                            */
+  int32_t reserved;
+} grid_kv_query;
+
+/* out[i][h] = sum_j p_j v_j, p = softmax over the row's positions j up to token
+ * i's own of scale * q[i][h] . k_j; d_lse gets log sum_j exp(scale q . k_j).  Products and sums are held in fp32; the
+ * probabilities are rounded to the cache's type for the product with v.
+ * Values of the pools at positions that no row uses are never part of a
+ * result, whatever their bits; cached keys and values must be finite.
+ * Uses the scratch held by `kv`, so attends on the same handle must not
+ * overlap on the GPU.  d_status as above.  Enqueue only. */
+int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_kv_query* query, int32_t* d_status,
+                   void* stream);
+
+/* ---- verification of drafted tokens ----
+ * Row b has K' = d_draft_len[b] (NULL: K; clipped to 0 .. K) drafted tokens
+ * x_0 .. and the target's logits of K' + 1 positions (position k follows k
+ * accepted tokens).  p_k = softmax(l_k / T_b) over the ids that the mask of
+ * position k admits, q_k the distribution that x_k was drawn from (d_probs;
+ * NULL: x_k was certain, as a forced span's or an n-gram's).  x_k is accepted
+ * when u_k q_k(x_k) < p_k(x_k), in order, up to the first refusal.  The token
+ * after the n accepted ones is drawn by the given noise e: the first largest
+ * w_i / e_i over the admitted ids, with w = max(p_n - q_n, 0) after a refusal
+ * (p_n where no score is above zero) and w = p_n when all were accepted; with u uniform
+ * in [0, 1) and e exponential the tokens are distributed as the target's own.
+ * T_b <= 0 is greedy: x_k is accepted when it is the first largest admitted
+ * logit, and that is the token drawn.  K = 0 samples one token per row.
+ *
+ * An id outside 0 .. V-1 or the mask is refused (p = 0).  NaN logits count as
+ * -inf; +inf as the largest finite value.  Noise that is not positive leaves
+ * its id out of the draw (where nothing is left: the first largest logit).  A
+ * position that is reached and admits no id ends the row there: no token is
+ * drawn and d_status[b] = GRID_ST_EMPTY_MASK.  An accepted or drawn `eos` ends
+ * the row too, with GRID_ST_COMPLETE. */
+typedef struct grid_draft_step {
+  const void* d_logits;         /* dtype; row b, position k at + b*logit_stride[0] + k*logit_stride[1] */
+  int64_t logit_stride[2];
+  const uint32_t* d_mask;       /* mask words as grid_masks writes them, or NULL: every id             */
+  int64_t mask_stride[2];       /* words, row and position: [K+1][B][W] as well as [B][K+1][W]         */
+  const float* d_probs;         /* [B][K][V] by strides, or NULL                                       */
+  int64_t prob_stride[2];
+  const int32_t* d_draft;       /* [B][K]                                                              */
+  const int32_t* d_draft_len;   /* [B] or NULL                                                         */
+  const float* d_u;             /* [B][K]                                                              */
+  const float* d_noise;         /* [B] rows of V, noise_stride apart                                   */
+  int64_t noise_stride;
+  const float* d_temperature;   /* [B] or NULL: 1                                                      */
+  int32_t dtype, B, K, V;       /* V ids, B and K within the handle's                                  */
+  int32_t eos, reserved;        /* -1: none                                                            */
+  int32_t* d_tokens;            /* out [B][K+1]: the accepted ids, the drawn one, then -1 (grid_advance */
+                                /* takes them as they are)                                             */
+  int32_t* d_accepted;          /* out [B]: how many drafted tokens were accepted                      */
+  float* d_logprob;             /* out [B][K+1] or NULL: log p_k of each token (T <= 0: of T = 1), 0 after them */
+  int32_t* d_status;            /* out [B]                                                             */
+} grid_draft_step;
+
+/* Scratch for verifications of up to B rows of K drafted tokens over V ids
+ * (1 <= B <= 65535, 0 <= K <= 64).  Allocates device memory and synchronizes.
+ * Free with grid_drafts_free. */
+int grid_drafts_create(int32_t B, int32_t K, int32_t V, grid_drafts** out);
+void grid_drafts_free(grid_drafts* d);
+
+/* Verify one step's drafts.  Uses the scratch held by `d`, so calls on the
+ * same handle must not overlap on the GPU.  Enqueue only. */
+int grid_draft_verify(const grid_drafts* d, const grid_draft_step* step, void* stream);
 
 #ifdef __cplusplus
 }

@@ -16,10 +16,10 @@ from .build import library_path
 
 GRID_OK = 0
 GRID_ST = {0: "OK", 1: "NONVIABLE", 2: "STACK_OVERFLOW", 3: "TOKEN_NOT_ALLOWED",
-           4: "EMPTY_MASK", 5: "BOUND", 6: "COMPLETE"}
+           4: "EMPTY_MASK", 5: "BOUND", 6: "COMPLETE", 7: "PAGES"}
 GRID_ST_OK, GRID_ST_NONVIABLE, GRID_ST_STACK_OVERFLOW, GRID_ST_TOKEN_NOT_ALLOWED = 0, 1, 2, 3
-GRID_ST_EMPTY_MASK, GRID_ST_BOUND, GRID_ST_COMPLETE = 4, 5, 6
-GRID_DTYPE_F32, GRID_DTYPE_BF16 = 0, 1
+GRID_ST_EMPTY_MASK, GRID_ST_BOUND, GRID_ST_COMPLETE, GRID_ST_PAGES = 4, 5, 6, 7
+GRID_DTYPE_F32, GRID_DTYPE_BF16, GRID_DTYPE_F16 = 0, 1, 2
 
 EXPORTED = ["grid_last_error", "grid_compile", "grid_grammar_free", "grid_grammar_info", "grid_grammar_lexicon_trie",
             "grid_load_vocab", "grid_vocab_free", "grid_vocab_info", "grid_specialize",
@@ -27,7 +27,8 @@ EXPORTED = ["grid_last_error", "grid_compile", "grid_grammar_free", "grid_gramma
             "grid_advance", "grid_masks", "grid_masks_apply", "grid_advance_masks", "grid_configs_set_events", "grid_spec_set_work_counters", "grid_masks_static", "grid_forced_span",
             "grid_reserve", "grid_cache_create", "grid_cache_free", "grid_cache_clear", "grid_cache_stats",
             "grid_masks_cached", "grid_configs_enable_audit", "grid_audit_append", "grid_audit_seal", "grid_audit_head", "grid_audit_verify",
-            "grid_audit_genesis", "grid_blake2b", "grid_fingerprint", "grid_apply_mask", "grid_configs_export"]
+            "grid_audit_genesis", "grid_blake2b", "grid_fingerprint", "grid_apply_mask", "grid_configs_export",
+            "grid_kv_create", "grid_kv_append", "grid_kv_attend", "grid_drafts_create", "grid_draft_verify"]
 
 
 class GridLibraryMissing(RuntimeError):
@@ -47,6 +48,45 @@ class _Lexicon(ctypes.Structure):
 
 class _Options(ctypes.Structure):
     _fields_ = [("max_depth", ctypes.c_int32), ("reserved", ctypes.c_int32 * 7)]
+
+
+def _fields(**kinds):
+    P, I32, I64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+    ty = {"p": P, "i": I32, "l": I64, "f": ctypes.c_float, "l2": I64 * 2, "l3": I64 * 3}
+    return [(name, ty[kind]) for name, kind in kinds.items()]
+
+
+class _KvPages(ctypes.Structure):
+    _fields_ = _fields(d_k="p", d_v="p", dtype="i", head_dim="i", n_heads="i", n_kv_heads="i", page_size="i", n_pages="i",
+                       k_stride="l3", v_stride="l3")
+
+
+class _KvChunk(ctypes.Structure):
+    _fields_ = _fields(d_table="p", table_stride="l", d_len="p", d_start="p", max_pages="i", B="i", n_tokens="i",
+                       reserved="i")
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = _fields(d="p", token_stride="l", head_stride="l")
+
+
+class _KvQuery(ctypes.Structure):
+    _fields_ = [("q", _Heads), ("out", _Heads)] + _fields(d_lse="p", scale="f", reserved="i")
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = _fields(d_cos="p", d_sin="p", n_pos="i", rot="i", pairs="i", reserved="i")
+
+
+class _HeadNorm(ctypes.Structure):
+    _fields_ = _fields(d_q="p", d_k="p", eps="f", reserved="i")
+
+
+class _DraftStep(ctypes.Structure):
+    _fields_ = _fields(d_logits="p", logit_stride="l2", d_mask="p", mask_stride="l2", d_probs="p", prob_stride="l2",
+                       d_draft="p", d_draft_len="p", d_u="p", d_noise="p", noise_stride="l", d_temperature="p", dtype="i",
+                       B="i", K="i", V="i", eos="i", reserved="i", d_tokens="p", d_accepted="p", d_logprob="p",
+                       d_status="p")
 
 
 _lib = None
@@ -101,6 +141,13 @@ def lib():
         "grid_masks_static": (I32, [P, P, P, P, P, P, I32, I32, P, P, P]),
         "grid_apply_mask": (I32, [P, P, I32, I32, I32, I64, P]),
         "grid_configs_export": (I32, [P, I32, P, I32, P, P, P, P]),
+        "grid_kv_create": (I32, [P, ctypes.POINTER(P)]),
+        "grid_kv_free": (None, [P]),
+        "grid_kv_append": (I32, [P, P, P, P, P, P, P, P, P, P]),
+        "grid_kv_attend": (I32, [P, P, P, P, P]),
+        "grid_drafts_create": (I32, [I32, I32, I32, ctypes.POINTER(P)]),
+        "grid_drafts_free": (None, [P]),
+        "grid_draft_verify": (I32, [P, P, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -501,6 +548,150 @@ def grid_configs_export(cfg, row: int, cap: int = 1 << 16):
                                      ctypes.byref(lx), ctypes.byref(fl)))
     return dict(stack=list(stack[:min(d.value, cap)]), depth=d.value, dfa_state=q.value,
                 lex_node=lx.value, flags=fl.value)
+
+
+# ---------------------------------------------------------------------------
+def _heads(x, kv, N, H):
+    """A [tokens, heads, D] tensor (any strides, D contiguous) as a grid_heads."""
+    shape, stride = x.shape, x.stride()
+    assert x.is_cuda and x.dtype == kv.dtype and shape == (N, H, kv.D) and stride[2] == 1, \
+        "CUDA tensor [tokens, heads, D] of the cache's type expected, D contiguous"
+    return _Heads(x.data_ptr(), stride[0], stride[1])
+
+
+def _chunk(table, lens, start, status, N):
+    import torch
+    i32, B = torch.int32, lens.shape[0]
+    assert table.dtype == i32 and lens.dtype == i32 and status.dtype == i32, "int32 table, lens and status expected"
+    assert table.is_cuda and lens.is_cuda and status.is_cuda and table.dim() == 2 and table.stride(1) == 1
+    assert table.shape[0] == B and lens.is_contiguous() and status.is_contiguous() and status.shape == (B,), \
+        "table [B, max_pages], lens [B] and status [B] expected"
+    if start is not None:
+        assert start.dtype == i32 and start.is_cuda and start.is_contiguous() and start.shape == (B + 1,), \
+            "int32 start [B + 1] expected"
+        start = start.data_ptr()
+    return _KvChunk(table.data_ptr(), table.stride(0), lens.data_ptr(), start, table.shape[1], B, N, 0)
+
+
+def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None, cos=None, sin=None, pairs=False,
+                   q_norm=None, k_norm=None, eps=1e-6, stream=None):
+    """Store a chunk's keys and values in the paged cache ``kv`` (a PagedKV).
+    k, v [tokens, kv heads, D] (slices of a projection's output, say); table
+    int32 [B, max_pages], lens int32 [B] (tokens cached before the chunk),
+    start int32 [B + 1] (None: the same number of tokens per row); q and q_out
+    [tokens, heads, D]; cos, sin float32 [positions, rot / 2]; norm weights [D]."""
+    import torch
+    N = k.shape[0]
+    chunk = _chunk(table, lens, start, status, N)
+    kh, vh = _heads(k, kv, N, kv.kv_heads), _heads(v, kv, N, kv.kv_heads)
+    qh = oh = rot = norm = None
+    assert (q is None) == (q_out is None), "q and q_out go together"
+    if q is not None:
+        qh, oh = ctypes.byref(_heads(q, kv, N, kv.heads)), ctypes.byref(_heads(q_out, kv, N, kv.heads))
+    assert (cos is None) == (sin is None), "cos and sin go together"
+    if cos is not None:
+        assert cos.dtype == torch.float32 and sin.dtype == torch.float32 and cos.is_cuda and sin.is_cuda and \
+            cos.is_contiguous() and sin.is_contiguous() and cos.dim() == 2 and cos.shape == sin.shape, \
+            "contiguous float32 CUDA tensors [positions, rot / 2] expected"
+        rot = ctypes.byref(_Rotation(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], pairs, 0))
+    if q_norm is not None or k_norm is not None:
+        for w in (q_norm, k_norm):
+            assert w is None or (w.is_cuda and w.dtype == kv.dtype and w.shape == (kv.D,) and w.is_contiguous()), \
+                "norm weights [D] of the cache's type expected"
+        norm = ctypes.byref(_HeadNorm(None if q_norm is None else q_norm.data_ptr(),
+                                      None if k_norm is None else k_norm.data_ptr(), eps, 0))
+    _check(lib().grid_kv_append(kv.h, ctypes.byref(chunk), ctypes.byref(kh), ctypes.byref(vh), qh, oh, rot, norm,
+                                status.data_ptr(), _stream(stream)))
+
+
+def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=None, stream=None):
+    """Attention of a chunk over the paged cache, after its append (table, lens
+    and start as there): q, out [tokens, heads, D], lse float32 [tokens, heads];
+    scale defaults to 1 / sqrt(D)."""
+    N = q.shape[0]
+    chunk = _chunk(table, lens, start, status, N)
+    if lse is not None:
+        import torch
+        assert lse.dtype == torch.float32 and lse.is_cuda and lse.is_contiguous() and lse.shape == (N, kv.heads), \
+            "float32 lse [tokens, heads] expected"
+        lse = lse.data_ptr()
+    query = _KvQuery(_heads(q, kv, N, kv.heads), _heads(out, kv, N, kv.heads), lse,
+                     kv.D ** -0.5 if scale is None else scale, 0)
+    _check(lib().grid_kv_attend(kv.h, ctypes.byref(chunk), ctypes.byref(query), status.data_ptr(), _stream(stream)))
+
+
+class PagedKV:
+    """A paged key/value cache: pools [pages, page_size, kv heads, D] (any
+    strides, D contiguous; bfloat16 or float16) read by ``heads`` query heads.
+    The pools stay the caller's tensors and are kept alive."""
+
+    def __init__(self, k_pages, v_pages, heads: int):
+        import torch
+        assert k_pages.is_cuda and v_pages.is_cuda and k_pages.dim() == 4 and k_pages.shape == v_pages.shape and \
+            k_pages.dtype == v_pages.dtype and k_pages.stride(3) == v_pages.stride(3) == 1, \
+            "two CUDA tensors [pages, page_size, kv heads, D] expected, D contiguous"
+        dt = {torch.bfloat16: GRID_DTYPE_BF16, torch.float16: GRID_DTYPE_F16}[k_pages.dtype]
+        n, page, self.kv_heads, self.D = k_pages.shape
+        self.heads, self.dtype, self.pools = heads, k_pages.dtype, (k_pages, v_pages)
+        p = _KvPages(k_pages.data_ptr(), v_pages.data_ptr(), dt, self.D, heads, self.kv_heads, page, n,
+                     k_pages.stride()[:3], v_pages.stride()[:3])
+        out = ctypes.c_void_p()
+        _check(lib().grid_kv_create(ctypes.byref(p), ctypes.byref(out)))
+        self.h = out
+
+    def __del__(self):
+        if getattr(self, "h", None) and _lib is not None:
+            _lib.grid_kv_free(self.h)
+            self.h = None
+
+
+def grid_draft_verify(drafts, logits, draft, u, noise, tokens, accepted, status, mask=None, probs=None, draft_len=None,
+                      temperature=None, logprob=None, eos=-1, stream=None):
+    """Verify drafted tokens: logits float32 or bfloat16 [B, K + 1, V], draft
+    int32 [B, K], u float32 [B, K], noise float32 [B, V]; mask int32
+    [B, K + 1, W], probs float32 [B, K, V], draft_len int32 [B], temperature
+    float32 [B] may be None; logits, mask, probs and noise may be strided (the
+    last axis contiguous).  Out: tokens int32 [B, K + 1], accepted and status
+    int32 [B], logprob float32 [B, K + 1] or None.  ``drafts``: a Drafts."""
+    import torch
+    f32, i32 = torch.float32, torch.int32
+    B, K1, V = logits.shape
+    K = K1 - 1
+    dt = {f32: GRID_DTYPE_F32, torch.bfloat16: GRID_DTYPE_BF16}[logits.dtype]
+
+    def dense(x, dtype, *shape):
+        assert x.dtype == dtype and x.is_cuda and x.shape == shape and x.is_contiguous(), \
+            "contiguous %s CUDA tensor %s expected" % (dtype, list(shape))
+        return x.data_ptr()
+
+    def rows(x, dtype, *shape):
+        assert x.dtype == dtype and x.is_cuda and x.shape == shape and (x.stride(-1) == 1 or shape[-1] == 1), \
+            "%s CUDA tensor %s expected, the last axis contiguous" % (dtype, list(shape))
+        return x.data_ptr(), x.stride()[:-1]
+
+    lp, ls = rows(logits, logits.dtype, B, K1, V)
+    np_, ns = rows(noise, f32, B, V)
+    mp, ms = (None, (0, 0)) if mask is None else rows(mask, i32, B, K1, (V + 31) // 32)
+    pp, ps = (None, (0, 0)) if probs is None or K == 0 else rows(probs, f32, B, K, V)
+    step = _DraftStep(lp, ls, mp, ms, pp, ps, dense(draft, i32, B, K), None if draft_len is None else dense(draft_len, i32, B),
+                      dense(u, f32, B, K), np_, ns[0], None if temperature is None else dense(temperature, f32, B), dt, B, K,
+                      V, eos, 0, dense(tokens, i32, B, K1), dense(accepted, i32, B),
+                      None if logprob is None else dense(logprob, f32, B, K1), dense(status, i32, B))
+    _check(lib().grid_draft_verify(drafts.h, ctypes.byref(step), _stream(stream)))
+
+
+class Drafts:
+    """Scratch for verifications of up to B rows of K drafted tokens over V ids."""
+
+    def __init__(self, B: int, K: int, V: int):
+        out = ctypes.c_void_p()
+        _check(lib().grid_drafts_create(B, K, V, ctypes.byref(out)))
+        self.h = out
+
+    def __del__(self):
+        if getattr(self, "h", None) and _lib is not None:
+            _lib.grid_drafts_free(self.h)
+            self.h = None
 
 
 # ---------------------------------------------------------------------------
