@@ -8,7 +8,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "_build")
-SOURCES = ["grid_host.cpp", "grid_kernels.cu", "grid_span.cu", "grid_audit.cu", "grid_kv.cu", "grid_draft.cu"]
+SOURCES = ["grid_host.cpp", "grid_kernels.cu", "grid_span.cu", "grid_audit.cu", "grid_kv.cu", "grid_attend.cu",
+           "grid_draft.cu"]
 NVCC = os.environ.get("NVCC", "nvcc")
 FLAGS = ["-gencode", "arch=compute_103a,code=sm_103a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC", "-Xcompiler", "-O2"]

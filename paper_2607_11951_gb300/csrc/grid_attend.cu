@@ -1,0 +1,810 @@
+// Attention of a chunk of new tokens over a paged cache (grid_kv_attend).
+//
+// out = sum_j p_j v_j with p = softmax(scale q k_j) over a token's visible
+// positions, in one pass over the keys: a tile of 128 keys gives scores
+// S = Q K^T (tensor cores, fp32), each query row keeps its maximum m and sum l
+// in fp32, P = exp2((S - m) scale log2 e) is rounded to the cache's type for
+// O += P V (tensor cores, fp32), and O and l are rescaled when m grows.
+//
+// Work.  The query rows of a row b and key head h are its tokens times the
+// H / Hk heads that read h (row = token * group + head), so that a key tile is
+// read once for all of them.  A unit is 256 such rows, or all of them where
+// there are at most 128, with the key tiles they can see.  The tiles of all
+// units, one after the other, are cut into equal runs, one per block: a block
+// takes the end of one unit, some whole ones and the beginning of another.  The
+// pieces of a unit that was cut are joined by the block that finishes last, in
+// the order of the keys whatever the order of the blocks.
+//
+// A block runs two streams of tiles side by side, each with its scores, output
+// rows and four softmax warps, so that the tensor cores work on one stream
+// while the other takes its exponentials.  With 256 rows the streams are the
+// two halves of the rows and share the key tiles; with up to 128 they take the
+// even and the odd tiles of the same rows and are merged at the end.
+#include <dlfcn.h>
+
+#include <cmath>
+
+#include "grid_kv.cuh"
+
+namespace grid {
+namespace {
+
+constexpr int kTile = 128;            // keys of a tile, query rows of a stream
+constexpr int kSoftWarps = 8;         // four per stream
+constexpr int kThreads = (kSoftWarps + 2) * 32;  // and one that loads, one that multiplies
+constexpr int kLoadWarp = kSoftWarps, kMmaWarp = kSoftWarps + 1;
+constexpr int kRing = 8;              // pieces whose bad-page flags are kept at once
+constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+
+struct AttendArgs {
+  Chunk c;
+  const void* q;
+  void* out;
+  float* lse;
+  long long qs[2], os[2];
+  int H, Hk, group;
+  float scale;
+  int32_t* status;
+  float4* parts;    // [2 blocks][D / 4][256 rows]
+  float2* part_ml;  // [2 blocks][256 rows]: maximum (in exponents of two) and sum
+  int* joined;      // [blocks]
+};
+
+// ---------------------------------------------------------------------------
+// what has no C++ name
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(uint64_t* b, int n) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_at(b)), "r"(n) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t* b) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_at(b)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t* b, int bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t* b, int parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok)
+      : "r"(smem_at(b)), "r"(parity)
+      : "memory");
+  return ok;
+}
+// Waits for a phase, for two seconds' clocks at most or until another warp
+// gave up; false then.  Whole warps wait, and leave together.
+__device__ __forceinline__ bool bar_wait(uint64_t* b, int parity, volatile int* gave_up) {
+  bool ok = bar_try(b, parity);
+  if (!ok) {
+    const long long t0 = clock64();
+    while (!(ok = bar_try(b, parity)) && !*gave_up)
+      if (clock64() - t0 > 4000000000LL) *gave_up = 1;
+  }
+  return __all_sync(~0u, ok);
+}
+__device__ __forceinline__ void load_tile(const CUtensorMap* m, uint32_t dst, uint64_t* bar, int x, int token, int head,
+                                          int page) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(
+          dst),
+      "l"(m), "r"(smem_at(bar)), "r"(x), "r"(token), "r"(head), "r"(page)
+      : "memory");
+}
+__device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tm_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tm_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tm_commit(uint64_t* b) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(b)) : "memory");
+}
+// D += A B^T, A and B in shared memory
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a),
+      "l"(b), "r"(what), "r"((uint32_t)add)
+      : "memory");
+}
+// D += A B, A in tensor memory
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a),
+      "l"(b), "r"(what), "r"((uint32_t)add)
+      : "memory");
+}
+#define O8(x, i) \
+  "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
+#define U8(x, i) \
+  "+r"(x[i]), "+r"(x[i + 1]), "+r"(x[i + 2]), "+r"(x[i + 3]), "+r"(x[i + 4]), "+r"(x[i + 5]), "+r"(x[i + 6]), "+r"(x[i + 7])
+#define I8(x, i) \
+  "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
+// 32 columns of this thread's row of tensor memory
+__device__ __forceinline__ void tm_load32(uint32_t at, uint32_t* x) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : O8(x, 0), O8(x, 8), O8(x, 16), O8(x, 24)
+      : "r"(at));
+}
+__device__ __forceinline__ void tm_store32(uint32_t at, const uint32_t* x) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::I8(x, 0),
+      I8(x, 8), I8(x, 16), I8(x, 24), "r"(at)
+      : "memory");
+}
+__device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t* x) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::I8(
+          x, 0),
+      I8(x, 8), "r"(at)
+      : "memory");
+}
+// (the registers are named, so that nothing uses them before the wait)
+__device__ __forceinline__ void tm_loaded(uint32_t* x) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : U8(x, 0), U8(x, 8), U8(x, 16), U8(x, 24) : : "memory");
+}
+__device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Shared memory operand of 128-byte swizzled lines of 64 values: 8 lines are
+// 1,024 bytes (the stride); `chunk` is the distance between the column halves
+// where the lines run along the output's columns (V), unused where they run
+// along the sum (Q, K).
+__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t chunk) {
+  return (uint64_t)((at >> 4) & 0x3FFF) | (uint64_t)((chunk >> 4) & 0x3FFF) << 16 | (uint64_t)(1024 >> 4) << 32 |
+         (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// fp32 accumulators, both operands of type T, 128 rows, n columns; b_rows: B's
+// lines run along the columns
+template <typename T>
+__device__ __forceinline__ uint32_t what_mma(int n, bool b_rows) {
+  const uint32_t t = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+  return 1u << 4 | t << 7 | t << 10 | (b_rows ? 1u << 16 : 0u) | (uint32_t)(n / 8) << 17 | (uint32_t)(kTile / 16) << 24;
+}
+
+// ---------------------------------------------------------------------------
+// the units of the batch, one after the other
+struct Units {
+  int b, a, n, len, rows;  // row, its first token, tokens, cached tokens, query rows per key head
+  int units, h, qt;        // units per key head; the current one
+  int tiles;               // key tiles of the current unit
+  long long at;            // the tile that it begins at
+};
+
+__device__ __forceinline__ int tiles_of(const Units& u, int group, int qt) {
+  const int last = min(u.rows, (qt + 1) * 256) - 1;  // its last query row
+  return (u.len + last / group + kTile) / kTile;
+}
+__device__ __forceinline__ bool open_row(const AttendArgs& g, Units& u, int b) {
+  u.b = b;
+  if (!row_span(g.c, b, u.a, u.n, u.len) || u.n == 0) return false;
+  u.rows = u.n * g.group;
+  u.units = u.rows <= kTile ? 1 : (u.rows + 255) / 256;
+  return true;
+}
+__device__ __forceinline__ long long head_tiles(const AttendArgs& g, const Units& u) {
+  long long t = 0;
+  for (int i = 0; i < u.units; ++i) t += tiles_of(u, g.group, i);
+  return t;
+}
+// The unit that tile `at` lies in; row b's first tile is `first`.
+__device__ __forceinline__ void find_unit(const AttendArgs& g, Units& u, int b, long long first, long long at) {
+  open_row(g, u, b);
+  const long long per = head_tiles(g, u);
+  u.h = (int)((at - first) / per);
+  u.at = first + u.h * per;
+  for (u.qt = 0;; ++u.qt) {
+    u.tiles = tiles_of(u, g.group, u.qt);
+    if (at < u.at + u.tiles || u.qt + 1 == u.units) break;
+    u.at += u.tiles;
+  }
+}
+__device__ __forceinline__ void next_unit(const AttendArgs& g, Units& u) {
+  u.at += u.tiles;
+  if (++u.qt == u.units) {
+    u.qt = 0;
+    if (++u.h == g.Hk) {
+      u.h = 0;
+      while (u.b + 1 < g.c.B && !open_row(g, u, u.b + 1)) {
+      }
+    }
+  }
+  u.tiles = tiles_of(u, g.group, u.qt);
+}
+
+struct Cut {  // of `total` tiles into runs: block i takes [total i / runs, total (i + 1) / runs)
+  long long total;
+  int runs;
+  __device__ long long begin(int i) const { return total * i / runs; }
+  __device__ int run_of(long long tile) const { return (int)(((tile + 1) * runs + total - 1) / total) - 1; }
+};
+
+// One block's part of one unit.
+struct Piece {
+  bool wide;     // 256 rows: the streams share the tiles; else even and odd tiles
+  int t0, t1;    // key tiles
+  int n[2];      // tiles of each stream
+  int r0;        // first query row
+};
+__device__ __forceinline__ Piece piece_of(const Units& u, long long lo, long long hi) {
+  Piece p;
+  p.t0 = (int)(max(lo, u.at) - u.at);
+  p.t1 = (int)(min(hi, u.at + u.tiles) - u.at);
+  p.wide = u.rows > kTile;
+  p.r0 = u.qt * 256;
+  const int n = p.t1 - p.t0;
+  p.n[0] = p.wide ? n : (n + 1) / 2;
+  p.n[1] = p.wide ? (u.rows - p.r0 > kTile ? n : 0) : n / 2;
+  return p;
+}
+
+template <int D>
+struct Layout {
+  static constexpr int kTileBytes = kTile * D * 2;
+  static constexpr int kStages = D == 128 ? 5 : 10;
+  static constexpr int kTiles = 2 * kTileBytes + kStages * kTileBytes;
+  static constexpr uint32_t kS = 0, kO = 256;                 // columns of tensor memory: scores, outputs,
+  static constexpr uint32_t kP = D == 128 ? 0 : 256 + 2 * D;  // probabilities (over the scores where all columns are taken)
+  static constexpr uint32_t kPStep = D == 128 ? 128 : 64;
+};
+
+struct Shared {
+  uint64_t full[10], empty[10];
+  uint64_t q_ready[2], s_ready[2], p_ready[2], o_ready[2], all;
+  float2 ml[2][kTile];
+  long long sums[kThreads / 32];
+  long long first;
+  int row, gave_up, last, bad[kRing];
+  uint32_t tmem;
+};
+
+constexpr int kSharedRoom = 3072;  // in front of the tiles, which begin on 1,024 bytes
+
+template <int D>
+constexpr size_t smem_bytes() {
+  static_assert(sizeof(Shared) <= kSharedRoom);
+  return kSharedRoom + Layout<D>::kTiles;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_attend(const AttendArgs g, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+  using L = Layout<D>;
+  extern __shared__ __align__(1024) uint8_t raw[];
+  Shared& sh = *reinterpret_cast<Shared*>(raw);
+  uint8_t* tiles = raw + kSharedRoom;
+  const uint32_t q_at = smem_at(tiles), ring = q_at + 2 * L::kTileBytes;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const Chunk& c = g.c;
+  if (tid == 0) {
+    for (int i = 0; i < L::kStages; ++i) {
+      bar_init(&sh.full[i], 1);
+      bar_init(&sh.empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      bar_init(&sh.q_ready[i], 4);
+      bar_init(&sh.s_ready[i], 1);
+      bar_init(&sh.p_ready[i], 4);
+      bar_init(&sh.o_ready[i], 1);
+    }
+    bar_init(&sh.all, kSoftWarps);
+    sh.gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  pdl_wait();
+
+  // How many tiles there are in all, and the row that this block begins in.
+  Cut cut;
+  {
+    const int per = (c.B + kThreads - 1) / kThreads;
+    Units u;
+    long long mine = 0;
+    for (int b = tid * per; b < min(c.B, (tid + 1) * per); ++b)
+      if (open_row(g, u, b)) mine += head_tiles(g, u) * g.Hk;
+    long long pre = mine;
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long x = __shfl_up_sync(~0u, pre, o);
+      if (lane >= o) pre += x;
+    }
+    if (lane == 31) sh.sums[warp] = pre;
+    __syncthreads();
+    cut.total = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) pre += sh.sums[w];
+      cut.total += sh.sums[w];
+    }
+    pre -= mine;
+    cut.runs = (int)min((long long)gridDim.x, (cut.total + 1) / 2);
+    if ((int)blockIdx.x < cut.runs) {
+      const long long lo = cut.begin(blockIdx.x);
+      if (pre <= lo && lo < pre + mine)
+        for (int b = tid * per; b < min(c.B, (tid + 1) * per); ++b) {
+          const long long t = open_row(g, u, b) ? head_tiles(g, u) * g.Hk : 0;
+          if (lo < pre + t) {
+            sh.row = b;
+            sh.first = pre;
+            break;
+          }
+          pre += t;
+        }
+    }
+  }
+  const bool works = (int)blockIdx.x < cut.runs;
+  if (works && warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_at(&sh.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    tm_before();
+  }
+  __syncthreads();
+  tm_after();
+  const uint32_t tmem = works ? sh.tmem : 0;
+  const long long lo = works ? cut.begin(blockIdx.x) : 0, hi = works ? cut.begin(blockIdx.x + 1) : 0;
+  volatile int* gave_up = &sh.gave_up;
+  Units u;
+  if (works) find_unit(g, u, sh.row, sh.first, lo);
+
+  if (warp == kLoadWarp) {
+    // ---- one warp keeps the ring of tiles full: a lane per page
+    int it = 0;
+    if (works) {
+      const int box = min(kTile, 1 << c.log_page), pages = kTile / box;
+      bool ok = true;
+      for (int k = 0; ok && u.at < hi; ++k) {
+        const Piece p = piece_of(u, lo, hi);
+        const int used = (u.len + u.n + (1 << c.log_page) - 1) >> c.log_page;  // pages of the row
+        int* bad = &sh.bad[k % kRing];
+        if (lane == 0) *bad = 0;
+        __syncwarp();
+        auto load = [&](int t, bool v) {
+          const int st = it % L::kStages, token = t * kTile + lane * box, pg = token >> c.log_page;
+          int page = c.n_pages;  // (one past the pool: the tile's part is filled with zeros)
+          if (lane < pages && pg < used) {
+            page = c.table[u.b * c.table_stride + pg];
+            if (page < 0 || page >= c.n_pages) {
+              page = c.n_pages;
+              *bad = 1;
+            }
+          }
+          if (!bar_wait(&sh.empty[st], ((it / L::kStages) & 1) ^ 1, gave_up)) return false;
+          if (lane == 0) bar_expect(&sh.full[st], L::kTileBytes);
+          __syncwarp();
+          if (lane < pages)
+            for (int x = 0; x < D / 64; ++x)
+              load_tile(v ? &v_map : &k_map, ring + st * L::kTileBytes + x * (kTile * 128) + lane * box * 128, &sh.full[st],
+                        x * 64, token & ((1 << c.log_page) - 1), u.h, page);
+          ++it;
+          return true;
+        };
+        if (p.wide) {
+          for (int t = p.t0; ok && t < p.t1; ++t) ok = load(t, false) && load(t, true);
+        } else {
+          ok = load(p.t0, false) && (p.t0 + 1 >= p.t1 || load(p.t0 + 1, false));
+          for (int t = p.t0; ok && t < p.t1; ++t) ok = load(t, true) && (t + 2 >= p.t1 || load(t + 2, false));
+        }
+        next_unit(g, u);
+      }
+    }
+    // ---- then reports the rows, and zeros those that are not in order
+    for (int b = blockIdx.x; b < c.B; b += gridDim.x) {
+      int a, n, len;
+      bool good = row_span(c, b, a, n, len);
+      if (good && n)
+        for (int p = lane; p <= (len + n - 1) >> c.log_page; p += 32) good = good && page_of(c, b, p << c.log_page) >= 0;
+      good = __all_sync(~0u, good);
+      if (lane == 0) g.status[b] = good ? GRID_ST_OK : GRID_ST_PAGES;
+      if (!row_span(c, b, a, n, len)) {
+        const int from = max(0, a), to = (int)min((long long)c.N, (long long)a + n);
+        for (long long i = (long long)from * g.H; i < (long long)to * g.H; ++i) {
+          const long long tok = i / g.H, h = i % g.H;
+          for (int x = lane; x < D / 8; x += 32)
+            *reinterpret_cast<uint4*>((T*)g.out + tok * g.os[0] + h * g.os[1] + x * 8) = make_uint4(0, 0, 0, 0);
+          if (g.lse && lane == 0) g.lse[i] = -INFINITY;
+        }
+      }
+    }
+    // (no copy is in flight when the block ends)
+    for (int i = max(0, it - L::kStages); i < it; ++i)
+      if (!bar_wait(&sh.full[i % L::kStages], (i / L::kStages) & 1, gave_up)) break;
+  } else if (warp == kMmaWarp) {
+    // ---- one warp issues the products
+    int it = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
+    const uint32_t what_qk = what_mma<T>(kTile, false), what_pv = what_mma<T>(D, true);
+    bool ok = works;
+    while (ok && u.at < hi) {
+      const Piece p = piece_of(u, lo, hi);
+      const bool both = p.n[1] > 0;
+      // ring places of the stream's operand: shared by the streams of a wide piece, in order otherwise
+      const int base = it;
+      auto place = [&](int s, int i, bool v) { return p.wide ? base + 2 * i + v : it++; };
+      auto done = [&](int s) { return !p.wide || s == 1 || !both; };  // the operand's last use
+      auto qk = [&](int s, int i) {
+        if (i >= p.n[s]) return true;
+        const int at = place(s, i, false), st = at % L::kStages;
+        if (i == 0 && !bar_wait(&sh.q_ready[s], n_q[s]++ & 1, gave_up)) return false;
+        if (!bar_wait(&sh.full[st], (at / L::kStages) & 1, gave_up)) return false;
+        tm_after();
+        if (lane == 0) {
+          const uint32_t a = q_at + s * L::kTileBytes, b = ring + st * L::kTileBytes;
+#pragma unroll
+          for (int x = 0; x < D / 16; ++x) {
+            const uint32_t at16 = (x / 4) * (kTile * 128) + (x % 4) * 32;
+            mma_ss(tmem + L::kS + s * 128, operand(a + at16, 16), operand(b + at16, 16), what_qk, x > 0);
+          }
+          if (done(s)) tm_commit(&sh.empty[st]);
+          tm_commit(&sh.s_ready[s]);
+        }
+        __syncwarp();
+        return true;
+      };
+      auto pv = [&](int s, int i) {
+        if (i >= p.n[s]) return true;
+        const int at = place(s, i, true), st = at % L::kStages;
+        if (!bar_wait(&sh.full[st], (at / L::kStages) & 1, gave_up)) return false;
+        const uint32_t b = ring + st * L::kTileBytes;
+        // values past the row's last token are not the row's: 0 times their bits may be NaN
+        const int t = p.wide ? p.t0 + i : p.t0 + 2 * i + s, rows = u.len + u.n - t * kTile;
+        if (rows < kTile && (s == 0 || !p.wide)) {
+          for (int x = rows * 8 + lane; x < kTile * 8; x += 32)
+            for (int half = 0; half < D / 64; ++half)
+              *reinterpret_cast<uint4*>(tiles + (b - q_at) + half * (kTile * 128) + x * 16) = make_uint4(0, 0, 0, 0);
+          async_fence();
+          __syncwarp();
+        }
+        if (!bar_wait(&sh.p_ready[s], n_p[s]++ & 1, gave_up)) return false;
+        tm_after();
+        if (lane == 0) {
+#pragma unroll
+          for (int x = 0; x < kTile / 16; ++x)
+            mma_ts(tmem + L::kO + s * D, tmem + L::kP + s * L::kPStep + x * 8, operand(b + x * 2048, kTile * 128), what_pv,
+                   i > 0 || x > 0);
+          if (done(s)) tm_commit(&sh.empty[st]);
+          if (i + 1 == p.n[s]) tm_commit(&sh.o_ready[s]);
+        }
+        __syncwarp();
+        return true;
+      };
+      ok = qk(0, 0) && qk(1, 0);
+      for (int i = 0; ok && i < p.n[0]; ++i) ok = pv(0, i) && qk(0, i + 1) && pv(1, i) && qk(1, i + 1);
+      if (p.wide) it = base + 2 * p.n[0];
+      next_unit(g, u);
+    }
+  } else if (works) {
+    // ---- eight warps: queries in, softmax of the tiles, rows out
+    const int s = warp / 4, r = tid & 127;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // (32 lanes of tensor memory, in the upper half of an address)
+    const uint32_t s_at = tmem + lanes + L::kS + s * 128, p_at = tmem + lanes + L::kP + s * L::kPStep;
+    const uint32_t o_at = tmem + lanes + L::kO;
+    const float sc = g.scale * kLog2e;
+    int n_s = 0, n_o[2] = {0, 0}, n_all = 0;
+    auto sync_all = [&]() {
+      __syncwarp();
+      if (lane == 0) bar_arrive(&sh.all);
+      return bar_wait(&sh.all, n_all++ & 1, gave_up);
+    };
+    bool ok = true;
+    for (int k = 0; ok && u.at < hi; ++k) {
+      const Piece p = piece_of(u, lo, hi);
+      const int row = p.r0 + r + (p.wide ? s * kTile : 0);
+      const bool live = row < u.rows;
+      const bool warp_live = __any_sync(~0u, live);
+      const int t = live ? row / g.group : u.n - 1, head = live ? u.h * g.group + row - t * g.group : 0;
+      const int sees = u.len + t;  // the last position that the row's token sees
+      if (p.n[s]) {
+        const T* src = (const T*)g.q + (long long)(u.a + t) * g.qs[0] + (long long)head * g.qs[1];
+        uint8_t* dst = tiles + s * L::kTileBytes + r * 128;
+#pragma unroll
+        for (int x = 0; x < D / 8; ++x) {
+          const uint4 v = live ? *reinterpret_cast<const uint4*>(src + x * 8) : make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(dst + (x / 8) * (kTile * 128) + ((x % 8) ^ (r & 7)) * 16) = v;
+        }
+        async_fence();
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sh.q_ready[s]);
+      }
+      float m = -INFINITY, l = 0.f;  // the maximum is scaled: in exponents of two
+      for (int i = 0; i < p.n[s]; ++i) {
+        if (!bar_wait(&sh.s_ready[s], n_s++ & 1, gave_up)) {
+          ok = false;
+          break;
+        }
+        if (warp_live) {
+          tm_after();
+          const int tile = p.wide ? p.t0 + i : p.t0 + 2 * i + s;
+          const int last = sees - tile * kTile;  // the tile's last visible key
+          uint32_t x[2][32];
+          // first the maximum, two loads of 32 columns under way at a time; the scores are read again for
+          // the exponentials, which costs less than 128 registers to hold them
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          tm_load32(s_at, x[0]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            tm_loaded(x[j & 1]);
+            if (j < 3) tm_load32(s_at + 32 * (j + 1), x[(j + 1) & 1]);
+            if (last < 32 * j + 31) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (32 * j + e > last) x[j & 1][e] = 0xFF800000u;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; ++e) top[e & 3] = fmaxf(top[e & 3], __uint_as_float(x[j & 1][e]));
+          }
+          const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sc;
+          // The maximum is moved only where it grew by more than 8 (the probabilities stay below 2^8 and
+          // lose nothing in floating point): few tiles rescale what came before them.
+          if (__any_sync(~0u, now - m > 8.f)) {
+            const float most = fmaxf(m, now), f = m > -INFINITY ? exp2_fast(m - most) : 0.f;
+            if (i > 0) {
+#pragma unroll
+              for (int j = 0; j < D; j += 32) {
+                uint32_t o[32];
+                tm_load32(o_at + s * D + j, o);
+                tm_loaded(o);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                tm_store32(o_at + s * D + j, o);
+              }
+            }
+            l *= f;
+            m = most;
+          }
+          tm_load32(s_at, x[0]);
+          const float base = m > -INFINITY ? m : 0.f;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            tm_loaded(x[j & 1]);
+            // (where the probabilities lie over the scores, their columns 16 j .. 16 j + 15 were read before)
+            if (j < 3) tm_load32(s_at + 32 * (j + 1), x[(j + 1) & 1]);
+            uint32_t* y = x[j & 1];
+            if (last < 32 * j + 31) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (32 * j + e > last) y[e] = 0xFF800000u;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              const float a = exp2_fast(fmaf(__uint_as_float(y[e]), sc, -base));
+              const float b = exp2_fast(fmaf(__uint_as_float(y[e + 1]), sc, -base));
+              sum[e & 2] += a;
+              sum[(e & 2) + 1] += b;
+              y[e / 2] = pack_of(a, b, T());
+            }
+            tm_store16(p_at + 16 * j, y);
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          tm_stored();
+          tm_before();
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sh.p_ready[s]);
+      }
+      if (!ok) break;
+      // ---- the rows' outcome
+      const bool whole = p.t0 == 0 && p.t1 == u.tiles;
+      const int c0 = cut.run_of(u.at);
+      const int slot = 2 * blockIdx.x + ((int)blockIdx.x == c0 ? 1 : 0);
+      float4* part = g.parts + (size_t)slot * (D / 4) * 256;
+      T* dst = (T*)g.out + (long long)(u.a + t) * g.os[0] + (long long)head * g.os[1];
+      float f[2];
+      if (!p.wide) {  // both streams hold the same rows: each of the two halves of the warps takes half of the columns
+        sh.ml[s][r] = make_float2(m, l);
+        if (!sync_all()) break;
+        const float2 x = sh.ml[0][r], y = sh.ml[1][r];
+        m = fmaxf(x.x, y.x);
+        f[0] = x.x > -INFINITY ? exp2_fast(x.x - m) : 0.f;
+        f[1] = y.x > -INFINITY ? exp2_fast(y.x - m) : 0.f;
+        l = x.y * f[0] + y.y * f[1];
+      } else {
+        f[0] = f[1] = 1.f;
+      }
+      for (int z = 0; z < 2 && ok; ++z)
+        if (p.n[z]) {
+          if (!p.wide || z == s) ok = bar_wait(&sh.o_ready[z], n_o[z] & 1, gave_up);
+          ++n_o[z];
+        }
+      if (!ok) break;
+      if (sh.bad[k % kRing]) l = NAN;  // (some key that the rows may read is in no page of the cache; known once all tiles were)
+      if (warp_live) {
+        tm_after();
+        const bool fine = l > 0.f;
+        const float inv = whole ? (fine ? 1.f / l : 0.f) : 1.f;
+        const int from = p.wide ? 0 : s * (D / 2), to = p.wide ? D : from + D / 2;
+        const int part_row = r + (p.wide ? s * kTile : 0);
+        for (int j = from; j < to; j += 32) {
+          uint32_t o[32], o1[32];
+          tm_load32(o_at + (p.wide ? s * D : 0) + j, o);
+          tm_loaded(o);
+          if (!p.wide && p.n[1]) {
+            tm_load32(o_at + D + j, o1);
+            tm_loaded(o1);
+          }
+          float y[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            y[e] = __uint_as_float(o[e]) * f[0];
+            if (!p.wide && p.n[1]) y[e] += __uint_as_float(o1[e]) * f[1];
+            y[e] = whole && !fine ? 0.f : y[e] * inv;
+          }
+          if (live && whole) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) *reinterpret_cast<uint4*>(dst + j + e) = pack8<T>(y + e);
+          } else if (live) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              __stcg(part + (size_t)((j + e) / 4) * 256 + part_row, make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]));
+          }
+          __syncwarp();
+        }
+        if (live && (p.wide || s == 0)) {
+          if (whole) {
+            if (g.lse) g.lse[(long long)(u.a + t) * g.H + head] = fine ? (m + log2f(l)) * kLn2 : -INFINITY;
+          } else {
+            __stcg(g.part_ml + (size_t)slot * 256 + part_row, make_float2(m, l));
+          }
+        }
+        tm_before();
+      }
+      if (!whole) {
+        // ---- the last block of the unit joins its pieces
+        const int c1 = cut.run_of(u.at + u.tiles - 1);
+        __threadfence();
+        if (!sync_all()) break;
+        if (tid == 0) {
+          const int n = atomicAdd(&g.joined[c0], 1);
+          sh.last = n == c1 - c0;
+          if (sh.last) g.joined[c0] = 0;
+          __threadfence();
+        }
+        if (!sync_all()) break;
+        if (sh.last) {
+          const int rows = min(256, u.rows - p.r0);
+          for (int x = tid; x < rows * (D / 8); x += kSoftWarps * 32) {
+            const int rr = x % rows, d8 = x / rows;
+            float most = -INFINITY;
+            for (int b = c0; b <= c1; ++b)
+              most = fmaxf(most, __ldcg(g.part_ml + (size_t)(2 * b + (b == c0)) * 256 + rr).x);
+            float acc[8] = {}, z = 0.f;
+            for (int b = c0; b <= c1; ++b) {
+              const size_t from = 2 * b + (b == c0);
+              const float2 e = __ldcg(g.part_ml + from * 256 + rr);
+              const float w = e.x > -INFINITY ? exp2_fast(e.x - most) : 0.f;
+              const float4* src = g.parts + from * (D / 4) * 256 + rr;
+              const float4 v0 = __ldcg(src + (size_t)(2 * d8) * 256), v1 = __ldcg(src + (size_t)(2 * d8 + 1) * 256);
+              z += e.y * w;
+              acc[0] += v0.x * w, acc[1] += v0.y * w, acc[2] += v0.z * w, acc[3] += v0.w * w;
+              acc[4] += v1.x * w, acc[5] += v1.y * w, acc[6] += v1.z * w, acc[7] += v1.w * w;
+            }
+            const bool fine = z > 0.f;
+            const float inv = fine ? 1.f / z : 0.f;
+            for (int e = 0; e < 8; ++e) acc[e] = fine ? acc[e] * inv : 0.f;
+            const int qrow = p.r0 + rr, tok = qrow / g.group, hh = u.h * g.group + qrow - tok * g.group;
+            *reinterpret_cast<uint4*>((T*)g.out + (long long)(u.a + tok) * g.os[0] + (long long)hh * g.os[1] + d8 * 8) =
+                pack8<T>(acc);
+            if (g.lse && d8 == 0) g.lse[(long long)(u.a + tok) * g.H + hh] = fine ? (most + log2f(z)) * kLn2 : -INFINITY;
+          }
+        }
+      } else if (!p.wide) {
+        ok = sync_all();  // both halves have read both streams' rows before the next piece writes them
+      }
+      next_unit(g, u);
+    }
+    if (!ok) *gave_up = 1;
+  }
+  __syncthreads();
+  if (sh.gave_up)
+    for (int b = tid; b < c.B; b += kThreads) g.status[b] = GRID_ST_BOUND;
+  if (works && warp == kMmaWarp) {
+    tm_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// A pool as a tensor map: boxes of 64 values of up to 128 tokens of one head of
+// one page.  The encoder is the driver library's, which the CUDA runtime has loaded.
+int make_map(const grid_kv_pages& p, void* pool, const int64_t* stride, CUtensorMap* map) {
+  static const auto encode = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>([]() -> void* {
+    void* lib = dlopen("libcuda.so.1", RTLD_LAZY);
+    return lib ? dlsym(lib, "cuTensorMapEncodeTiled") : nullptr;
+  }());
+  if (!encode) return set_error(GRID_E_CUDA, "grid_kv_create: no CUDA driver library");
+  const cuuint64_t dim[4] = {(cuuint64_t)p.head_dim, (cuuint64_t)p.page_size, (cuuint64_t)p.n_kv_heads, (cuuint64_t)p.n_pages};
+  const cuuint64_t step[3] = {(cuuint64_t)stride[1] * 2, (cuuint64_t)stride[2] * 2, (cuuint64_t)stride[0] * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)std::min(p.page_size, kTile), 1, 1}, one[4] = {1, 1, 1, 1};
+  const CUresult r = encode(map, p.dtype == GRID_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                            4, pool, dim, step, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS)
+    return set_error(GRID_E_INVALID_ARG, "grid_kv_create: the pools' strides make no tensor map (" + std::to_string((int)r) + ")");
+  return GRID_OK;
+}
+
+template <typename F>
+cudaError_t each_kernel(F f) {
+  cudaError_t e;
+  if ((e = f(k_attend<__nv_bfloat16, 64>, smem_bytes<64>())) || (e = f(k_attend<__nv_bfloat16, 128>, smem_bytes<128>())) ||
+      (e = f(k_attend<__half, 64>, smem_bytes<64>())))
+    return e;
+  return f(k_attend<__half, 128>, smem_bytes<128>());
+}
+
+}  // namespace
+}  // namespace grid
+
+using namespace grid;
+
+extern "C" int grid_kv_create(const grid_kv_pages* p, grid_kv** out) {
+  if (!p || !out || !p->d_k || !p->d_v || (uintptr_t)p->d_k % 16 || (uintptr_t)p->d_v % 16 || p->n_pages <= 0 ||
+      p->n_heads <= 0 || p->n_kv_heads <= 0 || p->n_heads % p->n_kv_heads)
+    return set_error(GRID_E_INVALID_ARG, "grid_kv_create: bad arguments");
+  if (p->dtype != GRID_DTYPE_BF16 && p->dtype != GRID_DTYPE_F16)
+    return set_error(GRID_E_INVALID_ARG, "grid_kv_create: a cache is of bf16 or f16");
+  if (p->head_dim != 64 && p->head_dim != 128)
+    return set_error(GRID_E_INVALID_ARG, "grid_kv_create: heads of 64 or 128 values");
+  if (p->page_size < 8 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)))
+    return set_error(GRID_E_INVALID_ARG, "grid_kv_create: page_size is a power of two in 8 .. 1024");
+  for (int i = 0; i < 3; ++i)
+    if (p->k_stride[i] <= 0 || p->v_stride[i] <= 0 || p->k_stride[i] % 8 || p->v_stride[i] % 8)
+      return set_error(GRID_E_INVALID_ARG, "grid_kv_create: strides are positive multiples of 8 elements");
+  grid_kv* kv = new grid_kv;
+  kv->p = *p;
+  while (1 << kv->log_page < p->page_size) ++kv->log_page;
+  int rc = make_map(*p, p->d_k, p->k_stride, &kv->k_map), dev = 0;
+  if (!rc) rc = make_map(*p, p->d_v, p->v_stride, &kv->v_map);
+  cudaError_t e = cudaSuccess;
+  if (!rc && (e = cudaGetDevice(&dev)) == cudaSuccess &&
+      (e = cudaDeviceGetAttribute(&kv->sms, cudaDevAttrMultiProcessorCount, dev)) == cudaSuccess) {
+    const size_t slots = 2 * (size_t)kv->sms * 256;
+    if (!(rc = kv->mem.alloc(slots * p->head_dim * 4, (void**)&kv->parts)) &&
+        !(rc = kv->mem.alloc(slots * sizeof(float2), (void**)&kv->part_ml)) &&
+        !(rc = kv->mem.alloc(kv->sms * sizeof(int), (void**)&kv->joined)) &&
+        (e = cudaMemset(kv->joined, 0, kv->sms * sizeof(int))) == cudaSuccess &&
+        (e = each_kernel([](auto kern, size_t smem) {
+           return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+         })) == cudaSuccess)
+      e = cudaDeviceSynchronize();
+  }
+  if (rc || e != cudaSuccess) {
+    kv->mem.release();
+    delete kv;
+    return rc ? rc : set_error(GRID_E_CUDA, std::string("grid_kv_create: ") + cudaGetErrorString(e));
+  }
+  *out = kv;
+  return GRID_OK;
+}
+
+extern "C" void grid_kv_free(grid_kv* kv) {
+  if (!kv) return;
+  kv->mem.release();
+  delete kv;
+}
+
+extern "C" int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_kv_query* query,
+                              int32_t* d_status, void* stream) {
+  AttendArgs a = {};
+  if (!kv || !query || !d_status || !make_chunk(kv, chunk, a.c) ||
+      (chunk->n_tokens && (!heads_ok(&query->q) || !heads_ok(&query->out))) || !std::isfinite(query->scale) ||
+      !(query->scale > 0.f) || (uintptr_t)query->d_lse % 4)
+    return set_error(GRID_E_INVALID_ARG, "grid_kv_attend: bad arguments");
+  if (chunk->B > 65535) return set_error(GRID_E_TOO_LARGE, "grid_kv_attend: more than 65535 rows");
+  const grid_kv_pages& p = kv->p;
+  if ((int64_t)chunk->n_tokens * (p.n_heads / p.n_kv_heads) > INT32_MAX - 256)
+    return set_error(GRID_E_TOO_LARGE, "grid_kv_attend: too many query rows in one call");
+  a.q = query->q.d, a.out = query->out.d, a.lse = query->d_lse;
+  a.qs[0] = query->q.token_stride, a.qs[1] = query->q.head_stride;
+  a.os[0] = query->out.token_stride, a.os[1] = query->out.head_stride;
+  a.H = p.n_heads, a.Hk = p.n_kv_heads, a.group = a.H / a.Hk, a.scale = query->scale, a.status = d_status;
+  a.parts = reinterpret_cast<float4*>(kv->parts), a.part_ml = kv->part_ml, a.joined = kv->joined;
+  auto go = [&](auto kern, size_t smem) {
+    return launch_pdl(kern, dim3(kv->sms), dim3(kThreads), smem, (cudaStream_t)stream, a, kv->k_map, kv->v_map);
+  };
+  if (p.dtype == GRID_DTYPE_BF16)
+    GRID_CUDA(p.head_dim == 64 ? go(k_attend<__nv_bfloat16, 64>, smem_bytes<64>())
+                               : go(k_attend<__nv_bfloat16, 128>, smem_bytes<128>()));
+  else
+    GRID_CUDA(p.head_dim == 64 ? go(k_attend<__half, 64>, smem_bytes<64>()) : go(k_attend<__half, 128>, smem_bytes<128>()));
+  GRID_CUDA(cudaGetLastError());
+  return GRID_OK;
+}

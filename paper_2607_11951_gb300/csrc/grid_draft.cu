@@ -398,7 +398,7 @@ extern "C" int grid_draft_verify(const grid_drafts* d, const grid_draft_step* s,
     return set_error(GRID_E_INVALID_ARG, "grid_draft_verify: bad arguments");
   if (s->B > d->B || s->K > d->K || s->V > d->V)
     return set_error(GRID_E_TOO_LARGE, "grid_draft_verify: B, K or V is larger than the handle's");
-  const int W = (s->V + 31) / 32, size = s->dtype == GRID_DTYPE_F32 ? 4 : 2;
+  const int size = s->dtype == GRID_DTYPE_F32 ? 4 : 2;
   if (s->logit_stride[0] < 0 || s->logit_stride[1] < 0 || s->mask_stride[0] < 0 || s->mask_stride[1] < 0 ||
       s->prob_stride[0] < 0 || s->prob_stride[1] < 0 || s->noise_stride < 0 || (uintptr_t)s->d_logits % size ||
       (uintptr_t)s->d_mask % 4 || (uintptr_t)s->d_probs % 4 || (uintptr_t)s->d_noise % 4)
