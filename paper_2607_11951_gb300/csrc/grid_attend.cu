@@ -31,8 +31,10 @@ namespace {
 
 constexpr int kTile = 128;            // keys of a tile, query rows of a stream
 constexpr int kSoftWarps = 8;         // four per stream
-constexpr int kThreads = (kSoftWarps + 2) * 32;  // and one that loads, one that multiplies
-constexpr int kLoadWarp = kSoftWarps, kMmaWarp = kSoftWarps + 1;
+constexpr int kLoadWarp = kSoftWarps, kMmaWarp = kSoftWarps + 1;  // one that loads tiles, one that multiplies,
+constexpr int kQueryWarp = kSoftWarps + 2, kQueryWarps = 2;        // two that load queries
+constexpr int kThreads = (kSoftWarps + 4) * 32;
+constexpr int kMinRun = 2;            // tiles of a run, at least (unless there are fewer)
 constexpr int kRing = 8;              // pieces whose bad-page flags are kept at once
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
@@ -73,14 +75,22 @@ __device__ __forceinline__ bool bar_try(uint64_t* b, int parity) {
 }
 // Waits for a phase, for two seconds' clocks at most or until another warp
 // gave up; false then.  Whole warps wait, and leave together.
+__device__ __noinline__ bool bar_wait_long(uint64_t* b, int parity, volatile int* gave_up) {
+  const long long t0 = clock64();
+  bool ok;
+  while (!(ok = bar_try(b, parity)) && !*gave_up)
+    if (clock64() - t0 > 4000000000LL) *gave_up = 1;
+  return ok;
+}
 __device__ __forceinline__ bool bar_wait(uint64_t* b, int parity, volatile int* gave_up) {
-  bool ok = bar_try(b, parity);
-  if (!ok) {
-    const long long t0 = clock64();
-    while (!(ok = bar_try(b, parity)) && !*gave_up)
-      if (clock64() - t0 > 4000000000LL) *gave_up = 1;
-  }
-  return __all_sync(~0u, ok);
+  if (__all_sync(~0u, bar_try(b, parity))) return true;
+  return __all_sync(~0u, bar_wait_long(b, parity, gave_up));
+}
+// One lane of a whole warp, always the same.
+__device__ __forceinline__ bool elected() {
+  uint32_t p;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+  return p;
 }
 __device__ __forceinline__ void load_tile(const CUtensorMap* m, uint32_t dst, uint64_t* bar, int x, int token, int head,
                                           int page) {
@@ -124,6 +134,12 @@ __device__ __forceinline__ void tm_load32(uint32_t at, uint32_t* x) {
       : O8(x, 0), O8(x, 8), O8(x, 16), O8(x, 24)
       : "r"(at));
 }
+__device__ __forceinline__ void tm_load16(uint32_t at, uint32_t* x) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : O8(x, 0), O8(x, 8)
+      : "r"(at));
+}
 __device__ __forceinline__ void tm_store32(uint32_t at, const uint32_t* x) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
@@ -141,6 +157,9 @@ __device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t* x) {
 // (the registers are named, so that nothing uses them before the wait)
 __device__ __forceinline__ void tm_loaded(uint32_t* x) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : U8(x, 0), U8(x, 8), U8(x, 16), U8(x, 24) : : "memory");
+}
+__device__ __forceinline__ void tm_loaded16(uint32_t* x, uint32_t* y) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : U8(x, 0), U8(x, 8), U8(y, 0), U8(y, 8) : : "memory");
 }
 __device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -171,36 +190,29 @@ struct Units {
   int b, a, n, len, rows;  // row, its first token, tokens, cached tokens, query rows per key head
   int units, h, qt;        // units per key head; the current one
   int tiles;               // key tiles of the current unit
-  long long at;            // the tile that it begins at
+  int at;                  // the tile that it begins at (their number is checked on the host to fit)
 };
 
 __device__ __forceinline__ int tiles_of(const Units& u, int group, int qt) {
+  if (u.units == 1) return (u.len + u.n + kTile - 1) / kTile;
   const int last = min(u.rows, (qt + 1) * 256) - 1;  // its last query row
   return (u.len + last / group + kTile) / kTile;
+}
+__device__ __forceinline__ void set_row(const AttendArgs& g, Units& u) {
+  u.rows = u.n * g.group;
+  u.units = u.rows <= 256 ? 1 : (u.rows + 255) / 256;
 }
 __device__ __forceinline__ bool open_row(const AttendArgs& g, Units& u, int b) {
   u.b = b;
   if (!row_span(g.c, b, u.a, u.n, u.len) || u.n == 0) return false;
-  u.rows = u.n * g.group;
-  u.units = u.rows <= kTile ? 1 : (u.rows + 255) / 256;
+  set_row(g, u);
   return true;
 }
-__device__ __forceinline__ long long head_tiles(const AttendArgs& g, const Units& u) {
-  long long t = 0;
+__device__ __forceinline__ int head_tiles(const AttendArgs& g, const Units& u) {
+  int t = 0;
+#pragma unroll 1
   for (int i = 0; i < u.units; ++i) t += tiles_of(u, g.group, i);
   return t;
-}
-// The unit that tile `at` lies in; row b's first tile is `first`.
-__device__ __forceinline__ void find_unit(const AttendArgs& g, Units& u, int b, long long first, long long at) {
-  open_row(g, u, b);
-  const long long per = head_tiles(g, u);
-  u.h = (int)((at - first) / per);
-  u.at = first + u.h * per;
-  for (u.qt = 0;; ++u.qt) {
-    u.tiles = tiles_of(u, g.group, u.qt);
-    if (at < u.at + u.tiles || u.qt + 1 == u.units) break;
-    u.at += u.tiles;
-  }
 }
 __device__ __forceinline__ void next_unit(const AttendArgs& g, Units& u) {
   u.at += u.tiles;
@@ -208,6 +220,7 @@ __device__ __forceinline__ void next_unit(const AttendArgs& g, Units& u) {
     u.qt = 0;
     if (++u.h == g.Hk) {
       u.h = 0;
+#pragma unroll 1
       while (u.b + 1 < g.c.B && !open_row(g, u, u.b + 1)) {
       }
     }
@@ -215,11 +228,14 @@ __device__ __forceinline__ void next_unit(const AttendArgs& g, Units& u) {
   u.tiles = tiles_of(u, g.group, u.qt);
 }
 
-struct Cut {  // of `total` tiles into runs: block i takes [total i / runs, total (i + 1) / runs)
-  long long total;
-  int runs;
-  __device__ long long begin(int i) const { return total * i / runs; }
-  __device__ int run_of(long long tile) const { return (int)(((tile + 1) * runs + total - 1) / total) - 1; }
+// All tiles cut into runs, one per block, the first `more` of them one tile longer.
+struct Cut {
+  int runs, each, more;
+  __device__ __forceinline__ int begin(int i) const { return i * each + min(i, more); }
+  __device__ __forceinline__ int run_of(int tile) const {
+    const int longer = more * (each + 1);
+    return tile < longer ? tile / (each + 1) : more + (tile - longer) / each;
+  }
 };
 
 // One block's part of one unit.
@@ -229,10 +245,10 @@ struct Piece {
   int n[2];      // tiles of each stream
   int r0;        // first query row
 };
-__device__ __forceinline__ Piece piece_of(const Units& u, long long lo, long long hi) {
+__device__ __forceinline__ Piece piece_of(const Units& u, int lo, int hi) {
   Piece p;
-  p.t0 = (int)(max(lo, u.at) - u.at);
-  p.t1 = (int)(min(hi, u.at + u.tiles) - u.at);
+  p.t0 = max(lo, u.at) - u.at;
+  p.t1 = min(hi, u.at + u.tiles) - u.at;
   p.wide = u.rows > kTile;
   p.r0 = u.qt * 256;
   const int n = p.t1 - p.t0;
@@ -253,11 +269,10 @@ struct Layout {
 
 struct Shared {
   uint64_t full[10], empty[10];
-  uint64_t q_ready[2], s_ready[2], p_ready[2], o_ready[2], all;
+  uint64_t q_ready[2], q_free[2], s_ready[2], p_ready[2], o_ready[2], all;
   float2 ml[2][kTile];
-  long long sums[kThreads / 32];
-  long long first;
-  int row, gave_up, last, bad[kRing];
+  int sums[kThreads / 32];
+  int first, row[4], gave_up, last, bad[kRing];
   uint32_t tmem;
 };
 
@@ -285,7 +300,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       bar_init(&sh.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      bar_init(&sh.q_ready[i], 4);
+      bar_init(&sh.q_ready[i], kQueryWarps);
+      bar_init(&sh.q_free[i], 1);
       bar_init(&sh.s_ready[i], 1);
       bar_init(&sh.p_ready[i], 4);
       bar_init(&sh.o_ready[i], 1);
@@ -298,38 +314,43 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   // How many tiles there are in all, and the row that this block begins in.
   Cut cut;
+  Units u;
   {
     const int per = (c.B + kThreads - 1) / kThreads;
-    Units u;
-    long long mine = 0;
+    int mine = 0;
+#pragma unroll 1
     for (int b = tid * per; b < min(c.B, (tid + 1) * per); ++b)
       if (open_row(g, u, b)) mine += head_tiles(g, u) * g.Hk;
-    long long pre = mine;
+    int pre = mine;
+#pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long x = __shfl_up_sync(~0u, pre, o);
+      const int x = __shfl_up_sync(~0u, pre, o);
       if (lane >= o) pre += x;
     }
     if (lane == 31) sh.sums[warp] = pre;
     __syncthreads();
-    cut.total = 0;
+    int total = 0;
+#pragma unroll
     for (int w = 0; w < kThreads / 32; ++w) {
       if (w < warp) pre += sh.sums[w];
-      cut.total += sh.sums[w];
+      total += sh.sums[w];
     }
     pre -= mine;
-    cut.runs = (int)min((long long)gridDim.x, (cut.total + 1) / 2);
-    if ((int)blockIdx.x < cut.runs) {
-      const long long lo = cut.begin(blockIdx.x);
-      if (pre <= lo && lo < pre + mine)
-        for (int b = tid * per; b < min(c.B, (tid + 1) * per); ++b) {
-          const long long t = open_row(g, u, b) ? head_tiles(g, u) * g.Hk : 0;
-          if (lo < pre + t) {
-            sh.row = b;
-            sh.first = pre;
-            break;
-          }
-          pre += t;
+    cut.runs = min((int)gridDim.x, (total + kMinRun - 1) / kMinRun);
+    cut.each = cut.runs ? total / cut.runs : 0;
+    cut.more = total - cut.runs * cut.each;
+    const int lo = cut.begin(blockIdx.x);
+    if ((int)blockIdx.x < cut.runs && pre <= lo && lo < pre + mine) {
+#pragma unroll 1
+      for (int b = per > 1 ? tid * per : tid; b < c.B; ++b) {
+        const int t = per == 1 ? mine : open_row(g, u, b) ? head_tiles(g, u) * g.Hk : 0;
+        if (lo < pre + t) {
+          sh.row[0] = b, sh.row[1] = u.a, sh.row[2] = u.n, sh.row[3] = u.len;
+          sh.first = pre;
+          break;
         }
+        pre += t;
+      }
     }
   }
   const bool works = (int)blockIdx.x < cut.runs;
@@ -341,48 +362,77 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tm_after();
   const uint32_t tmem = works ? sh.tmem : 0;
-  const long long lo = works ? cut.begin(blockIdx.x) : 0, hi = works ? cut.begin(blockIdx.x + 1) : 0;
+  const int lo = works ? cut.begin(blockIdx.x) : 0, hi = works ? cut.begin(blockIdx.x + 1) : 0;
   volatile int* gave_up = &sh.gave_up;
-  Units u;
-  if (works) find_unit(g, u, sh.row, sh.first, lo);
+  if (works) {  // the unit that the run begins in
+    u.b = sh.row[0], u.a = sh.row[1], u.n = sh.row[2], u.len = sh.row[3];
+    set_row(g, u);
+    const int per = head_tiles(g, u);
+    u.h = (lo - sh.first) / per;
+    u.at = sh.first + u.h * per;
+#pragma unroll 1
+    for (u.qt = 0;; ++u.qt) {
+      u.tiles = tiles_of(u, g.group, u.qt);
+      if (lo < u.at + u.tiles || u.qt + 1 == u.units) break;
+      u.at += u.tiles;
+    }
+  }
 
   if (warp == kLoadWarp) {
-    // ---- one warp keeps the ring of tiles full: a lane per page
+    // ---- one warp keeps the ring of tiles full: a lane per page and half of the columns
     int it = 0;
     if (works) {
-      const int box = min(kTile, 1 << c.log_page), pages = kTile / box;
+      const int box = min(kTile, 1 << c.log_page), pages = kTile / box, boxes = pages * (D / 64);
+      const int part = lane / pages, page_lane = lane - part * pages;
+      const uint32_t to = ring + part * (kTile * 128) + page_lane * box * 128;
       bool ok = true;
+      // the ids of 32 pages at a time, the lane's its own: those of the keys' tile, and before and after them
+      int row = -1, block = 0, id_was = 0, id = 0, id_next = 0;
+#pragma unroll 1
       for (int k = 0; ok && u.at < hi; ++k) {
         const Piece p = piece_of(u, lo, hi);
         const int used = (u.len + u.n + (1 << c.log_page) - 1) >> c.log_page;  // pages of the row
         int* bad = &sh.bad[k % kRing];
         if (lane == 0) *bad = 0;
         __syncwarp();
+        auto fetch = [&](int bl) {  // -1: outside the cache; past the row: one past the pool, which loads zeros
+          const int pg = bl * 32 + lane;
+          return pg < used ? page_of(c, u.b, pg << c.log_page) : c.n_pages;
+        };
         auto load = [&](int t, bool v) {
-          const int st = it % L::kStages, token = t * kTile + lane * box, pg = token >> c.log_page;
-          int page = c.n_pages;  // (one past the pool: the tile's part is filled with zeros)
-          if (lane < pages && pg < used) {
-            page = c.table[u.b * c.table_stride + pg];
-            if (page < 0 || page >= c.n_pages) {
-              page = c.n_pages;
-              *bad = 1;
-            }
+          const int st = it % L::kStages, token = t * kTile, pg = token >> c.log_page;
+          if (row != u.b || (!v && pg >> 5 != block)) {
+            id_was = id;
+            id = row == u.b && pg >> 5 == block + 1 ? id_next : fetch(pg >> 5);
+            row = u.b;
+            block = pg >> 5;
+            id_next = fetch(block + 1);
+          }
+          int page = __shfl_sync(~0u, pg >> 5 == block ? id : id_was, (pg + page_lane) & 31);
+          if (page < 0) {
+            page = c.n_pages;
+            if (lane < boxes) *bad = 1;
           }
           if (!bar_wait(&sh.empty[st], ((it / L::kStages) & 1) ^ 1, gave_up)) return false;
           if (lane == 0) bar_expect(&sh.full[st], L::kTileBytes);
           __syncwarp();
-          if (lane < pages)
-            for (int x = 0; x < D / 64; ++x)
-              load_tile(v ? &v_map : &k_map, ring + st * L::kTileBytes + x * (kTile * 128) + lane * box * 128, &sh.full[st],
-                        x * 64, token & ((1 << c.log_page) - 1), u.h, page);
+          if (lane < boxes)
+            load_tile(v ? &v_map : &k_map, to + st * L::kTileBytes, &sh.full[st], part * 64,
+                      token & ((1 << c.log_page) - 1), u.h, page);
           ++it;
           return true;
         };
+        // in the order in which the products take them
         if (p.wide) {
-          for (int t = p.t0; ok && t < p.t1; ++t) ok = load(t, false) && load(t, true);
+#pragma unroll 1
+          for (int x = 0; ok && x < 2 * (p.t1 - p.t0); ++x) ok = load(p.t0 + x / 2, x & 1);
         } else {
-          ok = load(p.t0, false) && (p.t0 + 1 >= p.t1 || load(p.t0 + 1, false));
-          for (int t = p.t0; ok && t < p.t1; ++t) ok = load(t, true) && (t + 2 >= p.t1 || load(t + 2, false));
+#pragma unroll 1
+          for (int x = -2; ok && x < 2 * (p.t1 - p.t0); ++x) {  // K0 K1 V0 K2 V1 K3 ...
+            const bool v = x >= 0 && !(x & 1);
+            const int t = p.t0 + (x < 0 ? x + 2 : x / 2 + (v ? 0 : 2));
+            if (t < p.t1) ok = load(t, v);
+          }
         }
         next_unit(g, u);
       }
@@ -426,15 +476,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (i == 0 && !bar_wait(&sh.q_ready[s], n_q[s]++ & 1, gave_up)) return false;
         if (!bar_wait(&sh.full[st], (at / L::kStages) & 1, gave_up)) return false;
         tm_after();
-        if (lane == 0) {
+        if (elected()) {
           const uint32_t a = q_at + s * L::kTileBytes, b = ring + st * L::kTileBytes;
 #pragma unroll
           for (int x = 0; x < D / 16; ++x) {
             const uint32_t at16 = (x / 4) * (kTile * 128) + (x % 4) * 32;
             mma_ss(tmem + L::kS + s * 128, operand(a + at16, 16), operand(b + at16, 16), what_qk, x > 0);
           }
-          if (done(s)) tm_commit(&sh.empty[st]);
           tm_commit(&sh.s_ready[s]);
+          if (done(s)) tm_commit(&sh.empty[st]);
+          if (i + 1 == p.n[s]) tm_commit(&sh.q_free[s]);
         }
         __syncwarp();
         return true;
@@ -455,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!bar_wait(&sh.p_ready[s], n_p[s]++ & 1, gave_up)) return false;
         tm_after();
-        if (lane == 0) {
+        if (elected()) {
 #pragma unroll
           for (int x = 0; x < kTile / 16; ++x)
             mma_ts(tmem + L::kO + s * D, tmem + L::kP + s * L::kPStep + x * 8, operand(b + x * 2048, kTile * 128), what_pv,
@@ -471,8 +522,48 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (p.wide) it = base + 2 * p.n[0];
       next_unit(g, u);
     }
+  } else if (warp >= kQueryWarp) {
+    // ---- two warps bring the next unit's queries as soon as the last product has read the ones before
+    constexpr int kPer = D / 8;  // 16-byte parts of a query row, a lane each
+    int n_f[2] = {0, 0};
+    bool ok = works;
+#pragma unroll 1
+    while (ok && u.at < hi) {
+      const Piece p = piece_of(u, lo, hi);
+#pragma unroll 1
+      for (int s = 0; ok && s < 2; ++s) {
+        if (!p.n[s]) continue;
+        ok = bar_wait(&sh.q_free[s], (n_f[s]++ & 1) ^ 1, gave_up);
+        if (!ok) break;
+        const int r0 = p.r0 + (p.wide ? s * kTile : 0), rows = min(kTile, u.rows - r0);
+        const int part = tid % kPer, step = kQueryWarps * 32 / kPer;
+        // (rows past the unit's last are left as they are: they have no part in any other row)
+#pragma unroll 1
+        for (int r = (tid - kQueryWarp * 32) / kPer; r < rows; r += 8 * step) {
+          uint4 v[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+            if (r + x * step < rows) {
+              const int row = r0 + r + x * step, t = row / g.group, head = u.h * g.group + row - t * g.group;
+              v[x] = *reinterpret_cast<const uint4*>((const T*)g.q + (long long)(u.a + t) * g.qs[0] +
+                                                     (long long)head * g.qs[1] + part * 8);
+            }
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+            if (r + x * step < rows) {
+              const int row = r + x * step;
+              *reinterpret_cast<uint4*>(tiles + s * L::kTileBytes + row * 128 + (part / 8) * (kTile * 128) +
+                                        ((part % 8) ^ (row & 7)) * 16) = v[x];
+            }
+        }
+        async_fence();
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sh.q_ready[s]);
+      }
+      next_unit(g, u);
+    }
   } else if (works) {
-    // ---- eight warps: queries in, softmax of the tiles, rows out
+    // ---- eight warps: softmax of the tiles, rows out
     const int s = warp / 4, r = tid & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // (32 lanes of tensor memory, in the upper half of an address)
     const uint32_t s_at = tmem + lanes + L::kS + s * 128, p_at = tmem + lanes + L::kP + s * L::kPStep;
@@ -492,18 +583,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool warp_live = __any_sync(~0u, live);
       const int t = live ? row / g.group : u.n - 1, head = live ? u.h * g.group + row - t * g.group : 0;
       const int sees = u.len + t;  // the last position that the row's token sees
-      if (p.n[s]) {
-        const T* src = (const T*)g.q + (long long)(u.a + t) * g.qs[0] + (long long)head * g.qs[1];
-        uint8_t* dst = tiles + s * L::kTileBytes + r * 128;
-#pragma unroll
-        for (int x = 0; x < D / 8; ++x) {
-          const uint4 v = live ? *reinterpret_cast<const uint4*>(src + x * 8) : make_uint4(0, 0, 0, 0);
-          *reinterpret_cast<uint4*>(dst + (x / 8) * (kTile * 128) + ((x % 8) ^ (r & 7)) * 16) = v;
-        }
-        async_fence();
-        __syncwarp();
-        if (lane == 0) bar_arrive(&sh.q_ready[s]);
-      }
       float m = -INFINITY, l = 0.f;  // the maximum is scaled: in exponents of two
       for (int i = 0; i < p.n[s]; ++i) {
         if (!bar_wait(&sh.s_ready[s], n_s++ & 1, gave_up)) {
@@ -514,65 +593,61 @@ __global__ void __launch_bounds__(kThreads, 1)
           tm_after();
           const int tile = p.wide ? p.t0 + i : p.t0 + 2 * i + s;
           const int last = sees - tile * kTile;  // the tile's last visible key
-          uint32_t x[2][32];
-          // first the maximum, two loads of 32 columns under way at a time; the scores are read again for
-          // the exponentials, which costs less than 128 registers to hold them
+          uint32_t x[32];
+          // first the maximum; the scores are read again for the exponentials, which costs less than
+          // 128 registers to hold them.  The loops are rolled: short calls wait for instructions otherwise.
           float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          tm_load32(s_at, x[0]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            tm_loaded(x[j & 1]);
-            if (j < 3) tm_load32(s_at + 32 * (j + 1), x[(j + 1) & 1]);
-            if (last < 32 * j + 31) {
+#pragma unroll 1
+          for (int j = 0; j < kTile; j += 32) {
+            tm_load32(s_at + j, x);
+            tm_loaded(x);
+            if (last < j + 31) {
 #pragma unroll
               for (int e = 0; e < 32; ++e)
-                if (32 * j + e > last) x[j & 1][e] = 0xFF800000u;
+                if (j + e > last) x[e] = 0xFF800000u;
             }
 #pragma unroll
-            for (int e = 0; e < 32; ++e) top[e & 3] = fmaxf(top[e & 3], __uint_as_float(x[j & 1][e]));
+            for (int e = 0; e < 32; ++e) top[e & 3] = fmaxf(top[e & 3], __uint_as_float(x[e]));
           }
           const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sc;
           // The maximum is moved only where it grew by more than 8 (the probabilities stay below 2^8 and
           // lose nothing in floating point): few tiles rescale what came before them.
-          if (__any_sync(~0u, now - m > 8.f)) {
+          if (__any_sync(~0u, live && now - m > 8.f)) {
             const float most = fmaxf(m, now), f = m > -INFINITY ? exp2_fast(m - most) : 0.f;
             if (i > 0) {
-#pragma unroll
+#pragma unroll 1
               for (int j = 0; j < D; j += 32) {
-                uint32_t o[32];
-                tm_load32(o_at + s * D + j, o);
-                tm_loaded(o);
+                tm_load32(o_at + s * D + j, x);
+                tm_loaded(x);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                tm_store32(o_at + s * D + j, o);
+                for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
+                tm_store32(o_at + s * D + j, x);
               }
             }
             l *= f;
             m = most;
           }
-          tm_load32(s_at, x[0]);
           const float base = m > -INFINITY ? m : 0.f;
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            tm_loaded(x[j & 1]);
-            // (where the probabilities lie over the scores, their columns 16 j .. 16 j + 15 were read before)
-            if (j < 3) tm_load32(s_at + 32 * (j + 1), x[(j + 1) & 1]);
-            uint32_t* y = x[j & 1];
-            if (last < 32 * j + 31) {
+#pragma unroll 1
+          for (int j = 0; j < kTile; j += 32) {
+            tm_load32(s_at + j, x);
+            tm_loaded(x);
+            if (last < j + 31) {
 #pragma unroll
               for (int e = 0; e < 32; ++e)
-                if (32 * j + e > last) y[e] = 0xFF800000u;
+                if (j + e > last) x[e] = 0xFF800000u;
             }
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-              const float a = exp2_fast(fmaf(__uint_as_float(y[e]), sc, -base));
-              const float b = exp2_fast(fmaf(__uint_as_float(y[e + 1]), sc, -base));
+              const float a = exp2_fast(fmaf(__uint_as_float(x[e]), sc, -base));
+              const float b = exp2_fast(fmaf(__uint_as_float(x[e + 1]), sc, -base));
               sum[e & 2] += a;
               sum[(e & 2) + 1] += b;
-              y[e / 2] = pack_of(a, b, T());
+              x[e / 2] = pack_of(a, b, T());
             }
-            tm_store16(p_at + 16 * j, y);
+            // (where the probabilities lie over the scores, these columns were read before)
+            tm_store16(p_at + j / 2, x);
           }
           l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
           tm_stored();
@@ -613,27 +688,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float inv = whole ? (fine ? 1.f / l : 0.f) : 1.f;
         const int from = p.wide ? 0 : s * (D / 2), to = p.wide ? D : from + D / 2;
         const int part_row = r + (p.wide ? s * kTile : 0);
-        for (int j = from; j < to; j += 32) {
-          uint32_t o[32], o1[32];
-          tm_load32(o_at + (p.wide ? s * D : 0) + j, o);
-          tm_loaded(o);
-          if (!p.wide && p.n[1]) {
-            tm_load32(o_at + D + j, o1);
-            tm_loaded(o1);
-          }
-          float y[32];
+#pragma unroll 1
+        for (int j = from; j < to; j += 16) {
+          uint32_t o[16], o1[16] = {};
+          tm_load16(o_at + (p.wide ? s * D : 0) + j, o);
+          if (!p.wide && p.n[1]) tm_load16(o_at + D + j, o1);
+          tm_loaded16(o, o1);
+          float y[16];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
+          for (int e = 0; e < 16; ++e) {
             y[e] = __uint_as_float(o[e]) * f[0];
             if (!p.wide && p.n[1]) y[e] += __uint_as_float(o1[e]) * f[1];
             y[e] = whole && !fine ? 0.f : y[e] * inv;
           }
           if (live && whole) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) *reinterpret_cast<uint4*>(dst + j + e) = pack8<T>(y + e);
+            for (int e = 0; e < 16; e += 8) *reinterpret_cast<uint4*>(dst + j + e) = pack8<T>(y + e);
           } else if (live) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
+            for (int e = 0; e < 16; e += 4)
               __stcg(part + (size_t)((j + e) / 4) * 256 + part_row, make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]));
           }
           __syncwarp();
@@ -790,8 +863,11 @@ extern "C" int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, con
     return set_error(GRID_E_INVALID_ARG, "grid_kv_attend: bad arguments");
   if (chunk->B > 65535) return set_error(GRID_E_TOO_LARGE, "grid_kv_attend: more than 65535 rows");
   const grid_kv_pages& p = kv->p;
-  if ((int64_t)chunk->n_tokens * (p.n_heads / p.n_kv_heads) > INT32_MAX - 256)
-    return set_error(GRID_E_TOO_LARGE, "grid_kv_attend: too many query rows in one call");
+  // (more than two billion tiles of 256 query rows by 128 keys would take minutes)
+  const double units = (double)chunk->n_tokens * (p.n_heads / p.n_kv_heads) / 256 + chunk->B;
+  if ((double)chunk->n_tokens * (p.n_heads / p.n_kv_heads) > INT32_MAX - 256 ||
+      units * p.n_kv_heads * (((double)chunk->max_pages * p.page_size) / kTile + 1) > INT32_MAX)
+    return set_error(GRID_E_TOO_LARGE, "grid_kv_attend: too many query rows or key tiles in one call");
   a.q = query->q.d, a.out = query->out.d, a.lse = query->d_lse;
   a.qs[0] = query->q.token_stride, a.qs[1] = query->q.head_stride;
   a.os[0] = query->out.token_stride, a.os[1] = query->out.head_stride;

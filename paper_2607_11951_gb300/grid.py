@@ -171,6 +171,10 @@ def _check(rc):
 def _stream(stream):
     if stream is None:
         import torch
+        # (the stream's handle without the object around it: 0.3 us where torch.cuda.current_stream() takes 3)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None and torch.cuda.is_initialized():
+            return raw(torch.cuda.current_device())
         return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
