@@ -86,6 +86,9 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, int parity, volatile int* 
   if (__all_sync(~0u, bar_try(b, parity))) return true;
   return __all_sync(~0u, bar_wait_long(b, parity, gave_up));
 }
+__device__ __forceinline__ bool bar_wait1(uint64_t* b, int parity, volatile int* gave_up) {  // a thread alone
+  return bar_try(b, parity) || bar_wait_long(b, parity, gave_up);
+}
 // One lane of a whole warp, always the same.
 __device__ __forceinline__ bool elected() {
   uint32_t p;
@@ -208,11 +211,12 @@ __device__ __forceinline__ bool open_row(const AttendArgs& g, Units& u, int b) {
   set_row(g, u);
   return true;
 }
-__device__ __forceinline__ int head_tiles(const AttendArgs& g, const Units& u) {
+// The tiles of a key head, by a warp (every lane gets the sum).
+__device__ __forceinline__ int head_tiles(const Units& u, int group, int lane) {
   int t = 0;
 #pragma unroll 1
-  for (int i = 0; i < u.units; ++i) t += tiles_of(u, g.group, i);
-  return t;
+  for (int i = lane; i < u.units; i += 32) t += tiles_of(u, group, i);
+  return __reduce_add_sync(~0u, t);
 }
 __device__ __forceinline__ void next_unit(const AttendArgs& g, Units& u) {
   u.at += u.tiles;
@@ -244,6 +248,7 @@ struct Piece {
   int t0, t1;    // key tiles
   int n[2];      // tiles of each stream
   int r0;        // first query row
+  __device__ __forceinline__ bool ends(const Units& u) const { return u.len + u.n < t1 * kTile; }  // past the row's last token
 };
 __device__ __forceinline__ Piece piece_of(const Units& u, int lo, int hi) {
   Piece p;
@@ -272,7 +277,7 @@ struct Shared {
   uint64_t q_ready[2], q_free[2], s_ready[2], p_ready[2], o_ready[2], all;
   float2 ml[2][kTile];
   int sums[kThreads / 32];
-  int first, row[4], gave_up, last, bad[kRing];
+  int first, per, row[4], gave_up, last, bad[kRing];
   uint32_t tmem;
 };
 
@@ -316,11 +321,24 @@ __global__ void __launch_bounds__(kThreads, 1)
   Cut cut;
   Units u;
   {
+    // (a thread's rows are `per` neighbours; a row of several units is summed by its warp)
     const int per = (c.B + kThreads - 1) / kThreads;
-    int mine = 0;
+    auto row_tiles = [&](int b) {
+      const bool some = b < min(c.B, (tid + 1) * per) && open_row(g, u, b);
+      int t = some && u.units == 1 ? tiles_of(u, g.group, 0) : 0;
+      for (unsigned big = __ballot_sync(~0u, some && u.units > 1); big; big &= big - 1) {
+        const int l = __ffs(big) - 1;
+        Units v;
+        v.n = __shfl_sync(~0u, u.n, l), v.len = __shfl_sync(~0u, u.len, l);
+        v.rows = __shfl_sync(~0u, u.rows, l), v.units = __shfl_sync(~0u, u.units, l);
+        const int sum = head_tiles(v, g.group, lane);
+        if (lane == l) t = sum;
+      }
+      return t;
+    };
+    int mine = 0, t = 0;
 #pragma unroll 1
-    for (int b = tid * per; b < min(c.B, (tid + 1) * per); ++b)
-      if (open_row(g, u, b)) mine += head_tiles(g, u) * g.Hk;
+    for (int i = 0; i < per; ++i) mine += (t = row_tiles(tid * per + i)) * g.Hk;
     int pre = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -340,16 +358,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     cut.each = cut.runs ? total / cut.runs : 0;
     cut.more = total - cut.runs * cut.each;
     const int lo = cut.begin(blockIdx.x);
-    if ((int)blockIdx.x < cut.runs && pre <= lo && lo < pre + mine) {
+    const bool here = (int)blockIdx.x < cut.runs && pre <= lo && lo < pre + mine;
+    if (__any_sync(~0u, here)) {
 #pragma unroll 1
-      for (int b = per > 1 ? tid * per : tid; b < c.B; ++b) {
-        const int t = per == 1 ? mine : open_row(g, u, b) ? head_tiles(g, u) * g.Hk : 0;
-        if (lo < pre + t) {
-          sh.row[0] = b, sh.row[1] = u.a, sh.row[2] = u.n, sh.row[3] = u.len;
+      for (int i = 0; i < per; ++i) {
+        if (per > 1) t = row_tiles(tid * per + i);
+        if (here && pre <= lo && lo < pre + t * g.Hk) {
+          sh.row[0] = u.b, sh.row[1] = u.a, sh.row[2] = u.n, sh.row[3] = u.len;
           sh.first = pre;
-          break;
+          sh.per = t;
         }
-        pre += t;
+        pre += t * g.Hk;
       }
     }
   }
@@ -367,14 +386,26 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (works) {  // the unit that the run begins in
     u.b = sh.row[0], u.a = sh.row[1], u.n = sh.row[2], u.len = sh.row[3];
     set_row(g, u);
-    const int per = head_tiles(g, u);
-    u.h = (lo - sh.first) / per;
-    u.at = sh.first + u.h * per;
+    u.h = (lo - sh.first) / sh.per;
+    u.at = sh.first + u.h * sh.per;
 #pragma unroll 1
-    for (u.qt = 0;; ++u.qt) {
-      u.tiles = tiles_of(u, g.group, u.qt);
-      if (lo < u.at + u.tiles || u.qt + 1 == u.units) break;
-      u.at += u.tiles;
+    for (int i = 0;; i += 32) {  // 32 units at once
+      const int mine = i + lane < u.units ? tiles_of(u, g.group, i + lane) : 0;
+      int sum = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(~0u, sum, o);
+        if (lane >= o) sum += x;
+      }
+      const unsigned past = __ballot_sync(~0u, lo < u.at + sum);
+      if (past || i + 32 >= u.units) {
+        const int l = past ? __ffs(past) - 1 : 0;
+        u.qt = i + l;
+        u.tiles = __shfl_sync(~0u, mine, l);
+        u.at += __shfl_sync(~0u, sum - mine, l);
+        break;
+      }
+      u.at += __shfl_sync(~0u, sum, 31);
     }
   }
 
@@ -459,69 +490,75 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = max(0, it - L::kStages); i < it; ++i)
       if (!bar_wait(&sh.full[i % L::kStages], (i / L::kStages) & 1, gave_up)) break;
   } else if (warp == kMmaWarp) {
-    // ---- one warp issues the products
-    int it = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
-    const uint32_t what_qk = what_mma<T>(kTile, false), what_pv = what_mma<T>(D, true);
-    bool ok = works;
-    while (ok && u.at < hi) {
-      const Piece p = piece_of(u, lo, hi);
-      const bool both = p.n[1] > 0;
-      // ring places of the stream's operand: shared by the streams of a wide piece, in order otherwise
-      const int base = it;
-      auto place = [&](int s, int i, bool v) { return p.wide ? base + 2 * i + v : it++; };
-      auto done = [&](int s) { return !p.wide || s == 1 || !both; };  // the operand's last use
-      auto qk = [&](int s, int i) {
-        if (i >= p.n[s]) return true;
-        const int at = place(s, i, false), st = at % L::kStages;
-        if (i == 0 && !bar_wait(&sh.q_ready[s], n_q[s]++ & 1, gave_up)) return false;
-        if (!bar_wait(&sh.full[st], (at / L::kStages) & 1, gave_up)) return false;
+    // ---- one thread issues the products, with as little as can be between them
+    if (works && elected()) {
+      const uint32_t what_qk = what_mma<T>(kTile, false), what_pv = what_mma<T>(D, true);
+      int st = 0, ph = 0;               // the next item of the ring and its phase
+      int n_q[2] = {0, 0}, n_p[2] = {0, 0};
+      auto step = [&](int& a, int& b) {
+        if (++a == L::kStages) a = 0, b ^= 1;
+      };
+      auto qk = [&](int s, bool first, bool last, int at, int phase, bool release) {
+        if (first && !bar_wait1(&sh.q_ready[s], n_q[s]++ & 1, gave_up)) return false;
+        if (!bar_wait1(&sh.full[at], phase, gave_up)) return false;
         tm_after();
-        if (elected()) {
-          const uint32_t a = q_at + s * L::kTileBytes, b = ring + st * L::kTileBytes;
+        const uint32_t a = q_at + s * L::kTileBytes, b = ring + at * L::kTileBytes;
 #pragma unroll
-          for (int x = 0; x < D / 16; ++x) {
-            const uint32_t at16 = (x / 4) * (kTile * 128) + (x % 4) * 32;
-            mma_ss(tmem + L::kS + s * 128, operand(a + at16, 16), operand(b + at16, 16), what_qk, x > 0);
+        for (int x = 0; x < D / 16; ++x) {
+          const uint32_t at16 = (x / 4) * (kTile * 128) + (x % 4) * 32;
+          mma_ss(tmem + L::kS + s * 128, operand(a + at16, 16), operand(b + at16, 16), what_qk, x > 0);
+        }
+        tm_commit(&sh.s_ready[s]);
+        if (release) tm_commit(&sh.empty[at]);
+        if (last) tm_commit(&sh.q_free[s]);
+        return true;
+      };
+      auto pv = [&](int s, bool first, bool last, int at, int phase, bool release) {
+        if (!bar_wait1(&sh.full[at], phase, gave_up)) return false;
+        if (!bar_wait1(&sh.p_ready[s], n_p[s]++ & 1, gave_up)) return false;
+        tm_after();
+        const uint32_t b = ring + at * L::kTileBytes;
+#pragma unroll
+        for (int x = 0; x < kTile / 16; ++x)
+          mma_ts(tmem + L::kO + s * D, tmem + L::kP + s * L::kPStep + x * 8, operand(b + x * 2048, kTile * 128), what_pv,
+                 !first || x > 0);
+        if (last) tm_commit(&sh.o_ready[s]);
+        if (release) tm_commit(&sh.empty[at]);
+        return true;
+      };
+      bool ok = true;
+#pragma unroll 1
+      while (ok && u.at < hi) {
+        const Piece p = piece_of(u, lo, hi);
+        if (p.wide) {
+          const int n = p.n[0];
+          const bool both = p.n[1] > 0;
+          ok = qk(0, true, n == 1, st, ph, !both) && (!both || qk(1, true, n == 1, st, ph, true));
+#pragma unroll 1
+          for (int i = 0; ok && i < n; ++i) {
+            step(st, ph);
+            const int v = st, vp = ph;
+            step(st, ph);
+            const bool last = i + 1 == n;
+            ok = pv(0, i == 0, last, v, vp, !both) && (last || qk(0, false, i + 2 == n, st, ph, !both));
+            if (ok && both) ok = pv(1, i == 0, last, v, vp, true) && (last || qk(1, false, i + 2 == n, st, ph, true));
           }
-          tm_commit(&sh.s_ready[s]);
-          if (done(s)) tm_commit(&sh.empty[st]);
-          if (i + 1 == p.n[s]) tm_commit(&sh.q_free[s]);
+        } else {
+          const int n = p.t1 - p.t0;
+#pragma unroll 1
+          for (int x = -2; ok && x < 2 * n; ++x) {  // K0 K1 V0 K2 V1 K3 ..., the even tiles to stream 0, the odd ones to 1
+            const bool v = x >= 0 && !(x & 1);
+            const int t = x < 0 ? x + 2 : x / 2 + (v ? 0 : 2);
+            if (t >= n) continue;
+            ok = v ? pv(t & 1, t < 2, t + 2 >= n, st, ph, true)
+                   : qk(t & 1, t < 2, t + 2 >= n, st, ph, true);
+            step(st, ph);
+          }
         }
-        __syncwarp();
-        return true;
-      };
-      auto pv = [&](int s, int i) {
-        if (i >= p.n[s]) return true;
-        const int at = place(s, i, true), st = at % L::kStages;
-        if (!bar_wait(&sh.full[st], (at / L::kStages) & 1, gave_up)) return false;
-        const uint32_t b = ring + st * L::kTileBytes;
-        // values past the row's last token are not the row's: 0 times their bits may be NaN
-        const int t = p.wide ? p.t0 + i : p.t0 + 2 * i + s, rows = u.len + u.n - t * kTile;
-        if (rows < kTile && (s == 0 || !p.wide)) {
-          for (int x = rows * 8 + lane; x < kTile * 8; x += 32)
-            for (int half = 0; half < D / 64; ++half)
-              *reinterpret_cast<uint4*>(tiles + (b - q_at) + half * (kTile * 128) + x * 16) = make_uint4(0, 0, 0, 0);
-          async_fence();
-          __syncwarp();
-        }
-        if (!bar_wait(&sh.p_ready[s], n_p[s]++ & 1, gave_up)) return false;
-        tm_after();
-        if (elected()) {
-#pragma unroll
-          for (int x = 0; x < kTile / 16; ++x)
-            mma_ts(tmem + L::kO + s * D, tmem + L::kP + s * L::kPStep + x * 8, operand(b + x * 2048, kTile * 128), what_pv,
-                   i > 0 || x > 0);
-          if (done(s)) tm_commit(&sh.empty[st]);
-          if (i + 1 == p.n[s]) tm_commit(&sh.o_ready[s]);
-        }
-        __syncwarp();
-        return true;
-      };
-      ok = qk(0, 0) && qk(1, 0);
-      for (int i = 0; ok && i < p.n[0]; ++i) ok = pv(0, i) && qk(0, i + 1) && pv(1, i) && qk(1, i + 1);
-      if (p.wide) it = base + 2 * p.n[0];
-      next_unit(g, u);
+        next_unit(g, u);
+      }
     }
+    __syncwarp();
   } else if (warp >= kQueryWarp) {
     // ---- two warps bring the next unit's queries as soon as the last product has read the ones before
     constexpr int kPer = D / 8;  // 16-byte parts of a query row, a lane each
@@ -569,7 +606,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t s_at = tmem + lanes + L::kS + s * 128, p_at = tmem + lanes + L::kP + s * L::kPStep;
     const uint32_t o_at = tmem + lanes + L::kO;
     const float sc = g.scale * kLog2e;
-    int n_s = 0, n_o[2] = {0, 0}, n_all = 0;
+    int n_s = 0, n_o[2] = {0, 0}, n_all = 0, items = 0;
     auto sync_all = [&]() {
       __syncwarp();
       if (lane == 0) bar_arrive(&sh.all);
@@ -583,6 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool warp_live = __any_sync(~0u, live);
       const int t = live ? row / g.group : u.n - 1, head = live ? u.h * g.group + row - t * g.group : 0;
       const int sees = u.len + t;  // the last position that the row's token sees
+      items += 2 * (p.t1 - p.t0);    // of the ring, up to the piece's end
       float m = -INFINITY, l = 0.f;  // the maximum is scaled: in exponents of two
       for (int i = 0; i < p.n[s]; ++i) {
         if (!bar_wait(&sh.s_ready[s], n_s++ & 1, gave_up)) {
@@ -652,6 +690,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
           tm_stored();
           tm_before();
+        }
+        if (i + 1 == p.n[s] && p.ends(u) && (p.wide ? s == 0 : ((p.t1 - p.t0 - 1) & 1) == s)) {
+          // values past the row's last token are not the row's, and 0 times their bits may be NaN: zeros in their place
+          // (the ring's place of the piece's last values cannot be taken again before their product)
+          const int st = (items - 1) % L::kStages, rows = u.len + u.n - (p.t1 - 1) * kTile;
+          ok = bar_wait(&sh.full[st], ((items - 1) / L::kStages) & 1, gave_up);
+          if (!ok) break;
+          for (int y = rows * 8 + r; y < kTile * 8; y += kTile)
+            for (int half = 0; half < D / 64; ++half)
+              *reinterpret_cast<uint4*>(tiles + (2 + st) * L::kTileBytes + half * (kTile * 128) + y * 16) = make_uint4(0, 0, 0, 0);
+          async_fence();
         }
         __syncwarp();
         if (lane == 0) bar_arrive(&sh.p_ready[s]);
