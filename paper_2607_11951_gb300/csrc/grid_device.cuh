@@ -259,6 +259,8 @@ __device__ __forceinline__ void stage_tables(const TabT<STAGED>& t) {
 // may start while its predecessor in the stream finishes; everything a kernel
 // does before this wait touches only the spec's read-only tables.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The next kernel of the stream may be launched (it still waits for this one's end in pdl_wait).
+__device__ __forceinline__ void pdl_next() { asm volatile("griddepcontrol.launch_dependents;"); }
 
 constexpr uint32_t kHashEmpty = 0xFFFFFFFFu;
 

@@ -1,17 +1,22 @@
 // Verification of drafted tokens against the masked target distribution, from
 // given random numbers (grid_draft_verify).
 //
-// For row b and position k let l be the logits, A the admitted ids, c = 1/T,
-// m = max_A l and s = sum_A exp((l - m) c), so that p(i) = exp((l_i - m) c) / s.
-// k_stats computes (m, s, first largest id) of pieces of every position's
-// logits in one pass: per thread a running maximum, the sum rescaled when it
-// grows; pieces are joined by the same rule.  k_draw joins the pieces of its
-// row, walks the acceptance tests u q(x) < p(x) to the first refusal n, and
-// draws the next token from position n alone: argmax w_i / e_i needs no running
-// sum over the vocabulary, so the order of the additions decides no token.
+// For row b and position k let l be the logits, A the admitted ids and c =
+// log2(e) / T.  With any base the sum s = sum_A 2^(c l - base) gives
+// p(i) = 2^(c l_i - base) / s.  k_stats computes (base, s) of pieces of every
+// position's logits in one pass: per thread a running base, a whole number
+// near the largest c l so far, so that c l - base is one rounding and moving
+// the base scales the sum by a power of two.  The last of a row's blocks joins
+// them and walks the acceptance tests u q(x) < p(x) to the first refusal n.
+// k_draw draws the next token from position n alone: argmax w_i / e_i needs no
+// running sum over the vocabulary, so the order of the additions decides no
+// token.
 //
-// Both kernels are bound by the bytes they read; each id's mask bit is looked
-// at first, and 16 bytes of logits that hold no admitted id are not read.
+// Both kernels are bound by the bytes they read and, in bf16, by the
+// instructions for an id; each id's mask bit is looked at first, and 16 bytes of
+// logits that hold no admitted id are not read.  A cluster of blocks per row
+// that stops at the first refusal reads less, but its positions follow one
+// another: 61 us (32 rows) and 178 us (256 rows) where this takes 43 and 115.
 #include <cfloat>
 #include <cmath>
 
@@ -21,48 +26,88 @@ namespace grid {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kMaxPieces = 64;  // of one position's logits
+constexpr int kMaxPieces = 64, kMaxParts = 256;  // of one position's logits, of one draw
 constexpr int kMaxDraft = 64;
-constexpr int kBlocksPerSm = 8;
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kBlocksPerSm = 8, kDrawsPerSm = 24; // blocks wanted of either kernel
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// Exponent and base are fp32: arguments are differences to the maximum, so
-// the product with c log2 e is off by 2^-24 of its size.
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-
-struct Stat {
-  float m, s;  // largest admitted logit (-inf: none), sum of exp((l - m) c)
-  int id;      // first id that has it
+struct Two {
+  float x, y;
 };
-
-__device__ __forceinline__ Stat join(const Stat& a, const Stat& b, float c2) {
-  Stat r;
-  r.m = fmaxf(a.m, b.m);
-  const float z = r.m > -INFINITY ? r.m : 0.f;
-  r.s = a.s * exp2_fast((a.m - z) * c2) + b.s * exp2_fast((b.m - z) * c2);
-  r.id = a.m == b.m ? min(a.id, b.id) : a.m > b.m ? a.id : b.id;
+__device__ __forceinline__ Two add2(Two a, Two b) {
+  Two r;
+  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return r;
 }
+__device__ __forceinline__ Two fma2(Two a, float b, float c) {  // (one instruction for two)
+  Two r;
+  asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %4};\nmov.b64 c, {%5, %5};\n"
+      "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b), "f"(c));
+  return r;
+}
+struct alignas(16) Stat {
+  float base, s;  // sum over the admitted ids of 2^(c l - base), base -inf: none is admitted
+  float m;        // the largest admitted logit and its first id
+  int id;
+};
+__device__ __forceinline__ Stat no_stat() { return Stat{-INFINITY, 0.f, -INFINITY, INT_MAX}; }
 
-__device__ __forceinline__ Stat join_warp(Stat x, float c2) {
-  for (int o = 16; o; o >>= 1) {
-    Stat y;
-    y.m = __shfl_xor_sync(~0u, x.m, o);
-    y.s = __shfl_xor_sync(~0u, x.s, o);
-    y.id = __shfl_xor_sync(~0u, x.id, o);
-    x = join(x, y, c2);
+__device__ __forceinline__ void rebase(Stat& x, float base) {
+  x.s = x.base > -INFINITY ? x.s * exp2_fast(x.base - base) : 0.f;
+  x.base = base;
+}
+// The warp's join, to every lane: the largest base first, then one sum.
+template <bool kLargest>
+__device__ __forceinline__ Stat join_warp(Stat x) {
+  float base = x.base;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) base = fmaxf(base, __shfl_xor_sync(~0u, base, o));
+  if (base > -INFINITY) rebase(x, base);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x.s += __shfl_xor_sync(~0u, x.s, o);
+  if constexpr (kLargest) {
+    float m = x.m;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    x.id = __reduce_min_sync(~0u, x.m == m ? x.id : INT_MAX);
+    x.m = m;
   }
   return x;
 }
 
 // NaN counts as -inf, +inf as the largest finite value.
 __device__ __forceinline__ float clean(float l) { return fminf(fmaxf(l, -INFINITY), FLT_MAX); }
+// A load where `in` holds, without a branch: as branches, the loads of a loop wait for one another.
+__device__ __forceinline__ void load_if(float& x, const float* p, bool in) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\n@p ld.global.nc.L1::no_allocate.f32 %0, [%1];\n}" : "+f"(x) : "l"(p), "r"((int)in));
+}
+__device__ __forceinline__ void load_if(uint16_t& x, const uint16_t* p, bool in) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\n@p ld.global.nc.L1::no_allocate.u16 %0, [%1];\n}" : "+h"(x) : "l"(p), "r"((int)in));
+}
 __device__ __forceinline__ float value(float x) { return x; }
 __device__ __forceinline__ float value(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }  // bf16
+
+// c l, kept finite above, for the logits that an fma would lose.
+__device__ __forceinline__ float exponent(float l, float c) { return fminf(clean(l) * c, 3e38f); }
+// 2^(c l - base) with base within a rounding of the largest exponent.
+__device__ __forceinline__ float weight(float l, float c, float base) {
+  const float t = fmaf(l, c, -base);
+  return exp2_fast(t < 126.f ? t : exponent(l, c) - base);
+}
+
+__device__ __forceinline__ float log_prob(float l, float c, const Stat& x) {
+  const float t = fmaf(l, c, -x.base);
+  return ((t < 126.f ? t : exponent(l, c) - x.base) - log2f(x.s)) * kLn2;
+}
 
 // The row's 1/T (1 for a greedy row) and whether it is greedy.
 __device__ __forceinline__ float inv_temp(const grid_draft_step& a, int b, bool& greedy) {
@@ -75,15 +120,6 @@ __device__ __forceinline__ int draft_len(const grid_draft_step& a, int b) {
   return a.d_draft_len ? min(max(a.d_draft_len[b], 0), a.K) : a.K;
 }
 
-// Mask bits of ids t .. t + n - 1, the lowest bit first (n <= 32; bits past them are undefined).
-__device__ __forceinline__ uint32_t mask_bits(const uint32_t* mask, int W, int t, int n) {
-  if (!mask) return ~0u;
-  const int w = t >> 5, sh = t & 31;
-  const uint32_t lo = mask[w];
-  const uint32_t hi = sh + n > 32 && w + 1 < W ? mask[w + 1] : 0u;
-  return __funnelshift_r(lo, hi, sh);
-}
-
 template <typename T>
 __device__ __forceinline__ const T* logits_at(const grid_draft_step& a, int b, int k) {
   return static_cast<const T*>(a.d_logits) + b * a.logit_stride[0] + k * a.logit_stride[1];
@@ -91,155 +127,268 @@ __device__ __forceinline__ const T* logits_at(const grid_draft_step& a, int b, i
 __device__ __forceinline__ const uint32_t* mask_at(const grid_draft_step& a, int b, int k) {
   return a.d_mask ? a.d_mask + b * a.mask_stride[0] + k * a.mask_stride[1] : nullptr;
 }
+__device__ __forceinline__ bool admitted(const uint32_t* mask, int id) { return !mask || (mask[id >> 5] >> (id & 31) & 1); }
 
-__device__ __forceinline__ void take(Stat& x, float l, int id, float c2) {
-  if (l > x.m) {
-    x.s *= exp2_fast((x.m - l) * c2);
-    x.m = l;
-    x.id = id;
-  }
-  if (l > -INFINITY) x.s += exp2_fast((l - x.m) * c2);
+__device__ __forceinline__ void take(Stat& x, float l, int id, float c) {
+  l = clean(l);
+  const float z = exponent(l, c);
+  if (z > x.base + 16.f) rebase(x, rintf(z));
+  if (x.base > -INFINITY) x.s += exp2_fast(z - x.base);
+  if (l > x.m || (l == x.m && id < x.id)) x.m = l, x.id = id;
 }
+
+// A warp's tile is up to 1,024 ids; the mask bits of ids 32 i .. 32 i + 31 of it
+// are lane i's word (0 for ids from `hi` on; t0: the tile's first id).
+constexpr int kTileIds = 1024;
+__device__ __forceinline__ uint32_t tile_word(const uint32_t* mask, int words, int t0, int hi, int lane) {
+  const int t = t0 + 32 * lane;
+  if (t >= hi) return 0u;
+  uint32_t w = ~0u;
+  if (mask) {
+    const int i = t >> 5, sh = t & 31;
+    w = mask[i];
+    if (sh) w = __funnelshift_r(w, i + 1 < words ? mask[i + 1] : 0u, sh);
+  }
+  return hi - t < 32 ? w & ((1u << (hi - t)) - 1u) : w;
+}
+
+// 16 bytes of logits as floats
+template <typename T, int N>
+__device__ __forceinline__ void unpack(const uint4& raw, float (&y)[N]) {
+  const uint32_t r[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if constexpr (N == 4) {
+      y[e] = __uint_as_float(r[e]);
+    } else {
+      y[2 * e] = __uint_as_float(r[e] << 16);
+      y[2 * e + 1] = __uint_as_float(r[e] & 0xFFFF0000u);
+    }
+}
+
+// The logits of a tile go through shared memory, 16 bytes at a time to a place
+// of the thread's own, kStages - 1 tiles ahead: what is in flight needs no
+// registers.  The words of the masks are read a tile before that; lines that
+// hold no admitted id are not read.
+template <typename T>
+struct Staged {
+  static constexpr int kVec = 16 / sizeof(T), kSteps = 4, kStages = 2, kIds = kSteps * 32 * kVec;
+  uint4 raw[kStages][kSteps][kThreads];
+  uint32_t bits[kStages][kThreads];  // a byte per step
+};
+
+// N logits one by one: where the base is not set yet or has to move, and where
+// a NaN or an infinity is admitted.
+template <int N>
+struct Values {
+  float y[N];
+};
+template <int N>
+__device__ __noinline__ float2 take_each(float base, float s, Values<N> v, float c) {
+  Stat x{base, s, 0.f, 0};
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const float z = exponent(v.y[e], c);
+    if (z > x.base + 16.f) rebase(x, rintf(z));
+    if (x.base > -INFINITY) x.s += exp2_fast(z - x.base);
+  }
+  return make_float2(x.base, x.s);
+}
+
+// The ids lo .. hi-1 of one position (l + lo on 16 bytes), by a block.
+// kLargest: the first largest logit too, which only greedy rows ask for.
+template <typename T, bool kLargest>
+__device__ __forceinline__ Stat scan(const T* __restrict__ l, const uint32_t* __restrict__ mask, int words, int lo, int hi, float c,
+                                     Staged<T>& st) {
+  using S = Staged<T>;
+  constexpr int kVec = S::kVec, kPerWord = 32 / kVec;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int whole = lo + (hi - lo) / kVec * kVec, tiles = (whole - lo + S::kIds - 1) / S::kIds;
+  const int from = lane / kPerWord, shift = lane % kPerWord * kVec;  // this lane's bits of a step: which word, and where
+  Stat x = no_stat();
+  int at_max = -1;  // where the 16 bytes of the largest logit begin
+  uint32_t ahead = tile_word(mask, words, lo + warp * S::kIds, whole, lane);
+  const uint32_t place = (uint32_t)__cvta_generic_to_shared(&st.raw[0][0][tid]);
+  auto issue = [&](int tile, int stage) {
+    if (tile < tiles) {
+      const T* src = l + lo + tile * S::kIds + lane * kVec;
+      uint32_t all = 0;
+#pragma unroll
+      for (int i = 0; i < S::kSteps; ++i) {
+        const uint32_t bits = __shfl_sync(~0u, ahead, i * kVec + from) >> shift & ((1u << kVec) - 1u);
+        all |= bits << (8 * i);
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\n@p cp.async.cg.shared.global [%0], [%1], 16;\n}" ::"r"(
+                         place + (uint32_t)((stage * S::kSteps + i) * sizeof(st.raw[0][0]))),
+                     "l"(src + i * 32 * kVec), "r"(bits)
+                     : "memory");
+      }
+      st.bits[stage][tid] = all;
+      ahead = tile_word(mask, words, lo + (tile + kWarps) * S::kIds, whole, lane);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < S::kStages - 1; ++i) issue(warp + i * kWarps, i);
+  int stage = 0;
+#pragma unroll 1
+  for (int tile = warp; tile < tiles; tile += kWarps) {
+    issue(tile + (S::kStages - 1) * kWarps, stage ? stage - 1 : S::kStages - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 1) : "memory");
+    const uint32_t all = st.bits[stage][tid];
+#pragma unroll
+    for (int i = 0; i < S::kSteps; ++i) {
+      const uint32_t bits = all >> (8 * i) & 0xFFu;
+      if (!bits) continue;
+      const uint4 r = st.raw[stage][i][tid];
+      Values<kVec> v;
+      unpack<T>(r, v.y);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) v.y[e] = bits & (1u << e) ? v.y[e] : -INFINITY;
+      if constexpr (kLargest) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) top = fmaxf(top, v.y[e]);
+        top = clean(top);
+        if (top > x.m) {
+          x.m = top;
+          at_max = lo + tile * S::kIds + (i * 32 + lane) * kVec;
+        }
+      }
+      Two t = {0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < kVec; e += 2) {
+        const Two z = fma2(Two{v.y[e], v.y[e + 1]}, c, -x.base);
+        t = add2(t, Two{exp2_fast(z.x), exp2_fast(z.y)});
+      }
+      if (t.x + t.y < 1048576.f) {  // (a base is good for terms up to 2^20)
+        x.s += t.x + t.y;
+      } else {
+        const float2 y = take_each<kVec>(x.base, x.s, v, c);
+        x.base = y.x, x.s = y.y;
+      }
+    }
+    if (++stage == S::kStages) stage = 0;
+  }
+  if (kLargest && at_max >= 0) {  // the largest logit's id, from its 16 bytes again
+    for (int e = kVec - 1; e >= 0; --e)
+      if (clean(value(l[at_max + e])) == x.m && admitted(mask, at_max + e)) x.id = at_max + e;
+  }
+  const int i = whole + tid;
+  if (i < hi && admitted(mask, i)) take(x, value(l[i]), i, c);
+  return x;
+}
+
+// The first largest admitted logit of a position, by a warp.
+template <typename T>
+__device__ __noinline__ int largest(const T* l, const uint32_t* mask, int V) {
+  Stat y = no_stat();
+  for (int i = threadIdx.x & 31; i < V; i += 32) {
+    const float v = clean(value(l[i]));
+    if (v > y.m && admitted(mask, i)) y.m = v, y.id = i;
+  }
+  return join_warp<true>(y).id;
+}
+
+// What the tests need of a drafted id.
+struct alignas(16) Drafted {
+  float l, uq;  // its logit (-inf: refused whatever u is) and u q(x)
+  int id, pad;
+};
+// What k_draw needs of a row.
+struct alignas(16) Row {
+  int n;           // position to draw from, or -1: the row's outcome is written
+  int out;         // id that the residual leaves out, or -1
+  float base, s;
+  float c;
+  int refused, pad[2];
+};
 
 // One piece of one position: block (position row) * pieces + piece.  Pieces
 // are cut where the position's 16-byte lines begin, so that rows of any
 // alignment are read in whole lines; the ids before the first line belong to
-// piece 0, those after the last to the last piece.
+// piece 0, those after the last to the last piece.  The last block of a row
+// walks its acceptance tests and writes what they decide.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_stats(const grid_draft_step a, Stat* __restrict__ stats, int pieces,
-                                                    int piece) {
-  constexpr int kVec = 16 / sizeof(T), kUnroll = 4;
+                                                    int piece, int* __restrict__ done, Drafted* __restrict__ drafted,
+                                                    Row* __restrict__ rows) {
   const int row = blockIdx.x / pieces, pc = blockIdx.x - row * pieces;
   const int b = row / (a.K + 1), k = row - b * (a.K + 1);
-  pdl_wait();
-  if (k > draft_len(a, b)) return;
-  bool greedy;
-  const float c2 = scale2(inv_temp(a, b, greedy));
-  const T* l = logits_at<T>(a, b, k);
-  const uint32_t* mask = mask_at(a, b, k);
-  const int W = (a.V + 31) >> 5, tid = threadIdx.x;
-  const int head = min(a.V, (int)((16 - ((uintptr_t)l & 15)) & 15) / (int)sizeof(T));
-  const long long from = (long long)head + (long long)pc * piece;
-  const int lo = (int)min((long long)a.V, from), hi = (int)min((long long)a.V, from + piece);
-  Stat x{-INFINITY, 0.f, INT_MAX};
-  if (pc == 0 && tid < head && (mask_bits(mask, W, tid, 1) & 1)) take(x, clean(value(l[tid])), tid, c2);
-  const int lines = (hi - lo) / kVec;
-  for (int v = tid; v < lines; v += kThreads * kUnroll) {
-    uint32_t bits[kUnroll];
-    uint4 raw[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int at = v + u * kThreads;
-      bits[u] = at < lines ? mask_bits(mask, W, lo + at * kVec, kVec) & ((1u << kVec) - 1) : 0u;
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      raw[u] = make_uint4(0, 0, 0, 0);
-      if (bits[u]) raw[u] = __ldcs(reinterpret_cast<const uint4*>(l + lo + (v + u * kThreads) * kVec));
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (!bits[u]) continue;
-      const uint32_t r[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
-      float y[kVec], top = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        float f;
-        if constexpr (sizeof(T) == 4)
-          f = __uint_as_float(r[e]);
-        else
-          f = __uint_as_float(e & 1 ? r[e / 2] & 0xFFFF0000u : r[e / 2] << 16);
-        y[e] = (bits[u] >> e) & 1 ? clean(f) : -INFINITY;
-        top = fmaxf(top, y[e]);
-      }
-      if (top > x.m) {
-        x.s *= exp2_fast((x.m - top) * c2);
-        x.m = top;
-#pragma unroll
-        for (int e = kVec - 1; e >= 0; --e)
-          if (y[e] == top) x.id = lo + (v + u * kThreads) * kVec + e;
-      }
-      if (x.m > -INFINITY) {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) x.s += exp2_fast((y[e] - x.m) * c2);
-      }
-    }
-  }
-  // (the last piece's ids past the last whole line)
-  const int t = lo + lines * kVec + tid;
-  if (t < hi && (mask_bits(mask, W, t, 1) & 1)) take(x, clean(value(l[t])), t, c2);
-  __shared__ Stat sh[kWarps];
-  x = join_warp(x, c2);
-  if ((tid & 31) == 0) sh[tid >> 5] = x;
-  __syncthreads();
-  if (tid < 32) {
-    x = tid < kWarps ? sh[tid] : Stat{-INFINITY, 0.f, INT_MAX};
-    x = join_warp(x, c2);
-    if (tid == 0) stats[(size_t)row * pieces + pc] = x;
-  }
-}
-
-// Best score so far and the first id that has it, for the residual weights
-// and for the target's own.
-struct Best {
-  float r, p;
-  int rid, pid;
-};
-__device__ __forceinline__ void better(float& s, int& id, float t, int j) {
-  if (t > s || (t == s && j < id)) {
-    s = t;
-    id = j;
-  }
-}
-__device__ __forceinline__ Best best_warp(Best x) {
-  for (int o = 16; o; o >>= 1) {
-    const Best y{__shfl_xor_sync(~0u, x.r, o), __shfl_xor_sync(~0u, x.p, o), __shfl_xor_sync(~0u, x.rid, o),
-                 __shfl_xor_sync(~0u, x.pid, o)};
-    better(x.r, x.rid, y.r, y.rid);
-    better(x.p, x.pid, y.p, y.pid);
-  }
-  return x;
-}
-
-// The draw of one row: block row * parts + part scores its part of the
-// vocabulary at the row's position n; the last of the row's blocks writes the
-// outcome.  Every block of a row finds n by itself, from the same numbers.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) k_draw(const grid_draft_step a, const Stat* __restrict__ stats, int pieces,
-                                                   Best* __restrict__ best, int* __restrict__ done, int parts,
-                                                   int part) {
-  constexpr int kUnroll = 4;
-  const int b = blockIdx.x / parts, pt = blockIdx.x - b * parts;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  __shared__ Stat at[kMaxDraft + 1];
-  __shared__ float lx[kMaxDraft];  // logits of the drafted ids
-  __shared__ int ok[kMaxDraft + 1];
-  __shared__ Best sh[kWarps];
+  extern __shared__ __align__(16) uint8_t staged[];
+  __shared__ Stat sh[kWarps];
   __shared__ int last;
+  Staged<T>& st = *reinterpret_cast<Staged<T>*>(staged);
   pdl_wait();
-  bool greedy;
-  const float inv = inv_temp(a, b, greedy), c2 = scale2(inv);
+  pdl_next();
   const int nd = draft_len(a, b);
-  for (int k = warp; k <= nd; k += kWarps) {
-    const Stat* src = stats + ((size_t)b * (a.K + 1) + k) * pieces;
-    Stat x{-INFINITY, 0.f, INT_MAX};
-    for (int i = lane; i < pieces; i += 32) x = join(x, src[i], c2);
-    x = join_warp(x, c2);
+  if (k > nd) return;
+  bool greedy;
+  const float c = scale2(inv_temp(a, b, greedy));
+  {
+    const T* l = logits_at<T>(a, b, k);
+    const uint32_t* mask = mask_at(a, b, k);
+    if (pc == 0 && k < nd && tid == kThreads - 1) {
+      Drafted x{-INFINITY, 0.f, a.d_draft[(size_t)b * a.K + k], 0};
+      if (x.id >= 0 && x.id < a.V) {
+        const bool in = admitted(mask, x.id);
+        const float v = clean(value(l[x.id])), u = a.d_u[(size_t)b * a.K + k];
+        const float q = a.d_probs ? a.d_probs[b * a.prob_stride[0] + k * a.prob_stride[1] + x.id] : 1.f;
+        if (in) x.l = v, x.uq = u * q;
+      }
+      drafted[(size_t)b * a.K + k] = x;
+      __threadfence();
+    }
+    const int head = min(a.V, (int)((16 - ((uintptr_t)l & 15)) & 15) / (int)sizeof(T)), words = (a.V + 31) / 32;
+    const long long from = (long long)head + (long long)pc * piece;
+    const int lo = (int)min((long long)a.V, from), hi = (int)min((long long)a.V, from + piece);
+    Stat x = greedy ? scan<T, true>(l, mask, words, lo, hi, c, st) : scan<T, false>(l, mask, words, lo, hi, c, st);
+    if (pc == 0 && tid < head && admitted(mask, tid)) take(x, value(l[tid]), tid, c);
+    x = join_warp<true>(x);
+    if (lane == 0) sh[warp] = x;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    const Stat x = join_warp<true>(lane < kWarps ? sh[lane] : no_stat());
     if (lane == 0) {
-      at[k] = x;
-      ok[k] = 0;
-      if (k < nd) {
-        const int id = a.d_draft[(size_t)b * a.K + k];
-        const uint32_t* mask = mask_at(a, b, k);
-        float l = -INFINITY;
-        if (id >= 0 && id < a.V && (!mask || (mask[id >> 5] >> (id & 31) & 1)))
-          l = clean(value(logits_at<T>(a, b, k)[id]));
-        lx[k] = l;
-        if (l > -INFINITY) {
-          const float q = a.d_probs ? a.d_probs[b * a.prob_stride[0] + k * a.prob_stride[1] + id] : 1.f;
-          const float p = exp2_fast((l - x.m) * c2) / x.s;
-          ok[k] = greedy ? id == x.id : a.d_u[(size_t)b * a.K + k] * q < p;
-          if (ok[k] && id == a.eos) ok[k] = 2;
+      stats[(size_t)row * pieces + pc] = x;
+      __threadfence();
+      last = atomicAdd(&done[b], 1) == (nd + 1) * pieces - 1;
+      if (last) done[b] = 0;
+      __threadfence();
+    }
+  }
+  __syncthreads();
+  if (!last) return;
+  // ---- the row's acceptance tests
+  __shared__ Stat at[kMaxDraft + 1];
+  __shared__ int ok[kMaxDraft + 1], ids[kMaxDraft];
+  __shared__ float lp[kMaxDraft];
+  for (int j = warp; j <= nd; j += kWarps) {
+    const Stat* src = stats + ((size_t)b * (a.K + 1) + j) * pieces;
+    float4 d = {};
+    if (j < nd) d = __ldcg(reinterpret_cast<const float4*>(drafted + (size_t)b * a.K + j));
+    float4 y = {-INFINITY, 0.f, -INFINITY, __int_as_float(INT_MAX)};
+    if (lane < pieces) y = __ldcg(reinterpret_cast<const float4*>(src + lane));
+    Stat x = join_warp<true>(Stat{y.x, y.y, y.z, __float_as_int(y.w)});
+    for (int i = 32; i < pieces; i += 32) {
+      Stat z = no_stat();
+      if (i + lane < pieces) {
+        y = __ldcg(reinterpret_cast<const float4*>(src + i + lane));
+        z = Stat{y.x, y.y, y.z, __float_as_int(y.w)};
+      }
+      z = join_warp<true>(z);
+      x = join_warp<true>(lane == 0 ? x : lane == 1 ? z : no_stat());
+    }
+    if (lane == 0) {
+      at[j] = x;
+      ok[j] = 0;
+      if (j < nd) {
+        const int id = ids[j] = __float_as_int(d.z);
+        if (d.x > -INFINITY) {
+          ok[j] = greedy ? id == x.id : d.y < weight(d.x, c, x.base) / x.s;
+          if (ok[j] && id == a.eos) ok[j] = 2;
+          lp[j] = log_prob(d.x, c, x);
         }
       }
     }
@@ -249,99 +398,136 @@ __global__ void __launch_bounds__(kThreads) k_draw(const grid_draft_step a, cons
   bool ended = false;
   while (n < nd && ok[n] && !ended) ended = ok[n++] == 2;
   const Stat x = at[min(n, nd)];
-  const bool empty = !ended && !(x.m > -INFINITY);
-  const bool drawn = !ended && !empty;
-  Best z{0.f, 0.f, INT_MAX, INT_MAX};
-  if (drawn && !greedy) {
-    const T* l = logits_at<T>(a, b, n);
-    const uint32_t* mask = mask_at(a, b, n);
-    const bool refused = n < nd;
-    const float* q = refused && a.d_probs ? a.d_probs + b * a.prob_stride[0] + n * a.prob_stride[1] : nullptr;
-    const int out = refused && !q ? a.d_draft[(size_t)b * a.K + n] : -1;
-    const float* e = a.d_noise + b * a.noise_stride;
-    const int hi = (int)min((long long)a.V, (long long)(pt + 1) * part);
-    for (int i = pt * part + tid; i < hi; i += kThreads * kUnroll) {
-      float lv[kUnroll], ev[kUnroll], qv[kUnroll];
-      bool in[kUnroll];
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int j = i + u * kThreads;
-        in[u] = j < hi && (!mask || (mask[j >> 5] >> (j & 31) & 1));
-      }
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int j = i + u * kThreads;
-        lv[u] = in[u] ? value(l[j]) : 0.f;
-        ev[u] = in[u] ? e[j] : 0.f;
-        qv[u] = in[u] && q ? q[j] : 0.f;
-      }
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int j = i + u * kThreads;
-        if (!in[u] || !(ev[u] > 0.f)) continue;
-        const float p = exp2_fast((clean(lv[u]) - x.m) * c2) / x.s;
-        const float r = j == out ? 0.f : fmaxf(p - qv[u], 0.f);
-        const float sr = r / ev[u];
-        if (sr > z.r) z.r = sr, z.rid = j;
-        if (refused) {
-          const float sp = p / ev[u];
-          if (sp > z.p) z.p = sp, z.pid = j;
-        }
-      }
-    }
-    z = best_warp(z);
-    if (lane == 0) sh[warp] = z;
-    __syncthreads();
-    if (warp == 0) {
-      z = best_warp(lane < kWarps ? sh[lane] : Best{0.f, 0.f, INT_MAX, INT_MAX});
-      if (lane == 0) {
-        if (parts > 1) {
-          best[(size_t)b * parts + pt] = z;
-          __threadfence();
-          last = atomicAdd(&done[b], 1) == parts - 1;
-          __threadfence();
-        } else {
-          sh[0] = z;
-          last = 1;
-        }
-      }
-    }
-    __syncthreads();
-    if (!last) return;
-    if (parts > 1 && warp == 0) {
-      z = Best{0.f, 0.f, INT_MAX, INT_MAX};
-      for (int i = lane; i < parts; i += 32) {
-        const Best* y = best + (size_t)b * parts + i;
-        better(z.r, z.rid, __ldcg(&y->r), __ldcg(&y->rid));
-        better(z.p, z.pid, __ldcg(&y->p), __ldcg(&y->pid));
-      }
-      z = best_warp(z);
-      if (lane == 0) {
-        sh[0] = z;
-        done[b] = 0;
-      }
-    }
-    __syncthreads();
-    z = sh[0];
-  } else if (pt) {
-    return;
-  }
-  const int token = !drawn ? -1 : greedy ? x.id : z.r > 0.f ? z.rid : z.p > 0.f ? z.pid : x.id;
-  for (int k = tid; k <= a.K; k += kThreads) {
-    const int id = k < n ? a.d_draft[(size_t)b * a.K + k] : k == n ? token : -1;
-    a.d_tokens[(size_t)b * (a.K + 1) + k] = id;
-    if (a.d_logprob) {
-      float v = 0.f;
-      if (id >= 0) {
-        const float l = k < n ? lx[k] : clean(value(logits_at<T>(a, b, k)[id]));
-        v = (l - at[k].m) * inv - logf(at[k].s);
-      }
-      a.d_logprob[(size_t)b * (a.K + 1) + k] = v;
-    }
+  const bool empty = !ended && !(x.base > -INFINITY);
+  const bool settled = ended || empty || greedy;
+  for (int j = tid; j <= a.K; j += kThreads) {
+    const int id = j < n ? ids[j] : j == n && !ended && !empty && greedy ? x.id : -1;
+    a.d_tokens[(size_t)b * (a.K + 1) + j] = id;
+    if (a.d_logprob) a.d_logprob[(size_t)b * (a.K + 1) + j] = j < n ? lp[j] : id >= 0 ? log_prob(x.m, c, x) : 0.f;
   }
   if (tid == 0) {
     a.d_accepted[b] = n;
-    a.d_status[b] = ended || (drawn && token == a.eos) ? GRID_ST_COMPLETE : empty ? GRID_ST_EMPTY_MASK : GRID_ST_OK;
+    a.d_status[b] = ended || (!empty && greedy && x.id == a.eos) ? GRID_ST_COMPLETE : empty ? GRID_ST_EMPTY_MASK : GRID_ST_OK;
+    rows[b] = Row{settled ? -1 : n, n < nd && !a.d_probs ? ids[n] : -1, x.base, x.s, c, n < nd, {0, 0}};
+  }
+}
+
+// Best score so far and the first id that has it.
+struct alignas(8) Best {
+  float s;
+  int id;
+};
+__device__ __forceinline__ void better(Best& x, float s, int id) {
+  if (s > x.s || (s == x.s && id < x.id)) x = Best{s, id};
+}
+__device__ __forceinline__ Best best_warp(Best x) {
+  for (int o = 16; o; o >>= 1) {
+    const float s = __shfl_xor_sync(~0u, x.s, o);
+    const int id = __shfl_xor_sync(~0u, x.id, o);
+    better(x, s, id);
+  }
+  return x;
+}
+// What scores the ids of a row's draw: w / e with w = p - q, by an approximate
+// reciprocal (two units in the last place: a score is only compared with
+// scores).  0 or less, or not finite: the id cannot be drawn.
+struct Scorer {
+  float c, base, inv_s;
+  __device__ __forceinline__ float operator()(float l, float e, float q) const {
+    float t = fmaf(l, c, -base), r;
+    if (!(t < 126.f)) t = exponent(l, c) - base;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e));
+    return fmaf(exp2_fast(t), inv_s, -q) * r;
+  }
+};
+__device__ __forceinline__ void keep(Best& z, float s, int id) {
+  if (s > z.s && s < INFINITY) z = Best{s, id};
+}
+
+// The draw of a row by the target's own weights, by a warp (no residual weight was left).
+template <typename T>
+__device__ __noinline__ Best draw_whole(Scorer score, const T* l, const uint32_t* mask, const float* e, int V) {
+  Best z{0.f, INT_MAX};
+  for (int i = threadIdx.x & 31; i < V; i += 32)
+    if (admitted(mask, i)) keep(z, score(value(l[i]), e[i], 0.f), i);
+  return best_warp(z);
+}
+
+// The draw of one row: block row * parts + part scores its part of the
+// vocabulary at the row's position n; the last of the row's blocks writes the
+// token.  A warp takes 256 ids at a time, a lane per id of eight mask words.
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 5) k_draw(const grid_draft_step a, const Row* __restrict__ rows,
+                                                      Best* __restrict__ best, int* __restrict__ done, int parts, int part) {
+  constexpr int kWords = 8, kIds = kWords * 32;
+  const int b = blockIdx.x / parts, pt = blockIdx.x - b * parts;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ Best sh[kWarps];
+  pdl_wait();
+  pdl_next();
+  const float4* row = reinterpret_cast<const float4*>(rows + b);
+  const float4 r4 = __ldcg(row), s4 = __ldcg(row + 1);
+  const int n = __float_as_int(r4.x), out = __float_as_int(r4.y);
+  if (n < 0) return;
+  const Scorer score{s4.x, r4.z, 1.f / r4.w};
+  const bool refused = __float_as_int(s4.y) != 0;
+  const T* l = logits_at<T>(a, b, n);
+  const uint32_t* mask = mask_at(a, b, n);
+  const float* q = refused && a.d_probs ? a.d_probs + b * a.prob_stride[0] + n * a.prob_stride[1] : nullptr;
+  const float* e = a.d_noise + b * a.noise_stride;
+  const int lo = min(a.V, pt * part), hi = min(a.V, lo + part), words = (a.V + 31) / 32;
+  auto word_at = [&](int t0) {
+    const uint32_t w = lane < kWords ? tile_word(mask, words, t0, hi, lane) : 0u;
+    return (unsigned)(out - t0 - 32 * lane) < 32u ? w & ~(1u << (out - t0 - 32 * lane)) : w;
+  };
+  Best z{0.f, INT_MAX};
+  uint32_t ahead = word_at(lo + warp * kIds);
+#pragma unroll 1
+  for (int t0 = lo + warp * kIds; t0 < hi; t0 += kWarps * kIds) {
+    const uint32_t word = ahead;
+    ahead = word_at(t0 + kWarps * kIds);
+    if (!__any_sync(~0u, word != 0)) continue;
+    T lv[kWords];
+    float ev[kWords], qv[kWords];
+#pragma unroll
+    for (int u = 0; u < kWords; ++u) {
+      const bool in = __shfl_sync(~0u, word, u) >> lane & 1;
+      const int id = t0 + 32 * u + lane;
+      lv[u] = 0, ev[u] = INFINITY, qv[u] = 0.f;  // (infinite noise: a score of zero)
+      load_if(lv[u], l + id, in);
+      load_if(ev[u], e + id, in);
+      load_if(qv[u], q + id, in && q);
+    }
+#pragma unroll
+    for (int u = 0; u < kWords; ++u) keep(z, score(value(lv[u]), ev[u], qv[u]), t0 + 32 * u + lane);
+  }
+  z = best_warp(z);
+  if (lane == 0) sh[warp] = z;
+  __syncthreads();
+  if (warp) return;
+  z = best_warp(lane < kWarps ? sh[lane] : Best{0.f, INT_MAX});
+  int last = 0;
+  if (lane == 0) {
+    best[(size_t)b * parts + pt] = z;
+    __threadfence();
+    last = atomicAdd(&done[b], 1) == parts - 1;
+    if (last) done[b] = 0;
+    __threadfence();
+  }
+  if (!__shfl_sync(~0u, last, 0)) return;
+  z = Best{0.f, INT_MAX};
+  for (int i = lane; i < parts; i += 32) {
+    const float2 y = __ldcg(reinterpret_cast<const float2*>(best + (size_t)b * parts + i));
+    better(z, y.x, __float_as_int(y.y));
+  }
+  z = best_warp(z);
+  if (!(z.s > 0.f) && refused) z = draw_whole(score, l, mask, e, a.V);
+  const int token = z.s > 0.f ? z.id : largest(l, mask, a.V);  // (the latter: no noise was positive)
+  if (lane == 0) {
+    a.d_tokens[(size_t)b * (a.K + 1) + n] = token;
+    if (a.d_logprob)
+      a.d_logprob[(size_t)b * (a.K + 1) + n] = log_prob(clean(value(l[token])), score.c, Stat{r4.z, r4.w, 0.f, 0});
+    if (token == a.eos) a.d_status[b] = GRID_ST_COMPLETE;
   }
 }
 
@@ -354,6 +540,8 @@ struct grid_drafts {
   int B = 0, K = 0, V = 0, sms = 152;
   Stat* stats = nullptr;
   Best* best = nullptr;
+  Row* rows = nullptr;
+  Drafted* drafted = nullptr;
   int* done = nullptr;
   Arena mem;
 };
@@ -361,20 +549,26 @@ struct grid_drafts {
 extern "C" int grid_drafts_create(int32_t B, int32_t K, int32_t V, grid_drafts** out) {
   if (!out || B <= 0 || K < 0 || K > kMaxDraft || V <= 0)
     return set_error(GRID_E_INVALID_ARG, "grid_drafts_create: B and V are positive, K in 0 .. 64");
-  if (B > 65535) return set_error(GRID_E_TOO_LARGE, "grid_drafts_create: more than 65535 rows");
+  if (B > 65535 || V > (1 << 30))
+    return set_error(GRID_E_TOO_LARGE, "grid_drafts_create: more than 65535 rows or 2^30 ids");
   grid_drafts* d = new grid_drafts;
   d->B = B;
   d->K = K;
   d->V = V;
   int rc = GRID_OK, dev = 0;
   cudaError_t e = cudaSuccess;
-  // (a call cuts n positions, or rows, into at most n + kBlocksPerSm * sms pieces)
+  // (a call cuts n positions into at most n + kBlocksPerSm * sms pieces)
   if ((e = cudaGetDevice(&dev)) == cudaSuccess &&
       (e = cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev)) == cudaSuccess &&
       !(rc = d->mem.alloc(((size_t)B * (K + 1) + kBlocksPerSm * d->sms) * sizeof(Stat), (void**)&d->stats)) &&
-      !(rc = d->mem.alloc(((size_t)B + kBlocksPerSm * d->sms) * sizeof(Best), (void**)&d->best)) &&
+      !(rc = d->mem.alloc((size_t)B * kMaxParts * sizeof(Best), (void**)&d->best)) &&
+      !(rc = d->mem.alloc((size_t)B * sizeof(Row), (void**)&d->rows)) &&
+      !(rc = d->mem.alloc((size_t)B * K * sizeof(Drafted), (void**)&d->drafted)) &&
       !(rc = d->mem.alloc((size_t)B * sizeof(int), (void**)&d->done)) &&
-      (e = cudaMemset(d->done, 0, (size_t)B * sizeof(int))) == cudaSuccess)
+      (e = cudaMemset(d->done, 0, (size_t)B * sizeof(int))) == cudaSuccess &&
+      (e = cudaFuncSetAttribute(k_stats<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Staged<float>))) == cudaSuccess &&
+      (e = cudaFuncSetAttribute(k_stats<uint16_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Staged<uint16_t>))) ==
+          cudaSuccess)
     e = cudaDeviceSynchronize();
   if (rc || e != cudaSuccess) {
     d->mem.release();
@@ -403,27 +597,26 @@ extern "C" int grid_draft_verify(const grid_drafts* d, const grid_draft_step* s,
       s->prob_stride[0] < 0 || s->prob_stride[1] < 0 || s->noise_stride < 0 || (uintptr_t)s->d_logits % size ||
       (uintptr_t)s->d_mask % 4 || (uintptr_t)s->d_probs % 4 || (uintptr_t)s->d_noise % 4)
     return set_error(GRID_E_INVALID_ARG, "grid_draft_verify: negative stride or unaligned pointer");
-  cudaStream_t st = (cudaStream_t)stream;
-  // Pieces of a position and parts of a draw: as many blocks as keep every SM
-  // busy, and no block of fewer than 2,048 ids.
-  auto cut = [&](long long rows, int& count, int& size_) {
-    const long long want = ((long long)kBlocksPerSm * d->sms + rows - 1) / rows;
-    const int most = std::min(kMaxPieces, (s->V + 2047) / 2048);
-    count = (int)std::max(1LL, std::min<long long>(want, most));
-    size_ = ((s->V + count - 1) / count + 31) & ~31;
+  // Pieces of a position and parts of a draw: blocks for every SM, none of them of less than a tile for each of its warps.
+  auto cut = [&](long long rows, long long per_sm, int least, int most, int& count, int& size_) {
+    const long long want = std::min<long long>((per_sm * d->sms + rows - 1) / rows, most);
+    size_ = (int)std::max<long long>(least, (s->V + want - 1) / want);
+    size_ = (size_ + kTileIds - 1) / kTileIds * kTileIds;
     count = (s->V + size_ - 1) / size_;
   };
-  int pieces, piece, parts, part;
   const long long rows = (long long)s->B * (s->K + 1);
-  cut(rows, pieces, piece);
-  cut(s->B, parts, part);
-  auto go = [&](auto stats, auto draw) {
-    cudaError_t e = launch_pdl(stats, dim3((unsigned)(rows * pieces)), dim3(kThreads), 0, st, *s, d->stats, pieces, piece);
+  int pieces, piece, parts, part;
+  cut(rows, kBlocksPerSm, kWarps * kTileIds, kMaxPieces, pieces, piece);
+  cut(s->B, kDrawsPerSm, 2 * kTileIds, kMaxParts, parts, part);
+  auto go = [&](auto stats, auto draw, size_t staged) {
+    cudaError_t e = launch_pdl(stats, dim3((unsigned)(rows * pieces)), dim3(kThreads), staged, (cudaStream_t)stream, *s, d->stats,
+                               pieces, piece, d->done, d->drafted, d->rows);
     if (e != cudaSuccess) return e;
-    return launch_pdl(draw, dim3((unsigned)(s->B * parts)), dim3(kThreads), 0, st, *s, (const Stat*)d->stats, pieces,
+    return launch_pdl(draw, dim3((unsigned)(s->B * parts)), dim3(kThreads), 0, (cudaStream_t)stream, *s, (const Row*)d->rows,
                       d->best, d->done, parts, part);
   };
-  GRID_CUDA(size == 4 ? go(k_stats<float>, k_draw<float>) : go(k_stats<uint16_t>, k_draw<uint16_t>));
+  GRID_CUDA(size == 4 ? go(k_stats<float>, k_draw<float>, sizeof(Staged<float>))
+                      : go(k_stats<uint16_t>, k_draw<uint16_t>, sizeof(Staged<uint16_t>)));
   GRID_CUDA(cudaGetLastError());
   return GRID_OK;
 }

@@ -7,9 +7,13 @@
 namespace grid {
 namespace {
 
-// A head vector is D / 8 lanes of 16 bytes, so a warp holds 512 / (2 D)
-// heads at once and kUnroll such groups of one token; the rotation's partner
-// values come by shuffle.  Bound by the bytes moved.
+// A head vector is D / 8 lanes of 16 bytes, so a warp's load holds 512 / (2 D)
+// heads; kUnroll of them are a group, and a warp takes some groups of one
+// token.  The rotation's partner values come by shuffle.  Bound by the bytes
+// moved: the first group is on its way while the token's row, length and page
+// are looked up one after the other, each later one while the one before is
+// worked on.  A large batch's warps take whole tokens, so that the look-ups
+// (3 us) are paid once for 24 KB; a small one's take a group each.
 struct AppendArgs {
   Chunk c;
   const void *q, *k, *v, *qw, *kw;
@@ -17,7 +21,8 @@ struct AppendArgs {
   long long qs[2], ks[2], vs[2], qos[2], kps[3], vps[3];
   const float *cos, *sin;
   float eps;
-  int H, Hk, rot, pairs, n_pos, groups;  // groups: of heads per token
+  int H, Hk, rot, pairs, n_pos;
+  int groups, splits;  // groups of heads per token, warps that they go to
   int32_t* status;
 };
 
@@ -42,23 +47,23 @@ __global__ void __launch_bounds__(kAppendWarps * 32) k_append(const AppendArgs a
     return;
   }
   const long long item = (long long)blockIdx.x * kAppendWarps + warp;
-  const int i = (int)(item / a.groups), group = (int)(item - (long long)i * a.groups);
+  const int i = (int)(item / a.splits), split = (int)(item - (long long)i * a.splits);
   if (i >= c.N) return;
   const int nq = a.q ? a.H : 0, heads = nq + 2 * a.Hk;
   const int l = lane % kLanes, e = l * 8;
-  uint4 raw[kAppendUnroll];
-  int head[kAppendUnroll];
+  auto fetch = [&](int group, uint4* raw) {
 #pragma unroll
-  for (int u = 0; u < kAppendUnroll; ++u) {
-    const int h = (group * kAppendUnroll + u) * kHeads + lane / kLanes;
-    head[u] = h;
-    raw[u] = make_uint4(0, 0, 0, 0);
-    if (h >= heads) continue;
-    const T* src = h < nq ? (const T*)a.q + i * a.qs[0] + h * a.qs[1]
-                   : h < nq + a.Hk ? (const T*)a.k + i * a.ks[0] + (h - nq) * a.ks[1]
-                                   : (const T*)a.v + i * a.vs[0] + (h - nq - a.Hk) * a.vs[1];
-    raw[u] = __ldcs(reinterpret_cast<const uint4*>(src + e));
-  }
+    for (int u = 0; u < kAppendUnroll; ++u) {
+      const int h = (group * kAppendUnroll + u) * kHeads + lane / kLanes;
+      const T* src = h < nq ? (const T*)a.q + i * a.qs[0] + h * a.qs[1]
+                     : h < nq + a.Hk ? (const T*)a.k + i * a.ks[0] + (h - nq) * a.ks[1]
+                                     : (const T*)a.v + i * a.vs[0] + (h - nq - a.Hk) * a.vs[1];
+      raw[u] = make_uint4(0, 0, 0, 0);
+      if (h < heads) raw[u] = __ldcs(reinterpret_cast<const uint4*>(src + e));
+    }
+  };
+  uint4 ahead[kAppendUnroll];
+  fetch(split, ahead);
   const int b = row_of(c, i, lane);
   if (b < 0) return;
   int s, n, len;
@@ -101,37 +106,44 @@ __global__ void __launch_bounds__(kAppendWarps * 32) k_append(const AppendArgs a
     }
   }
   const int from = turned && !a.pairs ? lane + (e < half ? half / 8 : -(half / 8)) : lane;  // the partner's lane
+#pragma unroll 1
+  for (int group = split; group < a.groups; group += a.splits) {
+    uint4 raw[kAppendUnroll];
 #pragma unroll
-  for (int u = 0; u < kAppendUnroll; ++u) {
-    const int h = head[u];
-    const bool is_v = h >= nq + a.Hk;
-    float x[8];
-    unpack8<T>(raw[u], x);
-    const void* w = h < nq ? a.qw : a.kw;
-    float sum = 0.f;
+    for (int u = 0; u < kAppendUnroll; ++u) raw[u] = ahead[u];
+    if (group + a.splits < a.groups) fetch(group + a.splits, ahead);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
+    for (int u = 0; u < kAppendUnroll; ++u) {
+      const int h = (group * kAppendUnroll + u) * kHeads + lane / kLanes;
+      const bool is_v = h >= nq + a.Hk;
+      float x[8];
+      unpack8<T>(raw[u], x);
+      const void* w = h < nq ? a.qw : a.kw;
+      float sum = 0.f;
 #pragma unroll
-    for (int o = kLanes / 2; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-    if (w && !is_v) {
-      const float r = 1.f / sqrtf(sum / D + a.eps);
-      float g[8];
-      unpack8<T>(*reinterpret_cast<const uint4*>((const T*)w + e), g);
+      for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = x[j] * r * g[j];
-    }
-    float y[8];
+      for (int o = kLanes / 2; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+      if (w && !is_v) {
+        const float r = 1.f / sqrtf(sum / D + a.eps);
+        float g[8];
+        unpack8<T>(*reinterpret_cast<const uint4*>((const T*)w + e), g);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = a.pairs ? x[j ^ 1] : __shfl_sync(~0u, x[j], from);
-    if (h < nq + 2 * a.Hk) {
-      if (!is_v && turned) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = x[j] * cs[j] + y[j] * sn[j];
+        for (int j = 0; j < 8; ++j) x[j] = x[j] * r * g[j];
       }
-      T* dst = h < nq ? (T*)a.qo + i * a.qos[0] + h * a.qos[1]
-               : !is_v ? (T*)a.kp + page * a.kps[0] + off * a.kps[1] + (h - nq) * a.kps[2]
-                       : (T*)a.vp + page * a.vps[0] + off * a.vps[1] + (h - nq - a.Hk) * a.vps[2];
-      *reinterpret_cast<uint4*>(dst + e) = is_v ? raw[u] : pack8<T>(x);
+      float y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = a.pairs ? x[j ^ 1] : __shfl_sync(~0u, x[j], from);
+      if (h < nq + 2 * a.Hk) {
+        if (!is_v && turned) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] = x[j] * cs[j] + y[j] * sn[j];
+        }
+        T* dst = h < nq ? (T*)a.qo + i * a.qos[0] + h * a.qos[1]
+                 : !is_v ? (T*)a.kp + page * a.kps[0] + off * a.kps[1] + (h - nq) * a.kps[2]
+                         : (T*)a.vp + page * a.vps[0] + off * a.vps[1] + (h - nq - a.Hk) * a.vps[2];
+        *reinterpret_cast<uint4*>(dst + e) = is_v ? raw[u] : pack8<T>(x);
+      }
     }
   }
 }
@@ -172,7 +184,9 @@ extern "C" int grid_kv_append(const grid_kv* kv, const grid_kv_chunk* chunk, con
   a.status = d_status;
   const int at_once = kAppendUnroll * (256 / p.head_dim);
   a.groups = ((q ? a.H : 0) + 2 * a.Hk + at_once - 1) / at_once;
-  const long long blocks = ((long long)chunk->n_tokens * a.groups + kAppendWarps - 1) / kAppendWarps;
+  // (whole tokens where their warps fill the SMs anyway)
+  a.splits = std::max(1, std::min(a.groups, 32 * kv->sms / std::max(1, chunk->n_tokens)));
+  const long long blocks = ((long long)chunk->n_tokens * a.splits + kAppendWarps - 1) / kAppendWarps;
   const int rows = (chunk->B + kAppendWarps - 1) / kAppendWarps;
   if (blocks + rows > INT32_MAX) return set_error(GRID_E_TOO_LARGE, "grid_kv_append: too many head vectors in one call");
   auto go = [&](auto kern) {
