@@ -8,21 +8,27 @@ namespace grid {
 namespace {
 
 // A head vector is D / 8 lanes of 16 bytes, so a warp's load holds 512 / (2 D)
-// heads; kUnroll of them are a group, and a warp takes some groups of one
-// token.  The rotation's partner values come by shuffle.  Bound by the bytes
-// moved: the first group is on its way while the token's row, length and page
-// are looked up one after the other, each later one while the one before is
-// worked on.  A large batch's warps take whole tokens, so that the look-ups
-// (3 us) are paid once for 24 KB; a small one's take a group each.
+// heads; kUnroll of them, all queries, all keys or all values, are a group, and
+// a warp takes some groups of one token.  With r = 1 / sqrt(mean(x^2) + eps),
+// weights w and the angle's c and s, a value is r (x_i (w_i c) + x_j (w_j s))
+// with x_j its partner, which comes by shuffle; the factors in brackets are the
+// token's own and made once for all of its heads.
+//
+// Bound by the bytes moved: the first group is on its way while the token's
+// row, length and page are looked up one after the other, each later one while
+// the one before is worked on.  A large batch's warps take whole tokens, so that
+// the look-ups (3 us) are paid once for 24 KB; a small one's take a group each.
 struct AppendArgs {
   Chunk c;
-  const void *q, *k, *v, *qw, *kw;
-  void *qo, *kp, *vp;
-  long long qs[2], ks[2], vs[2], qos[2], kps[3], vps[3];
+  const void* src[3];       // queries, keys, values
+  void* dst[3];             // queries out, the pools of keys and of values
+  const void* w[2];         // norm weights of queries and keys
+  long long ss[3][2], qos[2], ps[2][3];  // strides of src, of queries out and of the pools
   const float *cos, *sin;
   float eps;
   int H, Hk, rot, pairs, n_pos;
-  int groups, splits;  // groups of heads per token, warps that they go to
+  int groups[3];            // up to the last one of the queries, of the keys, of the values
+  int splits;               // warps that a token's groups go to
   int32_t* status;
 };
 
@@ -49,20 +55,18 @@ __global__ void __launch_bounds__(kAppendWarps * 32) k_append(const AppendArgs a
   const long long item = (long long)blockIdx.x * kAppendWarps + warp;
   const int i = (int)(item / a.splits), split = (int)(item - (long long)i * a.splits);
   if (i >= c.N) return;
-  const int nq = a.q ? a.H : 0, heads = nq + 2 * a.Hk;
-  const int l = lane % kLanes, e = l * 8;
+  const int e = lane % kLanes * 8, mine = lane / kLanes;
+  auto kind_of = [&](int group) { return group < a.groups[0] ? 0 : group < a.groups[1] ? 1 : 2; };
+  auto head_of = [&](int group, int kind) { return (group - (kind ? a.groups[kind - 1] : 0)) * kAppendUnroll * kHeads + mine; };
   auto fetch = [&](int group, uint4* raw) {
+    const int kind = kind_of(group), h = head_of(group, kind), heads = kind ? a.Hk : a.H;
+    const T* p = (const T*)a.src[kind] + i * a.ss[kind][0] + h * a.ss[kind][1] + e;
+    const long long step = kHeads * a.ss[kind][1];
 #pragma unroll
-    for (int u = 0; u < kAppendUnroll; ++u) {
-      const int h = (group * kAppendUnroll + u) * kHeads + lane / kLanes;
-      const T* src = h < nq ? (const T*)a.q + i * a.qs[0] + h * a.qs[1]
-                     : h < nq + a.Hk ? (const T*)a.k + i * a.ks[0] + (h - nq) * a.ks[1]
-                                     : (const T*)a.v + i * a.vs[0] + (h - nq - a.Hk) * a.vs[1];
-      raw[u] = make_uint4(0, 0, 0, 0);
-      if (h < heads) raw[u] = __ldcs(reinterpret_cast<const uint4*>(src + e));
-    }
+    for (int u = 0; u < kAppendUnroll; ++u)
+      if (h + u * kHeads < heads) raw[u] = __ldcs(reinterpret_cast<const uint4*>(p + u * step));
   };
-  uint4 ahead[kAppendUnroll];
+  uint4 ahead[kAppendUnroll] = {};
   fetch(split, ahead);
   const int b = row_of(c, i, lane);
   if (b < 0) return;
@@ -72,78 +76,88 @@ __global__ void __launch_bounds__(kAppendWarps * 32) k_append(const AppendArgs a
   if (a.cos && pos >= a.n_pos) return;
   const int page = page_of(c, b, pos);
   if (page < 0) return;
-  const int off = pos & ((1 << c.log_page) - 1);
-  // cosines and sines of this lane's values, -sin where the value is the first of its pair
-  float cs[8], sn[8];
+  const int off = pos & ((1 << c.log_page) - 1), half = a.rot / 2;
   const bool turned = a.cos && e < a.rot;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) cs[j] = 1.f, sn[j] = 0.f;
-  const int half = a.rot / 2;
-  if (turned) {
-    const float* ct = a.cos + (long long)pos * half;
-    const float* st = a.sin + (long long)pos * half;
-    if (a.pairs) {
-      const float4 x = *reinterpret_cast<const float4*>(ct + e / 2), y = *reinterpret_cast<const float4*>(st + e / 2);
-      const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        cs[2 * j] = cs[2 * j + 1] = xs[j];
-        sn[2 * j] = -ys[j];
-        sn[2 * j + 1] = ys[j];
-      }
-    } else {
-      const int m = e < half ? e : e - half;
-#pragma unroll
-      for (int j = 0; j < 8; j += 4) {
-        const float4 x = *reinterpret_cast<const float4*>(ct + m + j), y = *reinterpret_cast<const float4*>(st + m + j);
-        const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          cs[j + t] = xs[t];
-          sn[j + t] = e < half ? -ys[t] : ys[t];
-        }
-      }
-    }
-  }
-  const int from = turned && !a.pairs ? lane + (e < half ? half / 8 : -(half / 8)) : lane;  // the partner's lane
+  const int across = turned && !a.pairs ? (e < half ? half : -half) : 0;  // to the partner's value, where it is another lane's
+  const int from = lane + across / 8;
+  float wc[8], ws[8];  // w_i c and w_j s, s with the sign that it has for this value
+  int kind = -1;
 #pragma unroll 1
-  for (int group = split; group < a.groups; group += a.splits) {
+  for (int group = split; group < a.groups[2]; group += a.splits) {
     uint4 raw[kAppendUnroll];
 #pragma unroll
     for (int u = 0; u < kAppendUnroll; ++u) raw[u] = ahead[u];
-    if (group + a.splits < a.groups) fetch(group + a.splits, ahead);
+    if (group + a.splits < a.groups[2]) fetch(group + a.splits, ahead);
+    const bool changed = kind != kind_of(group);
+    kind = kind_of(group);
+    const int h = head_of(group, kind), heads = kind ? a.Hk : a.H;
+    T* dst = (T*)a.dst[kind] + e;
+    dst += kind ? page * a.ps[kind - 1][0] + off * a.ps[kind - 1][1] + h * a.ps[kind - 1][2] : i * a.qos[0] + h * a.qos[1];
+    const long long step = kHeads * (kind ? a.ps[kind - 1][2] : a.qos[1]);
+    if (kind == 2) {
+#pragma unroll
+      for (int u = 0; u < kAppendUnroll; ++u)
+        if (h + u * kHeads < heads) *reinterpret_cast<uint4*>(dst + u * step) = raw[u];
+      continue;
+    }
+    const T* w = (const T*)a.w[kind];
+    if (changed) {
+      float wp[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) wc[j] = wp[j] = 1.f, ws[j] = 0.f;
+      if (w) {
+        unpack8<T>(*reinterpret_cast<const uint4*>(w + e), wc);
+        unpack8<T>(*reinterpret_cast<const uint4*>(w + e + across), wp);
+      }
+      if (turned) {
+        const int m = a.pairs ? e / 2 : e < half ? e : e - half;
+        const float* ct = a.cos + (long long)pos * half + m;
+        const float* st = a.sin + (long long)pos * half + m;
+        float cs[8], sn[8];
+#pragma unroll
+        for (int j = 0; j < 8; j += 4) {
+          if (a.pairs && j) break;
+          const float4 x = *reinterpret_cast<const float4*>(ct + j), y = *reinterpret_cast<const float4*>(st + j);
+          cs[j] = x.x, cs[j + 1] = x.y, cs[j + 2] = x.z, cs[j + 3] = x.w;
+          sn[j] = y.x, sn[j + 1] = y.y, sn[j + 2] = y.z, sn[j + 3] = y.w;
+        }
+        float own[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) own[j] = wc[j];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (a.pairs) {
+            wc[j] = own[j] * cs[j / 2];
+            ws[j] = own[j ^ 1] * (j & 1 ? sn[j / 2] : -sn[j / 2]);
+          } else {
+            wc[j] = own[j] * cs[j];
+            ws[j] = wp[j] * (e < half ? -sn[j] : sn[j]);
+          }
+        }
+      }
+    }
 #pragma unroll
     for (int u = 0; u < kAppendUnroll; ++u) {
-      const int h = (group * kAppendUnroll + u) * kHeads + lane / kLanes;
-      const bool is_v = h >= nq + a.Hk;
-      float x[8];
+      float x[8], y[8], r = 1.f;
       unpack8<T>(raw[u], x);
-      const void* w = h < nq ? a.qw : a.kw;
-      float sum = 0.f;
+      if (w) {
+        float sum = x[0] * x[0];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
+        for (int j = 1; j < 8; ++j) sum = fmaf(x[j], x[j], sum);
 #pragma unroll
-      for (int o = kLanes / 2; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-      if (w && !is_v) {
-        const float r = 1.f / sqrtf(sum / D + a.eps);
-        float g[8];
-        unpack8<T>(*reinterpret_cast<const uint4*>((const T*)w + e), g);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = x[j] * r * g[j];
+        for (int o = kLanes / 2; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+        r = rsqrtf(sum * (1.f / D) + a.eps);
       }
-      float y[8];
+      if (a.cos && !a.pairs) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = a.pairs ? x[j ^ 1] : __shfl_sync(~0u, x[j], from);
-      if (h < nq + 2 * a.Hk) {
-        if (!is_v && turned) {
+        for (int j = 0; j < 8; ++j) y[j] = __shfl_sync(~0u, x[j], from);
+      } else {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = x[j] * cs[j] + y[j] * sn[j];
-        }
-        T* dst = h < nq ? (T*)a.qo + i * a.qos[0] + h * a.qos[1]
-                 : !is_v ? (T*)a.kp + page * a.kps[0] + off * a.kps[1] + (h - nq) * a.kps[2]
-                         : (T*)a.vp + page * a.vps[0] + off * a.vps[1] + (h - nq - a.Hk) * a.vps[2];
-        *reinterpret_cast<uint4*>(dst + e) = is_v ? raw[u] : pack8<T>(x);
+        for (int j = 0; j < 8; ++j) y[j] = x[j ^ 1];
       }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = (turned ? fmaf(x[j], wc[j], y[j] * ws[j]) : x[j] * wc[j]) * r;
+      if (h + u * kHeads < heads) *reinterpret_cast<uint4*>(dst + u * step) = pack8<T>(x);
     }
   }
 }
@@ -167,25 +181,23 @@ extern "C" int grid_kv_append(const grid_kv* kv, const grid_kv_chunk* chunk, con
     return set_error(GRID_E_INVALID_ARG, "grid_kv_append: bad norm");
   if (chunk->B > 65535) return set_error(GRID_E_TOO_LARGE, "grid_kv_append: more than 65535 rows");
   const grid_kv_pages& p = kv->p;
-  if (chunk->n_tokens) {
-    a.k = k->d, a.v = v->d;
-    a.ks[0] = k->token_stride, a.ks[1] = k->head_stride, a.vs[0] = v->token_stride, a.vs[1] = v->head_stride;
-    if (q) {
-      a.q = q->d, a.qo = q_out->d;
-      a.qs[0] = q->token_stride, a.qs[1] = q->head_stride;
-      a.qos[0] = q_out->token_stride, a.qos[1] = q_out->head_stride;
-    }
-  }
-  a.kp = p.d_k, a.vp = p.d_v;
-  for (int i = 0; i < 3; ++i) a.kps[i] = p.k_stride[i], a.vps[i] = p.v_stride[i];
+  const int at_once = kAppendUnroll * (256 / p.head_dim);
+  auto heads = [&](int kind, const grid_heads* h, int count) {
+    if (chunk->n_tokens && h) a.src[kind] = h->d, a.ss[kind][0] = h->token_stride, a.ss[kind][1] = h->head_stride;
+    a.groups[kind] = (kind ? a.groups[kind - 1] : 0) + (h ? (count + at_once - 1) / at_once : 0);
+  };
+  heads(0, q, p.n_heads);
+  heads(1, k, p.n_kv_heads);
+  heads(2, v, p.n_kv_heads);
+  if (q) a.dst[0] = q_out->d, a.qos[0] = q_out->token_stride, a.qos[1] = q_out->head_stride;
+  a.dst[1] = p.d_k, a.dst[2] = p.d_v;
+  for (int i = 0; i < 3; ++i) a.ps[0][i] = p.k_stride[i], a.ps[1][i] = p.v_stride[i];
   if (rot) a.cos = rot->d_cos, a.sin = rot->d_sin, a.rot = rot->rot, a.pairs = rot->pairs, a.n_pos = rot->n_pos;
-  if (norm) a.qw = norm->d_q, a.kw = norm->d_k, a.eps = norm->eps;
+  if (norm) a.w[0] = norm->d_q, a.w[1] = norm->d_k, a.eps = norm->eps;
   a.H = p.n_heads, a.Hk = p.n_kv_heads;
   a.status = d_status;
-  const int at_once = kAppendUnroll * (256 / p.head_dim);
-  a.groups = ((q ? a.H : 0) + 2 * a.Hk + at_once - 1) / at_once;
   // (whole tokens where their warps fill the SMs anyway)
-  a.splits = std::max(1, std::min(a.groups, 32 * kv->sms / std::max(1, chunk->n_tokens)));
+  a.splits = std::max(1, std::min(a.groups[2], 32 * kv->sms / std::max(1, chunk->n_tokens)));
   const long long blocks = ((long long)chunk->n_tokens * a.splits + kAppendWarps - 1) / kAppendWarps;
   const int rows = (chunk->B + kAppendWarps - 1) / kAppendWarps;
   if (blocks + rows > INT32_MAX) return set_error(GRID_E_TOO_LARGE, "grid_kv_append: too many head vectors in one call");
