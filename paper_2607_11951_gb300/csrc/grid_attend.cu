@@ -171,6 +171,81 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
+struct Two {
+  float x, y;
+};
+__device__ __forceinline__ Two fma2(Two a, float b, float c) {  // (one instruction for two)
+  Two r;
+  asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %4};\nmov.b64 c, {%5, %5};\n"
+      "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+  Two r;
+  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// The scores of N keys from column `at` on, those past `last` (of the N) as -inf.
+template <int N>
+__device__ __forceinline__ void load_scores(uint32_t at, int last, uint32_t (&x)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; j += 32) tm_load32(at + j, x + j);
+#pragma unroll
+  for (int j = 0; j < N; j += 32) tm_loaded(x + j);
+  if (last < N - 1) {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e > last) x[e] = 0xFF800000u;
+  }
+}
+// The largest score of a tile.
+template <int N>
+__device__ __forceinline__ float tile_max(uint32_t s_at, int last) {
+  float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+  for (int j = 0; j < kTile; j += N) {
+    uint32_t x[N];
+    load_scores<N>(s_at + j, last - j, x);
+#pragma unroll
+    for (int e = 0; e < N; e += 2) top[e / 2 & 3] = max3(top[e / 2 & 3], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+  }
+  return fmaxf(max3(top[0], top[1], top[2]), top[3]);
+}
+// A tile's probabilities 2^(sc s - base), to tensor memory; returns their sum.  half() is called once those of the
+// first 64 keys are there.
+template <typename T, int N, typename Half>
+__device__ __forceinline__ float tile_exp(uint32_t s_at, uint32_t p_at, int last, float sc, float base, Half half) {
+  Two sum[2] = {};
+#pragma unroll 1
+  for (int j = 0; j < kTile; j += N) {
+    uint32_t x[N];
+    load_scores<N>(s_at + j, last - j, x);
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+      Two a = fma2(Two{__uint_as_float(x[e]), __uint_as_float(x[e + 1])}, sc, -base);
+      a = Two{exp2_fast(a.x), exp2_fast(a.y)};
+      sum[e / 2 & 1] = add2(sum[e / 2 & 1], a);
+      x[e / 2] = pack_of(a.x, a.y, T());
+    }
+    // (where the probabilities lie over the scores, these columns were read before)
+#pragma unroll
+    for (int e = 0; e < N; e += 32) tm_store16(p_at + (j + e) / 2, x + e / 2);
+    if (j + N == kTile / 2) half();
+  }
+  sum[0] = add2(sum[0], sum[1]);
+  return sum[0].x + sum[0].y;
+}
+
 // Shared memory operand of 128-byte swizzled lines of 64 values: 8 lines are
 // 1,024 bytes (the stride); `chunk` is the distance between the column halves
 // where the lines run along the output's columns (V), unused where they run
@@ -274,7 +349,7 @@ struct Layout {
 
 struct Shared {
   uint64_t full[10], empty[10];
-  uint64_t q_ready[2], q_free[2], s_ready[2], p_ready[2], o_ready[2], all;
+  uint64_t q_ready[2], q_free[2], s_ready[2], p_half[2], p_ready[2], o_ready[2], all;
   float2 ml[2][kTile];
   int sums[kThreads / 32];
   int first, per, row[4], gave_up, last, bad[kRing];
@@ -308,6 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       bar_init(&sh.q_ready[i], kQueryWarps);
       bar_init(&sh.q_free[i], 1);
       bar_init(&sh.s_ready[i], 1);
+      bar_init(&sh.p_half[i], 4);
       bar_init(&sh.p_ready[i], 4);
       bar_init(&sh.o_ready[i], 1);
     }
@@ -494,7 +570,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (works && elected()) {
       const uint32_t what_qk = what_mma<T>(kTile, false), what_pv = what_mma<T>(D, true);
       int st = 0, ph = 0;               // the next item of the ring and its phase
-      int n_q[2] = {0, 0}, n_p[2] = {0, 0};
+      int n_q[2] = {0, 0}, n_p[2] = {0, 0}, n_h[2] = {0, 0};
       auto step = [&](int& a, int& b) {
         if (++a == L::kStages) a = 0, b ^= 1;
       };
@@ -513,15 +589,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (last) tm_commit(&sh.q_free[s]);
         return true;
       };
-      auto pv = [&](int s, bool first, bool last, int at, int phase, bool release) {
+      auto pv = [&](int s, bool first, bool last, int at, int phase, bool release, bool halves) {
         if (!bar_wait1(&sh.full[at], phase, gave_up)) return false;
-        if (!bar_wait1(&sh.p_ready[s], n_p[s]++ & 1, gave_up)) return false;
+        // (a wide piece's product begins with the first half of the probabilities)
+        if (halves && !bar_wait1(&sh.p_half[s], n_h[s]++ & 1, gave_up)) return false;
+        if (!halves && !bar_wait1(&sh.p_ready[s], n_p[s]++ & 1, gave_up)) return false;
         tm_after();
         const uint32_t b = ring + at * L::kTileBytes;
 #pragma unroll
-        for (int x = 0; x < kTile / 16; ++x)
+        for (int x = 0; x < kTile / 16; ++x) {
+          if (x == kTile / 32 && halves) {
+            if (!bar_wait1(&sh.p_ready[s], n_p[s]++ & 1, gave_up)) return false;
+            tm_after();
+          }
           mma_ts(tmem + L::kO + s * D, tmem + L::kP + s * L::kPStep + x * 8, operand(b + x * 2048, kTile * 128), what_pv,
                  !first || x > 0);
+        }
         if (last) tm_commit(&sh.o_ready[s]);
         if (release) tm_commit(&sh.empty[at]);
         return true;
@@ -540,8 +623,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int v = st, vp = ph;
             step(st, ph);
             const bool last = i + 1 == n;
-            ok = pv(0, i == 0, last, v, vp, !both) && (last || qk(0, false, i + 2 == n, st, ph, !both));
-            if (ok && both) ok = pv(1, i == 0, last, v, vp, true) && (last || qk(1, false, i + 2 == n, st, ph, true));
+            ok = pv(0, i == 0, last, v, vp, !both, true) && (last || qk(0, false, i + 2 == n, st, ph, !both));
+            if (ok && both) ok = pv(1, i == 0, last, v, vp, true, true) && (last || qk(1, false, i + 2 == n, st, ph, true));
           }
         } else {
           const int n = p.t1 - p.t0;
@@ -550,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool v = x >= 0 && !(x & 1);
             const int t = x < 0 ? x + 2 : x / 2 + (v ? 0 : 2);
             if (t >= n) continue;
-            ok = v ? pv(t & 1, t < 2, t + 2 >= n, st, ph, true)
+            ok = v ? pv(t & 1, t < 2, t + 2 >= n, st, ph, true, false)
                    : qk(t & 1, t < 2, t + 2 >= n, st, ph, true);
             step(st, ph);
           }
@@ -574,24 +657,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         const int r0 = p.r0 + (p.wide ? s * kTile : 0), rows = min(kTile, u.rows - r0);
         const int part = tid % kPer, step = kQueryWarps * 32 / kPer;
-        // (rows past the unit's last are left as they are: they have no part in any other row)
+        // (rows past the unit's last get its last one's values: they have no part in any other row, and loads under
+        // conditions would wait for one another)
 #pragma unroll 1
         for (int r = (tid - kQueryWarp * 32) / kPer; r < rows; r += 8 * step) {
           uint4 v[8];
 #pragma unroll
-          for (int x = 0; x < 8; ++x)
-            if (r + x * step < rows) {
-              const int row = r0 + r + x * step, t = row / g.group, head = u.h * g.group + row - t * g.group;
-              v[x] = *reinterpret_cast<const uint4*>((const T*)g.q + (long long)(u.a + t) * g.qs[0] +
-                                                     (long long)head * g.qs[1] + part * 8);
-            }
+          for (int x = 0; x < 8; ++x) {
+            const int row = r0 + min(r + x * step, rows - 1), t = row / g.group, head = u.h * g.group + row - t * g.group;
+            v[x] = *reinterpret_cast<const uint4*>((const T*)g.q + (long long)(u.a + t) * g.qs[0] +
+                                                   (long long)head * g.qs[1] + part * 8);
+          }
 #pragma unroll
-          for (int x = 0; x < 8; ++x)
-            if (r + x * step < rows) {
-              const int row = r + x * step;
-              *reinterpret_cast<uint4*>(tiles + s * L::kTileBytes + row * 128 + (part / 8) * (kTile * 128) +
-                                        ((part % 8) ^ (row & 7)) * 16) = v[x];
-            }
+          for (int x = 0; x < 8; ++x) {
+            const int row = r + x * step;
+            *reinterpret_cast<uint4*>(tiles + s * L::kTileBytes + row * 128 + (part / 8) * (kTile * 128) +
+                                      ((part % 8) ^ (row & 7)) * 16) = v[x];
+          }
         }
         async_fence();
         __syncwarp();
@@ -627,27 +709,24 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = false;
           break;
         }
+        if (i + 1 == p.n[s] && p.ends(u) && (p.wide ? s == 0 : ((p.t1 - p.t0 - 1) & 1) == s)) {
+          // values past the row's last token are not the row's, and 0 times their bits may be NaN: zeros in their place
+          // (the ring's place of the piece's last values cannot be taken again before their product)
+          const int st = (items - 1) % L::kStages, rows = u.len + u.n - (p.t1 - 1) * kTile;
+          ok = bar_wait(&sh.full[st], ((items - 1) / L::kStages) & 1, gave_up);
+          if (!ok) break;
+          for (int y = rows * 8 + r; y < kTile * 8; y += kTile)
+            for (int half = 0; half < D / 64; ++half)
+              *reinterpret_cast<uint4*>(tiles + (2 + st) * L::kTileBytes + half * (kTile * 128) + y * 16) = make_uint4(0, 0, 0, 0);
+          async_fence();
+        }
         if (warp_live) {
           tm_after();
           const int tile = p.wide ? p.t0 + i : p.t0 + 2 * i + s;
           const int last = sees - tile * kTile;  // the tile's last visible key
-          uint32_t x[32];
-          // first the maximum; the scores are read again for the exponentials, which costs less than
-          // 128 registers to hold them.  The loops are rolled: short calls wait for instructions otherwise.
-          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-          for (int j = 0; j < kTile; j += 32) {
-            tm_load32(s_at + j, x);
-            tm_loaded(x);
-            if (last < j + 31) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (j + e > last) x[e] = 0xFF800000u;
-            }
-#pragma unroll
-            for (int e = 0; e < 32; ++e) top[e & 3] = fmaxf(top[e & 3], __uint_as_float(x[e]));
-          }
-          const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sc;
+          // first the maximum; the scores are read again for the exponentials, which costs less than 128
+          // registers to hold them.  Short calls wait for instructions: their loops are rolled tighter.
+          const float now = (p.wide ? tile_max<64>(s_at, last) : tile_max<32>(s_at, last)) * sc;
           // The maximum is moved only where it grew by more than 8 (the probabilities stay below 2^8 and
           // lose nothing in floating point): few tiles rescale what came before them.
           if (__any_sync(~0u, live && now - m > 8.f)) {
@@ -655,6 +734,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (i > 0) {
 #pragma unroll 1
               for (int j = 0; j < D; j += 32) {
+                uint32_t x[32];
                 tm_load32(o_at + s * D + j, x);
                 tm_loaded(x);
 #pragma unroll
@@ -666,41 +746,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             m = most;
           }
           const float base = m > -INFINITY ? m : 0.f;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-          for (int j = 0; j < kTile; j += 32) {
-            tm_load32(s_at + j, x);
-            tm_loaded(x);
-            if (last < j + 31) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (j + e > last) x[e] = 0xFF800000u;
-            }
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const float a = exp2_fast(fmaf(__uint_as_float(x[e]), sc, -base));
-              const float b = exp2_fast(fmaf(__uint_as_float(x[e + 1]), sc, -base));
-              sum[e & 2] += a;
-              sum[(e & 2) + 1] += b;
-              x[e / 2] = pack_of(a, b, T());
-            }
-            // (where the probabilities lie over the scores, these columns were read before)
-            tm_store16(p_at + j / 2, x);
-          }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          if (p.wide)
+            l += tile_exp<T, 64>(s_at, p_at, last, sc, base, [&]() {
+              tm_stored();
+              tm_before();
+              __syncwarp();
+              if (lane == 0) bar_arrive(&sh.p_half[s]);
+            });
+          else
+            l += tile_exp<T, 32>(s_at, p_at, last, sc, base, []() {});
           tm_stored();
           tm_before();
-        }
-        if (i + 1 == p.n[s] && p.ends(u) && (p.wide ? s == 0 : ((p.t1 - p.t0 - 1) & 1) == s)) {
-          // values past the row's last token are not the row's, and 0 times their bits may be NaN: zeros in their place
-          // (the ring's place of the piece's last values cannot be taken again before their product)
-          const int st = (items - 1) % L::kStages, rows = u.len + u.n - (p.t1 - 1) * kTile;
-          ok = bar_wait(&sh.full[st], ((items - 1) / L::kStages) & 1, gave_up);
-          if (!ok) break;
-          for (int y = rows * 8 + r; y < kTile * 8; y += kTile)
-            for (int half = 0; half < D / 64; ++half)
-              *reinterpret_cast<uint4*>(tiles + (2 + st) * L::kTileBytes + half * (kTile * 128) + y * 16) = make_uint4(0, 0, 0, 0);
-          async_fence();
+        } else if (p.wide) {
+          if (lane == 0) bar_arrive(&sh.p_half[s]);
         }
         __syncwarp();
         if (lane == 0) bar_arrive(&sh.p_ready[s]);
