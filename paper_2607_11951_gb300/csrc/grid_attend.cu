@@ -34,7 +34,8 @@ constexpr int kSoftWarps = 8;         // four per stream
 constexpr int kLoadWarp = kSoftWarps, kMmaWarp = kSoftWarps + 1;  // one that loads tiles, one that multiplies,
 constexpr int kQueryWarp = kSoftWarps + 2, kQueryWarps = 2;        // two that load queries
 constexpr int kThreads = (kSoftWarps + 4) * 32;
-constexpr int kMinRun = 2;            // tiles of a run, at least (unless there are fewer)
+constexpr int kMinRun = 4;            // of a run, at least (unless there are fewer)
+constexpr int kUnitCost = 2;          // what a unit's beginning and end cost, in tiles
 constexpr int kRing = 8;              // pieces whose bad-page flags are kept at once
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
@@ -143,13 +144,6 @@ __device__ __forceinline__ void tm_load16(uint32_t at, uint32_t* x) {
       : O8(x, 0), O8(x, 8)
       : "r"(at));
 }
-__device__ __forceinline__ void tm_store32(uint32_t at, const uint32_t* x) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::I8(x, 0),
-      I8(x, 8), I8(x, 16), I8(x, 24), "r"(at)
-      : "memory");
-}
 __device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t* x) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::I8(
@@ -160,6 +154,9 @@ __device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t* x) {
 // (the registers are named, so that nothing uses them before the wait)
 __device__ __forceinline__ void tm_loaded(uint32_t* x) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : U8(x, 0), U8(x, 8), U8(x, 16), U8(x, 24) : : "memory");
+}
+__device__ __forceinline__ void tm_loaded16(uint32_t* x) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : U8(x, 0), U8(x, 8) : : "memory");
 }
 __device__ __forceinline__ void tm_loaded16(uint32_t* x, uint32_t* y) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : U8(x, 0), U8(x, 8), U8(y, 0), U8(y, 8) : : "memory");
@@ -195,52 +192,94 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// The scores of N keys from column `at` on, those past `last` (of the N) as -inf.
-template <int N>
-__device__ __forceinline__ void load_scores(uint32_t at, int last, uint32_t (&x)[N]) {
+// 32 keys' probabilities 2^(sc s - base) as pairs of T in the first 16 registers; their sums are added.
+template <typename T>
+__device__ __forceinline__ void exp32(uint32_t (&x)[32], float sc, float base, Two (&sum)[2]) {
 #pragma unroll
-  for (int j = 0; j < N; j += 32) tm_load32(at + j, x + j);
+  for (int e = 0; e < 32; e += 2) {
+    Two a = fma2(Two{__uint_as_float(x[e]), __uint_as_float(x[e + 1])}, sc, -base);
+    a = Two{exp2_fast(a.x), exp2_fast(a.y)};
+    sum[e / 2 & 1] = add2(sum[e / 2 & 1], a);
+    x[e / 2] = pack_of(a.x, a.y, T());
+  }
+}
+__device__ __forceinline__ void max32(const uint32_t (&x)[32], float (&top)[4]) {
 #pragma unroll
-  for (int j = 0; j < N; j += 32) tm_loaded(x + j);
-  if (last < N - 1) {
+  for (int e = 0; e < 32; e += 2) top[e / 2 & 3] = max3(top[e / 2 & 3], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+}
+__device__ __forceinline__ void hide32(uint32_t (&x)[32], int last) {  // scores past `last` as -inf
+  if (last < 31) {
 #pragma unroll
-    for (int e = 0; e < N; ++e)
+    for (int e = 0; e < 32; ++e)
       if (e > last) x[e] = 0xFF800000u;
   }
 }
-// The largest score of a tile.
-template <int N>
-__device__ __forceinline__ float tile_max(uint32_t s_at, int last) {
-  float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-  for (int j = 0; j < kTile; j += N) {
-    uint32_t x[N];
-    load_scores<N>(s_at + j, last - j, x);
-#pragma unroll
-    for (int e = 0; e < N; e += 2) top[e / 2 & 3] = max3(top[e / 2 & 3], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
-  }
-  return fmaxf(max3(top[0], top[1], top[2]), top[3]);
-}
-// A tile's probabilities 2^(sc s - base), to tensor memory; returns their sum.  half() is called once those of the
-// first 64 keys are there.
-template <typename T, int N, typename Half>
-__device__ __forceinline__ float tile_exp(uint32_t s_at, uint32_t p_at, int last, float sc, float base, Half half) {
+
+// One tile of a row's softmax: the maximum, base(maximum), then the
+// probabilities, from the last keys to the first: they lie (64-wide heads
+// apart) over the second half of the scores, which is read before.  half() is
+// called once those of the last 64 keys are there.  Returns their sum.
+//
+// The scores are read from tensor memory twice: 128 registers to hold them do
+// not fit.  kAhead: each 32 columns are on their way while the ones before are
+// worked on, and the last 64 are read once.  Without, the loops are rolled: short
+// calls wait for instructions.
+template <typename T, bool kAhead, typename Base, typename Half>
+__device__ __forceinline__ float tile_softmax(uint32_t s_at, uint32_t p_at, int last, float sc, Base base, Half half) {
   Two sum[2] = {};
+  float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  if constexpr (kAhead) {
+    uint32_t x[32], y[32];
+    tm_load32(s_at, x);
+    tm_loaded(x);
+    tm_load32(s_at + 32, y);
+    hide32(x, last);
+    max32(x, top);
+    tm_loaded(y);
+    tm_load32(s_at + 64, x);
+    hide32(y, last - 32);
+    max32(y, top);
+    tm_loaded(x);
+    tm_load32(s_at + 96, y);
+    hide32(x, last - 64);
+    max32(x, top);
+    tm_loaded(y);
+    hide32(y, last - 96);
+    max32(y, top);
+    const float b = base(fmaxf(max3(top[0], top[1], top[2]), top[3]));
+    exp32<T>(y, sc, b, sum);
+    tm_store16(p_at + 48, y);
+    tm_load32(s_at + 32, y);
+    exp32<T>(x, sc, b, sum);
+    tm_store16(p_at + 32, x);
+    half();
+    tm_loaded(y);
+    tm_load32(s_at, x);
+    hide32(y, last - 32);
+    exp32<T>(y, sc, b, sum);
+    tm_store16(p_at + 16, y);
+    tm_loaded(x);
+    hide32(x, last);
+    exp32<T>(x, sc, b, sum);
+    tm_store16(p_at, x);
+  } else {
+    uint32_t x[32];
 #pragma unroll 1
-  for (int j = 0; j < kTile; j += N) {
-    uint32_t x[N];
-    load_scores<N>(s_at + j, last - j, x);
-#pragma unroll
-    for (int e = 0; e < N; e += 2) {
-      Two a = fma2(Two{__uint_as_float(x[e]), __uint_as_float(x[e + 1])}, sc, -base);
-      a = Two{exp2_fast(a.x), exp2_fast(a.y)};
-      sum[e / 2 & 1] = add2(sum[e / 2 & 1], a);
-      x[e / 2] = pack_of(a.x, a.y, T());
+    for (int j = 0; j < kTile; j += 32) {
+      tm_load32(s_at + j, x);
+      tm_loaded(x);
+      hide32(x, last - j);
+      max32(x, top);
     }
-    // (where the probabilities lie over the scores, these columns were read before)
-#pragma unroll
-    for (int e = 0; e < N; e += 32) tm_store16(p_at + (j + e) / 2, x + e / 2);
-    if (j + N == kTile / 2) half();
+    const float b = base(fmaxf(max3(top[0], top[1], top[2]), top[3]));
+#pragma unroll 1
+    for (int j = kTile - 32; j >= 0; j -= 32) {
+      tm_load32(s_at + j, x);
+      tm_loaded(x);
+      hide32(x, last - j);
+      exp32<T>(x, sc, b, sum);
+      tm_store16(p_at + j / 2, x);
+    }
   }
   sum[0] = add2(sum[0], sum[1]);
   return sum[0].x + sum[0].y;
@@ -268,7 +307,7 @@ struct Units {
   int b, a, n, len, rows;  // row, its first token, tokens, cached tokens, query rows per key head
   int units, h, qt;        // units per key head; the current one
   int tiles;               // key tiles of the current unit
-  int at;                  // the tile that it begins at (their number is checked on the host to fit)
+  int at;                  // where its tiles begin, in costs (their sum is checked on the host to fit)
 };
 
 __device__ __forceinline__ int tiles_of(const Units& u, int group, int qt) {
@@ -286,15 +325,15 @@ __device__ __forceinline__ bool open_row(const AttendArgs& g, Units& u, int b) {
   set_row(g, u);
   return true;
 }
-// The tiles of a key head, by a warp (every lane gets the sum).
+// The cost of a key head, by a warp (every lane gets the sum).
 __device__ __forceinline__ int head_tiles(const Units& u, int group, int lane) {
   int t = 0;
 #pragma unroll 1
-  for (int i = lane; i < u.units; i += 32) t += tiles_of(u, group, i);
+  for (int i = lane; i < u.units; i += 32) t += kUnitCost + tiles_of(u, group, i);
   return __reduce_add_sync(~0u, t);
 }
 __device__ __forceinline__ void next_unit(const AttendArgs& g, Units& u) {
-  u.at += u.tiles;
+  u.at += u.tiles + kUnitCost;
   if (++u.qt == u.units) {
     u.qt = 0;
     if (++u.h == g.Hk) {
@@ -307,13 +346,13 @@ __device__ __forceinline__ void next_unit(const AttendArgs& g, Units& u) {
   u.tiles = tiles_of(u, g.group, u.qt);
 }
 
-// All tiles cut into runs, one per block, the first `more` of them one tile longer.
+// All costs cut into runs, one per block, the first `more` of them longer by one.
 struct Cut {
   int runs, each, more;
   __device__ __forceinline__ int begin(int i) const { return i * each + min(i, more); }
-  __device__ __forceinline__ int run_of(int tile) const {
+  __device__ __forceinline__ int run_of(int at) const {
     const int longer = more * (each + 1);
-    return tile < longer ? tile / (each + 1) : more + (tile - longer) / each;
+    return at < longer ? at / (each + 1) : more + (at - longer) / each;
   }
 };
 
@@ -343,7 +382,7 @@ struct Layout {
   static constexpr int kStages = D == 128 ? 5 : 10;
   static constexpr int kTiles = 2 * kTileBytes + kStages * kTileBytes;
   static constexpr uint32_t kS = 0, kO = 256;                 // columns of tensor memory: scores, outputs,
-  static constexpr uint32_t kP = D == 128 ? 0 : 256 + 2 * D;  // probabilities (over the scores where all columns are taken)
+  static constexpr uint32_t kP = D == 128 ? 64 : 256 + 2 * D;  // probabilities (over the scores where all columns are taken)
   static constexpr uint32_t kPStep = D == 128 ? 128 : 64;
 };
 
@@ -397,24 +436,33 @@ __global__ void __launch_bounds__(kThreads, 1)
   Cut cut;
   Units u;
   {
-    // (a thread's rows are `per` neighbours; a row of several units is summed by its warp)
+    // A thread's rows are `per` neighbours, one of them at a time; rows of several units go to the warps in turn.
     const int per = (c.B + kThreads - 1) / kThreads;
-    auto row_tiles = [&](int b) {
+    int* many = reinterpret_cast<int*>(tiles);  // [kThreads][3]: tokens, cached tokens, cost (the tiles come later)
+    auto row_cost = [&](int b) {
       const bool some = b < min(c.B, (tid + 1) * per) && open_row(g, u, b);
-      int t = some && u.units == 1 ? tiles_of(u, g.group, 0) : 0;
-      for (unsigned big = __ballot_sync(~0u, some && u.units > 1); big; big &= big - 1) {
-        const int l = __ffs(big) - 1;
-        Units v;
-        v.n = __shfl_sync(~0u, u.n, l), v.len = __shfl_sync(~0u, u.len, l);
-        v.rows = __shfl_sync(~0u, u.rows, l), v.units = __shfl_sync(~0u, u.units, l);
-        const int sum = head_tiles(v, g.group, lane);
-        if (lane == l) t = sum;
+      int t = some && u.units == 1 ? kUnitCost + tiles_of(u, g.group, 0) : 0, at = -1;
+      if (tid == 0) sh.last = 0;
+      __syncthreads();
+      if (some && u.units > 1) {
+        at = atomicAdd(&sh.last, 1);
+        many[3 * at] = u.n, many[3 * at + 1] = u.len;
       }
-      return t;
+      __syncthreads();
+#pragma unroll 1
+      for (int i = warp; i < sh.last; i += kThreads / 32) {
+        Units v;
+        v.n = many[3 * i], v.len = many[3 * i + 1];
+        set_row(g, v);
+        const int sum = head_tiles(v, g.group, lane);
+        if (lane == 0) many[3 * i + 2] = sum;
+      }
+      __syncthreads();
+      return at >= 0 ? many[3 * at + 2] : t;
     };
     int mine = 0, t = 0;
 #pragma unroll 1
-    for (int i = 0; i < per; ++i) mine += (t = row_tiles(tid * per + i)) * g.Hk;
+    for (int i = 0; i < per; ++i) mine += (t = row_cost(tid * per + i)) * g.Hk;
     int pre = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -435,10 +483,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     cut.more = total - cut.runs * cut.each;
     const int lo = cut.begin(blockIdx.x);
     const bool here = (int)blockIdx.x < cut.runs && pre <= lo && lo < pre + mine;
-    if (__any_sync(~0u, here)) {
+    {
 #pragma unroll 1
       for (int i = 0; i < per; ++i) {
-        if (per > 1) t = row_tiles(tid * per + i);
+        if (per > 1) t = row_cost(tid * per + i);
         if (here && pre <= lo && lo < pre + t * g.Hk) {
           sh.row[0] = u.b, sh.row[1] = u.a, sh.row[2] = u.n, sh.row[3] = u.len;
           sh.first = pre;
@@ -466,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     u.at = sh.first + u.h * sh.per;
 #pragma unroll 1
     for (int i = 0;; i += 32) {  // 32 units at once
-      const int mine = i + lane < u.units ? tiles_of(u, g.group, i + lane) : 0;
+      const int mine = i + lane < u.units ? kUnitCost + tiles_of(u, g.group, i + lane) : 0;
       int sum = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -477,8 +525,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (past || i + 32 >= u.units) {
         const int l = past ? __ffs(past) - 1 : 0;
         u.qt = i + l;
-        u.tiles = __shfl_sync(~0u, mine, l);
-        u.at += __shfl_sync(~0u, sum - mine, l);
+        u.tiles = __shfl_sync(~0u, mine, l) - kUnitCost;
+        u.at += __shfl_sync(~0u, sum - mine, l) + kUnitCost;
         break;
       }
       u.at += __shfl_sync(~0u, sum, 31);
@@ -487,6 +535,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == kLoadWarp) {
     // ---- one warp keeps the ring of tiles full: a lane per page and half of the columns
+    async_fence();  // (the plan was made where the tiles come)
     int it = 0;
     if (works) {
       const int box = min(kTile, 1 << c.log_page), pages = kTile / box, boxes = pages * (D / 64);
@@ -597,13 +646,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         tm_after();
         const uint32_t b = ring + at * L::kTileBytes;
 #pragma unroll
-        for (int x = 0; x < kTile / 16; ++x) {
-          if (x == kTile / 32 && halves) {
+        for (int y = 0; y < kTile / 16; ++y) {
+          if (y == kTile / 32 && halves) {
             if (!bar_wait1(&sh.p_ready[s], n_p[s]++ & 1, gave_up)) return false;
             tm_after();
           }
+          const int x = (y + kTile / 32) % (kTile / 16);
           mma_ts(tmem + L::kO + s * D, tmem + L::kP + s * L::kPStep + x * 8, operand(b + x * 2048, kTile * 128), what_pv,
-                 !first || x > 0);
+                 !first || y > 0);
         }
         if (last) tm_commit(&sh.o_ready[s]);
         if (release) tm_commit(&sh.empty[at]);
@@ -657,24 +707,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         const int r0 = p.r0 + (p.wide ? s * kTile : 0), rows = min(kTile, u.rows - r0);
         const int part = tid % kPer, step = kQueryWarps * 32 / kPer;
-        // (rows past the unit's last get its last one's values: they have no part in any other row, and loads under
-        // conditions would wait for one another)
-#pragma unroll 1
-        for (int r = (tid - kQueryWarp * 32) / kPer; r < rows; r += 8 * step) {
-          uint4 v[8];
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const int row = r0 + min(r + x * step, rows - 1), t = row / g.group, head = u.h * g.group + row - t * g.group;
-            v[x] = *reinterpret_cast<const uint4*>((const T*)g.q + (long long)(u.a + t) * g.qs[0] +
-                                                   (long long)head * g.qs[1] + part * 8);
-          }
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const int row = r + x * step;
-            *reinterpret_cast<uint4*>(tiles + s * L::kTileBytes + row * 128 + (part / 8) * (kTile * 128) +
-                                      ((part % 8) ^ (row & 7)) * 16) = v[x];
-          }
+        // (rows past the unit's last are left as they are: they have no part in any other row)
+#pragma unroll 4
+        for (int r = (tid - kQueryWarp * 32) / kPer; r < rows; r += step) {
+          const int row = r0 + r, t = row / g.group, head = u.h * g.group + row - t * g.group;
+          const T* src = (const T*)g.q + (long long)(u.a + t) * g.qs[0] + (long long)head * g.qs[1] + part * 8;
+          const uint32_t dst = q_at + s * L::kTileBytes + r * 128 + (part / 8) * (kTile * 128) + ((part % 8) ^ (r & 7)) * 16;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
         async_fence();
         __syncwarp();
         if (lane == 0) bar_arrive(&sh.q_ready[s]);
@@ -724,37 +765,39 @@ __global__ void __launch_bounds__(kThreads, 1)
           tm_after();
           const int tile = p.wide ? p.t0 + i : p.t0 + 2 * i + s;
           const int last = sees - tile * kTile;  // the tile's last visible key
-          // first the maximum; the scores are read again for the exponentials, which costs less than 128
-          // registers to hold them.  Short calls wait for instructions: their loops are rolled tighter.
-          const float now = (p.wide ? tile_max<64>(s_at, last) : tile_max<32>(s_at, last)) * sc;
-          // The maximum is moved only where it grew by more than 8 (the probabilities stay below 2^8 and
-          // lose nothing in floating point): few tiles rescale what came before them.
-          if (__any_sync(~0u, live && now - m > 8.f)) {
-            const float most = fmaxf(m, now), f = m > -INFINITY ? exp2_fast(m - most) : 0.f;
-            if (i > 0) {
+          auto base = [&](float top) {
+            const float now = top * sc;
+            // The maximum is moved only where it grew by more than 8 (the probabilities stay below 2^8 and
+            // lose nothing in floating point): few tiles rescale what came before them.
+            if (__any_sync(~0u, live && now - m > 8.f)) {
+              const float most = fmaxf(m, now), f = m > -INFINITY ? exp2_fast(m - most) : 0.f;
+              if (i > 0) {
 #pragma unroll 1
-              for (int j = 0; j < D; j += 32) {
-                uint32_t x[32];
-                tm_load32(o_at + s * D + j, x);
-                tm_loaded(x);
+                for (int j = 0; j < D; j += 16) {
+                  uint32_t o[16];
+                  tm_load16(o_at + s * D + j, o);
+                  tm_loaded16(o);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
-                tm_store32(o_at + s * D + j, x);
+                  for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                  tm_store16(o_at + s * D + j, o);
+                }
               }
+              l *= f;
+              m = most;
             }
-            l *= f;
-            m = most;
-          }
-          const float base = m > -INFINITY ? m : 0.f;
+            return m > -INFINITY ? m : 0.f;
+          };
+          float added;  // (the base may rescale l first)
           if (p.wide)
-            l += tile_exp<T, 64>(s_at, p_at, last, sc, base, [&]() {
+            added = tile_softmax<T, true>(s_at, p_at, last, sc, base, [&]() {
               tm_stored();
               tm_before();
               __syncwarp();
               if (lane == 0) bar_arrive(&sh.p_half[s]);
             });
           else
-            l += tile_exp<T, 32>(s_at, p_at, last, sc, base, []() {});
+            added = tile_softmax<T, false>(s_at, p_at, last, sc, base, []() {});
+          l += added;
           tm_stored();
           tm_before();
         } else if (p.wide) {
@@ -973,7 +1016,7 @@ extern "C" int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, con
   // (more than two billion tiles of 256 query rows by 128 keys would take minutes)
   const double units = (double)chunk->n_tokens * (p.n_heads / p.n_kv_heads) / 256 + chunk->B;
   if ((double)chunk->n_tokens * (p.n_heads / p.n_kv_heads) > INT32_MAX - 256 ||
-      units * p.n_kv_heads * (((double)chunk->max_pages * p.page_size) / kTile + 1) > INT32_MAX)
+      units * p.n_kv_heads * (((double)chunk->max_pages * p.page_size) / kTile + 1 + kUnitCost) > INT32_MAX)
     return set_error(GRID_E_TOO_LARGE, "grid_kv_attend: too many query rows or key tiles in one call");
   a.q = query->q.d, a.out = query->out.d, a.lse = query->d_lse;
   a.qs[0] = query->q.token_stride, a.qs[1] = query->q.head_stride;
