@@ -23,6 +23,7 @@
 #include <dlfcn.h>
 
 #include <cmath>
+#include <utility>
 
 #include "grid_kv.cuh"
 
@@ -45,7 +46,7 @@ struct AttendArgs {
   void* out;
   float* lse;
   long long qs[2], os[2];
-  int H, Hk, group;
+  int H, Hk, group, sectors;  // sectors: the rows of out begin on 32 bytes
   float scale;
   int32_t* status;
   float4* parts;    // [2 blocks][D / 4][256 rows]
@@ -110,18 +111,23 @@ __device__ __forceinline__ void tm_after() { asm volatile("tcgen05.fence::after_
 __device__ __forceinline__ void tm_commit(uint64_t* b) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(b)) : "memory");
 }
-// D += A B^T, A and B in shared memory
+// D += A B^T, A and B in shared memory, `off` (16-byte units) further on; the
+// addition is in here so that it is not made, and kept, ahead of time
+template <int kOff>
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a),
-      "l"(b), "r"(what), "r"((uint32_t)add)
+      "{\n.reg .pred p;\n.reg .b64 a, b;\nadd.s64 a, %1, %5;\nadd.s64 b, %2, %5;\nsetp.ne.u32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(what), "r"((uint32_t)add), "n"(kOff)
       : "memory");
 }
-// D += A B, A in tensor memory
+// D += A B, A in tensor memory: step kStep of 16 keys
+template <int kStep>
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a),
-      "l"(b), "r"(what), "r"((uint32_t)add)
+      "{\n.reg .pred p;\n.reg .b32 a;\n.reg .b64 b;\nadd.s32 a, %1, %5;\nadd.s64 b, %2, %6;\nsetp.ne.u32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, p;\n}" ::"r"(d),
+      "r"(a), "l"(b), "r"(what), "r"((uint32_t)add), "n"(kStep * 8), "n"(kStep * 128)
       : "memory");
 }
 #define O8(x, i) \
@@ -215,72 +221,99 @@ __device__ __forceinline__ void hide32(uint32_t (&x)[32], int last) {  // scores
   }
 }
 
-// One tile of a row's softmax: the maximum, base(maximum), then the
-// probabilities, from the last keys to the first: they lie (64-wide heads
-// apart) over the second half of the scores, which is read before.  half() is
-// called once those of the last 64 keys are there.  Returns their sum.
-//
-// The scores are read from tensor memory twice: 128 registers to hold them do
-// not fit.  kAhead: each 32 columns are on their way while the ones before are
-// worked on, and the last 64 are read once.  Without, the loops are rolled: short
-// calls wait for instructions.
-template <typename T, bool kAhead, typename Base, typename Half>
-__device__ __forceinline__ float tile_softmax(uint32_t s_at, uint32_t p_at, int last, float sc, Base base, Half half) {
+// One tile of a row's softmax from nothing: the maximum, base(maximum), then
+// the probabilities, from the last keys to the first: they lie (64-wide heads
+// apart) over the second half of the scores, which is read before.  Returns their
+// sum.  The scores are read from tensor memory twice, the loops are rolled: few
+// tiles come here, and those of short calls wait for instructions.
+template <typename T, typename Base>
+__device__ __forceinline__ float softmax_anew(uint32_t s_at, uint32_t p_at, int last, float sc, Base base) {
   Two sum[2] = {};
   float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  if constexpr (kAhead) {
-    uint32_t x[32], y[32];
-    tm_load32(s_at, x);
-    tm_loaded(x);
-    tm_load32(s_at + 32, y);
-    hide32(x, last);
-    max32(x, top);
-    tm_loaded(y);
-    tm_load32(s_at + 64, x);
-    hide32(y, last - 32);
-    max32(y, top);
-    tm_loaded(x);
-    tm_load32(s_at + 96, y);
-    hide32(x, last - 64);
-    max32(x, top);
-    tm_loaded(y);
-    hide32(y, last - 96);
-    max32(y, top);
-    const float b = base(fmaxf(max3(top[0], top[1], top[2]), top[3]));
-    exp32<T>(y, sc, b, sum);
-    tm_store16(p_at + 48, y);
-    tm_load32(s_at + 32, y);
-    exp32<T>(x, sc, b, sum);
-    tm_store16(p_at + 32, x);
-    half();
-    tm_loaded(y);
-    tm_load32(s_at, x);
-    hide32(y, last - 32);
-    exp32<T>(y, sc, b, sum);
-    tm_store16(p_at + 16, y);
-    tm_loaded(x);
-    hide32(x, last);
-    exp32<T>(x, sc, b, sum);
-    tm_store16(p_at, x);
-  } else {
-    uint32_t x[32];
+  uint32_t x[32];
 #pragma unroll 1
-    for (int j = 0; j < kTile; j += 32) {
-      tm_load32(s_at + j, x);
-      tm_loaded(x);
-      hide32(x, last - j);
-      max32(x, top);
-    }
-    const float b = base(fmaxf(max3(top[0], top[1], top[2]), top[3]));
-#pragma unroll 1
-    for (int j = kTile - 32; j >= 0; j -= 32) {
-      tm_load32(s_at + j, x);
-      tm_loaded(x);
-      hide32(x, last - j);
-      exp32<T>(x, sc, b, sum);
-      tm_store16(p_at + j / 2, x);
-    }
+  for (int j = 0; j < kTile; j += 32) {
+    tm_load32(s_at + j, x);
+    tm_loaded(x);
+    hide32(x, last - j);
+    max32(x, top);
   }
+  const float b = base(fmaxf(max3(top[0], top[1], top[2]), top[3]));
+#pragma unroll 1
+  for (int j = kTile - 32; j >= 0; j -= 32) {
+    tm_load32(s_at + j, x);
+    tm_loaded(x);
+    hide32(x, last - j);
+    exp32<T>(x, sc, b, sum);
+    tm_store16(p_at + j / 2, x);
+  }
+  sum[0] = add2(sum[0], sum[1]);
+  return sum[0].x + sum[0].y;
+}
+// The same for many tiles, with loads on their way while the columns before
+// are worked on; the last 64 scores are read once.  half() is called once the
+// probabilities of the last 64 keys are there.
+template <typename T, typename Base, typename Half>
+__device__ __forceinline__ float softmax_twice(uint32_t s_at, uint32_t p_at, int last, float sc, Base base, Half half) {
+  Two sum[2] = {};
+  float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  uint32_t x[32], y[32];
+  tm_load32(s_at, x);
+  tm_loaded(x);
+  tm_load32(s_at + 32, y);
+  hide32(x, last);
+  max32(x, top);
+  tm_loaded(y);
+  tm_load32(s_at + 64, x);
+  hide32(y, last - 32);
+  max32(y, top);
+  tm_loaded(x);
+  tm_load32(s_at + 96, y);
+  hide32(x, last - 64);
+  max32(x, top);
+  tm_loaded(y);
+  hide32(y, last - 96);
+  max32(y, top);
+  const float b = base(fmaxf(max3(top[0], top[1], top[2]), top[3]));
+  exp32<T>(y, sc, b, sum);
+  tm_store16(p_at + 48, y);
+  tm_load32(s_at + 32, y);
+  exp32<T>(x, sc, b, sum);
+  tm_store16(p_at + 32, x);
+  half();
+  tm_loaded(y);
+  tm_load32(s_at, x);
+  hide32(y, last - 32);
+  exp32<T>(y, sc, b, sum);
+  tm_store16(p_at + 16, y);
+  tm_loaded(x);
+  hide32(x, last);
+  exp32<T>(x, sc, b, sum);
+  tm_store16(p_at, x);
+  sum[0] = add2(sum[0], sum[1]);
+  return sum[0].x + sum[0].y;
+}
+// The same in one pass on the maximum b of the tiles before, where the
+// probabilities have columns of their own.  `top` gets the tile's own maximum; if
+// it turns out to be too far above b, the scores are as they were and the
+// result is of no use.
+template <typename T>
+__device__ __forceinline__ float softmax_once(uint32_t s_at, uint32_t p_at, int last, float sc, float b, float& top) {
+  Two sum[2] = {};
+  float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  uint32_t x[2][32];
+  tm_load32(s_at, x[0]);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t(&y)[32] = x[j & 1];
+    tm_loaded(y);
+    if (j < 3) tm_load32(s_at + 32 * (j + 1), x[(j + 1) & 1]);
+    hide32(y, last - 32 * j);
+    max32(y, tops);
+    exp32<T>(y, sc, b, sum);
+    tm_store16(p_at + 16 * j, y);
+  }
+  top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]);
   sum[0] = add2(sum[0], sum[1]);
   return sum[0].x + sum[0].y;
 }
@@ -292,6 +325,14 @@ __device__ __forceinline__ float tile_softmax(uint32_t s_at, uint32_t p_at, int 
 __device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t chunk) {
   return (uint64_t)((at >> 4) & 0x3FFF) | (uint64_t)((chunk >> 4) & 0x3FFF) << 16 | (uint64_t)(1024 >> 4) << 32 |
          (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+template <int N, typename F, int... X>
+__device__ __forceinline__ void each_step(F f, std::integer_sequence<int, X...>) {
+  (f(std::integral_constant<int, X>()), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each_step(F f) {  // f(0), f(1) .. f(N - 1), the numbers known to the compiler
+  each_step<N>(f, std::make_integer_sequence<int, N>());
 }
 // fp32 accumulators, both operands of type T, 128 rows, n columns; b_rows: B's
 // lines run along the columns
@@ -383,6 +424,7 @@ struct Layout {
   static constexpr int kTiles = 2 * kTileBytes + kStages * kTileBytes;
   static constexpr uint32_t kS = 0, kO = 256;                 // columns of tensor memory: scores, outputs,
   static constexpr uint32_t kP = D == 128 ? 64 : 256 + 2 * D;  // probabilities (over the scores where all columns are taken)
+  static constexpr bool kApart = D == 64;                     // probabilities have columns of their own
   static constexpr uint32_t kPStep = D == 128 ? 128 : 64;
 };
 
@@ -390,6 +432,7 @@ struct Shared {
   uint64_t full[10], empty[10];
   uint64_t q_ready[2], q_free[2], s_ready[2], p_half[2], p_ready[2], o_ready[2], all;
   float2 ml[2][kTile];
+  Units units[kSoftWarps];
   int sums[kThreads / 32];
   int first, per, row[4], gave_up, last, bad[kRing];
   uint32_t tmem;
@@ -413,6 +456,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t q_at = smem_at(tiles), ring = q_at + 2 * L::kTileBytes;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const Chunk& c = g.c;
+  if (warp == kLoadWarp && lane < 2)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &v_map : &k_map) : "memory");
   if (tid == 0) {
     for (int i = 0; i < L::kStages; ++i) {
       bar_init(&sh.full[i], 1);
@@ -628,11 +673,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!bar_wait1(&sh.full[at], phase, gave_up)) return false;
         tm_after();
         const uint32_t a = q_at + s * L::kTileBytes, b = ring + at * L::kTileBytes;
-#pragma unroll
-        for (int x = 0; x < D / 16; ++x) {
-          const uint32_t at16 = (x / 4) * (kTile * 128) + (x % 4) * 32;
-          mma_ss(tmem + L::kS + s * 128, operand(a + at16, 16), operand(b + at16, 16), what_qk, x > 0);
-        }
+        const uint64_t da = operand(a, 16), db = operand(b, 16);
+        each_step<D / 16>([&](auto x) {
+          constexpr int kX = decltype(x)::value;
+          mma_ss<(kX / 4) * (kTile * 128 / 16) + (kX % 4) * 2>(tmem + L::kS + s * 128, da, db, what_qk, kX > 0);
+        });
         tm_commit(&sh.s_ready[s]);
         if (release) tm_commit(&sh.empty[at]);
         if (last) tm_commit(&sh.q_free[s]);
@@ -640,21 +685,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       auto pv = [&](int s, bool first, bool last, int at, int phase, bool release, bool halves) {
         if (!bar_wait1(&sh.full[at], phase, gave_up)) return false;
-        // (a wide piece's product begins with the first half of the probabilities)
-        if (halves && !bar_wait1(&sh.p_half[s], n_h[s]++ & 1, gave_up)) return false;
-        if (!halves && !bar_wait1(&sh.p_ready[s], n_p[s]++ & 1, gave_up)) return false;
+        // (a wide piece's product begins with the second half of the probabilities, which is there first)
+        if (halves ? !bar_wait1(&sh.p_half[s], n_h[s]++ & 1, gave_up) : !bar_wait1(&sh.p_ready[s], n_p[s]++ & 1, gave_up)) return false;
         tm_after();
         const uint32_t b = ring + at * L::kTileBytes;
-#pragma unroll
-        for (int y = 0; y < kTile / 16; ++y) {
-          if (y == kTile / 32 && halves) {
-            if (!bar_wait1(&sh.p_ready[s], n_p[s]++ & 1, gave_up)) return false;
-            tm_after();
-          }
-          const int x = (y + kTile / 32) % (kTile / 16);
-          mma_ts(tmem + L::kO + s * D, tmem + L::kP + s * L::kPStep + x * 8, operand(b + x * 2048, kTile * 128), what_pv,
-                 !first || y > 0);
+        const uint64_t db = operand(b, kTile * 128);
+        constexpr int kHalf = kTile / 32;
+        const uint32_t d = tmem + L::kO + s * D, pr = tmem + L::kP + s * L::kPStep;
+        each_step<kHalf>([&](auto x) {
+          constexpr int kX = decltype(x)::value;
+          mma_ts<kHalf + kX>(d, pr, db, what_pv, !first || kX > 0);
+        });
+        if (halves) {
+          if (!bar_wait1(&sh.p_ready[s], n_p[s]++ & 1, gave_up)) return false;
+          tm_after();
         }
+        each_step<kHalf>([&](auto x) { mma_ts<decltype(x)::value>(d, pr, db, what_pv, true); });
         if (last) tm_commit(&sh.o_ready[s]);
         if (release) tm_commit(&sh.empty[at]);
         return true;
@@ -673,8 +719,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int v = st, vp = ph;
             step(st, ph);
             const bool last = i + 1 == n;
-            ok = pv(0, i == 0, last, v, vp, !both, true) && (last || qk(0, false, i + 2 == n, st, ph, !both));
-            if (ok && both) ok = pv(1, i == 0, last, v, vp, true, true) && (last || qk(1, false, i + 2 == n, st, ph, true));
+            ok = pv(0, i == 0, last, v, vp, !both, !L::kApart) && (last || qk(0, false, i + 2 == n, st, ph, !both));
+            if (ok && both) ok = pv(1, i == 0, last, v, vp, true, !L::kApart) && (last || qk(1, false, i + 2 == n, st, ph, true));
           }
         } else {
           const int n = p.t1 - p.t0;
@@ -724,6 +770,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (works) {
     // ---- eight warps: softmax of the tiles, rows out
+    // (the warp's unit lies in shared memory: registers are short)
+    Units& w = sh.units[warp];
+    if (lane == 0) w = u;
+    __syncwarp();
     const int s = warp / 4, r = tid & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // (32 lanes of tensor memory, in the upper half of an address)
     const uint32_t s_at = tmem + lanes + L::kS + s * 128, p_at = tmem + lanes + L::kP + s * L::kPStep;
@@ -736,13 +786,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       return bar_wait(&sh.all, n_all++ & 1, gave_up);
     };
     bool ok = true;
-    for (int k = 0; ok && u.at < hi; ++k) {
-      const Piece p = piece_of(u, lo, hi);
+    for (int k = 0; ok && w.at < hi; ++k) {
+      const Piece p = piece_of(w, lo, hi);
       const int row = p.r0 + r + (p.wide ? s * kTile : 0);
-      const bool live = row < u.rows;
+      const bool live = row < w.rows;
       const bool warp_live = __any_sync(~0u, live);
-      const int t = live ? row / g.group : u.n - 1, head = live ? u.h * g.group + row - t * g.group : 0;
-      const int sees = u.len + t;  // the last position that the row's token sees
+      const int t = live ? row / g.group : w.n - 1, head = live ? w.h * g.group + row - t * g.group : 0;
+      const int sees = w.len + t;  // the last position that the row's token sees
       items += 2 * (p.t1 - p.t0);    // of the ring, up to the piece's end
       float m = -INFINITY, l = 0.f;  // the maximum is scaled: in exponents of two
       for (int i = 0; i < p.n[s]; ++i) {
@@ -750,10 +800,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = false;
           break;
         }
-        if (i + 1 == p.n[s] && p.ends(u) && (p.wide ? s == 0 : ((p.t1 - p.t0 - 1) & 1) == s)) {
+        if (i + 1 == p.n[s] && p.ends(w) && (p.wide ? s == 0 : ((p.t1 - p.t0 - 1) & 1) == s)) {
           // values past the row's last token are not the row's, and 0 times their bits may be NaN: zeros in their place
           // (the ring's place of the piece's last values cannot be taken again before their product)
-          const int st = (items - 1) % L::kStages, rows = u.len + u.n - (p.t1 - 1) * kTile;
+          const int st = (items - 1) % L::kStages, rows = w.len + w.n - (p.t1 - 1) * kTile;
           ok = bar_wait(&sh.full[st], ((items - 1) / L::kStages) & 1, gave_up);
           if (!ok) break;
           for (int y = rows * 8 + r; y < kTile * 8; y += kTile)
@@ -787,20 +837,28 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             return m > -INFINITY ? m : 0.f;
           };
-          float added;  // (the base may rescale l first)
-          if (p.wide)
-            added = tile_softmax<T, true>(s_at, p_at, last, sc, base, [&]() {
-              tm_stored();
-              tm_before();
-              __syncwarp();
-              if (lane == 0) bar_arrive(&sh.p_half[s]);
-            });
-          else
-            added = tile_softmax<T, false>(s_at, p_at, last, sc, base, []() {});
+          float added, top;  // (the base may rescale l first)
+          if constexpr (L::kApart) {
+            bool fits = false;
+            if (p.wide && i > 0) {
+              added = softmax_once<T>(s_at, p_at, last, sc, m > -INFINITY ? m : 0.f, top);
+              fits = !__any_sync(~0u, live && top * sc - m > 8.f);
+            }
+            if (!fits) added = softmax_anew<T>(s_at, p_at, last, sc, base);
+          } else {
+            added = p.wide ? softmax_twice<T>(s_at, p_at, last, sc, base,
+                                              [&]() {
+                                                tm_stored();
+                                                tm_before();
+                                                __syncwarp();
+                                                if (lane == 0) bar_arrive(&sh.p_half[s]);
+                                              })
+                           : softmax_anew<T>(s_at, p_at, last, sc, base);
+          }
           l += added;
           tm_stored();
           tm_before();
-        } else if (p.wide) {
+        } else if (!L::kApart && p.wide) {
           if (lane == 0) bar_arrive(&sh.p_half[s]);
         }
         __syncwarp();
@@ -808,11 +866,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
       // ---- the rows' outcome
-      const bool whole = p.t0 == 0 && p.t1 == u.tiles;
-      const int c0 = cut.run_of(u.at);
+      const bool whole = p.t0 == 0 && p.t1 == w.tiles;
+      const int c0 = cut.run_of(w.at);
       const int slot = 2 * blockIdx.x + ((int)blockIdx.x == c0 ? 1 : 0);
       float4* part = g.parts + (size_t)slot * (D / 4) * 256;
-      T* dst = (T*)g.out + (long long)(u.a + t) * g.os[0] + (long long)head * g.os[1];
+      T* dst = (T*)g.out + (long long)(w.a + t) * g.os[0] + (long long)head * g.os[1];
       float f[2];
       if (!p.wide) {  // both streams hold the same rows: each of the two halves of the warps takes half of the columns
         sh.ml[s][r] = make_float2(m, l);
@@ -852,8 +910,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             y[e] = whole && !fine ? 0.f : y[e] * inv;
           }
           if (live && whole) {
-#pragma unroll
-            for (int e = 0; e < 16; e += 8) *reinterpret_cast<uint4*>(dst + j + e) = pack8<T>(y + e);
+            const uint4 a = pack8<T>(y), b = pack8<T>(y + 8);
+            if (g.sectors) {
+              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + j), "r"(a.x), "r"(a.y), "r"(a.z),
+                           "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                           : "memory");
+            } else {
+              *reinterpret_cast<uint4*>(dst + j) = a;
+              *reinterpret_cast<uint4*>(dst + j + 8) = b;
+            }
           } else if (live) {
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
@@ -863,7 +928,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (live && (p.wide || s == 0)) {
           if (whole) {
-            if (g.lse) g.lse[(long long)(u.a + t) * g.H + head] = fine ? (m + log2f(l)) * kLn2 : -INFINITY;
+            if (g.lse) g.lse[(long long)(w.a + t) * g.H + head] = fine ? (m + log2f(l)) * kLn2 : -INFINITY;
           } else {
             __stcg(g.part_ml + (size_t)slot * 256 + part_row, make_float2(m, l));
           }
@@ -872,7 +937,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!whole) {
         // ---- the last block of the unit joins its pieces
-        const int c1 = cut.run_of(u.at + u.tiles - 1);
+        const int c1 = cut.run_of(w.at + w.tiles - 1);
         __threadfence();
         if (!sync_all()) break;
         if (tid == 0) {
@@ -883,7 +948,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!sync_all()) break;
         if (sh.last) {
-          const int rows = min(256, u.rows - p.r0);
+          const int rows = min(256, w.rows - p.r0);
           for (int x = tid; x < rows * (D / 8); x += kSoftWarps * 32) {
             const int rr = x % rows, d8 = x / rows;
             float most = -INFINITY;
@@ -903,16 +968,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool fine = z > 0.f;
             const float inv = fine ? 1.f / z : 0.f;
             for (int e = 0; e < 8; ++e) acc[e] = fine ? acc[e] * inv : 0.f;
-            const int qrow = p.r0 + rr, tok = qrow / g.group, hh = u.h * g.group + qrow - tok * g.group;
-            *reinterpret_cast<uint4*>((T*)g.out + (long long)(u.a + tok) * g.os[0] + (long long)hh * g.os[1] + d8 * 8) =
+            const int qrow = p.r0 + rr, tok = qrow / g.group, hh = w.h * g.group + qrow - tok * g.group;
+            *reinterpret_cast<uint4*>((T*)g.out + (long long)(w.a + tok) * g.os[0] + (long long)hh * g.os[1] + d8 * 8) =
                 pack8<T>(acc);
-            if (g.lse && d8 == 0) g.lse[(long long)(u.a + tok) * g.H + hh] = fine ? (most + log2f(z)) * kLn2 : -INFINITY;
+            if (g.lse && d8 == 0) g.lse[(long long)(w.a + tok) * g.H + hh] = fine ? (most + log2f(z)) * kLn2 : -INFINITY;
           }
         }
       } else if (!p.wide) {
         ok = sync_all();  // both halves have read both streams' rows before the next piece writes them
       }
-      next_unit(g, u);
+      __syncwarp();
+      if (lane == 0) next_unit(g, w);
+      __syncwarp();
     }
     if (!ok) *gave_up = 1;
   }
@@ -1022,6 +1089,7 @@ extern "C" int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, con
   a.qs[0] = query->q.token_stride, a.qs[1] = query->q.head_stride;
   a.os[0] = query->out.token_stride, a.os[1] = query->out.head_stride;
   a.H = p.n_heads, a.Hk = p.n_kv_heads, a.group = a.H / a.Hk, a.scale = query->scale, a.status = d_status;
+  a.sectors = (uintptr_t)a.out % 32 == 0 && a.os[0] % 16 == 0 && a.os[1] % 16 == 0;
   a.parts = reinterpret_cast<float4*>(kv->parts), a.part_ml = kv->part_ml, a.joined = kv->joined;
   auto go = [&](auto kern, size_t smem) {
     return launch_pdl(kern, dim3(kv->sms), dim3(kThreads), smem, (cudaStream_t)stream, a, kv->k_map, kv->v_map);
