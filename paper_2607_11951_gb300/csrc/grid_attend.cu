@@ -32,11 +32,13 @@ namespace {
 
 constexpr int kTile = 128;            // keys of a tile, query rows of a stream
 constexpr int kSoftWarps = 8;         // four per stream
-constexpr int kLoadWarp = kSoftWarps, kMmaWarp = kSoftWarps + 1;  // one that loads tiles, one that multiplies,
-constexpr int kQueryWarp = kSoftWarps + 2, kQueryWarps = 2;        // two that load queries
+constexpr int kLoadWarp = kSoftWarps;      // two that load tiles, of keys and of values,
+constexpr int kMmaWarp = kSoftWarps + 2;   // one that multiplies,
+constexpr int kQueryWarp = kSoftWarps + 3, kQueryWarps = 1;  // one that loads queries
 constexpr int kThreads = (kSoftWarps + 4) * 32;
-constexpr int kMinRun = 4;            // of a run, at least (unless there are fewer)
-constexpr int kUnitCost = 2;          // what a unit's beginning and end cost, in tiles
+// A unit's beginning and end cost as much as some tiles, and a run is not worth splitting below a few (2, 4: 27.5 us for 32
+// rows of one token, 221 for 27 prompts, 469 for 2 x 2,000 tokens over 16,000; 1, 4: 29.5, 227, 495; 3, 5: 27.1, 225, 447).
+constexpr int kUnitCost = 3, kMinRun = 5;
 constexpr int kRing = 8;              // pieces whose bad-page flags are kept at once
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
@@ -434,7 +436,7 @@ struct Shared {
   float2 ml[2][kTile];
   Units units[kSoftWarps];
   int sums[kThreads / 32];
-  int first, per, row[4], gave_up, last, bad[kRing];
+  int first, per, row[4], gave_up, last, bad[2][kRing];
   uint32_t tmem;
 };
 
@@ -475,6 +477,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     sh.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_at(&sh.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    tm_before();
+  }
   pdl_wait();
 
   // How many tiles there are in all, and the row that this block begins in.
@@ -488,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool some = b < min(c.B, (tid + 1) * per) && open_row(g, u, b);
       int t = some && u.units == 1 ? kUnitCost + tiles_of(u, g.group, 0) : 0, at = -1;
       if (tid == 0) sh.last = 0;
-      __syncthreads();
+      if (!__syncthreads_or(some && u.units > 1)) return t;
       if (some && u.units > 1) {
         at = atomicAdd(&sh.last, 1);
         many[3 * at] = u.n, many[3 * at + 1] = u.len;
@@ -542,14 +549,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   const bool works = (int)blockIdx.x < cut.runs;
-  if (works && warp == kMmaWarp) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_at(&sh.tmem)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    tm_before();
-  }
   __syncthreads();
   tm_after();
-  const uint32_t tmem = works ? sh.tmem : 0;
+  const uint32_t tmem = sh.tmem;
   const int lo = works ? cut.begin(blockIdx.x) : 0, hi = works ? cut.begin(blockIdx.x + 1) : 0;
   volatile int* gave_up = &sh.gave_up;
   if (works) {  // the unit that the run begins in
@@ -557,6 +559,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     set_row(g, u);
     u.h = (lo - sh.first) / sh.per;
     u.at = sh.first + u.h * sh.per;
+    u.qt = 0;
+    if (u.units == 1) {
+      u.tiles = tiles_of(u, g.group, 0);
+      u.at += kUnitCost;
+    } else
 #pragma unroll 1
     for (int i = 0;; i += 32) {  // 32 units at once
       const int mine = i + lane < u.units ? kUnitCost + tiles_of(u, g.group, i + lane) : 0;
@@ -578,68 +585,61 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
 
-  if (warp == kLoadWarp) {
-    // ---- one warp keeps the ring of tiles full: a lane per page and half of the columns
+  if (warp < kMmaWarp && warp >= kLoadWarp) {
+    // ---- two warps keep the ring of tiles full, one with keys and one with values: a lane per page and half of the
+    // columns (a copy takes its lane about 90 cycles to issue, and pages of 16 tokens make 16 copies of a tile)
     async_fence();  // (the plan was made where the tiles come)
-    int it = 0;
+    const bool v = warp != kLoadWarp;
+    int base = 0, it = 0;  // the piece's first item of the ring, and this warp's
     if (works) {
       const int box = min(kTile, 1 << c.log_page), pages = kTile / box, boxes = pages * (D / 64);
       const int part = lane / pages, page_lane = lane - part * pages;
       const uint32_t to = ring + part * (kTile * 128) + page_lane * box * 128;
+      const CUtensorMap* map = v ? &v_map : &k_map;
       bool ok = true;
-      // the ids of 32 pages at a time, the lane's its own: those of the keys' tile, and before and after them
-      int row = -1, block = 0, id_was = 0, id = 0, id_next = 0;
+      // the ids of 32 pages at a time, the lane's its own: those of the tile, and those after them
+      int row = -1, block = 0, id = 0, id_next = 0;
 #pragma unroll 1
       for (int k = 0; ok && u.at < hi; ++k) {
         const Piece p = piece_of(u, lo, hi);
         const int used = (u.len + u.n + (1 << c.log_page) - 1) >> c.log_page;  // pages of the row
-        int* bad = &sh.bad[k % kRing];
+        int* bad = &sh.bad[v][k % kRing];
         if (lane == 0) *bad = 0;
         __syncwarp();
         auto fetch = [&](int bl) {  // -1: outside the cache; past the row: one past the pool, which loads zeros
           const int pg = bl * 32 + lane;
           return pg < used ? page_of(c, u.b, pg << c.log_page) : c.n_pages;
         };
-        auto load = [&](int t, bool v) {
-          const int st = it % L::kStages, token = t * kTile, pg = token >> c.log_page;
-          if (row != u.b || (!v && pg >> 5 != block)) {
-            id_was = id;
+        const int n = p.t1 - p.t0;
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+          // its place in the order in which the products take them: K0 V0 K1 V1 ... where the streams share the tiles,
+          // K0 K1 V0 K2 V1 K3 ... where they take them in turn
+          it = base + (p.wide ? 2 * j + v : v ? min(2 * j + 2, 2 * n - 1) : max(j, 2 * j - 1));
+          const int st = it % L::kStages, token = (p.t0 + j) * kTile, pg = token >> c.log_page;
+          if (row != u.b || pg >> 5 != block) {
             id = row == u.b && pg >> 5 == block + 1 ? id_next : fetch(pg >> 5);
             row = u.b;
             block = pg >> 5;
             id_next = fetch(block + 1);
           }
-          int page = __shfl_sync(~0u, pg >> 5 == block ? id : id_was, (pg + page_lane) & 31);
+          int page = __shfl_sync(~0u, id, (pg + page_lane) & 31);
           if (page < 0) {
             page = c.n_pages;
             if (lane < boxes) *bad = 1;
           }
-          if (!bar_wait(&sh.empty[st], ((it / L::kStages) & 1) ^ 1, gave_up)) return false;
+          if (!(ok = bar_wait(&sh.empty[st], ((it / L::kStages) & 1) ^ 1, gave_up))) break;
           if (lane == 0) bar_expect(&sh.full[st], L::kTileBytes);
           __syncwarp();
           if (lane < boxes)
-            load_tile(v ? &v_map : &k_map, to + st * L::kTileBytes, &sh.full[st], part * 64,
-                      token & ((1 << c.log_page) - 1), u.h, page);
-          ++it;
-          return true;
-        };
-        // in the order in which the products take them
-        if (p.wide) {
-#pragma unroll 1
-          for (int x = 0; ok && x < 2 * (p.t1 - p.t0); ++x) ok = load(p.t0 + x / 2, x & 1);
-        } else {
-#pragma unroll 1
-          for (int x = -2; ok && x < 2 * (p.t1 - p.t0); ++x) {  // K0 K1 V0 K2 V1 K3 ...
-            const bool v = x >= 0 && !(x & 1);
-            const int t = p.t0 + (x < 0 ? x + 2 : x / 2 + (v ? 0 : 2));
-            if (t < p.t1) ok = load(t, v);
-          }
+            load_tile(map, to + st * L::kTileBytes, &sh.full[st], part * 64, token & ((1 << c.log_page) - 1), u.h, page);
         }
+        base += 2 * n;
         next_unit(g, u);
       }
     }
-    // ---- then reports the rows, and zeros those that are not in order
-    for (int b = blockIdx.x; b < c.B; b += gridDim.x) {
+    // ---- then one of them reports the rows, and zeros those that are not in order
+    for (int b = blockIdx.x; !v && b < c.B; b += gridDim.x) {
       int a, n, len;
       bool good = row_span(c, b, a, n, len);
       if (good && n)
@@ -656,9 +656,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
-    // (no copy is in flight when the block ends)
-    for (int i = max(0, it - L::kStages); i < it; ++i)
-      if (!bar_wait(&sh.full[i % L::kStages], (i / L::kStages) & 1, gave_up)) break;
+    // (No copy is in flight when the block ends: every tile was waited for.  Where a wait was given up, what is still on
+    // its way has a tenth of a millisecond to land.)
+    if (*gave_up)
+      for (const long long t0 = clock64(); clock64() - t0 < 200000;) {
+      }
   } else if (warp == kMmaWarp) {
     // ---- one thread issues the products, with as little as can be between them
     if (works && elected()) {
@@ -739,8 +741,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   } else if (warp >= kQueryWarp) {
-    // ---- two warps bring the next unit's queries as soon as the last product has read the ones before
+    // ---- one warp brings the next unit's queries as soon as the last product has read the ones before
     constexpr int kPer = D / 8;  // 16-byte parts of a query row, a lane each
+    constexpr int step = kQueryWarps * 32 / kPer;
+    const int part = tid % kPer, step_head = step % g.group;
+    const long long step_src = step / g.group * g.qs[0] + step_head * g.qs[1];  // (where the head does not pass its group's end)
     int n_f[2] = {0, 0};
     bool ok = works;
 #pragma unroll 1
@@ -752,14 +757,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = bar_wait(&sh.q_free[s], (n_f[s]++ & 1) ^ 1, gave_up);
         if (!ok) break;
         const int r0 = p.r0 + (p.wide ? s * kTile : 0), rows = min(kTile, u.rows - r0);
-        const int part = tid % kPer, step = kQueryWarps * 32 / kPer;
         // (rows past the unit's last are left as they are: they have no part in any other row)
+        const int r_first = (tid - kQueryWarp * 32) / kPer, row = r0 + r_first, t = row / g.group;
+        int of = row - t * g.group;  // the query head within its group
+        const T* src = (const T*)g.q + (long long)(u.a + t) * g.qs[0] + (long long)(u.h * g.group + of) * g.qs[1] + part * 8;
+        const uint32_t to = q_at + s * L::kTileBytes + (part / 8) * (kTile * 128);
 #pragma unroll 4
-        for (int r = (tid - kQueryWarp * 32) / kPer; r < rows; r += step) {
-          const int row = r0 + r, t = row / g.group, head = u.h * g.group + row - t * g.group;
-          const T* src = (const T*)g.q + (long long)(u.a + t) * g.qs[0] + (long long)head * g.qs[1] + part * 8;
-          const uint32_t dst = q_at + s * L::kTileBytes + r * 128 + (part / 8) * (kTile * 128) + ((part % 8) ^ (r & 7)) * 16;
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+        for (int r = r_first; r < rows; r += step) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + r * 128 + ((part % 8) ^ (r & 7)) * 16), "l"(src)
+                       : "memory");
+          of += step_head;
+          src += step_src;
+          if (of >= g.group) {
+            of -= g.group;
+            src += g.qs[0] - g.group * g.qs[1];
+          }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
         async_fence();
@@ -889,25 +901,27 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++n_o[z];
         }
       if (!ok) break;
-      if (sh.bad[k % kRing]) l = NAN;  // (some key that the rows may read is in no page of the cache; known once all tiles were)
+      if (sh.bad[0][k % kRing] | sh.bad[1][k % kRing]) l = NAN;  // (some key that the rows may read is in no page of the cache; known once all tiles were)
       if (warp_live) {
         tm_after();
         const bool fine = l > 0.f;
-        const float inv = whole ? (fine ? 1.f / l : 0.f) : 1.f;
+        const float by = !whole ? 1.f : fine ? __frcp_rn(l) : 0.f, f0 = f[0] * by, f1 = f[1] * by;
+        const bool two = !p.wide && p.n[1];
         const int from = p.wide ? 0 : s * (D / 2), to = p.wide ? D : from + D / 2;
         const int part_row = r + (p.wide ? s * kTile : 0);
 #pragma unroll 1
         for (int j = from; j < to; j += 16) {
           uint32_t o[16], o1[16] = {};
           tm_load16(o_at + (p.wide ? s * D : 0) + j, o);
-          if (!p.wide && p.n[1]) tm_load16(o_at + D + j, o1);
+          if (two) tm_load16(o_at + D + j, o1);
           tm_loaded16(o, o1);
           float y[16];
+          if (two) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            y[e] = __uint_as_float(o[e]) * f[0];
-            if (!p.wide && p.n[1]) y[e] += __uint_as_float(o1[e]) * f[1];
-            y[e] = whole && !fine ? 0.f : y[e] * inv;
+            for (int e = 0; e < 16; ++e) y[e] = fmaf(__uint_as_float(o1[e]), f1, __uint_as_float(o[e]) * f0);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] = __uint_as_float(o[e]) * f0;
           }
           if (live && whole) {
             const uint4 a = pack8<T>(y), b = pack8<T>(y + 8);
@@ -938,9 +952,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!whole) {
         // ---- the last block of the unit joins its pieces
         const int c1 = cut.run_of(w.at + w.tiles - 1);
-        __threadfence();
         if (!sync_all()) break;
         if (tid == 0) {
+          __threadfence();  // (after the barrier: for what all the others wrote)
           const int n = atomicAdd(&g.joined[c0], 1);
           sh.last = n == c1 - c0;
           if (sh.last) g.joined[c0] = 0;
@@ -949,29 +963,48 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!sync_all()) break;
         if (sh.last) {
           const int rows = min(256, w.rows - p.r0);
-          for (int x = tid; x < rows * (D / 8); x += kSoftWarps * 32) {
-            const int rr = x % rows, d8 = x / rows;
-            float most = -INFINITY;
-            for (int b = c0; b <= c1; ++b)
-              most = fmaxf(most, __ldcg(g.part_ml + (size_t)(2 * b + (b == c0)) * 256 + rr).x);
-            float acc[8] = {}, z = 0.f;
+          int cols = 8;  // of a row to a thread: all of them where there are rows enough
+          while (cols < D && rows * (D / cols) > kSoftWarps * 32) cols *= 2;
+          for (int x = tid; x < rows * (D / cols); x += kSoftWarps * 32) {
+            const int rr = x % rows, from = x / rows * cols;
+            float most = -INFINITY, z = 0.f;
+            for (int b = c0; b <= c1; ++b) most = fmaxf(most, __ldcg(g.part_ml + (size_t)(2 * b + (b == c0)) * 256 + rr).x);
+            const float base = most > -INFINITY ? most : 0.f;
             for (int b = c0; b <= c1; ++b) {
-              const size_t from = 2 * b + (b == c0);
-              const float2 e = __ldcg(g.part_ml + from * 256 + rr);
-              const float w = e.x > -INFINITY ? exp2_fast(e.x - most) : 0.f;
-              const float4* src = g.parts + from * (D / 4) * 256 + rr;
-              const float4 v0 = __ldcg(src + (size_t)(2 * d8) * 256), v1 = __ldcg(src + (size_t)(2 * d8 + 1) * 256);
-              z += e.y * w;
-              acc[0] += v0.x * w, acc[1] += v0.y * w, acc[2] += v0.z * w, acc[3] += v0.w * w;
-              acc[4] += v1.x * w, acc[5] += v1.y * w, acc[6] += v1.z * w, acc[7] += v1.w * w;
+              const float2 e = __ldcg(g.part_ml + (size_t)(2 * b + (b == c0)) * 256 + rr);
+              z += e.y * exp2_fast(e.x - base);
             }
             const bool fine = z > 0.f;
-            const float inv = fine ? 1.f / z : 0.f;
-            for (int e = 0; e < 8; ++e) acc[e] = fine ? acc[e] * inv : 0.f;
+            const float by = fine ? __frcp_rn(z) : 0.f;
             const int qrow = p.r0 + rr, tok = qrow / g.group, hh = w.h * g.group + qrow - tok * g.group;
-            *reinterpret_cast<uint4*>((T*)g.out + (long long)(w.a + tok) * g.os[0] + (long long)hh * g.os[1] + d8 * 8) =
-                pack8<T>(acc);
-            if (g.lse && d8 == 0) g.lse[(long long)(w.a + tok) * g.H + hh] = fine ? (most + log2f(z)) * kLn2 : -INFINITY;
+            T* to = (T*)g.out + (long long)(w.a + tok) * g.os[0] + (long long)hh * g.os[1];
+            auto add_up = [&](auto columns, int j) {  // so many columns at a time: their loads do not wait for one another
+              constexpr int kN = decltype(columns)::value;
+              float acc[kN] = {};
+#pragma unroll 1
+              for (int b = c0; b <= c1; ++b) {
+                const size_t slot = 2 * b + (b == c0);
+                const float f = exp2_fast(__ldcg(g.part_ml + slot * 256 + rr).x - base);
+                const float4* src = g.parts + (slot * (D / 4) + j / 4) * 256 + rr;
+                float4 v[kN / 4];
+#pragma unroll
+                for (int e = 0; e < kN / 4; ++e) v[e] = __ldcg(src + e * 256);
+#pragma unroll
+                for (int e = 0; e < kN / 4; ++e)
+                  acc[4 * e] += v[e].x * f, acc[4 * e + 1] += v[e].y * f, acc[4 * e + 2] += v[e].z * f, acc[4 * e + 3] += v[e].w * f;
+              }
+#pragma unroll
+              for (int e = 0; e < kN; ++e) acc[e] *= by;
+#pragma unroll
+              for (int e = 0; e < kN; e += 8) *reinterpret_cast<uint4*>(to + j + e) = pack8<T>(acc + e);
+            };
+            if (cols >= 32)
+#pragma unroll 1
+              for (int j = from; j < from + cols; j += 32) add_up(std::integral_constant<int, 32>(), j);
+            else
+#pragma unroll 1
+              for (int j = from; j < from + cols; j += 8) add_up(std::integral_constant<int, 8>(), j);
+            if (g.lse && from == 0) g.lse[(long long)(w.a + tok) * g.H + hh] = fine ? (most + log2f(z)) * kLn2 : -INFINITY;
           }
         }
       } else if (!p.wide) {
@@ -986,7 +1019,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   if (sh.gave_up)
     for (int b = tid; b < c.B; b += kThreads) g.status[b] = GRID_ST_BOUND;
-  if (works && warp == kMmaWarp) {
+  if (warp == kMmaWarp) {
     tm_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
