@@ -36,9 +36,10 @@ constexpr int kLoadWarp = kSoftWarps;      // two that load tiles, of keys and o
 constexpr int kMmaWarp = kSoftWarps + 2;   // one that multiplies,
 constexpr int kQueryWarp = kSoftWarps + 3, kQueryWarps = 1;  // one that loads queries
 constexpr int kThreads = (kSoftWarps + 4) * 32;
-// A unit's beginning and end cost as much as some tiles, and a run is not worth splitting below a few (2, 4: 27.5 us for 32
-// rows of one token, 221 for 27 prompts, 469 for 2 x 2,000 tokens over 16,000; 1, 4: 29.5, 227, 495; 3, 5: 27.1, 225, 447).
-constexpr int kUnitCost = 3, kMinRun = 5;
+// A unit's beginning and end cost as much as some tiles, and runs are not made shorter than a few (cost 2: 27.8 us for 32
+// rows of one token, 205 for 27 prompts, 440 for 2 x 2,000 tokens over 16,000; cost 3: 27.1, 212, 441; runs of 4 and cost
+// 1: one token over 400 takes 14.7 us where it takes 11.3).
+constexpr int kUnitCost = 2, kMinRun = 5;
 constexpr int kRing = 8;              // pieces whose bad-page flags are kept at once
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
@@ -81,10 +82,13 @@ __device__ __forceinline__ bool bar_try(uint64_t* b, int parity) {
 // gave up; false then.  Whole warps wait, and leave together.
 __device__ __noinline__ bool bar_wait_long(uint64_t* b, int parity, volatile int* gave_up) {
   const long long t0 = clock64();
-  bool ok;
-  while (!(ok = bar_try(b, parity)) && !*gave_up)
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 32; ++i)
+      if (bar_try(b, parity)) return true;
+    if (*gave_up) return false;
     if (clock64() - t0 > 4000000000LL) *gave_up = 1;
-  return ok;
+  }
 }
 __device__ __forceinline__ bool bar_wait(uint64_t* b, int parity, volatile int* gave_up) {
   if (__all_sync(~0u, bar_try(b, parity))) return true;
@@ -742,10 +746,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else if (warp >= kQueryWarp) {
     // ---- one warp brings the next unit's queries as soon as the last product has read the ones before
-    constexpr int kPer = D / 8;  // 16-byte parts of a query row, a lane each
-    constexpr int step = kQueryWarps * 32 / kPer;
-    const int part = tid % kPer, step_head = step % g.group;
-    const long long step_src = step / g.group * g.qs[0] + step_head * g.qs[1];  // (where the head does not pass its group's end)
+    constexpr int kPer = D / 16, kRows = 16;  // a row's 16-byte parts, half of them to each of two lanes
+    const int part = lane % 2 * kPer, step_head = kRows % g.group;
+    const long long step_src = kRows / g.group * g.qs[0] + step_head * g.qs[1];  // (where the head does not pass its group's end)
     int n_f[2] = {0, 0};
     bool ok = works;
 #pragma unroll 1
@@ -758,14 +761,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         const int r0 = p.r0 + (p.wide ? s * kTile : 0), rows = min(kTile, u.rows - r0);
         // (rows past the unit's last are left as they are: they have no part in any other row)
-        const int r_first = (tid - kQueryWarp * 32) / kPer, row = r0 + r_first, t = row / g.group;
+        const int r_first = lane / 2, row = r0 + r_first, t = row / g.group;
         int of = row - t * g.group;  // the query head within its group
         const T* src = (const T*)g.q + (long long)(u.a + t) * g.qs[0] + (long long)(u.h * g.group + of) * g.qs[1] + part * 8;
-        const uint32_t to = q_at + s * L::kTileBytes + (part / 8) * (kTile * 128);
-#pragma unroll 4
-        for (int r = r_first; r < rows; r += step) {
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + r * 128 + ((part % 8) ^ (r & 7)) * 16), "l"(src)
-                       : "memory");
+        const uint32_t to = q_at + s * L::kTileBytes;
+#pragma unroll 1
+        for (int r = r_first; r < rows; r += kRows) {
+#pragma unroll
+          for (int x = 0; x < kPer; ++x) {
+            const int y = part + x;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + r * 128 + (y / 8) * (kTile * 128) + ((y % 8) ^ (r & 7)) * 16),
+                         "l"(src + x * 8)
+                         : "memory");
+          }
           of += step_head;
           src += step_src;
           if (of >= g.group) {

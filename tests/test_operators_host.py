@@ -109,4 +109,4 @@ def test_launches_cover_every_position(fake, B, K, V):
         (_, g0, *_), (_, g1, *_) = rt.launches()
         rows = B * (K + 1)
         assert g0[0] % rows == 0 and rows <= g0[0] <= rows + 8 * 152 and g0[1] == g0[2] == 1
-        assert g1[0] % B == 0 and B <= g1[0] <= B + 8 * 152
+        assert g1[0] % B == 0 and B <= g1[0] <= B + 24 * 152
