@@ -28,6 +28,7 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxPieces = 64, kMaxParts = 256;  // of one position's logits, of one draw
 constexpr int kMaxDraft = 64;
+constexpr int kAlone = 4096;  // ids that a row's last block draws from by itself
 constexpr int kBlocksPerSm = 8, kDrawsPerSm = 24; // blocks wanted of either kernel
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -289,12 +290,48 @@ __device__ __noinline__ int largest(const T* l, const uint32_t* mask, int V) {
   return join_warp<true>(y).id;
 }
 
-// What the tests need of a drafted id.
-struct alignas(16) Drafted {
-  float l, uq;  // its logit (-inf: refused whatever u is) and u q(x)
-  int id, pad;
+// Best score so far and the first id that has it.
+struct alignas(8) Best {
+  float s;
+  int id;
 };
-// What k_draw needs of a row.
+__device__ __forceinline__ void better(Best& x, float s, int id) {
+  if (s > x.s || (s == x.s && id < x.id)) x = Best{s, id};
+}
+__device__ __forceinline__ Best best_warp(Best x) {
+  for (int o = 16; o; o >>= 1) {
+    const float s = __shfl_xor_sync(~0u, x.s, o);
+    const int id = __shfl_xor_sync(~0u, x.id, o);
+    better(x, s, id);
+  }
+  return x;
+}
+// What scores the ids of a row's draw: w / e with w = p - q, by an approximate
+// reciprocal (two units in the last place: a score is only compared with
+// scores).  0 or less, or not finite: the id cannot be drawn.
+struct Scorer {
+  float c, base, inv_s;
+  __device__ __forceinline__ float operator()(float l, float e, float q) const {
+    float t = fmaf(l, c, -base), r;
+    if (!(t < 126.f)) t = exponent(l, c) - base;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e));
+    return fmaf(exp2_fast(t), inv_s, -q) * r;
+  }
+};
+__device__ __forceinline__ void keep(Best& z, float s, int id) {
+  if (s > z.s && s < INFINITY) z = Best{s, id};
+}
+
+// The draw of a row by the target's own weights, by a warp (no residual weight was left).
+template <typename T>
+__device__ __noinline__ Best draw_whole(Scorer score, const T* l, const uint32_t* mask, const float* e, int V) {
+  Best z{0.f, INT_MAX};
+  for (int i = threadIdx.x & 31; i < V; i += 32)
+    if (admitted(mask, i)) keep(z, score(value(l[i]), e[i], 0.f), i);
+  return best_warp(z);
+}
+
+// What a draw needs to know of its row.
 struct alignas(16) Row {
   int n;           // position to draw from, or -1: the row's outcome is written
   int out;         // id that the residual leaves out, or -1
@@ -303,12 +340,76 @@ struct alignas(16) Row {
   int refused, pad[2];
 };
 
+// The best of the ids lo .. hi-1 of row b's draw, by a block; warp 0 gets it.  A
+// warp takes 256 ids at a time, a lane per id of eight mask words.
+template <typename T>
+__device__ __forceinline__ Best draw_part(const grid_draft_step& a, int b, const Row& r, int lo, int hi) {
+  constexpr int kWords = 8, kIds = kWords * 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, words = (a.V + 31) / 32;
+  __shared__ Best sh[kWarps];
+  const Scorer score{r.c, r.base, 1.f / r.s};
+  const T* l = logits_at<T>(a, b, r.n);
+  const uint32_t* mask = mask_at(a, b, r.n);
+  const float* q = r.refused && a.d_probs ? a.d_probs + b * a.prob_stride[0] + r.n * a.prob_stride[1] : nullptr;
+  const float* e = a.d_noise + b * a.noise_stride;
+  auto word_at = [&](int t0) {
+    const uint32_t w = lane < kWords ? tile_word(mask, words, t0, hi, lane) : 0u;
+    return (unsigned)(r.out - t0 - 32 * lane) < 32u ? w & ~(1u << (r.out - t0 - 32 * lane)) : w;
+  };
+  Best z{0.f, INT_MAX};
+  uint32_t ahead = word_at(lo + warp * kIds);
+#pragma unroll 1
+  for (int t0 = lo + warp * kIds; t0 < hi; t0 += kWarps * kIds) {
+    const uint32_t word = ahead;
+    ahead = word_at(t0 + kWarps * kIds);
+    if (!__any_sync(~0u, word != 0)) continue;
+    T lv[kWords];
+    float ev[kWords], qv[kWords];
+#pragma unroll
+    for (int u = 0; u < kWords; ++u) {
+      const bool in = __shfl_sync(~0u, word, u) >> lane & 1;
+      const int id = t0 + 32 * u + lane;
+      lv[u] = 0, ev[u] = INFINITY, qv[u] = 0.f;  // (infinite noise: a score of zero)
+      load_if(lv[u], l + id, in);
+      load_if(ev[u], e + id, in);
+      load_if(qv[u], q + id, in && q);
+    }
+#pragma unroll
+    for (int u = 0; u < kWords; ++u) keep(z, score(value(lv[u]), ev[u], qv[u]), t0 + 32 * u + lane);
+  }
+  z = best_warp(z);
+  if (lane == 0) sh[warp] = z;
+  __syncthreads();
+  return best_warp(lane < kWarps ? sh[lane] : Best{0.f, INT_MAX});
+}
+// The token that the row's best id makes, by a warp.
+template <typename T>
+__device__ __forceinline__ void draw_end(const grid_draft_step& a, int b, const Row& r, Best z) {
+  const T* l = logits_at<T>(a, b, r.n);
+  const uint32_t* mask = mask_at(a, b, r.n);
+  if (!(z.s > 0.f) && r.refused)
+    z = draw_whole(Scorer{r.c, r.base, 1.f / r.s}, l, mask, a.d_noise + b * a.noise_stride, a.V);
+  const int token = z.s > 0.f ? z.id : largest(l, mask, a.V);  // (the latter: no noise was positive)
+  if ((threadIdx.x & 31) == 0) {
+    a.d_tokens[(size_t)b * (a.K + 1) + r.n] = token;
+    if (a.d_logprob)
+      a.d_logprob[(size_t)b * (a.K + 1) + r.n] = log_prob(clean(value(l[token])), r.c, Stat{r.base, r.s, 0.f, 0});
+    if (token == a.eos) a.d_status[b] = GRID_ST_COMPLETE;
+  }
+}
+
+// What the tests need of a drafted id.
+struct alignas(16) Drafted {
+  float l, uq;  // its logit (-inf: refused whatever u is) and u q(x)
+  int id, pad;
+};
 // One piece of one position: block (position row) * pieces + piece.  Pieces
 // are cut where the position's 16-byte lines begin, so that rows of any
 // alignment are read in whole lines; the ids before the first line belong to
 // piece 0, those after the last to the last piece.  The last block of a row
-// walks its acceptance tests and writes what they decide.
-template <typename T>
+// walks its acceptance tests and writes what they decide; over a small
+// vocabulary (kDraws) it also draws, which saves a launch.
+template <typename T, bool kDraws>
 __global__ void __launch_bounds__(kThreads) k_stats(const grid_draft_step a, Stat* __restrict__ stats, int pieces,
                                                     int piece, int* __restrict__ done, Drafted* __restrict__ drafted,
                                                     Row* __restrict__ rows) {
@@ -405,107 +506,34 @@ __global__ void __launch_bounds__(kThreads) k_stats(const grid_draft_step a, Sta
     a.d_tokens[(size_t)b * (a.K + 1) + j] = id;
     if (a.d_logprob) a.d_logprob[(size_t)b * (a.K + 1) + j] = j < n ? lp[j] : id >= 0 ? log_prob(x.m, c, x) : 0.f;
   }
+  const Row r{settled ? -1 : n, n < nd && !a.d_probs ? ids[n] : -1, x.base, x.s, c, n < nd, {0, 0}};
   if (tid == 0) {
     a.d_accepted[b] = n;
     a.d_status[b] = ended || (!empty && greedy && x.id == a.eos) ? GRID_ST_COMPLETE : empty ? GRID_ST_EMPTY_MASK : GRID_ST_OK;
-    rows[b] = Row{settled ? -1 : n, n < nd && !a.d_probs ? ids[n] : -1, x.base, x.s, c, n < nd, {0, 0}};
+    if (!kDraws) rows[b] = r;
   }
-}
-
-// Best score so far and the first id that has it.
-struct alignas(8) Best {
-  float s;
-  int id;
-};
-__device__ __forceinline__ void better(Best& x, float s, int id) {
-  if (s > x.s || (s == x.s && id < x.id)) x = Best{s, id};
-}
-__device__ __forceinline__ Best best_warp(Best x) {
-  for (int o = 16; o; o >>= 1) {
-    const float s = __shfl_xor_sync(~0u, x.s, o);
-    const int id = __shfl_xor_sync(~0u, x.id, o);
-    better(x, s, id);
+  if (kDraws && !settled) {
+    const Best z = draw_part<T>(a, b, r, 0, a.V);  // (its barrier lies between what was written above and the token)
+    if (warp == 0) draw_end<T>(a, b, r, z);
   }
-  return x;
-}
-// What scores the ids of a row's draw: w / e with w = p - q, by an approximate
-// reciprocal (two units in the last place: a score is only compared with
-// scores).  0 or less, or not finite: the id cannot be drawn.
-struct Scorer {
-  float c, base, inv_s;
-  __device__ __forceinline__ float operator()(float l, float e, float q) const {
-    float t = fmaf(l, c, -base), r;
-    if (!(t < 126.f)) t = exponent(l, c) - base;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e));
-    return fmaf(exp2_fast(t), inv_s, -q) * r;
-  }
-};
-__device__ __forceinline__ void keep(Best& z, float s, int id) {
-  if (s > z.s && s < INFINITY) z = Best{s, id};
-}
-
-// The draw of a row by the target's own weights, by a warp (no residual weight was left).
-template <typename T>
-__device__ __noinline__ Best draw_whole(Scorer score, const T* l, const uint32_t* mask, const float* e, int V) {
-  Best z{0.f, INT_MAX};
-  for (int i = threadIdx.x & 31; i < V; i += 32)
-    if (admitted(mask, i)) keep(z, score(value(l[i]), e[i], 0.f), i);
-  return best_warp(z);
 }
 
 // The draw of one row: block row * parts + part scores its part of the
 // vocabulary at the row's position n; the last of the row's blocks writes the
-// token.  A warp takes 256 ids at a time, a lane per id of eight mask words.
+// token.
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 5) k_draw(const grid_draft_step a, const Row* __restrict__ rows,
                                                       Best* __restrict__ best, int* __restrict__ done, int parts, int part) {
-  constexpr int kWords = 8, kIds = kWords * 32;
-  const int b = blockIdx.x / parts, pt = blockIdx.x - b * parts;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  __shared__ Best sh[kWarps];
+  const int b = blockIdx.x / parts, pt = blockIdx.x - b * parts, lane = threadIdx.x & 31;
   pdl_wait();
   pdl_next();
   const float4* row = reinterpret_cast<const float4*>(rows + b);
   const float4 r4 = __ldcg(row), s4 = __ldcg(row + 1);
-  const int n = __float_as_int(r4.x), out = __float_as_int(r4.y);
-  if (n < 0) return;
-  const Scorer score{s4.x, r4.z, 1.f / r4.w};
-  const bool refused = __float_as_int(s4.y) != 0;
-  const T* l = logits_at<T>(a, b, n);
-  const uint32_t* mask = mask_at(a, b, n);
-  const float* q = refused && a.d_probs ? a.d_probs + b * a.prob_stride[0] + n * a.prob_stride[1] : nullptr;
-  const float* e = a.d_noise + b * a.noise_stride;
-  const int lo = min(a.V, pt * part), hi = min(a.V, lo + part), words = (a.V + 31) / 32;
-  auto word_at = [&](int t0) {
-    const uint32_t w = lane < kWords ? tile_word(mask, words, t0, hi, lane) : 0u;
-    return (unsigned)(out - t0 - 32 * lane) < 32u ? w & ~(1u << (out - t0 - 32 * lane)) : w;
-  };
-  Best z{0.f, INT_MAX};
-  uint32_t ahead = word_at(lo + warp * kIds);
-#pragma unroll 1
-  for (int t0 = lo + warp * kIds; t0 < hi; t0 += kWarps * kIds) {
-    const uint32_t word = ahead;
-    ahead = word_at(t0 + kWarps * kIds);
-    if (!__any_sync(~0u, word != 0)) continue;
-    T lv[kWords];
-    float ev[kWords], qv[kWords];
-#pragma unroll
-    for (int u = 0; u < kWords; ++u) {
-      const bool in = __shfl_sync(~0u, word, u) >> lane & 1;
-      const int id = t0 + 32 * u + lane;
-      lv[u] = 0, ev[u] = INFINITY, qv[u] = 0.f;  // (infinite noise: a score of zero)
-      load_if(lv[u], l + id, in);
-      load_if(ev[u], e + id, in);
-      load_if(qv[u], q + id, in && q);
-    }
-#pragma unroll
-    for (int u = 0; u < kWords; ++u) keep(z, score(value(lv[u]), ev[u], qv[u]), t0 + 32 * u + lane);
-  }
-  z = best_warp(z);
-  if (lane == 0) sh[warp] = z;
-  __syncthreads();
-  if (warp) return;
-  z = best_warp(lane < kWarps ? sh[lane] : Best{0.f, INT_MAX});
+  const Row r{__float_as_int(r4.x), __float_as_int(r4.y), r4.z, r4.w, s4.x, __float_as_int(s4.y), {0, 0}};
+  if (r.n < 0) return;
+  const int lo = min(a.V, pt * part);
+  Best z = draw_part<T>(a, b, r, lo, min(a.V, lo + part));
+  if (threadIdx.x >= 32) return;
   int last = 0;
   if (lane == 0) {
     best[(size_t)b * parts + pt] = z;
@@ -520,15 +548,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_draw(const grid_draft_step a, c
     const float2 y = __ldcg(reinterpret_cast<const float2*>(best + (size_t)b * parts + i));
     better(z, y.x, __float_as_int(y.y));
   }
-  z = best_warp(z);
-  if (!(z.s > 0.f) && refused) z = draw_whole(score, l, mask, e, a.V);
-  const int token = z.s > 0.f ? z.id : largest(l, mask, a.V);  // (the latter: no noise was positive)
-  if (lane == 0) {
-    a.d_tokens[(size_t)b * (a.K + 1) + n] = token;
-    if (a.d_logprob)
-      a.d_logprob[(size_t)b * (a.K + 1) + n] = log_prob(clean(value(l[token])), score.c, Stat{r4.z, r4.w, 0.f, 0});
-    if (token == a.eos) a.d_status[b] = GRID_ST_COMPLETE;
-  }
+  draw_end<T>(a, b, r, best_warp(z));
 }
 
 }  // namespace
@@ -557,6 +577,9 @@ extern "C" int grid_drafts_create(int32_t B, int32_t K, int32_t V, grid_drafts**
   d->V = V;
   int rc = GRID_OK, dev = 0;
   cudaError_t e = cudaSuccess;
+  auto room = [](auto kernel, size_t bytes) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  };
   // (a call cuts n positions into at most n + kBlocksPerSm * sms pieces)
   if ((e = cudaGetDevice(&dev)) == cudaSuccess &&
       (e = cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev)) == cudaSuccess &&
@@ -566,9 +589,10 @@ extern "C" int grid_drafts_create(int32_t B, int32_t K, int32_t V, grid_drafts**
       !(rc = d->mem.alloc((size_t)B * K * sizeof(Drafted), (void**)&d->drafted)) &&
       !(rc = d->mem.alloc((size_t)B * sizeof(int), (void**)&d->done)) &&
       (e = cudaMemset(d->done, 0, (size_t)B * sizeof(int))) == cudaSuccess &&
-      (e = cudaFuncSetAttribute(k_stats<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Staged<float>))) == cudaSuccess &&
-      (e = cudaFuncSetAttribute(k_stats<uint16_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Staged<uint16_t>))) ==
-          cudaSuccess)
+      (e = room(k_stats<float, false>, sizeof(Staged<float>))) == cudaSuccess &&
+      (e = room(k_stats<float, true>, sizeof(Staged<float>))) == cudaSuccess &&
+      (e = room(k_stats<uint16_t, false>, sizeof(Staged<uint16_t>))) == cudaSuccess &&
+      (e = room(k_stats<uint16_t, true>, sizeof(Staged<uint16_t>))) == cudaSuccess)
     e = cudaDeviceSynchronize();
   if (rc || e != cudaSuccess) {
     d->mem.release();
@@ -608,15 +632,20 @@ extern "C" int grid_draft_verify(const grid_drafts* d, const grid_draft_step* s,
   int pieces, piece, parts, part;
   cut(rows, kBlocksPerSm, kWarps * kTileIds, kMaxPieces, pieces, piece);
   cut(s->B, kDrawsPerSm, 2 * kTileIds, kMaxParts, parts, part);
+  const bool alone = s->V <= kAlone;
   auto go = [&](auto stats, auto draw, size_t staged) {
     cudaError_t e = launch_pdl(stats, dim3((unsigned)(rows * pieces)), dim3(kThreads), staged, (cudaStream_t)stream, *s, d->stats,
                                pieces, piece, d->done, d->drafted, d->rows);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || alone) return e;
     return launch_pdl(draw, dim3((unsigned)(s->B * parts)), dim3(kThreads), 0, (cudaStream_t)stream, *s, (const Row*)d->rows,
                       d->best, d->done, parts, part);
   };
-  GRID_CUDA(size == 4 ? go(k_stats<float>, k_draw<float>, sizeof(Staged<float>))
-                      : go(k_stats<uint16_t>, k_draw<uint16_t>, sizeof(Staged<uint16_t>)));
+  using H = uint16_t;
+  if (size == 4)
+    GRID_CUDA(alone ? go(k_stats<float, true>, k_draw<float>, sizeof(Staged<float>))
+                    : go(k_stats<float, false>, k_draw<float>, sizeof(Staged<float>)));
+  else
+    GRID_CUDA(alone ? go(k_stats<H, true>, k_draw<H>, sizeof(Staged<H>)) : go(k_stats<H, false>, k_draw<H>, sizeof(Staged<H>)));
   GRID_CUDA(cudaGetLastError());
   return GRID_OK;
 }

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 from .build import library_path
 
@@ -59,34 +60,6 @@ def _fields(**kinds):
 class _KvPages(ctypes.Structure):
     _fields_ = _fields(d_k="p", d_v="p", dtype="i", head_dim="i", n_heads="i", n_kv_heads="i", page_size="i", n_pages="i",
                        k_stride="l3", v_stride="l3")
-
-
-class _KvChunk(ctypes.Structure):
-    _fields_ = _fields(d_table="p", table_stride="l", d_len="p", d_start="p", max_pages="i", B="i", n_tokens="i",
-                       reserved="i")
-
-
-class _Heads(ctypes.Structure):
-    _fields_ = _fields(d="p", token_stride="l", head_stride="l")
-
-
-class _KvQuery(ctypes.Structure):
-    _fields_ = [("q", _Heads), ("out", _Heads)] + _fields(d_lse="p", scale="f", reserved="i")
-
-
-class _Rotation(ctypes.Structure):
-    _fields_ = _fields(d_cos="p", d_sin="p", n_pos="i", rot="i", pairs="i", reserved="i")
-
-
-class _HeadNorm(ctypes.Structure):
-    _fields_ = _fields(d_q="p", d_k="p", eps="f", reserved="i")
-
-
-class _DraftStep(ctypes.Structure):
-    _fields_ = _fields(d_logits="p", logit_stride="l2", d_mask="p", mask_stride="l2", d_probs="p", prob_stride="l2",
-                       d_draft="p", d_draft_len="p", d_u="p", d_noise="p", noise_stride="l", d_temperature="p", dtype="i",
-                       B="i", K="i", V="i", eos="i", reserved="i", d_tokens="p", d_accepted="p", d_logprob="p",
-                       d_status="p")
 
 
 _lib = None
@@ -168,14 +141,18 @@ def _check(rc):
         raise GridError(rc, last_error())
 
 
+_raw_stream = None
+
+
 def _stream(stream):
     if stream is None:
+        # (the handle alone where torch has a call for it: 0.4 us where torch.cuda.current_stream() takes 3)
+        global _raw_stream
         import torch
-        # (the stream's handle without the object around it: 0.3 us where torch.cuda.current_stream() takes 3)
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if raw is not None and torch.cuda.is_initialized():
-            return raw(torch.cuda.current_device())
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        if _raw_stream is None:
+            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+                (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        return _raw_stream(torch.cuda.current_device())
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)
@@ -555,26 +532,31 @@ def grid_configs_export(cfg, row: int, cap: int = 1 << 16):
 
 
 # ---------------------------------------------------------------------------
+# The structures of include/grid.h that calls fill: packed by struct, which takes half the time of ctypes (padding included).
+_HEADS, _CHUNK, _ROTATION, _NORM = struct.Struct("Pqq"), struct.Struct("PqPPiiii"), struct.Struct("PPiiii"), struct.Struct("PPfi")
+_QUERY, _STEP = struct.Struct("PqqPqqPfi"), struct.Struct("PqqPqqPqqPPPPqPiiiiiiPPPP")
+
+
 def _heads(x, kv, N, H):
-    """A [tokens, heads, D] tensor (any strides, D contiguous) as a grid_heads."""
-    shape, stride = x.shape, x.stride()
-    assert x.is_cuda and x.dtype == kv.dtype and shape == (N, H, kv.D) and stride[2] == 1, \
+    """A [tokens, heads, D] tensor (any strides, D contiguous) as (address, strides)."""
+    a, b, c = x.stride()
+    assert x.is_cuda and x.dtype == kv.dtype and x.shape == (N, H, kv.D) and c == 1, \
         "CUDA tensor [tokens, heads, D] of the cache's type expected, D contiguous"
-    return _Heads(x.data_ptr(), stride[0], stride[1])
+    return x.data_ptr(), a, b
 
 
-def _chunk(table, lens, start, status, N):
-    import torch
-    i32, B = torch.int32, lens.shape[0]
-    assert table.dtype == i32 and lens.dtype == i32 and status.dtype == i32, "int32 table, lens and status expected"
-    assert table.is_cuda and lens.is_cuda and status.is_cuda and table.dim() == 2 and table.stride(1) == 1
-    assert table.shape[0] == B and lens.is_contiguous() and status.is_contiguous() and status.shape == (B,), \
+def _chunk(kv, table, lens, start, status, N):
+    i32, B = kv.i32, len(lens)
+    shape, stride = table.shape, table.stride()
+    assert table.dtype is i32 and lens.dtype is i32 and status.dtype is i32, "int32 table, lens and status expected"
+    assert table.is_cuda and lens.is_cuda and status.is_cuda and len(shape) == 2 and stride[1] == 1, \
+        "table [B, max_pages] on the GPU expected, its rows contiguous"
+    assert shape[0] == B and lens.shape == status.shape == (B,) and lens.is_contiguous() and status.is_contiguous(), \
         "table [B, max_pages], lens [B] and status [B] expected"
     if start is not None:
-        assert start.dtype == i32 and start.is_cuda and start.is_contiguous() and start.shape == (B + 1,), \
+        assert start.dtype is i32 and start.is_cuda and start.is_contiguous() and start.shape == (B + 1,), \
             "int32 start [B + 1] expected"
-        start = start.data_ptr()
-    return _KvChunk(table.data_ptr(), table.stride(0), lens.data_ptr(), start, table.shape[1], B, N, 0)
+    return _CHUNK.pack(table.data_ptr(), stride[0], lens.data_ptr(), 0 if start is None else start.data_ptr(), shape[1], B, N, 0)
 
 
 def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None, cos=None, sin=None, pairs=False,
@@ -584,44 +566,40 @@ def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None
     int32 [B, max_pages], lens int32 [B] (tokens cached before the chunk),
     start int32 [B + 1] (None: the same number of tokens per row); q and q_out
     [tokens, heads, D]; cos, sin float32 [positions, rot / 2]; norm weights [D]."""
-    import torch
-    N = k.shape[0]
-    chunk = _chunk(table, lens, start, status, N)
-    kh, vh = _heads(k, kv, N, kv.kv_heads), _heads(v, kv, N, kv.kv_heads)
+    N = len(k)
+    chunk = _chunk(kv, table, lens, start, status, N)
+    kh, vh = _HEADS.pack(*_heads(k, kv, N, kv.kv_heads)), _HEADS.pack(*_heads(v, kv, N, kv.kv_heads))
     qh = oh = rot = norm = None
     assert (q is None) == (q_out is None), "q and q_out go together"
     if q is not None:
-        qh, oh = ctypes.byref(_heads(q, kv, N, kv.heads)), ctypes.byref(_heads(q_out, kv, N, kv.heads))
+        qh, oh = _HEADS.pack(*_heads(q, kv, N, kv.heads)), _HEADS.pack(*_heads(q_out, kv, N, kv.heads))
     assert (cos is None) == (sin is None), "cos and sin go together"
     if cos is not None:
-        assert cos.dtype == torch.float32 and sin.dtype == torch.float32 and cos.is_cuda and sin.is_cuda and \
-            cos.is_contiguous() and sin.is_contiguous() and cos.dim() == 2 and cos.shape == sin.shape, \
+        shape = cos.shape
+        assert cos.dtype is sin.dtype is kv.f32 and cos.is_cuda and sin.is_cuda and cos.is_contiguous() and \
+            sin.is_contiguous() and len(shape) == 2 and shape == sin.shape, \
             "contiguous float32 CUDA tensors [positions, rot / 2] expected"
-        rot = ctypes.byref(_Rotation(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], pairs, 0))
+        rot = _ROTATION.pack(cos.data_ptr(), sin.data_ptr(), shape[0], 2 * shape[1], pairs, 0)
     if q_norm is not None or k_norm is not None:
         for w in (q_norm, k_norm):
-            assert w is None or (w.is_cuda and w.dtype == kv.dtype and w.shape == (kv.D,) and w.is_contiguous()), \
+            assert w is None or (w.is_cuda and w.dtype is kv.dtype and w.shape == (kv.D,) and w.is_contiguous()), \
                 "norm weights [D] of the cache's type expected"
-        norm = ctypes.byref(_HeadNorm(None if q_norm is None else q_norm.data_ptr(),
-                                      None if k_norm is None else k_norm.data_ptr(), eps, 0))
-    _check(lib().grid_kv_append(kv.h, ctypes.byref(chunk), ctypes.byref(kh), ctypes.byref(vh), qh, oh, rot, norm,
-                                status.data_ptr(), _stream(stream)))
+        norm = _NORM.pack(0 if q_norm is None else q_norm.data_ptr(), 0 if k_norm is None else k_norm.data_ptr(), eps, 0)
+    _check(lib().grid_kv_append(kv.h, chunk, kh, vh, qh, oh, rot, norm, status.data_ptr(), _stream(stream)))
 
 
 def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=None, stream=None):
     """Attention of a chunk over the paged cache, after its append (table, lens
     and start as there): q, out [tokens, heads, D], lse float32 [tokens, heads];
     scale defaults to 1 / sqrt(D)."""
-    N = q.shape[0]
-    chunk = _chunk(table, lens, start, status, N)
+    N = len(q)
+    chunk = _chunk(kv, table, lens, start, status, N)
     if lse is not None:
-        import torch
-        assert lse.dtype == torch.float32 and lse.is_cuda and lse.is_contiguous() and lse.shape == (N, kv.heads), \
+        assert lse.dtype is kv.f32 and lse.is_cuda and lse.is_contiguous() and lse.shape == (N, kv.heads), \
             "float32 lse [tokens, heads] expected"
-        lse = lse.data_ptr()
-    query = _KvQuery(_heads(q, kv, N, kv.heads), _heads(out, kv, N, kv.heads), lse,
-                     kv.D ** -0.5 if scale is None else scale, 0)
-    _check(lib().grid_kv_attend(kv.h, ctypes.byref(chunk), ctypes.byref(query), status.data_ptr(), _stream(stream)))
+    query = _QUERY.pack(*_heads(q, kv, N, kv.heads), *_heads(out, kv, N, kv.heads), 0 if lse is None else lse.data_ptr(),
+                        kv.D ** -0.5 if scale is None else scale, 0)
+    _check(lib().grid_kv_attend(kv.h, chunk, query, status.data_ptr(), _stream(stream)))
 
 
 class PagedKV:
@@ -637,6 +615,7 @@ class PagedKV:
         dt = {torch.bfloat16: GRID_DTYPE_BF16, torch.float16: GRID_DTYPE_F16}[k_pages.dtype]
         n, page, self.kv_heads, self.D = k_pages.shape
         self.heads, self.dtype, self.pools = heads, k_pages.dtype, (k_pages, v_pages)
+        self.i32, self.f32 = torch.int32, torch.float32
         p = _KvPages(k_pages.data_ptr(), v_pages.data_ptr(), dt, self.D, heads, self.kv_heads, page, n,
                      k_pages.stride()[:3], v_pages.stride()[:3])
         out = ctypes.c_void_p()
@@ -657,37 +636,39 @@ def grid_draft_verify(drafts, logits, draft, u, noise, tokens, accepted, status,
     float32 [B] may be None; logits, mask, probs and noise may be strided (the
     last axis contiguous).  Out: tokens int32 [B, K + 1], accepted and status
     int32 [B], logprob float32 [B, K + 1] or None.  ``drafts``: a Drafts."""
-    import torch
-    f32, i32 = torch.float32, torch.int32
+    f32, i32 = drafts.f32, drafts.i32
     B, K1, V = logits.shape
     K = K1 - 1
-    dt = {f32: GRID_DTYPE_F32, torch.bfloat16: GRID_DTYPE_BF16}[logits.dtype]
+    dt = drafts.dtypes[logits.dtype]
 
     def dense(x, dtype, *shape):
-        assert x.dtype == dtype and x.is_cuda and x.shape == shape and x.is_contiguous(), \
+        assert x.dtype is dtype and x.is_cuda and x.shape == shape and x.is_contiguous(), \
             "contiguous %s CUDA tensor %s expected" % (dtype, list(shape))
         return x.data_ptr()
 
     def rows(x, dtype, *shape):
-        assert x.dtype == dtype and x.is_cuda and x.shape == shape and (x.stride(-1) == 1 or shape[-1] == 1), \
+        stride = x.stride()
+        assert x.dtype is dtype and x.is_cuda and x.shape == shape and (stride[-1] == 1 or shape[-1] == 1), \
             "%s CUDA tensor %s expected, the last axis contiguous" % (dtype, list(shape))
-        return x.data_ptr(), x.stride()[:-1]
+        return x.data_ptr(), *stride[:-1]
 
-    lp, ls = rows(logits, logits.dtype, B, K1, V)
-    np_, ns = rows(noise, f32, B, V)
-    mp, ms = (None, (0, 0)) if mask is None else rows(mask, i32, B, K1, (V + 31) // 32)
-    pp, ps = (None, (0, 0)) if probs is None or K == 0 else rows(probs, f32, B, K, V)
-    step = _DraftStep(lp, ls, mp, ms, pp, ps, dense(draft, i32, B, K), None if draft_len is None else dense(draft_len, i32, B),
-                      dense(u, f32, B, K), np_, ns[0], None if temperature is None else dense(temperature, f32, B), dt, B, K,
-                      V, eos, 0, dense(tokens, i32, B, K1), dense(accepted, i32, B),
-                      None if logprob is None else dense(logprob, f32, B, K1), dense(status, i32, B))
-    _check(lib().grid_draft_verify(drafts.h, ctypes.byref(step), _stream(stream)))
+    none = (0, 0, 0)
+    step = _STEP.pack(
+        *rows(logits, logits.dtype, B, K1, V), *(none if mask is None else rows(mask, i32, B, K1, (V + 31) // 32)),
+        *(none if probs is None or K == 0 else rows(probs, f32, B, K, V)), dense(draft, i32, B, K),
+        0 if draft_len is None else dense(draft_len, i32, B), dense(u, f32, B, K), *rows(noise, f32, B, V),
+        0 if temperature is None else dense(temperature, f32, B), dt, B, K, V, eos, 0, dense(tokens, i32, B, K1),
+        dense(accepted, i32, B), 0 if logprob is None else dense(logprob, f32, B, K1), dense(status, i32, B))
+    _check(lib().grid_draft_verify(drafts.h, step, _stream(stream)))
 
 
 class Drafts:
     """Scratch for verifications of up to B rows of K drafted tokens over V ids."""
 
     def __init__(self, B: int, K: int, V: int):
+        import torch
+        self.i32, self.f32 = torch.int32, torch.float32
+        self.dtypes = {torch.float32: GRID_DTYPE_F32, torch.bfloat16: GRID_DTYPE_BF16}
         out = ctypes.c_void_p()
         _check(lib().grid_drafts_create(B, K, V, ctypes.byref(out)))
         self.h = out

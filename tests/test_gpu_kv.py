@@ -427,3 +427,67 @@ def test_refusals_of_the_binding():
         G.grid_kv_attend(b.kv, b.table, b.lens, b.q, b.out, b.status, scale=math.inf)
     with pytest.raises(G.GridError):
         G.grid_kv_attend(b.kv, b.table, b.lens, b.qkv.flatten(1)[:, 4:4 + 4 * 64].view(2, 4, 64), b.out, b.status)
+
+
+CHUNK = [dict(d_table=None), dict(d_len=None), dict(B=0), dict(B=-1), dict(n_tokens=-1), dict(max_pages=0), dict(table_stride=2),
+         dict(d_start=None, n_tokens=1), dict(max_pages=1 << 30, table_stride=1 << 31)]
+
+
+@pytest.mark.parametrize("what,bad,code", [("chunk", c, -1) for c in CHUNK] + [
+    ("chunk", dict(B=65_536), -8), ("heads", dict(d=None), -1), ("heads", dict(d=(1 << 20) + 8), -1),
+    ("heads", dict(token_stride=260), -1), ("heads", dict(head_stride=-64), -1), ("rot", dict(d_cos=None), -1),
+    ("rot", dict(d_sin=(1 << 20) + 4), -1), ("rot", dict(rot=8), -1), ("rot", dict(rot=24), -1), ("rot", dict(rot=80), -1),
+    ("rot", dict(n_pos=0), -1), ("norm", dict(d_q=(1 << 20) + 2), -1), ("norm", dict(eps=-1.0), -1),
+    ("norm", dict(eps=math.nan), -1), ("query", dict(scale=0.0), -1), ("query", dict(scale=-1.0), -1),
+    ("query", dict(scale=math.nan), -1), ("query", dict(d_lse=(1 << 20) + 2), -1), ("status", {}, -1)])
+def test_calls_that_are_refused(what, bad, code):
+    """Refused on the host, before anything is launched (the addresses here are never read)."""
+    import ctypes
+    from paper_2607_11951_gb300 import grid as G
+    from tests import structs as S
+    b = Batch([3, 4], [1, 1], 4, 2, 64, 16)
+    at = 1 << 20
+    parts = dict(chunk=S.KvChunk(at, 3, at, at, 3, 2, 2, 0), heads=S.Heads(at, 256, 64), rot=S.Rotation(at, at, 9, 64, 0, 0),
+                 norm=S.HeadNorm(at, at, 1e-6, 0))
+    parts["query"] = S.KvQuery(S.Heads(at, 256, 64), S.Heads(at, 256, 64), None, 0.125, 0)
+    for k, v in bad.items():
+        setattr(parts[what], k, v)
+    if what == "heads":
+        parts["query"].q = parts["heads"]
+    p = {k: ctypes.byref(v) for k, v in parts.items()}
+    status = None if what == "status" else at
+    L, good = G.lib(), ctypes.byref(S.Heads(at, 256, 64))
+    if what != "query":
+        for where in range(4) if what == "heads" else [0]:
+            args = [good] * 4
+            args[where] = p["heads"]
+            assert L.grid_kv_append(b.kv.h, p["chunk"], *args, p["rot"], p["norm"], status, None) == code
+            assert G.last_error().startswith("grid_kv_append:")
+    if what in ("chunk", "heads", "query", "status"):
+        assert L.grid_kv_attend(b.kv.h, p["chunk"], p["query"], status, None) == code
+        assert G.last_error().startswith("grid_kv_attend:")
+    if what == "status":
+        assert L.grid_kv_append(b.kv.h, p["chunk"], good, good, good, None, None, None, at, None) == -1  # q without q_out
+
+
+def test_too_many_tiles_in_one_call():
+    import ctypes
+    from paper_2607_11951_gb300 import grid as G
+    from tests import structs as S
+    b = Batch([3, 4], [1, 1], 4, 2, 64, 16)
+    at = 1 << 20
+    chunk = S.KvChunk(at, 1 << 26, at, at, 1 << 26, 2, 1 << 28, 0)
+    query = S.KvQuery(S.Heads(at, 256, 64), S.Heads(at, 256, 64), None, 0.125, 0)
+    assert G.lib().grid_kv_attend(b.kv.h, ctypes.byref(chunk), ctypes.byref(query), at, None) == -8
+
+
+def test_pages_of_other_rows_and_stale_tables_are_not_read():
+    """Entries of the table past a row's tokens may hold anything; two rows may share a page of a common prefix."""
+    import torch
+    b = Batch([64, 64, 64], [5, 1, 150], 8, 2, 128, 64)
+    b.fill()
+    b.table[1, 0] = b.table[0, 0]  # rows 0 and 1 begin with the same 64 tokens
+    b.cached[1] = b.cached[0]
+    b.table[:, 4:] = torch.tensor([[-1], [1 << 30], [-(1 << 31)]], dtype=torch.int32, device="cuda")
+    b.attend()
+    b.check()

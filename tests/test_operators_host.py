@@ -7,6 +7,7 @@ import pytest
 
 from paper_2607_11951_gb300 import grid as G
 from tests import fakes
+from tests import structs as S
 
 INVALID, CUDA, TOO_LARGE = -1, -7, -8
 AT = 1 << 20  # an aligned address
@@ -71,7 +72,7 @@ def test_draft_scratch_is_freed_when_a_call_fails(fake):
 
 def step(**kw):
     two = ctypes.c_int64 * 2
-    s = G._DraftStep(d_logits=AT, logit_stride=two(300, 100), d_mask=AT, mask_stride=two(12, 4), d_probs=AT,
+    s = S.DraftStep(d_logits=AT, logit_stride=two(300, 100), d_mask=AT, mask_stride=two(12, 4), d_probs=AT,
                      prob_stride=two(200, 100), d_draft=AT, d_draft_len=AT, d_u=AT, d_noise=AT, noise_stride=100,
                      d_temperature=AT, dtype=G.GRID_DTYPE_F32, B=4, K=2, V=100, eos=-1, d_tokens=AT, d_accepted=AT,
                      d_logprob=AT, d_status=AT)
@@ -106,7 +107,30 @@ def test_launches_cover_every_position(fake, B, K, V):
         d = G.Drafts(B, K, V)
         rt.reset()
         assert G.lib().grid_draft_verify(d.h, ctypes.byref(step(B=B, K=K, V=V, noise_stride=V)), None) == 0
-        (_, g0, *_), (_, g1, *_) = rt.launches()
+        (_, g0, *_), *draw = rt.launches()
         rows = B * (K + 1)
         assert g0[0] % rows == 0 and rows <= g0[0] <= rows + 8 * 152 and g0[1] == g0[2] == 1
-        assert g1[0] % B == 0 and B <= g1[0] <= B + 24 * 152
+        assert len(draw) == (V > 4096)
+        for _, g1, *_ in draw:
+            assert g1[0] % B == 0 and B <= g1[0] <= B + 24 * 152
+
+
+def test_packed_arguments_have_the_layout_of_the_structures():
+    """What the binding packs is, byte for byte, the structure with these values."""
+    for packed, structure in ((G._HEADS, S.Heads), (G._CHUNK, S.KvChunk), (G._ROTATION, S.Rotation), (G._NORM, S.HeadNorm),
+                              (G._QUERY, S.KvQuery), (G._STEP, S.DraftStep)):
+        assert packed.size == ctypes.sizeof(structure)
+        values = list(range(1, len(packed.unpack(bytes(packed.size))) + 1))
+
+        def fill(st, left):
+            for name, kind in st._fields_:
+                if issubclass(kind, ctypes.Structure):
+                    setattr(st, name, fill(kind(), left))
+                elif issubclass(kind, ctypes.Array):
+                    setattr(st, name, kind(left.pop(0), left.pop(0)))
+                else:
+                    setattr(st, name, left.pop(0))
+            return st
+
+        want = fill(structure(), list(values))
+        assert bytes(want) == packed.pack(*values)
