@@ -513,9 +513,12 @@ int grid_configs_export(const grid_configs* c, int32_t row, int32_t* stack, int3
  * Checked on the device, per row: 0 <= d_len, tokens in order and within
  * n_tokens, chunk within max_pages pages, page ids within the cache (and, in an
  * append, positions within the rotation's table).  A row that fails gets
- * GRID_ST_PAGES; an append leaves out its tokens whose own place fails, an
- * attend writes zeros for the whole row (lse -inf).  Entries of d_table that
- * no token of the row lies in are not read. */
+ * GRID_ST_PAGES.  An append leaves out its tokens whose own place fails.  An
+ * attend writes zeros (lse -inf) for all tokens of a row whose length or order
+ * fails, and where a page id fails for the tokens that would read that page at
+ * least (the row's earlier tokens get zeros too, or their own result).  Tokens
+ * that belong to no row, from d_start[B] on, are left alone.  Entries of
+ * d_table that no token of the row lies in are not read. */
 typedef struct grid_kv_pages {
   void *d_k, *d_v;       /* pools of n_pages pages, 16-byte aligned                      */
   int32_t dtype;         /* GRID_DTYPE_BF16 or GRID_DTYPE_F16, of every head vector here */
@@ -610,9 +613,9 @@ int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_kv_
  * logit, and that is the token drawn.  K = 0 samples one token per row.
  *
  * An id outside 0 .. V-1 or the mask is refused (p = 0).  NaN logits count as
- * -inf; +inf as the largest finite value.  Noise that is not positive leaves
- * its id out of the draw (where nothing is left: the first largest logit).  A
- * position that is reached and admits no id ends the row there: no token is
+ * -inf; +inf as the largest finite value.  Noise below 2^-126 or not a number
+ * leaves its id out of the draw (where nothing is left: the first largest
+ * logit).  A position that is reached and admits no id ends the row there: no token is
  * drawn and d_status[b] = GRID_ST_EMPTY_MASK.  An accepted or drawn `eos` ends
  * the row too, with GRID_ST_COMPLETE. */
 typedef struct grid_draft_step {
@@ -638,7 +641,7 @@ typedef struct grid_draft_step {
 } grid_draft_step;
 
 /* Scratch for verifications of up to B rows of K drafted tokens over V ids
- * (1 <= B <= 65535, 0 <= K <= 64).  Allocates device memory and synchronizes.
+ * (1 <= B <= 65535, 0 <= K <= 64, 1 <= V <= 2^30).  Allocates device memory and synchronizes.
  * Free with grid_drafts_free. */
 int grid_drafts_create(int32_t B, int32_t K, int32_t V, grid_drafts** out);
 void grid_drafts_free(grid_drafts* d);

@@ -23,6 +23,7 @@
 #include <dlfcn.h>
 
 #include <cmath>
+#include <new>
 #include <utility>
 
 #include "grid_kv.cuh"
@@ -174,30 +175,7 @@ __device__ __forceinline__ void tm_loaded16(uint32_t* x, uint32_t* y) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : U8(x, 0), U8(x, 8), U8(y, 0), U8(y, 8) : : "memory");
 }
 __device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
-struct Two {
-  float x, y;
-};
-__device__ __forceinline__ Two fma2(Two a, float b, float c) {  // (one instruction for two)
-  Two r;
-  asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %4};\nmov.b64 c, {%5, %5};\n"
-      "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
-      : "=f"(r.x), "=f"(r.y)
-      : "f"(a.x), "f"(a.y), "f"(b), "f"(c));
-  return r;
-}
-__device__ __forceinline__ Two add2(Two a, Two b) {
-  Two r;
-  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
-      : "=f"(r.x), "=f"(r.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return r;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -444,7 +422,7 @@ struct Shared {
   uint32_t tmem;
 };
 
-constexpr int kSharedRoom = 3072;  // in front of the tiles, which begin on 1,024 bytes
+constexpr int kSharedRoom = 3 << 10;  // in front of the tiles, which begin on 1,024 bytes
 
 template <int D>
 constexpr size_t smem_bytes() {
@@ -1079,7 +1057,8 @@ extern "C" int grid_kv_create(const grid_kv_pages* p, grid_kv** out) {
   for (int i = 0; i < 3; ++i)
     if (p->k_stride[i] <= 0 || p->v_stride[i] <= 0 || p->k_stride[i] % 8 || p->v_stride[i] % 8)
       return set_error(GRID_E_INVALID_ARG, "grid_kv_create: strides are positive multiples of 8 elements");
-  grid_kv* kv = new grid_kv;
+  grid_kv* kv = new (std::nothrow) grid_kv;
+  if (!kv) return set_error(GRID_E_TOO_LARGE, "grid_kv_create: out of host memory");
   kv->p = *p;
   while (1 << kv->log_page < p->page_size) ++kv->log_page;
   int rc = make_map(*p, p->d_k, p->k_stride, &kv->k_map), dev = 0;

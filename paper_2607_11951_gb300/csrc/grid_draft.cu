@@ -19,6 +19,7 @@
 // another: 61 us (32 rows) and 178 us (256 rows) where this takes 43 and 115.
 #include <cfloat>
 #include <cmath>
+#include <new>
 
 #include "grid_state.cuh"
 
@@ -32,29 +33,6 @@ constexpr int kAlone = 4096;  // ids that a row's last block draws from by itsel
 constexpr int kBlocksPerSm = 8, kDrawsPerSm = 24; // blocks wanted of either kernel
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-struct Two {
-  float x, y;
-};
-__device__ __forceinline__ Two add2(Two a, Two b) {
-  Two r;
-  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
-      : "=f"(r.x), "=f"(r.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return r;
-}
-__device__ __forceinline__ Two fma2(Two a, float b, float c) {  // (one instruction for two)
-  Two r;
-  asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %4};\nmov.b64 c, {%5, %5};\n"
-      "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
-      : "=f"(r.x), "=f"(r.y)
-      : "f"(a.x), "f"(a.y), "f"(b), "f"(c));
-  return r;
-}
 struct alignas(16) Stat {
   float base, s;  // sum over the admitted ids of 2^(c l - base), base -inf: none is admitted
   float m;        // the largest admitted logit and its first id
@@ -306,7 +284,7 @@ __device__ __forceinline__ Best best_warp(Best x) {
   }
   return x;
 }
-// What scores the ids of a row's draw: w / e with w = p - q, by an approximate
+// What scores the ids of a row's draw: w / e with w = max(p - q, 0), by an approximate
 // reciprocal (two units in the last place: a score is only compared with
 // scores).  0 or less, or not finite: the id cannot be drawn.
 struct Scorer {
@@ -315,7 +293,7 @@ struct Scorer {
     float t = fmaf(l, c, -base), r;
     if (!(t < 126.f)) t = exponent(l, c) - base;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e));
-    return fmaf(exp2_fast(t), inv_s, -q) * r;
+    return fmaxf(fmaf(exp2_fast(t), inv_s, -q), 0.f) * r;
   }
 };
 __device__ __forceinline__ void keep(Best& z, float s, int id) {
@@ -571,7 +549,8 @@ extern "C" int grid_drafts_create(int32_t B, int32_t K, int32_t V, grid_drafts**
     return set_error(GRID_E_INVALID_ARG, "grid_drafts_create: B and V are positive, K in 0 .. 64");
   if (B > 65535 || V > (1 << 30))
     return set_error(GRID_E_TOO_LARGE, "grid_drafts_create: more than 65535 rows or 2^30 ids");
-  grid_drafts* d = new grid_drafts;
+  grid_drafts* d = new (std::nothrow) grid_drafts;
+  if (!d) return set_error(GRID_E_TOO_LARGE, "grid_drafts_create: out of host memory");
   d->B = B;
   d->K = K;
   d->V = V;

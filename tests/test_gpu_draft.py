@@ -331,6 +331,18 @@ def test_noise_that_is_not_positive():
         assert tokens[b, 0] == np.argmax(np.where(s.bits[b, 0], s.logits[b, 0], -np.inf))
 
 
+@pytest.mark.parametrize("V", [300, 5000])
+def test_negative_noise_after_a_refusal(V):
+    """Weights below zero over noise below zero are no scores."""
+    s = Step(24, 2, V, seed=16, mask=False)
+    s.temp[:] = 1
+    s.u[:] = 0.99999
+    s.noise[:, ::3] = -s.noise[:, ::3]
+    s.device()
+    s.run().check(most_near=0.1)
+    assert (s.got()[1] < 2).any()
+
+
 def test_a_drafter_equal_to_the_target_is_always_accepted():
     s = Step(50, 4, 800, seed=14, mask=False)
     s.temp[:] = 1
