@@ -259,8 +259,6 @@ __device__ __forceinline__ void stage_tables(const TabT<STAGED>& t) {
 // may start while its predecessor in the stream finishes; everything a kernel
 // does before this wait touches only the spec's read-only tables.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-// The next kernel of the stream may be launched (it still waits for this one's end in pdl_wait).
-__device__ __forceinline__ void pdl_next() { asm volatile("griddepcontrol.launch_dependents;"); }
 
 constexpr uint32_t kHashEmpty = 0xFFFFFFFFu;
 
@@ -1111,38 +1109,5 @@ __device__ __forceinline__ int eval_record(const T& t, Walker& w, const uint16_t
   if (f == kClsAcc) return 1;
   return trailing_set(t, w, t.set4(f), max_chain);
 }
-
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// Two floats, one instruction for both.
-struct Two {
-  float x, y;
-};
-__device__ __forceinline__ Two add2(Two a, Two b) {
-  Two r;
-  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
-      : "=f"(r.x), "=f"(r.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return r;
-}
-__device__ __forceinline__ Two mul2(Two a, Two b) {
-  Two r;
-  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
-      : "=f"(r.x), "=f"(r.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return r;
-}
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-  Two r;
-  asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
-      "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
-      : "=f"(r.x), "=f"(r.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return r;
-}
-__device__ __forceinline__ Two fma2(Two a, float b, float c) { return fma2(a, Two{b, b}, Two{c, c}); }
 
 }  // namespace grid

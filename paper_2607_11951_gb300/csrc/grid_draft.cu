@@ -21,7 +21,7 @@
 #include <cmath>
 #include <new>
 
-#include "grid_state.cuh"
+#include "grid_model.cuh"
 
 namespace grid {
 namespace {

@@ -1996,6 +1996,25 @@ __global__ void __launch_bounds__(256) k_apply(const uint32_t* __restrict__ mask
                          blockIdx.x * blockDim.x + threadIdx.x, gridDim.x * blockDim.x);
 }
 
+// Launch with programmatic stream serialization: the kernel may begin (stage
+// its tables) while the previous kernel in the stream drains; it waits for
+// that kernel's results with griddepcontrol.wait (pdl_wait).
+template <typename... KArgs, typename... Args>
+static cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
+                              Args&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...);
+}
+
 size_t align16(size_t x) { return (x + 15) & ~size_t(15); }
 
 }  // namespace

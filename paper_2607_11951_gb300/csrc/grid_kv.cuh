@@ -7,7 +7,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include "grid_state.cuh"
+#include "grid_model.cuh"
 
 namespace grid {
 

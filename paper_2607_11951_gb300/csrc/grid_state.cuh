@@ -22,25 +22,6 @@
 
 namespace grid {
 
-// Launch with programmatic stream serialization: the kernel may begin (stage
-// its tables) while the previous kernel in the stream drains; it waits for
-// that kernel's results with griddepcontrol.wait (pdl_wait).
-template <typename... KArgs, typename... Args>
-inline cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
-                              Args&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...);
-}
-
 // Per-row scratch of one grid_masks call.
 struct RowCtx {
   uint32_t A0[4];   // allowed terminals at sigma
