@@ -594,7 +594,10 @@ typedef struct grid_kv_query {
  * Values of the pools at positions that no row uses are never part of a
  * result, whatever their bits; cached keys and values must be finite.
  * Uses the scratch held by `kv`, so attends on the same handle must not
- * overlap on the GPU.  d_status as above.  Enqueue only. */
+ * overlap on the GPU; `out` must not overlap the queries or the pools.  d_status
+ * as above; GRID_ST_BOUND in every row: a wait of the kernel ran out (two
+ * seconds; the outputs are not to be used, and the handle is to be freed).
+ * Enqueue only. */
 int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_kv_query* query, int32_t* d_status,
                    void* stream);
 
