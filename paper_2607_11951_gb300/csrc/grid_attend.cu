@@ -51,10 +51,12 @@ constexpr int kLoadWarp = kSoftWarps;      // two that load tiles, of keys and o
 constexpr int kMmaWarp = kSoftWarps + 2;   // one that multiplies,
 constexpr int kQueryWarp = kSoftWarps + 3, kQueryWarps = 1;  // one that loads queries
 constexpr int kThreads = (kSoftWarps + 4) * 32;
-// A unit's beginning and end cost as much as some tiles, and runs are not made shorter than a few (cost 2: 27.8 us for 32
-// rows of one token, 205 for 27 prompts, 440 for 2 x 2,000 tokens over 16,000; cost 3: 27.1, 212, 441; runs of 4 and cost
-// 1: one token over 400 takes 14.7 us where it takes 11.3).
-constexpr int kUnitCost = 2, kMinRun = 5;
+// A unit's beginning and end cost as much as some tiles (2: 28.4 us for 32 rows of one token, 208 for 27 prompts, 440 for
+// 2 x 2,000 tokens over 16,000; 3: 28.1, 213, 438), and runs are not made shorter than a few (3: one token over 2,000 and
+// 16,000 takes 12.5 and 25 us, 200 tokens over 500 24; 5: 15, 25 and 29).  Where every key head can have a block of its own
+// and the dearest is no longer than a run and what it costs to join pieces, none is cut (16 rows of one token over up to
+// 500: 15.1 -> 11.2 us; a prompt of 64: 16.0 -> 10.4).
+constexpr int kUnitCost = 2, kMinRun = 3, kJoinCost = 4;
 constexpr int kRing = 8;              // pieces whose bad-page flags are kept at once
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
@@ -431,7 +433,7 @@ struct Shared {
   uint64_t q_ready[2], q_free[2], s_ready[2], p_half[2], p_ready[2], o_ready[2], all;
   float2 ml[2][kTile];
   Units units[kSoftWarps];
-  int sums[kThreads / 32];
+  int3 sums[kThreads / 32];  // of the warps: cost, rows, dearest row
   int first, per, row[4], gave_up, last, bad[2][kRing];
   uint32_t tmem;
 };
@@ -482,6 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   // How many tiles there are in all, and the row that this block begins in.
   Cut cut;
+  bool whole_heads;
   Units u;
   {
     // A thread's rows are `per` neighbours, one of them at a time; rows of several units go to the warps in turn.
@@ -508,53 +511,64 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncthreads();
       return at >= 0 ? many[3 * at + 2] : t;
     };
-    int mine = 0, t = 0;
+    int mine = 0, rows = 0, most = 0, t = 0;  // of this thread: their cost, how many have tokens, the dearest
 #pragma unroll 1
-    for (int i = 0; i < per; ++i) mine += (t = row_cost(tid * per + i)) * g.Hk;
-    int pre = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(~0u, pre, o);
-      if (lane >= o) pre += x;
+    for (int i = 0; i < per; ++i) {
+      t = row_cost(tid * per + i);
+      mine += t * g.Hk, rows += t > 0, most = max(most, t);
     }
-    if (lane == 31) sh.sums[warp] = pre;
+    auto up_to = [&](int x) {  // the sum over the lanes up to this one
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(~0u, x, o);
+        if (lane >= o) x += y;
+      }
+      return x;
+    };
+    int pre = up_to(mine), pre_rows = up_to(rows);
+    most = __reduce_max_sync(~0u, most);
+    if (lane == 31) sh.sums[warp] = make_int3(pre, pre_rows, most);
     __syncthreads();
-    int total = 0;
+    int total = 0, all_rows = 0;
 #pragma unroll
     for (int w = 0; w < kThreads / 32; ++w) {
-      if (w < warp) pre += sh.sums[w];
-      total += sh.sums[w];
+      const int3 x = sh.sums[w];
+      if (w < warp) pre += x.x, pre_rows += x.y;
+      total += x.x, all_rows += x.y, most = max(most, x.z);
     }
-    pre -= mine;
+    pre -= mine, pre_rows -= rows;
     cut.runs = min((int)gridDim.x, (total + kMinRun - 1) / kMinRun);
     cut.each = cut.runs ? total / cut.runs : 0;
+    // A key head to a block, where that makes no block's work longer than a run and what joining takes.
+    whole_heads = all_rows <= (int)gridDim.x / g.Hk && most <= cut.each + kJoinCost;
+    if (whole_heads) cut.runs = all_rows * g.Hk, pre = pre_rows * g.Hk, mine = rows * g.Hk;
+    cut.each = cut.runs ? total / cut.runs : 0;
     cut.more = total - cut.runs * cut.each;
-    const int lo = cut.begin(blockIdx.x);
+    const int lo = whole_heads ? (int)blockIdx.x : cut.begin(blockIdx.x);
     const bool here = (int)blockIdx.x < cut.runs && pre <= lo && lo < pre + mine;
-    {
 #pragma unroll 1
-      for (int i = 0; i < per; ++i) {
-        if (per > 1) t = row_cost(tid * per + i);
-        if (here && pre <= lo && lo < pre + t * g.Hk) {
-          sh.row[0] = u.b, sh.row[1] = u.a, sh.row[2] = u.n, sh.row[3] = u.len;
-          sh.first = pre;
-          sh.per = t;
-        }
-        pre += t * g.Hk;
+    for (int i = 0; i < per; ++i) {
+      if (per > 1) t = row_cost(tid * per + i);
+      const int each = whole_heads ? t > 0 : t;
+      if (here && pre <= lo && lo < pre + each * g.Hk) {
+        sh.row[0] = u.b, sh.row[1] = u.a, sh.row[2] = u.n, sh.row[3] = u.len;
+        sh.first = pre;
+        sh.per = t;
       }
+      pre += each * g.Hk;
     }
   }
   const bool works = (int)blockIdx.x < cut.runs;
   __syncthreads();
   tm_after();
   const uint32_t tmem = sh.tmem;
-  const int lo = works ? cut.begin(blockIdx.x) : 0, hi = works ? cut.begin(blockIdx.x + 1) : 0;
+  const int lo = !works || whole_heads ? 0 : cut.begin(blockIdx.x), hi = !works ? 0 : whole_heads ? sh.per : cut.begin(blockIdx.x + 1);
   volatile int* gave_up = &sh.gave_up;
   if (works) {  // the unit that the run begins in
     u.b = sh.row[0], u.a = sh.row[1], u.n = sh.row[2], u.len = sh.row[3];
     set_row(g, u);
-    u.h = (lo - sh.first) / sh.per;
-    u.at = sh.first + u.h * sh.per;
+    u.h = whole_heads ? (int)blockIdx.x - sh.first : (lo - sh.first) / sh.per;
+    u.at = whole_heads ? 0 : sh.first + u.h * sh.per;
     u.qt = 0;
     if (u.units == 1) {
       u.tiles = tiles_of(u, g.group, 0);
@@ -968,35 +982,47 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int rr = x % rows, from = x / rows * cols;
             const int qrow = p.r0 + rr, tok = qrow / g.group, hh = w.h * g.group + qrow - tok * g.group;
             T* to = (T*)g.out + (long long)(w.a + tok) * g.os[0] + (long long)hh * g.os[1];
-            // So many columns of two pieces at a time, the sums rescaled as they go: no load of a round waits for another
-            // (maximum, sum and values in three passes: one token over 16,000 32 us instead of 25, over 400 10.7 instead of
-            // 9.5; 16 columns at most instead of 32: 2 x 2,000 tokens over 16,000 445 instead of 439).
-            auto add_up = [&](auto columns, int j) {
-              constexpr int kN = decltype(columns)::value;
+            // So many columns of so many pieces at a time, the sums rescaled as they go: no load of a round waits for another
+            // (maximum, sum and values in three passes: one token over 16,000 32 us instead of 24; 16 columns at most instead
+            // of 32: 2 x 2,000 tokens over 16,000 445 instead of 438; eight pieces instead of four: 5 tokens over 1,200 13.6
+            // instead of 12.8).
+            auto add_up = [&](auto columns, auto pieces, int j) {
+              constexpr int kN = decltype(columns)::value, kP = decltype(pieces)::value;
               float acc[kN] = {}, most = -INFINITY, z = 0.f;
 #pragma unroll 1
-              for (int b = c0; b <= c1; b += 2) {
-                const size_t slot0 = 2 * b + (b == c0), slot1 = 2 * min(b + 1, c1);
-                const float4* src0 = g.parts + (slot0 * (D / 4) + j / 4) * 256 + rr;
-                const float4* src1 = g.parts + (slot1 * (D / 4) + j / 4) * 256 + rr;
-                const float2 e0 = __ldcg(g.part_ml + slot0 * 256 + rr);
-                float2 e1 = __ldcg(g.part_ml + slot1 * 256 + rr);
-                float4 v0[kN / 4], v1[kN / 4];
+              for (int b = c0; b <= c1; b += kP) {
+                float2 e[kP];
+                float4 v[kP][kN / 4];
 #pragma unroll
-                for (int e = 0; e < kN / 4; ++e) v0[e] = __ldcg(src0 + e * 256);
+                for (int y = 0; y < kP; ++y) {
+                  const int piece = min(b + y, c1);
+                  const size_t slot = 2 * piece + (piece == c0);
+                  e[y] = __ldcg(g.part_ml + slot * 256 + rr);
 #pragma unroll
-                for (int e = 0; e < kN / 4; ++e) v1[e] = __ldcg(src1 + e * 256);
-                if (b == c1) e1 = make_float2(-INFINITY, 0.f);  // (there is no second one)
-                const float now = fmaxf(most, fmaxf(e0.x, e1.x)), base = now > -INFINITY ? now : 0.f;
-                const float f = exp2_fast(most - base), f0 = exp2_fast(e0.x - base), f1 = exp2_fast(e1.x - base);
+                  for (int x = 0; x < kN / 4; ++x) v[y][x] = __ldcg(g.parts + (slot * (D / 4) + j / 4 + x) * 256 + rr);
+                }
+                float now = most;
+#pragma unroll
+                for (int y = 0; y < kP; ++y) {
+                  if (b + y > c1) e[y] = make_float2(-INFINITY, 0.f);  // (past the last)
+                  now = fmaxf(now, e[y].x);
+                }
+                const float base = now > -INFINITY ? now : 0.f, f = exp2_fast(most - base);
                 most = now;
-                z = fmaf(e1.y, f1, fmaf(e0.y, f0, z * f));
+                z *= f;
 #pragma unroll
-                for (int e = 0; e < kN / 4; ++e) {
-                  acc[4 * e] = fmaf(v1[e].x, f1, fmaf(v0[e].x, f0, acc[4 * e] * f));
-                  acc[4 * e + 1] = fmaf(v1[e].y, f1, fmaf(v0[e].y, f0, acc[4 * e + 1] * f));
-                  acc[4 * e + 2] = fmaf(v1[e].z, f1, fmaf(v0[e].z, f0, acc[4 * e + 2] * f));
-                  acc[4 * e + 3] = fmaf(v1[e].w, f1, fmaf(v0[e].w, f0, acc[4 * e + 3] * f));
+                for (int x = 0; x < kN; ++x) acc[x] *= f;
+#pragma unroll
+                for (int y = 0; y < kP; ++y) {
+                  const float fy = exp2_fast(e[y].x - base);
+                  z = fmaf(e[y].y, fy, z);
+#pragma unroll
+                  for (int x = 0; x < kN / 4; ++x) {
+                    acc[4 * x] = fmaf(v[y][x].x, fy, acc[4 * x]);
+                    acc[4 * x + 1] = fmaf(v[y][x].y, fy, acc[4 * x + 1]);
+                    acc[4 * x + 2] = fmaf(v[y][x].z, fy, acc[4 * x + 2]);
+                    acc[4 * x + 3] = fmaf(v[y][x].w, fy, acc[4 * x + 3]);
+                  }
                 }
               }
               const bool fine = z > 0.f;
@@ -1009,10 +1035,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             };
             if (cols >= 32)
 #pragma unroll 1
-              for (int j = from; j < from + cols; j += 32) add_up(std::integral_constant<int, 32>(), j);
+              for (int j = from; j < from + cols; j += 32) add_up(std::integral_constant<int, 32>(), std::integral_constant<int, 3>(), j);
             else
 #pragma unroll 1
-              for (int j = from; j < from + cols; j += 8) add_up(std::integral_constant<int, 8>(), j);
+              for (int j = from; j < from + cols; j += 8) add_up(std::integral_constant<int, 8>(), std::integral_constant<int, 4>(), j);
           }
         }
       } else if (!p.wide) {
