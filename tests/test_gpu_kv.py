@@ -144,6 +144,22 @@ def test_attend_long_axes(B, n, old, heads, kv_heads, D):
     b.check()
 
 
+@pytest.mark.parametrize("old,new,heads,kv_heads,D", [
+    ([60] * 19, [1] * 19, 16, 8, 64),                # 152 key heads alike: a block each
+    ([60] * 20, [1] * 20, 16, 8, 64),                # eight more than blocks
+    ([100 * (i % 7) for i in range(19)], [i % 3 for i in range(19)], 8, 8, 128),  # rows without tokens between them
+    ([0], [100], 32, 8, 64),                         # two units of 256 query rows to a key head
+    ([0, 0, 130], [300, 0, 260], 14, 2, 64),         # several, of several lengths
+    ([700], [1], 8, 4, 128), ([900], [1], 8, 4, 128), ([1100], [1], 8, 4, 128), ([1300], [3], 4, 4, 64),
+    ([5000] + [10] * 5, [1] * 6, 4, 2, 128),         # one key head far dearer than the others
+])
+def test_attend_key_heads_whole_and_cut(old, new, heads, kv_heads, D):
+    b = Batch(old, new, heads, kv_heads, D, 16, seed=len(old))
+    b.fill()
+    b.attend()
+    b.check()
+
+
 def test_attend_one_prompt_among_single_tokens():
     b = Batch([40 * i for i in range(60)], [1] * 30 + [900] + [1] * 29, 8, 2, 128, 16)
     b.fill()
