@@ -11,7 +11,8 @@
 // read once for all of them.  A unit is 256 such rows, or all of them where
 // there are at most 128, with the key tiles they can see.  The tiles of all
 // units, one after the other, are cut into equal runs, one per block: a block
-// takes the end of one unit, some whole ones and the beginning of another.  The
+// takes the end of one unit, some whole ones and the beginning of another (or
+// one key head each, where that is shorter: kJoinCost).  The
 // pieces of a unit that was cut are joined by the block that finishes last, in
 // the order of the keys whatever the order of the blocks.
 //
@@ -29,11 +30,11 @@
 //
 // Bound by the cached bytes where few rows read many keys: 32 rows of up to 5
 // tokens over up to 16,000 (724 MB) take 119 us, 6.1 TB/s; 32 rows of one token
-// over up to 2,000 (90 MB) 28 us, of which the start and the joins are some 10;
-// one token over 400 takes 10.5.  Bound by the products and the exponentials
+// over up to 2,000 (90 MB) 29 us, of which the start and the joins are some 10;
+// one token over 400 takes 9.5.  Bound by the products and the exponentials
 // between them where a chunk is long: 2 x 2,000 tokens over 16,000 (605 GF) take
-// 440 us, 1,370 TFLOP/s; 27 prompts of up to 2,000 with 64-wide heads, an
-// exponential for every 256 operations, 205 us.
+// 434 us, 1,390 TFLOP/s; 27 prompts of up to 2,000 with 64-wide heads, an
+// exponential for every 256 operations, 208 us.
 #include <dlfcn.h>
 
 #include <cmath>
@@ -984,8 +985,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             T* to = (T*)g.out + (long long)(w.a + tok) * g.os[0] + (long long)hh * g.os[1];
             // So many columns of so many pieces at a time, the sums rescaled as they go: no load of a round waits for another
             // (maximum, sum and values in three passes: one token over 16,000 32 us instead of 24; 16 columns at most instead
-            // of 32: 2 x 2,000 tokens over 16,000 445 instead of 438; eight pieces instead of four: 5 tokens over 1,200 13.6
-            // instead of 12.8).
+            // of 32: 2 x 2,000 tokens over 16,000 446 instead of 434; three pieces of 32 columns instead of two 441; two of 8
+            // columns instead of six: one token over 16,000 with one key head 17.9 instead of 16.6).
             auto add_up = [&](auto columns, auto pieces, int j) {
               constexpr int kN = decltype(columns)::value, kP = decltype(pieces)::value;
               float acc[kN] = {}, most = -INFINITY, z = 0.f;
@@ -1035,10 +1036,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             };
             if (cols >= 32)
 #pragma unroll 1
-              for (int j = from; j < from + cols; j += 32) add_up(std::integral_constant<int, 32>(), std::integral_constant<int, 3>(), j);
+              for (int j = from; j < from + cols; j += 32) add_up(std::integral_constant<int, 32>(), std::integral_constant<int, 2>(), j);
             else
 #pragma unroll 1
-              for (int j = from; j < from + cols; j += 8) add_up(std::integral_constant<int, 8>(), std::integral_constant<int, 4>(), j);
+              for (int j = from; j < from + cols; j += 8) add_up(std::integral_constant<int, 8>(), std::integral_constant<int, 6>(), j);
           }
         }
       } else if (!p.wide) {
