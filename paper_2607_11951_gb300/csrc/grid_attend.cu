@@ -12,9 +12,9 @@
 // there are at most 128, with the key tiles they can see.  The tiles of all
 // units, one after the other, are cut into equal runs, one per block: a block
 // takes the end of one unit, some whole ones and the beginning of another (or
-// one key head each, where that is shorter: kJoinCost).  The
-// pieces of a unit that was cut are joined by the block that finishes last, in
-// the order of the keys whatever the order of the blocks.
+// one key head each, where that is shorter: kJoinCost).  The pieces of a unit
+// that was cut are joined by the block that finishes last, in the order of the
+// keys whatever the order of the blocks.
 //
 // A block runs two streams of tiles side by side, each with its scores, output
 // rows and four softmax warps, so that the tensor cores work on one stream

@@ -16,9 +16,10 @@
 // instructions for an id; each id's mask bit is looked at first, and 16 bytes of
 // logits that hold no admitted id are not read.  256 rows of 5 positions over
 // 151,937 ids (bf16, 414 MB read) take 117 us, 32 rows in fp32 43, one row of 3
-// positions over 512 ids 3 (one launch).  A cluster of blocks per row
-// that stops at the first refusal reads less, but its positions follow one
-// another: 61 us (32 rows) and 178 us (256 rows) where this takes 43 and 115.
+// positions over 512 ids 8 (one launch, a chain of dependent loads).  A cluster
+// of blocks per row that stops at the first refusal reads less, but its
+// positions follow one another: 61 us (32 rows) and 178 us (256 rows) where this
+// takes 43 and 117.
 #include <cfloat>
 #include <cmath>
 #include <new>
