@@ -15,11 +15,11 @@
 // Both kernels are bound by the bytes they read and, in bf16, by the
 // instructions for an id; each id's mask bit is looked at first, and 16 bytes of
 // logits that hold no admitted id are not read.  256 rows of 5 positions over
-// 151,937 ids (bf16, 414 MB read) take 117 us, 32 rows in fp32 43, one row of 3
-// positions over 512 ids 8 (one launch, a chain of dependent loads).  A cluster
+// 151,937 ids (bf16, 414 MB read) take 117 us, 32 rows in fp32 37, one row of 3
+// positions over 512 ids 7.5 (one launch, a chain of dependent loads).  A cluster
 // of blocks per row that stops at the first refusal reads less, but its
 // positions follow one another: 61 us (32 rows) and 178 us (256 rows) where this
-// takes 43 and 117.
+// takes 37 and 117.
 #include <cfloat>
 #include <cmath>
 #include <new>
@@ -33,7 +33,9 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxPieces = 64, kMaxParts = 256;  // of one position's logits, of one draw
 constexpr int kMaxDraft = 64;
 constexpr int kAlone = 4096;  // ids that a row's last block draws from by itself
-constexpr int kBlocksPerSm = 8, kDrawsPerSm = 24; // blocks wanted of either kernel
+// Blocks wanted of either kernel.  Of k_stats, what the SMs hold at once (32 rows of 5 positions in fp32: 38.2 us with 5,
+// 39.1 with 8); of k_draw, many short ones (256 rows over 151,937 ids: 118 us with 24, 122 with 12).
+constexpr int kBlocksPerSm = 5, kDrawsPerSm = 24;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct alignas(16) Stat {
@@ -47,19 +49,21 @@ __device__ __forceinline__ void rebase(Stat& x, float base) {
   x.s = x.base > -INFINITY ? x.s * exp2_fast(x.base - base) : 0.f;
   x.base = base;
 }
+// The largest of a warp's floats (none a NaN), to every lane: their bits in the order of integers.
+__device__ __forceinline__ float max_warp(float x) {
+  int i = __float_as_int(x);
+  i = __reduce_max_sync(~0u, i ^ (i >> 31 & INT_MAX));
+  return __int_as_float(i ^ (i >> 31 & INT_MAX));
+}
 // The warp's join, to every lane: the largest base first, then one sum.
 template <bool kLargest>
 __device__ __forceinline__ Stat join_warp(Stat x) {
-  float base = x.base;
-#pragma unroll
-  for (int o = 16; o; o >>= 1) base = fmaxf(base, __shfl_xor_sync(~0u, base, o));
+  const float base = max_warp(x.base);
   if (base > -INFINITY) rebase(x, base);
 #pragma unroll
   for (int o = 16; o; o >>= 1) x.s += __shfl_xor_sync(~0u, x.s, o);
   if constexpr (kLargest) {
-    float m = x.m;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    const float m = max_warp(x.m);
     x.id = __reduce_min_sync(~0u, x.m == m ? x.id : INT_MAX);
     x.m = m;
   }
@@ -279,13 +283,9 @@ struct alignas(8) Best {
 __device__ __forceinline__ void better(Best& x, float s, int id) {
   if (s > x.s || (s == x.s && id < x.id)) x = Best{s, id};
 }
-__device__ __forceinline__ Best best_warp(Best x) {
-  for (int o = 16; o; o >>= 1) {
-    const float s = __shfl_xor_sync(~0u, x.s, o);
-    const int id = __shfl_xor_sync(~0u, x.id, o);
-    better(x, s, id);
-  }
-  return x;
+__device__ __forceinline__ Best best_warp(Best x) {  // (scores are not negative: their bits are in their order)
+  const unsigned s = __reduce_max_sync(~0u, __float_as_uint(x.s));
+  return Best{__uint_as_float(s), __reduce_min_sync(~0u, __float_as_uint(x.s) == s ? x.id : INT_MAX)};
 }
 // What scores the ids of a row's draw: w / e with w = max(p - q, 0), by an approximate
 // reciprocal (two units in the last place: a score is only compared with
@@ -613,7 +613,10 @@ extern "C" int grid_draft_verify(const grid_drafts* d, const grid_draft_step* s,
   const long long rows = (long long)s->B * (s->K + 1);
   int pieces, piece, parts, part;
   cut(rows, kBlocksPerSm, kWarps * kTileIds, kMaxPieces, pieces, piece);
-  cut(s->B, kDrawsPerSm, 2 * kTileIds, kMaxParts, parts, part);
+  // (a warp draws from twice 256 ids, or once where the SMs would not all have a block: 32 rows over 151,936 ids take 36.7 us
+  // so and 39 with one; 8 rows over 32,000 14.5 and 13.8)
+  const bool few = (long long)s->B * s->V < 4LL * kTileIds * d->sms;
+  cut(s->B, kDrawsPerSm, (few ? 2 : 4) * kTileIds, kMaxParts, parts, part);
   const bool alone = s->V <= kAlone;
   auto go = [&](auto stats, auto draw, size_t staged) {
     cudaError_t e = launch_pdl(stats, dim3((unsigned)(rows * pieces)), dim3(kThreads), staged, (cudaStream_t)stream, *s, d->stats,
