@@ -546,12 +546,13 @@ def _heads(x, kv, N, H):
 
 
 def _chunk(kv, table, lens, start, status, N):
-    i32, B = kv.i32, len(lens)
+    i32, rows = kv.i32, lens.shape
+    B = rows[0] if rows else 0  # (len() of a tensor takes 0.5 us)
     shape, stride = table.shape, table.stride()
     assert table.dtype is i32 and lens.dtype is i32 and status.dtype is i32, "int32 table, lens and status expected"
     assert table.is_cuda and lens.is_cuda and status.is_cuda and len(shape) == 2 and stride[1] == 1, \
         "table [B, max_pages] on the GPU expected, its rows contiguous"
-    assert shape[0] == B and lens.shape == status.shape == (B,) and lens.is_contiguous() and status.is_contiguous(), \
+    assert shape[0] == B and rows == status.shape == (B,) and lens.is_contiguous() and status.is_contiguous(), \
         "table [B, max_pages], lens [B] and status [B] expected"
     if start is not None:
         assert start.dtype is i32 and start.is_cuda and start.is_contiguous() and start.shape == (B + 1,), \
@@ -566,7 +567,7 @@ def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None
     int32 [B, max_pages], lens int32 [B] (tokens cached before the chunk),
     start int32 [B + 1] (None: the same number of tokens per row); q and q_out
     [tokens, heads, D]; cos, sin float32 [positions, rot / 2]; norm weights [D]."""
-    N = len(k)
+    N = k.shape[0]
     chunk = _chunk(kv, table, lens, start, status, N)
     kh, vh = _HEADS.pack(*_heads(k, kv, N, kv.kv_heads)), _HEADS.pack(*_heads(v, kv, N, kv.kv_heads))
     qh = oh = rot = norm = None
@@ -592,7 +593,7 @@ def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=
     """Attention of a chunk over the paged cache, after its append (table, lens
     and start as there): q, out [tokens, heads, D], lse float32 [tokens, heads];
     scale defaults to 1 / sqrt(D)."""
-    N = len(q)
+    N = q.shape[0]
     chunk = _chunk(kv, table, lens, start, status, N)
     if lse is not None:
         assert lse.dtype is kv.f32 and lse.is_cuda and lse.is_contiguous() and lse.shape == (N, kv.heads), \
