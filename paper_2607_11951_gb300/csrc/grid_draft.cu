@@ -2,12 +2,14 @@
 // given random numbers (grid_draft_verify).
 //
 // For row b and position k let l be the logits, A the admitted ids and c =
-// log2(e) / T.  With any base the sum s = sum_A 2^(c l - base) gives
-// p(i) = 2^(c l_i - base) / s.  k_stats computes (base, s) of pieces of every
-// position's logits in one pass: per thread a running base, a whole number
-// near the largest c l so far, so that c l - base is one rounding and moving
-// the base scales the sum by a power of two.  The last of a row's blocks joins
-// them and walks the acceptance tests u q(x) < p(x) to the first refusal n.
+// log2(e) / T.  With any base the sum s = sum_A 2^((l - base) c) gives
+// p(i) = 2^((l_i - base) c) / s.  k_stats computes (base, s) of pieces of every
+// position's logits in one pass: per thread a running base, one of the
+// admitted logits, within 16 exponents of the largest so far.  The difference
+// comes before the product with c everywhere: at T = 1e-6 the roundings of l c
+// alone are whole exponents, while (l - base) c is off by 2^-23 of itself
+// whatever T is.  The last of a row's blocks joins the pieces and walks the
+// acceptance tests u q(x) < p(x) to the first refusal n.
 // k_draw draws the next token from position n alone: argmax w_i / e_i needs no
 // running sum over the vocabulary, so the order of the additions decides no
 // token.
@@ -39,14 +41,15 @@ constexpr int kBlocksPerSm = 5, kDrawsPerSm = 24;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct alignas(16) Stat {
-  float base, s;  // sum over the admitted ids of 2^(c l - base), base -inf: none is admitted
+  float base, s;  // a logit and the sum over the admitted ids of 2^((l - base) c); base -inf: none is admitted
   float m;        // the largest admitted logit and its first id
   int id;
 };
 __device__ __forceinline__ Stat no_stat() { return Stat{-INFINITY, 0.f, -INFINITY, INT_MAX}; }
 
-__device__ __forceinline__ void rebase(Stat& x, float base) {
-  x.s = x.base > -INFINITY ? x.s * exp2_fast(x.base - base) : 0.f;
+__device__ __forceinline__ float exponent(float l, float base, float c) { return (l - base) * c; }
+__device__ __forceinline__ void rebase(Stat& x, float base, float c) {
+  x.s = x.base > -INFINITY ? x.s * exp2_fast(exponent(x.base, base, c)) : 0.f;
   x.base = base;
 }
 // The largest of a warp's floats (none a NaN), to every lane: their bits in the order of integers.
@@ -57,9 +60,9 @@ __device__ __forceinline__ float max_warp(float x) {
 }
 // The warp's join, to every lane: the largest base first, then one sum.
 template <bool kLargest>
-__device__ __forceinline__ Stat join_warp(Stat x) {
+__device__ __forceinline__ Stat join_warp(Stat x, float c) {
   const float base = max_warp(x.base);
-  if (base > -INFINITY) rebase(x, base);
+  if (base > -INFINITY) rebase(x, base, c);
 #pragma unroll
   for (int o = 16; o; o >>= 1) x.s += __shfl_xor_sync(~0u, x.s, o);
   if constexpr (kLargest) {
@@ -82,17 +85,9 @@ __device__ __forceinline__ void load_if(uint16_t& x, const uint16_t* p, bool in)
 __device__ __forceinline__ float value(float x) { return x; }
 __device__ __forceinline__ float value(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }  // bf16
 
-// c l, kept finite above, for the logits that an fma would lose.
-__device__ __forceinline__ float exponent(float l, float c) { return fminf(clean(l) * c, 3e38f); }
-// 2^(c l - base) with base within a rounding of the largest exponent.
-__device__ __forceinline__ float weight(float l, float c, float base) {
-  const float t = fmaf(l, c, -base);
-  return exp2_fast(t < 126.f ? t : exponent(l, c) - base);
-}
-
+// (p is at most 1; the sum of one weight alone may come out a rounding below it)
 __device__ __forceinline__ float log_prob(float l, float c, const Stat& x) {
-  const float t = fmaf(l, c, -x.base);
-  return ((t < 126.f ? t : exponent(l, c) - x.base) - log2f(x.s)) * kLn2;
+  return fminf((exponent(l, x.base, c) - log2f(x.s)) * kLn2, 0.f);
 }
 
 // The row's 1/T (1 for a greedy row) and whether it is greedy.
@@ -115,11 +110,14 @@ __device__ __forceinline__ const uint32_t* mask_at(const grid_draft_step& a, int
 }
 __device__ __forceinline__ bool admitted(const uint32_t* mask, int id) { return !mask || (mask[id >> 5] >> (id & 31) & 1); }
 
+// One more term of the sum; l is clean.
+__device__ __forceinline__ void add(Stat& x, float l, float c) {
+  if (exponent(l, x.base, c) > 16.f) rebase(x, l, c);
+  if (x.base > -INFINITY) x.s += exp2_fast(exponent(l, x.base, c));
+}
 __device__ __forceinline__ void take(Stat& x, float l, int id, float c) {
   l = clean(l);
-  const float z = exponent(l, c);
-  if (z > x.base + 16.f) rebase(x, rintf(z));
-  if (x.base > -INFINITY) x.s += exp2_fast(z - x.base);
+  add(x, l, c);
   if (l > x.m || (l == x.m && id < x.id)) x.m = l, x.id = id;
 }
 
@@ -173,11 +171,7 @@ template <int N>
 __device__ __noinline__ float2 take_each(float base, float s, Values<N> v, float c) {
   Stat x{base, s, 0.f, 0};
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const float z = exponent(v.y[e], c);
-    if (z > x.base + 16.f) rebase(x, rintf(z));
-    if (x.base > -INFINITY) x.s += exp2_fast(z - x.base);
-  }
+  for (int e = 0; e < N; ++e) add(x, clean(v.y[e]), c);
   return make_float2(x.base, x.s);
 }
 
@@ -243,7 +237,7 @@ __device__ __forceinline__ Stat scan(const T* __restrict__ l, const uint32_t* __
       Two t = {0.f, 0.f};
 #pragma unroll
       for (int e = 0; e < kVec; e += 2) {
-        const Two z = fma2(Two{v.y[e], v.y[e + 1]}, c, -x.base);
+        const Two z = mul2(add2(Two{v.y[e], v.y[e + 1]}, Two{-x.base, -x.base}), Two{c, c});
         t = add2(t, Two{exp2_fast(z.x), exp2_fast(z.y)});
       }
       if (t.x + t.y < 1048576.f) {  // (a base is good for terms up to 2^20)
@@ -272,7 +266,7 @@ __device__ __noinline__ int largest(const T* l, const uint32_t* mask, int V) {
     const float v = clean(value(l[i]));
     if (v > y.m && admitted(mask, i)) y.m = v, y.id = i;
   }
-  return join_warp<true>(y).id;
+  return join_warp<true>(y, 0.f).id;
 }
 
 // Best score so far and the first id that has it.
@@ -293,8 +287,8 @@ __device__ __forceinline__ Best best_warp(Best x) {  // (scores are not negative
 struct Scorer {
   float c, base, inv_s;
   __device__ __forceinline__ float operator()(float l, float e, float q) const {
-    float t = fmaf(l, c, -base), r;
-    if (!(t < 126.f)) t = exponent(l, c) - base;
+    float t = exponent(l, base, c), r;
+    if (!(t < 126.f)) t = exponent(clean(l), base, c);
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e));
     return fmaxf(fmaf(exp2_fast(t), inv_s, -q), 0.f) * r;
   }
@@ -426,12 +420,12 @@ __global__ void __launch_bounds__(kThreads) k_stats(const grid_draft_step a, Sta
     const int lo = (int)min((long long)a.V, from), hi = (int)min((long long)a.V, from + piece);
     Stat x = greedy ? scan<T, true>(l, mask, words, lo, hi, c, st) : scan<T, false>(l, mask, words, lo, hi, c, st);
     if (pc == 0 && tid < head && admitted(mask, tid)) take(x, value(l[tid]), tid, c);
-    x = join_warp<true>(x);
+    x = join_warp<true>(x, c);
     if (lane == 0) sh[warp] = x;
   }
   __syncthreads();
   if (warp == 0) {
-    const Stat x = join_warp<true>(lane < kWarps ? sh[lane] : no_stat());
+    const Stat x = join_warp<true>(lane < kWarps ? sh[lane] : no_stat(), c);
     if (lane == 0) {
       stats[(size_t)row * pieces + pc] = x;
       __threadfence();
@@ -452,15 +446,15 @@ __global__ void __launch_bounds__(kThreads) k_stats(const grid_draft_step a, Sta
     if (j < nd) d = __ldcg(reinterpret_cast<const float4*>(drafted + (size_t)b * a.K + j));
     float4 y = {-INFINITY, 0.f, -INFINITY, __int_as_float(INT_MAX)};
     if (lane < pieces) y = __ldcg(reinterpret_cast<const float4*>(src + lane));
-    Stat x = join_warp<true>(Stat{y.x, y.y, y.z, __float_as_int(y.w)});
+    Stat x = join_warp<true>(Stat{y.x, y.y, y.z, __float_as_int(y.w)}, c);
     for (int i = 32; i < pieces; i += 32) {
       Stat z = no_stat();
       if (i + lane < pieces) {
         y = __ldcg(reinterpret_cast<const float4*>(src + i + lane));
         z = Stat{y.x, y.y, y.z, __float_as_int(y.w)};
       }
-      z = join_warp<true>(z);
-      x = join_warp<true>(lane == 0 ? x : lane == 1 ? z : no_stat());
+      z = join_warp<true>(z, c);
+      x = join_warp<true>(lane == 0 ? x : lane == 1 ? z : no_stat(), c);
     }
     if (lane == 0) {
       at[j] = x;
@@ -468,7 +462,7 @@ __global__ void __launch_bounds__(kThreads) k_stats(const grid_draft_step a, Sta
       if (j < nd) {
         const int id = ids[j] = __float_as_int(d.z);
         if (d.x > -INFINITY) {
-          ok[j] = greedy ? id == x.id : d.y < weight(d.x, c, x.base) / x.s;
+          ok[j] = greedy ? id == x.id : d.y < exp2_fast(exponent(d.x, x.base, c)) / x.s;
           if (ok[j] && id == a.eos) ok[j] = 2;
           lp[j] = log_prob(d.x, c, x);
         }
