@@ -47,7 +47,11 @@ struct alignas(16) Stat {
 };
 __device__ __forceinline__ Stat no_stat() { return Stat{-INFINITY, 0.f, -INFINITY, INT_MAX}; }
 
-__device__ __forceinline__ float exponent(float l, float base, float c) { return (l - base) * c; }
+// (l - base) c of a clean l.  By halves, since the difference of two logits may be past the type (c is at most half of the
+// largest value); and an id of logit -inf has no weight where T is infinite (c = 0) either.
+__device__ __forceinline__ float exponent(float l, float base, float c) {
+  return l > -INFINITY ? fmaf(0.5f, l, -0.5f * base) * (2.f * c) : -INFINITY;
+}
 __device__ __forceinline__ void rebase(Stat& x, float base, float c) {
   x.s = x.base > -INFINITY ? x.s * exp2_fast(exponent(x.base, base, c)) : 0.f;
   x.base = base;
@@ -96,7 +100,7 @@ __device__ __forceinline__ float inv_temp(const grid_draft_step& a, int b, bool&
   greedy = !(t > 0.f);
   return greedy ? 1.f : fminf(1.f / t, FLT_MAX);
 }
-__device__ __forceinline__ float scale2(float inv) { return fminf(inv * kLog2e, FLT_MAX); }
+__device__ __forceinline__ float scale2(float inv) { return fminf(inv * kLog2e, 0.5f * FLT_MAX); }
 __device__ __forceinline__ int draft_len(const grid_draft_step& a, int b) {
   return a.d_draft_len ? min(max(a.d_draft_len[b], 0), a.K) : a.K;
 }
@@ -112,8 +116,9 @@ __device__ __forceinline__ bool admitted(const uint32_t* mask, int id) { return 
 
 // One more term of the sum; l is clean.
 __device__ __forceinline__ void add(Stat& x, float l, float c) {
-  if (exponent(l, x.base, c) > 16.f) rebase(x, l, c);
-  if (x.base > -INFINITY) x.s += exp2_fast(exponent(l, x.base, c));
+  if (!(l > -INFINITY)) return;
+  if (!(x.base > -INFINITY) || exponent(l, x.base, c) > 16.f) rebase(x, l, c);
+  x.s += exp2_fast(exponent(l, x.base, c));
 }
 __device__ __forceinline__ void take(Stat& x, float l, int id, float c) {
   l = clean(l);
@@ -237,10 +242,10 @@ __device__ __forceinline__ Stat scan(const T* __restrict__ l, const uint32_t* __
       Two t = {0.f, 0.f};
 #pragma unroll
       for (int e = 0; e < kVec; e += 2) {
-        const Two z = mul2(add2(Two{v.y[e], v.y[e + 1]}, Two{-x.base, -x.base}), Two{c, c});
+        const Two z = mul2(fma2(Two{v.y[e], v.y[e + 1]}, 0.5f, -0.5f * x.base), Two{2.f * c, 2.f * c});
         t = add2(t, Two{exp2_fast(z.x), exp2_fast(z.y)});
       }
-      if (t.x + t.y < 1048576.f) {  // (a base is good for terms up to 2^20)
+      if (t.x + t.y < 1048576.f) {  // (a base is good for terms up to 2^20; no NaN, of a logit or of -inf x 0, is below it)
         x.s += t.x + t.y;
       } else {
         const float2 y = take_each<kVec>(x.base, x.s, v, c);
@@ -287,7 +292,7 @@ __device__ __forceinline__ Best best_warp(Best x) {  // (scores are not negative
 struct Scorer {
   float c, base, inv_s;
   __device__ __forceinline__ float operator()(float l, float e, float q) const {
-    float t = exponent(l, base, c), r;
+    float t = fmaf(0.5f, l, -0.5f * base) * (2.f * c), r;
     if (!(t < 126.f)) t = exponent(clean(l), base, c);
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e));
     return fmaxf(fmaf(exp2_fast(t), inv_s, -q), 0.f) * r;

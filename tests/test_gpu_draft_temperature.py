@@ -78,3 +78,28 @@ def test_admitted_ids_at_the_lowest_finite_logit(dt, V):
     check(s)
     tokens, accepted, status, _ = s.got()
     assert (status == 0).all() and (tokens[:, 0] >= 0).all() and (accepted[::6] == 2).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("V,K", [(100, 2), (5000, 1), (33_000, 0)])
+@pytest.mark.parametrize("T", [np.inf, np.finfo(np.float32).max, 1e30, 1e20])
+def test_the_largest_temperatures(T, dt, V, K):
+    """At an infinite temperature all admitted ids but those of logit -inf (or NaN) are equally likely; below it logits at
+    both ends of the type's range still differ by l / T.  Masks of nothing end their row."""
+    import torch
+    top = torch.finfo(torch.float32 if dt == "f32" else torch.bfloat16).max
+    s = Step(36, K, V, dt, probs=False, seed=V)
+    s.draft_len[:] = K
+    g = np.random.default_rng(V)
+    odd = g.choice(np.array([np.nan, -np.inf, np.inf, top, -top, 0], np.float32), s.logits.shape)
+    s.logits[:12] = np.where(g.random(s.logits[:12].shape) < 0.3, odd[:12], s.logits[:12])
+    s.bits[12:16, K] = False
+    s.logits[16:20, K] = np.where(np.arange(V) % 2, np.float32(np.nan), np.float32(-np.inf))
+    s.temp[:] = T
+    s.device()
+    s.run()
+    if np.isinf(T):
+        s.temp = np.full(36, 1e300)
+    check(s)
+    status = s.got()[2]
+    assert K or (status[12:20] == 4).all()
