@@ -24,9 +24,12 @@
 //
 // Roundings: S, m, l and O are fp32.  P is rounded to the cache's type since the
 // tensor cores take both operands of a 16-bit product in one type; m may lag
-// behind the maximum by 8 exponents (fewer rescalings of O), so P is at most
-// 2^8, and its relative error of 2^-9 (2^-12) a term is that of the values it
-// meets.  l is summed before that rounding; out is rounded once.
+// behind the maximum by 8 exponents (fewer rescalings of O).  In bf16 P is at
+// most 2^8, and its relative error of 2^-8 a term is that of the values it
+// meets.  In f16 P is 2^7 times as large (at most 2^15, f16 ends below 2^16):
+// its relative error is 2^-11 down to 2^-21 of the largest term, below that it
+// is held in steps of 2^-24, so that n terms are off by n 2^-32 of the largest
+// at most.  l is summed before that rounding; out is rounded once.
 //
 // Bound by the cached bytes where few rows read many keys: 32 rows of up to 5
 // tokens over up to 16,000 (724 MB) take 119 us, 6.1 TB/s; 32 rows of one token
@@ -71,7 +74,7 @@ struct AttendArgs {
   float scale;
   int32_t* status;
   float4* parts;    // [2 blocks][D / 4][256 rows]
-  float2* part_ml;  // [2 blocks][256 rows]: maximum (in exponents of two) and sum
+  float2* part_ml;  // [2 blocks][256 rows]: maximum (in exponents of two) and sum (2^kLift times it, as the parts are)
   int* joined;      // [blocks]
 };
 
@@ -198,6 +201,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
+
+// P is 2^kLift times the probabilities' numerators.
+template <typename T>
+constexpr float kLift = std::is_same<T, __half>::value ? 7.f : 0.f;
 
 // 32 keys' probabilities 2^(sc s - base) as pairs of T in the first 16 registers; their sums are added.
 template <typename T>
@@ -844,8 +851,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int last = sees - tile * kTile;  // the tile's last visible key
           auto base = [&](float top) {
             const float now = top * sc;
-            // The maximum is moved only where it grew by more than 8 (the probabilities stay below 2^8 and
-            // lose nothing in floating point): few tiles rescale what came before them.
+            // The maximum is moved only where it grew by more than 8 (the probabilities stay below 2^8, or 2^15 in
+            // f16, and lose nothing in floating point): few tiles rescale what came before them.
             if (__any_sync(~0u, live && now - m > 8.f)) {
               const float most = fmaxf(m, now), f = m > -INFINITY ? exp2_fast(m - most) : 0.f;
               if (i > 0) {
@@ -862,13 +869,13 @@ __global__ void __launch_bounds__(kThreads, 1)
               l *= f;
               m = most;
             }
-            return m > -INFINITY ? m : 0.f;
+            return (m > -INFINITY ? m : 0.f) - kLift<T>;
           };
           float added, top;  // (the base may rescale l first)
           if constexpr (L::kApart) {
             bool fits = false;
             if (p.wide && i > 0) {
-              added = softmax_once<T>(s_at, p_at, last, sc, m > -INFINITY ? m : 0.f, top);
+              added = softmax_once<T>(s_at, p_at, last, sc, (m > -INFINITY ? m : 0.f) - kLift<T>, top);
               fits = !__any_sync(~0u, live && top * sc - m > 8.f);
             }
             if (!fits) added = softmax_anew<T>(s_at, p_at, last, sc, base);
@@ -957,7 +964,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (live && (p.wide || s == 0)) {
           if (whole) {
-            if (g.lse) g.lse[(long long)(w.a + t) * g.H + head] = fine ? (m + log2f(l)) * kLn2 : -INFINITY;
+            if (g.lse) g.lse[(long long)(w.a + t) * g.H + head] = fine ? (m - kLift<T> + log2f(l)) * kLn2 : -INFINITY;
           } else {
             __stcg(g.part_ml + (size_t)slot * 256 + part_row, make_float2(m, l));
           }
@@ -1032,7 +1039,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int e = 0; e < kN; ++e) acc[e] = fine ? acc[e] * by : 0.f;
 #pragma unroll
               for (int e = 0; e < kN; e += 8) *reinterpret_cast<uint4*>(to + j + e) = pack8<T>(acc + e);
-              if (g.lse && j == 0) g.lse[(long long)(w.a + tok) * g.H + hh] = fine ? (most + log2f(z)) * kLn2 : -INFINITY;
+              if (g.lse && j == 0) g.lse[(long long)(w.a + tok) * g.H + hh] = fine ? (most - kLift<T> + log2f(z)) * kLn2 : -INFINITY;
             };
             if (cols >= 32)
 #pragma unroll 1
