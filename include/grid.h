@@ -592,7 +592,8 @@ typedef struct grid_kv_query {
  * i's own of scale * q[i][h] . k_j; d_lse gets log sum_j exp(scale q . k_j).  Products and sums are held in fp32; the
  * probabilities are rounded to the cache's type for the product with v.
  * Values of the pools at positions that no row uses are never part of a
- * result, whatever their bits; cached keys and values must be finite.
+ * result, whatever their bits; cached keys and values must be finite.  A query
+ * that is not finite makes its own result NaN, and no other.
  * Uses the scratch held by `kv`, so attends on the same handle must not
  * overlap on the GPU; `out` must not overlap the queries or the pools.  d_status
  * as above; GRID_ST_BOUND in every row: a wait of the kernel ran out (two

@@ -923,11 +923,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++n_o[z];
         }
       if (!ok) break;
-      if (sh.bad[0][k % kRing] | sh.bad[1][k % kRing]) l = NAN;  // (some key that the rows may read is in no page of the cache; known once all tiles were)
+      // A sum below zero: some key that the rows may read is in no page of the cache (known once all tiles were), and they
+      // get zeros.  A sum that is no number, of a query that is none, gives NaN.
+      if (sh.bad[0][k % kRing] | sh.bad[1][k % kRing]) l = -1.f;
       if (warp_live) {
         tm_after();
-        const bool fine = l > 0.f;
-        const float by = !whole ? 1.f : fine ? __frcp_rn(l) : 0.f, f0 = f[0] * by, f1 = f[1] * by;
+        const float by = !whole ? 1.f : __frcp_rn(l), f0 = f[0] * by, f1 = f[1] * by;
         const bool two = !p.wide && p.n[1];
         const int from = p.wide ? 0 : s * (D / 2), to = p.wide ? D : from + D / 2;
         const int part_row = r + (p.wide ? s * kTile : 0);
@@ -946,7 +947,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int e = 0; e < 16; ++e) y[e] = __uint_as_float(o[e]) * f0;
           }
           if (live && whole) {
-            const uint4 a = pack8<T>(y), b = pack8<T>(y + 8);
+            const uint4 none = {}, a = l < 0.f ? none : pack8<T>(y), b = l < 0.f ? none : pack8<T>(y + 8);
             if (g.sectors) {
               asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + j), "r"(a.x), "r"(a.y), "r"(a.z),
                            "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
@@ -964,7 +965,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (live && (p.wide || s == 0)) {
           if (whole) {
-            if (g.lse) g.lse[(long long)(w.a + t) * g.H + head] = fine ? (m - kLift<T> + log2f(l)) * kLn2 : -INFINITY;
+            if (g.lse) g.lse[(long long)(w.a + t) * g.H + head] = l < 0.f ? -INFINITY : (m - kLift<T> + log2f(l)) * kLn2;
           } else {
             __stcg(g.part_ml + (size_t)slot * 256 + part_row, make_float2(m, l));
           }
@@ -997,6 +998,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             auto add_up = [&](auto columns, auto pieces, int j) {
               constexpr int kN = decltype(columns)::value, kP = decltype(pieces)::value;
               float acc[kN] = {}, most = -INFINITY, z = 0.f;
+              bool bad = false;
 #pragma unroll 1
               for (int b = c0; b <= c1; b += kP) {
                 float2 e[kP];
@@ -1014,6 +1016,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int y = 0; y < kP; ++y) {
                   if (b + y > c1) e[y] = make_float2(-INFINITY, 0.f);  // (past the last)
                   now = fmaxf(now, e[y].x);
+                  bad |= e[y].y < 0.f;
                 }
                 const float base = now > -INFINITY ? now : 0.f, f = exp2_fast(most - base);
                 most = now;
@@ -1033,13 +1036,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                   }
                 }
               }
-              const bool fine = z > 0.f;
-              const float by = fine ? __frcp_rn(z) : 0.f;
+              const float by = __frcp_rn(z);
 #pragma unroll
-              for (int e = 0; e < kN; ++e) acc[e] = fine ? acc[e] * by : 0.f;
+              for (int e = 0; e < kN; ++e) acc[e] = bad ? 0.f : acc[e] * by;
 #pragma unroll
               for (int e = 0; e < kN; e += 8) *reinterpret_cast<uint4*>(to + j + e) = pack8<T>(acc + e);
-              if (g.lse && j == 0) g.lse[(long long)(w.a + tok) * g.H + hh] = fine ? (most - kLift<T> + log2f(z)) * kLn2 : -INFINITY;
+              if (g.lse && j == 0) g.lse[(long long)(w.a + tok) * g.H + hh] = bad ? -INFINITY : (most - kLift<T> + log2f(z)) * kLn2;
             };
             if (cols >= 32)
 #pragma unroll 1

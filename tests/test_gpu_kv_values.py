@@ -1,4 +1,5 @@
-"""grid_kv_attend where a lost share of the values shows in the result: keys far below the largest."""
+"""grid_kv_attend where a lost share of the values shows in the result: keys far below the largest; and what is not a
+number in a query."""
 import math
 
 import pytest
@@ -49,3 +50,26 @@ def test_f16_values_of_many_keys_far_below_one(old, new, heads, kv_heads, D, bel
         assert float(((b.lse[a:a + n].double() - lse[:, None]).abs() - 2.0 ** -18 * (1 + lse[:, None])).max()) <= 0
         assert int(b.status[i]) == 0
         a += n
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("old,new,heads,kv_heads,D", [([400, 90, 5], [1, 1, 1], 8, 2, 64), ([9_000, 90, 700], [2, 5, 1], 8, 2, 128),
+                                                       ([100, 3_000, 0], [40, 700, 300], 4, 1, 128), ([100, 0, 7], [400, 300, 20], 14, 2, 64)])
+def test_what_is_not_a_number_in_a_query_stays_in_its_own_result(bad, old, new, heads, kv_heads, D):
+    import torch
+    b = Batch(old, new, heads, kv_heads, D, 16)
+    b.fill()
+    b.attend()
+    out, lse = b.out.clone(), b.lse.clone()
+    at = b.start.tolist()
+    places = [(at[1], heads - 1), (at[2] - 1, 0)]  # of row 1
+    for i, h in places:
+        b.q[i, h, :] = bad  # (infinite: scores of both signs, or infinity less infinity)
+    b.attend()
+    assert b.status.tolist() == [0, 0, 0]
+    for i, h in places:
+        assert bool(b.out[i, h].isnan().all()) and bool(b.lse[i, h].isnan()), (i, h)
+        b.out[i, h], b.lse[i, h] = out[i, h], lse[i, h]
+    for r in (0, 2):  # nothing of these rows is shared with row 1
+        assert torch.equal(b.out[at[r]:at[r + 1]], out[at[r]:at[r + 1]])
+    assert float((b.out - out).abs().max()) <= 2.0 ** -6 * float(out.abs().max()) and float((b.lse - lse).abs().max()) < 1e-4
