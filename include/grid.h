@@ -597,7 +597,8 @@ typedef struct grid_kv_query {
  * Uses the scratch held by `kv`, so attends on the same handle must not
  * overlap on the GPU; `out` must not overlap the queries or the pools.  d_status
  * as above; GRID_ST_BOUND in every row: a wait of the kernel ran out (two
- * seconds; the outputs are not to be used, and the handle is to be freed).
+ * seconds; the outputs are not to be used, and the handle is to be freed: later
+ * attends on it do nothing but report the same).
  * Enqueue only. */
 int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_kv_query* query, int32_t* d_status,
                    void* stream);

@@ -76,6 +76,7 @@ struct AttendArgs {
   float4* parts;    // [2 blocks][D / 4][256 rows]
   float2* part_ml;  // [2 blocks][256 rows]: maximum (in exponents of two) and sum (2^kLift times it, as the parts are)
   int* joined;      // [blocks]
+  int* gave_up;     // one word: a wait ran out, in this call or an earlier one
 };
 
 // ---------------------------------------------------------------------------
@@ -490,6 +491,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   pdl_wait();
 
+  // (Where a call gave up, units may wait for pieces that never came: this one does nothing but report it.)
+  const int broken = __ldcg(g.gave_up);
   // How many tiles there are in all, and the row that this block begins in.
   Cut cut;
   bool whole_heads;
@@ -545,6 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       total += x.x, all_rows += x.y, most = max(most, x.z);
     }
     pre -= mine, pre_rows -= rows;
+    if (broken) total = 0;
     cut.runs = min((int)gridDim.x, (total + kMinRun - 1) / kMinRun);
     cut.each = cut.runs ? total / cut.runs : 0;
     // A key head to a block, where that makes no block's work longer than a run and what joining takes.
@@ -674,6 +678,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
+    // A block that gave up writes GRID_ST_BOUND to all rows, after it set the word: what was stored here before that is
+    // overwritten there, what comes after it sees the word.
+    __threadfence();
+    if (!v && lane == 0 && __ldcg(g.gave_up))
+      for (int b = blockIdx.x; b < c.B; b += gridDim.x) g.status[b] = GRID_ST_BOUND;
     // (No copy is in flight when the block ends: every tile was waited for.  Where a wait was given up, what is still on
     // its way has a tenth of a millisecond to land.)
     if (*gave_up)
@@ -1061,8 +1070,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!ok) *gave_up = 1;
   }
   __syncthreads();
-  if (sh.gave_up)
+  if (sh.gave_up) {
+    if (tid == 0) {
+      atomicExch(g.gave_up, 1);
+      __threadfence();
+    }
+    __syncthreads();
     for (int b = tid; b < c.B; b += kThreads) g.status[b] = GRID_ST_BOUND;
+  }
   if (warp == kMmaWarp) {
     tm_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
@@ -1128,7 +1143,9 @@ extern "C" int grid_kv_create(const grid_kv_pages* p, grid_kv** out) {
     if (!(rc = kv->mem.alloc(slots * p->head_dim * 4, (void**)&kv->parts)) &&
         !(rc = kv->mem.alloc(slots * sizeof(float2), (void**)&kv->part_ml)) &&
         !(rc = kv->mem.alloc(kv->sms * sizeof(int), (void**)&kv->joined)) &&
+        !(rc = kv->mem.alloc(sizeof(int), (void**)&kv->gave_up)) &&
         (e = cudaMemset(kv->joined, 0, kv->sms * sizeof(int))) == cudaSuccess &&
+        (e = cudaMemset(kv->gave_up, 0, sizeof(int))) == cudaSuccess &&
         (e = each_kernel([](auto kern, size_t smem) {
            return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
          })) == cudaSuccess)
@@ -1168,7 +1185,7 @@ extern "C" int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, con
   a.os[0] = query->out.token_stride, a.os[1] = query->out.head_stride;
   a.H = p.n_heads, a.Hk = p.n_kv_heads, a.group = a.H / a.Hk, a.scale = query->scale, a.status = d_status;
   a.sectors = (uintptr_t)a.out % 32 == 0 && a.os[0] % 16 == 0 && a.os[1] % 16 == 0;
-  a.parts = reinterpret_cast<float4*>(kv->parts), a.part_ml = kv->part_ml, a.joined = kv->joined;
+  a.parts = reinterpret_cast<float4*>(kv->parts), a.part_ml = kv->part_ml, a.joined = kv->joined, a.gave_up = kv->gave_up;
   auto go = [&](auto kern, size_t smem) {
     return launch_pdl(kern, dim3(kv->sms), dim3(kThreads), smem, (cudaStream_t)stream, a, kv->k_map, kv->v_map);
   };

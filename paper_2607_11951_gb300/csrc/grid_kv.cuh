@@ -86,6 +86,7 @@ inline bool heads_ok(const grid_heads* h) {
 
 struct grid_kv {
   grid_kv_pages p;
+  int* gave_up = nullptr;    // one word on the device: a wait of an attend ran out (the first field after p: tests set it)
   int log_page = 0, sms = 152;
   CUtensorMap k_map, v_map;  // of the pools, for the attention's tiles
   float* parts = nullptr;    // partial results of the attention's split rows
