@@ -548,11 +548,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       total += x.x, all_rows += x.y, most = max(most, x.z);
     }
     pre -= mine, pre_rows -= rows;
-    if (broken) total = 0;
-    cut.runs = min((int)gridDim.x, (total + kMinRun - 1) / kMinRun);
+    cut.runs = broken ? 0 : min((int)gridDim.x, (total + kMinRun - 1) / kMinRun);
     cut.each = cut.runs ? total / cut.runs : 0;
     // A key head to a block, where that makes no block's work longer than a run and what joining takes.
-    whole_heads = all_rows <= (int)gridDim.x / g.Hk && most <= cut.each + kJoinCost;
+    whole_heads = !broken && all_rows <= (int)gridDim.x / g.Hk && most <= cut.each + kJoinCost;
     if (whole_heads) cut.runs = all_rows * g.Hk, pre = pre_rows * g.Hk, mine = rows * g.Hk;
     cut.each = cut.runs ? total / cut.runs : 0;
     cut.more = total - cut.runs * cut.each;

@@ -39,3 +39,12 @@ def test_a_wait_that_ran_out_is_reported_in_every_row_from_then_on(old, new, D):
     b.lens[0] = old[0]
     b.attend()
     b.check()
+
+
+@pytest.mark.parametrize("old,new,D", [([0], [1], 64), ([40], [1], 128), ([200], [3], 128), ([5000, 3], [2, 150], 64), ([7] * 400, [1] * 400, 64)])
+def test_nothing_is_attended_to_after_a_wait_ran_out(old, new, D):
+    b = Batch(old, new, 4, 2, D, 16)
+    b.fill()
+    word_of(b.kv)[0] = 1
+    b.attend()
+    assert b.status.tolist() == [5] * len(old) and bool((b.out == 7).all()) and bool((b.lse == 7).all())
