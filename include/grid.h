@@ -516,7 +516,10 @@ int grid_configs_export(const grid_configs* c, int32_t row, int32_t* stack, int3
  * GRID_ST_PAGES.  An append leaves out its tokens whose own place fails.  An
  * attend writes zeros (lse -inf) for all tokens of a row whose length or order
  * fails, and where a page id fails for the tokens that would read that page at
- * least (the row's earlier tokens get zeros too, or their own result).  Tokens
+ * least (the row's earlier tokens get zeros too, or their own result).  Where
+ * d_start is not in order and rows overlap, tokens of several rows get any of
+ * their results, or zeros; an attend whose overlapping rows are more work than
+ * one call takes fails all rows.  Tokens
  * that belong to no row, from d_start[B] on, are left alone.  Entries of
  * d_table that no token of the row lies in are not read. */
 typedef struct grid_kv_pages {

@@ -61,6 +61,10 @@ constexpr int kThreads = (kSoftWarps + 4) * 32;
 // and the dearest is no longer than a run and what it costs to join pieces, none is cut (16 rows of one token over up to
 // 500: 15.1 -> 11.2 us; a prompt of 64: 16.0 -> 10.4).
 constexpr int kUnitCost = 2, kMinRun = 3, kJoinCost = 4;
+// The costs of all units together, so that places among them are ints.  Rows of an ordered `start` share the tokens of the
+// chunk, and what they can cost is checked on the host; rows that overlap, of a start that is not in order, can each be in
+// order and cost any multiple of it, which the plan finds (counting in 65,536, less one a warp) before it uses a place.
+constexpr int kMostCost = INT32_MAX - (1 << 20);
 constexpr int kRing = 8;              // pieces whose bad-page flags are kept at once
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
@@ -357,7 +361,7 @@ struct Units {
   int b, a, n, len, rows;  // row, its first token, tokens, cached tokens, query rows per key head
   int units, h, qt;        // units per key head; the current one
   int tiles;               // key tiles of the current unit
-  int at;                  // where its tiles begin, in costs (their sum is checked on the host to fit)
+  int at;                  // where its tiles begin, in costs (kMostCost at most: see there)
 };
 
 __device__ __forceinline__ int tiles_of(const Units& u, int group, int qt) {
@@ -442,8 +446,8 @@ struct Shared {
   uint64_t q_ready[2], q_free[2], s_ready[2], p_half[2], p_ready[2], o_ready[2], all;
   float2 ml[2][kTile];
   Units units[kSoftWarps];
-  int3 sums[kThreads / 32];  // of the warps: cost, rows, dearest row
-  int first, per, row[4], gave_up, last, bad[2][kRing];
+  int4 sums[kThreads / 32];  // of the warps: cost, rows, dearest row, cost in 65,536
+  int first, per, row[4], gave_up, last, crowded, bad[2][kRing];
   uint32_t tmem;
 };
 
@@ -523,10 +527,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       return at >= 0 ? many[3 * at + 2] : t;
     };
     int mine = 0, rows = 0, most = 0, t = 0;  // of this thread: their cost, how many have tokens, the dearest
+    unsigned high = 0, low = 0;               // the cost in halves, which no 65,535 rows overflow
 #pragma unroll 1
     for (int i = 0; i < per; ++i) {
       t = row_cost(tid * per + i);
       mine += t * g.Hk, rows += t > 0, most = max(most, t);
+      high += (unsigned)(t * g.Hk) >> 16, low += (unsigned)(t * g.Hk) & 0xFFFFu;
     }
     auto up_to = [&](int x) {  // the sum over the lanes up to this one
 #pragma unroll
@@ -538,20 +544,23 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     int pre = up_to(mine), pre_rows = up_to(rows);
     most = __reduce_max_sync(~0u, most);
-    if (lane == 31) sh.sums[warp] = make_int3(pre, pre_rows, most);
+    high = __reduce_add_sync(~0u, high) + (__reduce_add_sync(~0u, low) >> 16);
+    if (lane == 31) sh.sums[warp] = make_int4(pre, pre_rows, most, (int)high);
     __syncthreads();
-    int total = 0, all_rows = 0;
+    int total = 0, all_rows = 0, coarse = 0;
 #pragma unroll
     for (int w = 0; w < kThreads / 32; ++w) {
-      const int3 x = sh.sums[w];
+      const int4 x = sh.sums[w];
       if (w < warp) pre += x.x, pre_rows += x.y;
-      total += x.x, all_rows += x.y, most = max(most, x.z);
+      total += x.x, all_rows += x.y, most = max(most, x.z), coarse += x.w;
     }
+    const bool crowded = coarse > (kMostCost >> 16), none = broken || crowded;
+    if (tid == 0) sh.crowded = crowded;
     pre -= mine, pre_rows -= rows;
-    cut.runs = broken ? 0 : min((int)gridDim.x, (total + kMinRun - 1) / kMinRun);
+    cut.runs = none ? 0 : min((int)gridDim.x, (total + kMinRun - 1) / kMinRun);
     cut.each = cut.runs ? total / cut.runs : 0;
     // A key head to a block, where that makes no block's work longer than a run and what joining takes.
-    whole_heads = !broken && all_rows <= (int)gridDim.x / g.Hk && most <= cut.each + kJoinCost;
+    whole_heads = !none && all_rows <= (int)gridDim.x / g.Hk && most <= cut.each + kJoinCost;
     if (whole_heads) cut.runs = all_rows * g.Hk, pre = pre_rows * g.Hk, mine = rows * g.Hk;
     cut.each = cut.runs ? total / cut.runs : 0;
     cut.more = total - cut.runs * cut.each;
@@ -662,12 +671,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---- then one of them reports the rows, and zeros those that are not in order
     for (int b = blockIdx.x; !v && b < c.B; b += gridDim.x) {
       int a, n, len;
-      bool good = row_span(c, b, a, n, len);
+      const bool ordered = row_span(c, b, a, n, len) && !sh.crowded;
+      bool good = ordered;
       if (good && n)
         for (int p = lane; p <= (len + n - 1) >> c.log_page; p += 32) good = good && page_of(c, b, p << c.log_page) >= 0;
       good = __all_sync(~0u, good);
       if (lane == 0) g.status[b] = good ? GRID_ST_OK : GRID_ST_PAGES;
-      if (!row_span(c, b, a, n, len)) {
+      if (!ordered) {
         const int from = max(0, a), to = (int)min((long long)c.N, (long long)a + n);
         for (long long i = (long long)from * g.H; i < (long long)to * g.H; ++i) {
           const long long tok = i / g.H, h = i % g.H;
@@ -1177,7 +1187,7 @@ extern "C" int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, con
   // (more than two billion tiles of 256 query rows by 128 keys would take minutes)
   const double units = (double)chunk->n_tokens * (p.n_heads / p.n_kv_heads) / 256 + chunk->B;
   if ((double)chunk->n_tokens * (p.n_heads / p.n_kv_heads) > INT32_MAX - 256 ||
-      units * p.n_kv_heads * (((double)chunk->max_pages * p.page_size) / kTile + 1 + kUnitCost) > INT32_MAX)
+      units * p.n_kv_heads * (((double)chunk->max_pages * p.page_size) / kTile + 1 + kUnitCost) > kMostCost)
     return set_error(GRID_E_TOO_LARGE, "grid_kv_attend: too many query rows or key tiles in one call");
   a.q = query->q.d, a.out = query->out.d, a.lse = query->d_lse;
   a.qs[0] = query->q.token_stride, a.qs[1] = query->q.head_stride;
