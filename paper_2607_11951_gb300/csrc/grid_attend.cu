@@ -447,7 +447,7 @@ struct Shared {
   float2 ml[2][kTile];
   Units units[kSoftWarps];
   int4 sums[kThreads / 32];  // of the warps: cost, rows, dearest row, cost in 65,536
-  int first, per, row[4], gave_up, last, crowded, bad[2][kRing];
+  int first, per, row[4], gave_up, last, broken, crowded, bad[2][kRing];
   uint32_t tmem;
 };
 
@@ -457,6 +457,23 @@ template <int D>
 constexpr size_t smem_bytes() {
   static_assert(sizeof(Shared) <= kSharedRoom);
   return kSharedRoom + Layout<D>::kTiles;
+}
+
+// A block that gave up sets the handle's word, then writes GRID_ST_BOUND to all rows.
+__device__ __noinline__ void report_bound(int* gave_up, int32_t* status, int B) {
+  if (threadIdx.x == 0) {
+    atomicExch(gave_up, 1);
+    __threadfence();
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < B; b += kThreads) status[b] = GRID_ST_BOUND;
+}
+// By a warp that stored its rows' status: what it stored before a block set the word is overwritten by that block, what it
+// stored after it sees the word.
+__device__ __noinline__ void report_again(int* gave_up, int32_t* status, int B) {
+  __threadfence();
+  if (__ldcg(gave_up) && threadIdx.x % 32 == 0)
+    for (int b = blockIdx.x; b < B; b += gridDim.x) status[b] = GRID_ST_BOUND;
 }
 
 template <typename T, int D>
@@ -495,8 +512,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   pdl_wait();
 
-  // (Where a call gave up, units may wait for pieces that never came: this one does nothing but report it.)
-  const int broken = __ldcg(g.gave_up);
+  const int broken = tid == 0 ? __ldcg(g.gave_up) : 0;
   // How many tiles there are in all, and the row that this block begins in.
   Cut cut;
   bool whole_heads;
@@ -554,13 +570,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (w < warp) pre += x.x, pre_rows += x.y;
       total += x.x, all_rows += x.y, most = max(most, x.z), coarse += x.w;
     }
-    const bool crowded = coarse > (kMostCost >> 16), none = broken || crowded;
+    const bool crowded = coarse > (kMostCost >> 16);
     if (tid == 0) sh.crowded = crowded;
     pre -= mine, pre_rows -= rows;
-    cut.runs = none ? 0 : min((int)gridDim.x, (total + kMinRun - 1) / kMinRun);
+    cut.runs = crowded ? 0 : min((int)gridDim.x, (total + kMinRun - 1) / kMinRun);
     cut.each = cut.runs ? total / cut.runs : 0;
     // A key head to a block, where that makes no block's work longer than a run and what joining takes.
-    whole_heads = !none && all_rows <= (int)gridDim.x / g.Hk && most <= cut.each + kJoinCost;
+    whole_heads = !crowded && all_rows <= (int)gridDim.x / g.Hk && most <= cut.each + kJoinCost;
     if (whole_heads) cut.runs = all_rows * g.Hk, pre = pre_rows * g.Hk, mine = rows * g.Hk;
     cut.each = cut.runs ? total / cut.runs : 0;
     cut.more = total - cut.runs * cut.each;
@@ -578,8 +594,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       pre += each * g.Hk;
     }
   }
-  const bool works = (int)blockIdx.x < cut.runs;
+  if (tid == 0) sh.broken = broken;
   __syncthreads();
+  // (Where a call gave up, units may wait for pieces that never came: this one does nothing but report it.)
+  const bool works = (int)blockIdx.x < cut.runs && !sh.broken;
   tm_after();
   const uint32_t tmem = sh.tmem;
   const int lo = !works || whole_heads ? 0 : cut.begin(blockIdx.x), hi = !works ? 0 : whole_heads ? sh.per : cut.begin(blockIdx.x + 1);
@@ -687,11 +705,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
-    // A block that gave up writes GRID_ST_BOUND to all rows, after it set the word: what was stored here before that is
-    // overwritten there, what comes after it sees the word.
-    __threadfence();
-    if (!v && lane == 0 && __ldcg(g.gave_up))
-      for (int b = blockIdx.x; b < c.B; b += gridDim.x) g.status[b] = GRID_ST_BOUND;
+    if (!v) report_again(g.gave_up, g.status, c.B);
     // (No copy is in flight when the block ends: every tile was waited for.  Where a wait was given up, what is still on
     // its way has a tenth of a millisecond to land.)
     if (*gave_up)
@@ -1079,14 +1093,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!ok) *gave_up = 1;
   }
   __syncthreads();
-  if (sh.gave_up) {
-    if (tid == 0) {
-      atomicExch(g.gave_up, 1);
-      __threadfence();
-    }
-    __syncthreads();
-    for (int b = tid; b < c.B; b += kThreads) g.status[b] = GRID_ST_BOUND;
-  }
+  if (sh.gave_up) report_bound(g.gave_up, g.status, c.B);
   if (warp == kMmaWarp) {
     tm_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
