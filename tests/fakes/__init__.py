@@ -27,13 +27,17 @@ def link(folder):
 class Runtime:
     def __init__(self, path):
         self.L = ctypes.CDLL(path)
-        self.L.fake_launches.restype = ctypes.c_char_p
+        self.L.fake_launches.restype = self.L.fake_allocations.restype = ctypes.c_char_p
 
     def reset(self, fail_at=0, ones=0):
         self.L.fake_reset(ctypes.c_long(fail_at), ctypes.c_long(ones))
 
     def get(self, name):
         return ctypes.c_long.in_dll(self.L, "fake_" + name).value
+
+    def allocations(self):
+        """Bytes of each device allocation since the last reset."""
+        return list(map(int, self.L.fake_allocations().decode().split()))
 
     def launches(self):
         """(kernel, grid, threads, dynamic shared memory, its limit) per launch since the last reset."""

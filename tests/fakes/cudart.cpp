@@ -18,6 +18,7 @@ struct Config {  // the start of cudaLaunchConfig_t
 };
 std::map<const void*, std::string> names;
 std::map<std::string, int> limits;  // cudaFuncAttributeMaxDynamicSharedMemorySize per kernel
+std::string allocations;             // "bytes\n" per cudaMalloc
 std::string launches;                // "name gx gy gz threads smem limit\n" per launch
 constexpr int kOk = 0, kMalloc = 2, kUnknown = 999, kDefaultSmem = 48 * 1024;
 int last = kOk;
@@ -28,12 +29,14 @@ extern "C" {
 long fake_calls, fake_fail_at, fake_live, fake_ones;  // ones: device-to-host copies deliver 32-bit ones
 
 const char* fake_launches() { return launches.c_str(); }
+const char* fake_allocations() { return allocations.c_str(); }
 void fake_reset(long fail_at, long ones) {
   fake_calls = 0;
   fake_fail_at = fail_at;
   fake_ones = ones;
   last = kOk;
   launches.clear();
+  allocations.clear();
 }
 
 static int step(int error) {
@@ -52,6 +55,7 @@ static int launch(const void* f, Dim g, Dim b, size_t smem) {
 int cudaMalloc(void** p, size_t n) {
   if (int e = step(kMalloc)) return e;
   *p = calloc(1, n ? n : 1);
+  allocations += std::to_string(n) + "\n";
   ++fake_live;
   return kOk;
 }
