@@ -617,8 +617,9 @@ int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_kv_
  * w_i / e_i over the admitted ids, with w = max(p_n - q_n, 0) after a refusal
  * (p_n where no score is above zero) and w = p_n when all were accepted; with u uniform
  * in [0, 1) and e exponential the tokens are distributed as the target's own.
- * T_b <= 0 is greedy: x_k is accepted when it is the first largest admitted
- * logit, and that is the token drawn.  K = 0 samples one token per row.
+ * T_b <= 0 (or not a number) is greedy: x_k is accepted when it is the first
+ * largest admitted logit, and that is the token drawn; an infinite T_b makes all
+ * admitted ids of finite logit equally likely.  K = 0 samples one token per row.
  *
  * An id outside 0 .. V-1 or the mask is refused (p = 0).  NaN logits count as
  * -inf; +inf as the largest finite value.  Noise below 2^-126 or not a number

@@ -32,12 +32,14 @@
 // at most.  l is summed before that rounding; out is rounded once.
 //
 // Bound by the cached bytes where few rows read many keys: 32 rows of up to 5
-// tokens over up to 16,000 (724 MB) take 119 us, 6.1 TB/s; 32 rows of one token
+// tokens over up to 16,000 (724 MB) take 118 us, 6.1 TB/s; 32 rows of one token
 // over up to 2,000 (90 MB) 29 us, of which the start and the joins are some 10;
-// one token over 400 takes 9.5.  Bound by the products and the exponentials
-// between them where a chunk is long: 2 x 2,000 tokens over 16,000 (605 GF) take
-// 434 us, 1,390 TFLOP/s; 27 prompts of up to 2,000 with 64-wide heads, an
-// exponential for every 256 operations, 208 us.
+// one token over 400 takes 9.9.  Bound by the products and the exponentials
+// between them where a chunk is long: a call for 2 x 2,000 tokens over 16,000
+// (605 GF) takes 454 us, 1,330 TFLOP/s (440 back to back in a graph, 1,370); 27
+// prompts of up to 2,000 with 64-wide heads, an exponential for every 256
+// operations, 208 us.  The constants' figures below are of 32 + 8 heads of 128
+// (prompts: 14 + 2 of 64) in a graph.
 #include <dlfcn.h>
 
 #include <cmath>
@@ -55,11 +57,11 @@ constexpr int kLoadWarp = kSoftWarps;      // two that load tiles, of keys and o
 constexpr int kMmaWarp = kSoftWarps + 2;   // one that multiplies,
 constexpr int kQueryWarp = kSoftWarps + 3, kQueryWarps = 1;  // one that loads queries
 constexpr int kThreads = (kSoftWarps + 4) * 32;
-// A unit's beginning and end cost as much as some tiles (2: 28.4 us for 32 rows of one token, 208 for 27 prompts, 440 for
-// 2 x 2,000 tokens over 16,000; 3: 28.1, 213, 438), and runs are not made shorter than a few (3: one token over 2,000 and
-// 16,000 takes 12.5 and 25 us, 200 tokens over 500 24; 5: 15, 25 and 29).  Where every key head can have a block of its own
-// and the dearest is no longer than a run and what it costs to join pieces, none is cut (16 rows of one token over up to
-// 500: 15.1 -> 11.2 us; a prompt of 64: 16.0 -> 10.4).
+// A unit's beginning and end cost as much as some tiles (2: 29.1 us for 32 rows of one token, 208 for 27 prompts, 439 for
+// 2 x 2,000 tokens over 16,000; 3: 28.8, 214, 442), and runs are not made shorter than a few (3: one token over 2,000 and
+// 16,000 takes 12.2 and 24.2 us, 200 tokens over 500 24.7; 5: 15.0, 24.2 and 31.0).  Where every key head can have a block
+// of its own and the dearest is no longer than a run and what it costs to join pieces, none is cut (16 rows of one token
+// over up to 500: 13.3 -> 11.3 us; one token over 400, 8 + 2 heads of 64: 10.9 -> 9.9).
 constexpr int kUnitCost = 2, kMinRun = 3, kJoinCost = 4;
 // The costs of all units together, so that places among them are ints.  Rows of an ordered `start` share the tokens of the
 // chunk, and what they can cost is checked on the host; rows that overlap, of a start that is not in order, can each be in
@@ -1024,9 +1026,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int qrow = p.r0 + rr, tok = qrow / g.group, hh = w.h * g.group + qrow - tok * g.group;
             T* to = (T*)g.out + (long long)(w.a + tok) * g.os[0] + (long long)hh * g.os[1];
             // So many columns of so many pieces at a time, the sums rescaled as they go: no load of a round waits for another
-            // (maximum, sum and values in three passes: one token over 16,000 32 us instead of 24; 16 columns at most instead
-            // of 32: 2 x 2,000 tokens over 16,000 446 instead of 434; three pieces of 32 columns instead of two 441; two of 8
-            // columns instead of six: one token over 16,000 with one key head 17.9 instead of 16.6).
+            // (16 columns at most instead of 32: 27 prompts 212 us instead of 208; three pieces of 32 columns instead of two: 2 x
+            // 2,000 tokens over 16,000 450 instead of 443; two of 8 columns instead of six: one token over 16,000 with 16 query
+            // heads and one key head 18.7 instead of 17.1).
             auto add_up = [&](auto columns, auto pieces, int j) {
               constexpr int kN = decltype(columns)::value, kP = decltype(pieces)::value;
               float acc[kN] = {}, most = -INFINITY, z = 0.f;

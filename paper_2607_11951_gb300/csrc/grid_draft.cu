@@ -17,11 +17,11 @@
 // Both kernels are bound by the bytes they read and, in bf16, by the
 // instructions for an id; each id's mask bit is looked at first, and 16 bytes of
 // logits that hold no admitted id are not read.  256 rows of 5 positions over
-// 151,937 ids (bf16, 414 MB read) take 117 us, 32 rows in fp32 37, one row of 3
-// positions over 512 ids 7.5 (one launch, a chain of dependent loads).  A cluster
-// of blocks per row that stops at the first refusal reads less, but its
-// positions follow one another: 61 us (32 rows) and 178 us (256 rows) where this
-// takes 37 and 117.
+// 151,937 ids (bf16, 414 MB read) take 120 us in a graph, 32 rows in fp32 37, one
+// row of 3 positions over 512 ids 7.1 (one launch, a chain of dependent loads);
+// calls take 119, 36 and 10.  K = 0, 32 rows over 151,936 ids: 24 in either type.
+// A cluster of blocks per row that stops at the first refusal reads less, but its
+// positions follow one another: 61 us (32 rows) and 178 us (256 rows).
 #include <cfloat>
 #include <cmath>
 #include <new>
@@ -35,8 +35,8 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxPieces = 64, kMaxParts = 256;  // of one position's logits, of one draw
 constexpr int kMaxDraft = 64;
 constexpr int kAlone = 4096;  // ids that a row's last block draws from by itself
-// Blocks wanted of either kernel.  Of k_stats, what the SMs hold at once (32 rows of 5 positions in fp32: 38.2 us with 5,
-// 39.1 with 8); of k_draw, many short ones (256 rows over 151,937 ids: 118 us with 24, 122 with 12).
+// Blocks wanted of either kernel.  Of k_stats, what the SMs hold at once (32 rows of 5 positions in fp32: 36.9 us with 5,
+// 39.5 with 8); of k_draw, many short ones (256 rows over 151,937 ids: 120 us with 24, 124 with 12).
 constexpr int kBlocksPerSm = 5, kDrawsPerSm = 24;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -612,8 +612,8 @@ extern "C" int grid_draft_verify(const grid_drafts* d, const grid_draft_step* s,
   const long long rows = (long long)s->B * (s->K + 1);
   int pieces, piece, parts, part;
   cut(rows, kBlocksPerSm, kWarps * kTileIds, kMaxPieces, pieces, piece);
-  // (a warp draws from twice 256 ids, or once where the SMs would not all have a block: 32 rows over 151,936 ids take 36.7 us
-  // so and 39 with one; 8 rows over 32,000 14.5 and 13.8)
+  // (a warp draws from twice 256 ids, or once where the SMs would not all have a block: 32 rows over 151,936 ids take 36.9 us
+  // so and 40.1 with one; 8 rows over 32,000 14.6 and 13.8)
   const bool few = (long long)s->B * s->V < 4LL * kTileIds * d->sms;
   cut(s->B, kDrawsPerSm, (few ? 2 : 4) * kTileIds, kMaxParts, parts, part);
   const bool alone = s->V <= kAlone;

@@ -17,12 +17,12 @@ namespace {
 // that partners are one lane's and its arithmetic is on two values at once.
 //
 // Bound by the bytes moved: 32 prompts of 2,000 tokens (32 + 8 heads of 128,
-// normed and turned, 1.19 GB) take 188 us, 6.3 TB/s (partners by shuffle: 221
+// normed and turned, 1.19 GB) take 187 us, 6.4 TB/s (partners by shuffle: 221
 // us, with 61% of the issue slots taken).  The first group is on its way while
 // the token's row, length and page are looked up one after the other, each later
 // one while the one before is worked on.  A large batch's warps take whole
 // tokens, so that the look-ups (3 us) are paid once for 24 KB; a small one's take
-// a group each (256 tokens 3.6 us, one 2.5).  Eight heads at once: four took 197
+// a group each (256 tokens 3.2 us, one 2.1).  Eight heads at once: four took 197
 // us, and twelve 203.
 struct AppendArgs {
   Chunk c;
