@@ -117,8 +117,12 @@ __device__ __forceinline__ bool admitted(const uint32_t* mask, int id) { return 
 // One more term of the sum; l is clean.
 __device__ __forceinline__ void add(Stat& x, float l, float c) {
   if (!(l > -INFINITY)) return;
-  if (!(x.base > -INFINITY) || exponent(l, x.base, c) > 16.f) rebase(x, l, c);
-  x.s += exp2_fast(exponent(l, x.base, c));
+  float t = fmaf(0.5f, l, -0.5f * x.base) * (2.f * c);
+  if (!(t <= 16.f)) {  // (infinite or no number where no base is set yet)
+    rebase(x, l, c);
+    t = 0.f;
+  }
+  x.s += exp2_fast(t);
 }
 __device__ __forceinline__ void take(Stat& x, float l, int id, float c) {
   l = clean(l);
