@@ -17,9 +17,10 @@
 // Both kernels are bound by the bytes they read and, in bf16, by the
 // instructions for an id; each id's mask bit is looked at first, and 16 bytes of
 // logits that hold no admitted id are not read.  256 rows of 5 positions over
-// 151,937 ids (bf16, 414 MB read) take 120 us in a graph, 32 rows in fp32 37, one
-// row of 3 positions over 512 ids 7.1 (one launch, a chain of dependent loads);
-// calls take 119, 36 and 10.  K = 0, 32 rows over 151,936 ids: 24 in either type.
+// 151,937 ids (bf16, 414 MB read) take 118 us in a graph, 32 rows in fp32 37, one
+// row of 3 positions over 512 ids 7.1 (one launch, a chain of dependent loads; a
+// call takes 10); low temperatures move the bases more often: 199 at T = 1e-3 for
+// the 256 rows.  K = 0, 32 rows over 151,936 ids: 24 in either type.
 // A cluster of blocks per row that stops at the first refusal reads less, but its
 // positions follow one another: 61 us (32 rows) and 178 us (256 rows).
 #include <cfloat>
@@ -36,7 +37,7 @@ constexpr int kMaxPieces = 64, kMaxParts = 256;  // of one position's logits, of
 constexpr int kMaxDraft = 64;
 constexpr int kAlone = 4096;  // ids that a row's last block draws from by itself
 // Blocks wanted of either kernel.  Of k_stats, what the SMs hold at once (32 rows of 5 positions in fp32: 36.9 us with 5,
-// 39.5 with 8); of k_draw, many short ones (256 rows over 151,937 ids: 120 us with 24, 124 with 12).
+// 39.5 with 8); of k_draw, many short ones (256 rows over 151,937 ids: 118 us with 24, 4 more with 12).
 constexpr int kBlocksPerSm = 5, kDrawsPerSm = 24;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
