@@ -32,7 +32,10 @@
  * chain, Sec. 6.4).  The model's side of a step that brings several tokens a
  * row: grid_kv_append and grid_kv_attend (a chunk through attention over a
  * paged cache) and grid_draft_verify (drafted tokens against the masked
- * target distribution).
+ * target distribution).  Where several continuations are drafted at once, the
+ * chunk is a tree: grid_tree_plan, grid_kv_append_tree, grid_kv_attend_tree,
+ * grid_tree_accept and grid_kv_compact; grid_pages_update and grid_kv_copy hand
+ * out, share, fork and take back the pages of the cache.
  *
  * Conventions
  *   - Every call returns 0 (GRID_OK) or a negative GRID_E_* code; the message of
@@ -102,8 +105,11 @@ extern "C" {
 #define GRID_ST_BOUND 5             /* a per-token overlay or reduce-chain bound hit  */
 #define GRID_ST_COMPLETE 6          /* the row accepted EOS; its mask is all zero     */
 #define GRID_ST_PAGES 7             /* a row's chunk does not fit its pages or its    */
-                                    /* positions' table, or a page id is outside the  */
-                                    /* cache                                          */
+                                    /* positions' table, a page id is outside the     */
+                                    /* cache, or no page is left                      */
+#define GRID_ST_TREE 8              /* a row's tree has more tokens than its words     */
+                                    /* hold, a parent that does not come before its   */
+                                    /* child, or a path that does not go down in it   */
 
 /* ---- dtypes of logits (F32, BF16) and of heads and caches (BF16, F16) ---- */
 #define GRID_DTYPE_F32 0
@@ -117,6 +123,7 @@ typedef struct grid_configs grid_configs;
 typedef struct grid_cache grid_cache;
 typedef struct grid_kv grid_kv;
 typedef struct grid_drafts grid_drafts;
+typedef struct grid_pages grid_pages;
 
 /* One L3 lexicon: the allowed words W_c of category terminal `category`
  * (Sec. 2, L3).  Word i is words[offsets[i] .. offsets[i+1]); host memory,
@@ -658,6 +665,125 @@ void grid_drafts_free(grid_drafts* d);
 /* Verify one step's drafts.  Uses the scratch held by `d`, so calls on the
  * same handle must not overlap on the GPU.  Enqueue only. */
 int grid_draft_verify(const grid_drafts* d, const grid_draft_step* step, void* stream);
+
+/* ---- a tree of drafted tokens ----
+ * A drafter that proposes several continuations at once makes a row's chunk a
+ * tree: its tokens, a parent before its children, are d_start[b] ..
+ * d_start[b+1]-1 of the packed arrays as for any chunk (d_start NULL: n_tokens /
+ * B tokens a row).  Token i of a row has parent d_parent[start + i] < i, the
+ * index of another token of the row, or -1: it follows what is cached.  Token 0
+ * is what the model reads next in any case (the last sampled token), the others
+ * are drafted.  A step: plan, append and attend (each layer), one token drawn
+ * at every token of the tree (its mask is that of the path to it), accept,
+ * compact (each layer), d_len += d_count. */
+typedef struct grid_tree {
+  const int32_t* d_parent; /* [n_tokens]       */
+  const int32_t* d_start;  /* [B + 1] or NULL  */
+  int32_t B, n_tokens;
+} grid_tree;
+
+/* d_depth[i] is the number of token i's ancestors, bit j of its words
+ * d_sees[i * n_words ..] is set for the row's token j if that is an ancestor or
+ * i itself.  1 <= n_words <= 32; a row has up to 32 n_words tokens.  A row with
+ * more of them, or out of order, is left alone, one with a bad parent gets
+ * depth 0 and its tokens see themselves; d_status[b] = GRID_ST_TREE for these.
+ * 1 <= B <= 65535; n_tokens may be 0.  Enqueue only. */
+int grid_tree_plan(const grid_tree* tree, int32_t* d_depth, uint32_t* d_sees, int32_t n_words, int32_t* d_status,
+                   void* stream);
+
+/* grid_kv_append of a tree: token i of row b is stored at position d_len[b] + i
+ * and turned by the angles of position d_len[b] + d_depth[...] (NULL: of its
+ * own position).  A token whose depth is negative, or whose angles are outside
+ * the table, is left out, and its row gets GRID_ST_PAGES. */
+int grid_kv_append_tree(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_heads* k, const grid_heads* v,
+                        const grid_heads* q, const grid_heads* q_out, const grid_rotation* rot, const grid_head_norm* norm,
+                        const int32_t* d_depth, int32_t* d_status, void* stream);
+
+/* grid_kv_attend of a tree: token i of a row sees what was cached before the
+ * chunk and those of the chunk's tokens j <= i whose bit is set (d_sees as
+ * grid_tree_plan writes it, or any other bits; NULL: all j <= i).  A token that
+ * sees nothing gets zeros (lse -inf).  A row of more than 32 n_words tokens gets
+ * zeros and GRID_ST_TREE.  Keys and values of all of the row's tokens must be
+ * finite, those that a token does not see too. */
+int grid_kv_attend_tree(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_kv_query* query, const uint32_t* d_sees,
+                        int32_t n_words, int32_t* d_status, void* stream);
+
+/* The path that the sampled tokens take: from token 0 on, to the first child
+ * whose token is the one that was sampled at its parent, up to a token without
+ * such a child or max_path tokens.  d_path[b][0 .. d_count[b]-1] are the path's
+ * tokens, as indices in the row, d_out[b][..] what was sampled at them: the
+ * accepted drafts, then the token that continues them; -1 after that
+ * (grid_advance takes d_out as it is).  A sampled `eos` (-1: none) ends the path
+ * and gives GRID_ST_COMPLETE; a negative sampled token ends it too.  A row of no
+ * tokens has an empty path; one out of order, too, and GRID_ST_TREE.
+ * d_path, d_out: [B][max_path]; 1 <= B <= 65535.  Enqueue only. */
+int grid_tree_accept(const grid_tree* tree, const int32_t* d_tokens, const int32_t* d_sampled, int32_t eos,
+                     int32_t max_path, int32_t* d_path, int32_t* d_count, int32_t* d_out, int32_t* d_status, void* stream);
+
+/* The path's keys and values next to what was cached before the chunk: position
+ * d_len[b] + j gets those of position d_len[b] + d_path[b][j], j < d_count[b]
+ * (the chunk as in the append).  A path that does not rise from token to token,
+ * or leaves the chunk, gives GRID_ST_TREE, a bad row or page GRID_ST_PAGES; such
+ * a row is left as it was.  Enqueue only. */
+int grid_kv_compact(const grid_kv* kv, const grid_kv_chunk* chunk, const int32_t* d_path, const int32_t* d_count,
+                    int32_t max_path, int32_t* d_status, void* stream);
+
+/* ---- the pages of a cache ----
+ * What a batch's rows hold of a pool of pages is its table and, per row, how
+ * many tokens are cached.  grid_pages_update makes the next step's table from
+ * the present one: new row b continues old row d_parent[b] (NULL: b; -1: it
+ * begins anew) with the first d_keep[b] of its tokens (NULL: all that it holds;
+ * ignored for -1) and gets pages for d_want[b] >= d_keep[b] tokens.  Several new
+ * rows may continue one old row (forks), tokens that are not kept give their
+ * pages back, and an old row that none continues gives back all.
+ *
+ * Pages that are kept whole are shared.  A page that is kept in part stays with
+ * the lowest-numbered new row that keeps it so, where no row keeps it whole and
+ * it is not pinned; any other row gets a fresh page for it and an entry of
+ * d_copies (grid_kv_copy then copies what is kept of it, in each layer's
+ * cache).  Fresh pages are the lowest-numbered ones that no new row keeps and
+ * that are not pinned, given out in the order of the rows.  From the first row
+ * on whose pages are not there, rows that need any get none: such a row has
+ * GRID_ST_PAGES and keeps its whole pages, and the one in part if that stayed
+ * (d_held_out says how many tokens).  A row whose table has no room for d_want
+ * is treated the same, but those after it get theirs.  A row whose parent, keep,
+ * want or kept pages are not valid keeps nothing, with GRID_ST_PAGES.
+ *
+ * d_refs[p] is the number of times that page p is in the new table.  Pinned
+ * pages (d_pinned[p] != 0: held by someone else, a prefix store, say) are not
+ * given out. */
+typedef struct grid_pages_step {
+  const int32_t* d_table;  /* A rows of `width` pages, table_stride apart              */
+  int64_t table_stride;
+  const int32_t* d_held;   /* [A] tokens cached per old row                            */
+  const int32_t *d_parent, *d_keep; /* [B] or NULL (d_parent NULL: B <= A)             */
+  const int32_t* d_want;   /* [B]                                                      */
+  const int32_t* d_pinned; /* [n_pages] or NULL                                        */
+  int32_t A, width, B, width_out;
+  int32_t* d_table_out;    /* out: B rows of width_out pages, table_out_stride apart,  */
+  int64_t table_out_stride; /* -1 past a row's own; not the old table                  */
+  int32_t* d_held_out;     /* out [B]: d_want where the pages are there; not d_held     */
+  int32_t* d_copies;       /* out [3][B]: from page, to page (-1: none), tokens        */
+  int32_t* d_refs;         /* out [n_pages]                                            */
+  int32_t* d_status;       /* out [B]                                                  */
+} grid_pages_step;
+
+/* Scratch for updates over a pool of n_pages pages of page_size tokens (a power
+ * of two in 8 .. 1024).  Allocates device memory and synchronizes.  Free with
+ * grid_pages_free. */
+int grid_pages_create(int32_t n_pages, int32_t page_size, grid_pages** out);
+void grid_pages_free(grid_pages* p);
+
+/* Uses the scratch held by `p`, so updates on the same handle must not overlap
+ * on the GPU.  1 <= A, B <= 65535.  Enqueue only. */
+int grid_pages_update(const grid_pages* p, const grid_pages_step* step, void* stream);
+
+/* Copy pages within a cache: the first d_copies[2n + i] tokens of page
+ * d_copies[i] to page d_copies[n + i], i < n; none where the former is negative.
+ * A page that is copied to must not be copied from, nor to twice.  d_status[i]:
+ * GRID_ST_PAGES where an id is outside the cache or the tokens are more than a
+ * page's (nothing is copied).  1 <= n <= 65535.  Enqueue only. */
+int grid_kv_copy(const grid_kv* kv, const int32_t* d_copies, int32_t n, int32_t* d_status, void* stream);
 
 #ifdef __cplusplus
 }

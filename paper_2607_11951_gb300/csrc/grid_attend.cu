@@ -83,6 +83,8 @@ struct AttendArgs {
   float2* part_ml;  // [2 blocks][256 rows]: maximum (in exponents of two) and sum (2^kLift times it, as the parts are)
   int* joined;      // [blocks]
   int* gave_up;     // one word: a wait ran out, in this call or an earlier one
+  const uint32_t* sees;  // of a tree: a token's words, a bit for each of its row's tokens that it sees
+  int words;
 };
 
 // ---------------------------------------------------------------------------
@@ -236,13 +238,42 @@ __device__ __forceinline__ void hide32(uint32_t (&x)[32], int last) {  // scores
   }
 }
 
+// What hides the keys that a query row does not see: h(x, j) hides among the scores of the tile's keys j .. j + 31.
+struct HideLater {
+  int last;  // the tile's last visible key
+  __device__ __forceinline__ void operator()(uint32_t (&x)[32], int j) const { hide32(x, last - j); }
+};
+// Of a tree: what is cached is seen, of the chunk's tokens up to the row's own those whose bit is set.  The bits are read
+// from memory where they are used (registers are short; few tiles hold tokens of the chunk).
+struct HideTree {
+  const uint32_t* words;  // of the row's token
+  int n_words, t;         // t: which token of the chunk it is
+  int first;              // the tile's first key, as a token of the chunk (negative: cached)
+  __device__ __forceinline__ void operator()(uint32_t (&x)[32], int j) const {
+    const int d = first + j;
+    if (d <= -32) return;
+    uint32_t bits = 0;
+    if (d <= t) {
+      const int w = d >> 5;  // (-1: all cached)
+      const uint32_t lo = w < 0 ? ~0u : words[w], hi = w + 1 < n_words ? words[w + 1] : 0u;
+      bits = __funnelshift_r(lo, hi, d & 31);
+      if (t - d < 31) bits &= (2u << (t - d)) - 1u;
+    }
+    if (bits != ~0u) {
+#pragma unroll
+      for (int e = 0; e < 32; ++e)
+        if (!(bits >> e & 1u)) x[e] = 0xFF800000u;
+    }
+  }
+};
+
 // One tile of a row's softmax from nothing: the maximum, base(maximum), then
 // the probabilities, from the last keys to the first: they lie (64-wide heads
 // apart) over the second half of the scores, which is read before.  Returns their
 // sum.  The scores are read from tensor memory twice, the loops are rolled: few
 // tiles come here, and those of short calls wait for instructions.
-template <typename T, typename Base>
-__device__ __forceinline__ float softmax_anew(uint32_t s_at, uint32_t p_at, int last, float sc, Base base) {
+template <typename T, typename Hide, typename Base>
+__device__ __forceinline__ float softmax_anew(uint32_t s_at, uint32_t p_at, const Hide& hide, float sc, Base base) {
   Two sum[2] = {};
   float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
   uint32_t x[32];
@@ -250,7 +281,7 @@ __device__ __forceinline__ float softmax_anew(uint32_t s_at, uint32_t p_at, int 
   for (int j = 0; j < kTile; j += 32) {
     tm_load32(s_at + j, x);
     tm_loaded(x);
-    hide32(x, last - j);
+    hide(x, j);
     max32(x, top);
   }
   const float b = base(fmaxf(max3(top[0], top[1], top[2]), top[3]));
@@ -258,7 +289,7 @@ __device__ __forceinline__ float softmax_anew(uint32_t s_at, uint32_t p_at, int 
   for (int j = kTile - 32; j >= 0; j -= 32) {
     tm_load32(s_at + j, x);
     tm_loaded(x);
-    hide32(x, last - j);
+    hide(x, j);
     exp32<T>(x, sc, b, sum);
     tm_store16(p_at + j / 2, x);
   }
@@ -268,26 +299,26 @@ __device__ __forceinline__ float softmax_anew(uint32_t s_at, uint32_t p_at, int 
 // The same for many tiles, with loads on their way while the columns before
 // are worked on; the last 64 scores are read once.  half() is called once the
 // probabilities of the last 64 keys are there.
-template <typename T, typename Base, typename Half>
-__device__ __forceinline__ float softmax_twice(uint32_t s_at, uint32_t p_at, int last, float sc, Base base, Half half) {
+template <typename T, typename Hide, typename Base, typename Half>
+__device__ __forceinline__ float softmax_twice(uint32_t s_at, uint32_t p_at, const Hide& hide, float sc, Base base, Half half) {
   Two sum[2] = {};
   float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
   uint32_t x[32], y[32];
   tm_load32(s_at, x);
   tm_loaded(x);
   tm_load32(s_at + 32, y);
-  hide32(x, last);
+  hide(x, 0);
   max32(x, top);
   tm_loaded(y);
   tm_load32(s_at + 64, x);
-  hide32(y, last - 32);
+  hide(y, 32);
   max32(y, top);
   tm_loaded(x);
   tm_load32(s_at + 96, y);
-  hide32(x, last - 64);
+  hide(x, 64);
   max32(x, top);
   tm_loaded(y);
-  hide32(y, last - 96);
+  hide(y, 96);
   max32(y, top);
   const float b = base(fmaxf(max3(top[0], top[1], top[2]), top[3]));
   exp32<T>(y, sc, b, sum);
@@ -298,11 +329,11 @@ __device__ __forceinline__ float softmax_twice(uint32_t s_at, uint32_t p_at, int
   half();
   tm_loaded(y);
   tm_load32(s_at, x);
-  hide32(y, last - 32);
+  hide(y, 32);
   exp32<T>(y, sc, b, sum);
   tm_store16(p_at + 16, y);
   tm_loaded(x);
-  hide32(x, last);
+  hide(x, 0);
   exp32<T>(x, sc, b, sum);
   tm_store16(p_at, x);
   sum[0] = add2(sum[0], sum[1]);
@@ -312,8 +343,8 @@ __device__ __forceinline__ float softmax_twice(uint32_t s_at, uint32_t p_at, int
 // probabilities have columns of their own.  `top` gets the tile's own maximum; if
 // it turns out to be too far above b, the scores are as they were and the
 // result is of no use.
-template <typename T>
-__device__ __forceinline__ float softmax_once(uint32_t s_at, uint32_t p_at, int last, float sc, float b, float& top) {
+template <typename T, typename Hide>
+__device__ __forceinline__ float softmax_once(uint32_t s_at, uint32_t p_at, const Hide& hide, float sc, float b, float& top) {
   Two sum[2] = {};
   float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
   uint32_t x[2][32];
@@ -323,7 +354,7 @@ __device__ __forceinline__ float softmax_once(uint32_t s_at, uint32_t p_at, int 
     uint32_t(&y)[32] = x[j & 1];
     tm_loaded(y);
     if (j < 3) tm_load32(s_at + 32 * (j + 1), x[(j + 1) & 1]);
-    hide32(y, last - 32 * j);
+    hide(y, 32 * j);
     max32(y, tops);
     exp32<T>(y, sc, b, sum);
     tm_store16(p_at + 16 * j, y);
@@ -478,7 +509,7 @@ __device__ __noinline__ void report_again(int* gave_up, int32_t* status, int B) 
     for (int b = blockIdx.x; b < B; b += gridDim.x) status[b] = GRID_ST_BOUND;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kTree>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attend(const AttendArgs g, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using L = Layout<D>;
@@ -696,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (good && n)
         for (int p = lane; p <= (len + n - 1) >> c.log_page; p += 32) good = good && page_of(c, b, p << c.log_page) >= 0;
       good = __all_sync(~0u, good);
-      if (lane == 0) g.status[b] = good ? GRID_ST_OK : GRID_ST_PAGES;
+      if (lane == 0) g.status[b] = good ? GRID_ST_OK : n > c.max_n ? GRID_ST_TREE : GRID_ST_PAGES;
       if (!ordered) {
         const int from = max(0, a), to = (int)min((long long)c.N, (long long)a + n);
         for (long long i = (long long)from * g.H; i < (long long)to * g.H; ++i) {
@@ -882,7 +913,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (warp_live) {
           tm_after();
           const int tile = p.wide ? p.t0 + i : p.t0 + 2 * i + s;
-          const int last = sees - tile * kTile;  // the tile's last visible key
+          auto hide = [&]() {
+            if constexpr (kTree)
+              return HideTree{g.sees + (long long)(w.a + t) * g.words, g.words, t, tile * kTile - w.len};
+            else
+              return HideLater{sees - tile * kTile};
+          }();
           auto base = [&](float top) {
             const float now = top * sc;
             // The maximum is moved only where it grew by more than 8 (the probabilities stay below 2^8, or 2^15 in
@@ -909,19 +945,19 @@ __global__ void __launch_bounds__(kThreads, 1)
           if constexpr (L::kApart) {
             bool fits = false;
             if (p.wide && i > 0) {
-              added = softmax_once<T>(s_at, p_at, last, sc, (m > -INFINITY ? m : 0.f) - kLift<T>, top);
+              added = softmax_once<T>(s_at, p_at, hide, sc, (m > -INFINITY ? m : 0.f) - kLift<T>, top);
               fits = !__any_sync(~0u, live && top * sc - m > 8.f);
             }
-            if (!fits) added = softmax_anew<T>(s_at, p_at, last, sc, base);
+            if (!fits) added = softmax_anew<T>(s_at, p_at, hide, sc, base);
           } else {
-            added = p.wide ? softmax_twice<T>(s_at, p_at, last, sc, base,
+            added = p.wide ? softmax_twice<T>(s_at, p_at, hide, sc, base,
                                               [&]() {
                                                 tm_stored();
                                                 tm_before();
                                                 __syncwarp();
                                                 if (lane == 0) bar_arrive(&sh.p_half[s]);
                                               })
-                           : softmax_anew<T>(s_at, p_at, last, sc, base);
+                           : softmax_anew<T>(s_at, p_at, hide, sc, base);
           }
           l += added;
           tm_stored();
@@ -957,7 +993,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++n_o[z];
         }
       if (!ok) break;
-      // A sum below zero: some key that the rows may read is in no page of the cache (known once all tiles were), and they
+      // A sum of zero: the row sees no key, and gets zeros.  A sum below zero: some key that the rows may read is in no page of the cache (known once all tiles were), and they
       // get zeros.  A sum that is no number, of a query that is none, gives NaN.
       if (sh.bad[0][k % kRing] | sh.bad[1][k % kRing]) l = -1.f;
       if (warp_live) {
@@ -981,7 +1017,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int e = 0; e < 16; ++e) y[e] = __uint_as_float(o[e]) * f0;
           }
           if (live && whole) {
-            const uint4 none = {}, a = l < 0.f ? none : pack8<T>(y), b = l < 0.f ? none : pack8<T>(y + 8);
+            const uint4 none = {}, a = l <= 0.f ? none : pack8<T>(y), b = l <= 0.f ? none : pack8<T>(y + 8);
             if (g.sectors) {
               asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + j), "r"(a.x), "r"(a.y), "r"(a.z),
                            "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
@@ -999,7 +1035,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (live && (p.wide || s == 0)) {
           if (whole) {
-            if (g.lse) g.lse[(long long)(w.a + t) * g.H + head] = l < 0.f ? -INFINITY : (m - kLift<T> + log2f(l)) * kLn2;
+            if (g.lse) g.lse[(long long)(w.a + t) * g.H + head] = l <= 0.f ? -INFINITY : (m - kLift<T> + log2f(l)) * kLn2;
           } else {
             __stcg(g.part_ml + (size_t)slot * 256 + part_row, make_float2(m, l));
           }
@@ -1070,6 +1106,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                   }
                 }
               }
+              bad |= z == 0.f;
               const float by = __frcp_rn(z);
 #pragma unroll
               for (int e = 0; e < kN; ++e) acc[e] = bad ? 0.f : acc[e] * by;
@@ -1124,10 +1161,12 @@ int make_map(const grid_kv_pages& p, void* pool, const int64_t* stride, CUtensor
 template <typename F>
 cudaError_t each_kernel(F f) {
   cudaError_t e;
-  if ((e = f(k_attend<__nv_bfloat16, 64>, smem_bytes<64>())) || (e = f(k_attend<__nv_bfloat16, 128>, smem_bytes<128>())) ||
-      (e = f(k_attend<__half, 64>, smem_bytes<64>())))
+  if ((e = f(k_attend<__nv_bfloat16, 64, false>, smem_bytes<64>())) || (e = f(k_attend<__nv_bfloat16, 128, false>, smem_bytes<128>())) ||
+      (e = f(k_attend<__half, 64, false>, smem_bytes<64>())) || (e = f(k_attend<__half, 128, false>, smem_bytes<128>())) ||
+      (e = f(k_attend<__nv_bfloat16, 64, true>, smem_bytes<64>())) || (e = f(k_attend<__nv_bfloat16, 128, true>, smem_bytes<128>())) ||
+      (e = f(k_attend<__half, 64, true>, smem_bytes<64>())))
     return e;
-  return f(k_attend<__half, 128>, smem_bytes<128>());
+  return f(k_attend<__half, 128, true>, smem_bytes<128>());
 }
 
 }  // namespace
@@ -1184,20 +1223,21 @@ extern "C" void grid_kv_free(grid_kv* kv) {
   delete kv;
 }
 
-extern "C" int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_kv_query* query,
-                              int32_t* d_status, void* stream) {
+static int attend(const char* name, const grid_kv* kv, const grid_kv_chunk* chunk, const grid_kv_query* query,
+                  const uint32_t* d_sees, int32_t n_words, int32_t* d_status, void* stream) {
+  auto refuse = [&](int code, const char* why) { return set_error(code, std::string(name) + ": " + why); };
   AttendArgs a = {};
   if (!kv || !query || !d_status || !make_chunk(kv, chunk, a.c) ||
       (chunk->n_tokens && (!heads_ok(&query->q) || !heads_ok(&query->out))) || !std::isfinite(query->scale) ||
       !(query->scale > 0.f) || (uintptr_t)query->d_lse % 4)
-    return set_error(GRID_E_INVALID_ARG, "grid_kv_attend: bad arguments");
-  if (chunk->B > 65535) return set_error(GRID_E_TOO_LARGE, "grid_kv_attend: more than 65535 rows");
+    return refuse(GRID_E_INVALID_ARG, "bad arguments");
+  if (chunk->B > 65535) return refuse(GRID_E_TOO_LARGE, "more than 65535 rows");
   const grid_kv_pages& p = kv->p;
   // (more than two billion tiles of 256 query rows by 128 keys would take minutes)
   const double units = (double)chunk->n_tokens * (p.n_heads / p.n_kv_heads) / 256 + chunk->B;
   if ((double)chunk->n_tokens * (p.n_heads / p.n_kv_heads) > INT32_MAX - 256 ||
       units * p.n_kv_heads * (((double)chunk->max_pages * p.page_size) / kTile + 1 + kUnitCost) > kMostCost)
-    return set_error(GRID_E_TOO_LARGE, "grid_kv_attend: too many query rows or key tiles in one call");
+    return refuse(GRID_E_TOO_LARGE, "too many query rows or key tiles in one call");
   a.q = query->q.d, a.out = query->out.d, a.lse = query->d_lse;
   a.qs[0] = query->q.token_stride, a.qs[1] = query->q.head_stride;
   a.os[0] = query->out.token_stride, a.os[1] = query->out.head_stride;
@@ -1207,11 +1247,32 @@ extern "C" int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, con
   auto go = [&](auto kern, size_t smem) {
     return launch_pdl(kern, dim3(kv->sms), dim3(kThreads), smem, (cudaStream_t)stream, a, kv->k_map, kv->v_map);
   };
-  if (p.dtype == GRID_DTYPE_BF16)
-    GRID_CUDA(p.head_dim == 64 ? go(k_attend<__nv_bfloat16, 64>, smem_bytes<64>())
-                               : go(k_attend<__nv_bfloat16, 128>, smem_bytes<128>()));
-  else
-    GRID_CUDA(p.head_dim == 64 ? go(k_attend<__half, 64>, smem_bytes<64>()) : go(k_attend<__half, 128>, smem_bytes<128>()));
+  auto launch = [&](auto tree) {
+    constexpr bool kTree = decltype(tree)::value;
+    if (p.dtype == GRID_DTYPE_BF16)
+      return p.head_dim == 64 ? go(k_attend<__nv_bfloat16, 64, kTree>, smem_bytes<64>())
+                              : go(k_attend<__nv_bfloat16, 128, kTree>, smem_bytes<128>());
+    return p.head_dim == 64 ? go(k_attend<__half, 64, kTree>, smem_bytes<64>()) : go(k_attend<__half, 128, kTree>, smem_bytes<128>());
+  };
+  if (d_sees) {
+    a.sees = d_sees, a.words = n_words;
+    a.c.max_n = (int)std::min<int64_t>(INT32_MAX, 32LL * n_words);
+    GRID_CUDA(launch(std::true_type()));
+  } else {
+    GRID_CUDA(launch(std::false_type()));
+  }
   GRID_CUDA(cudaGetLastError());
   return GRID_OK;
+}
+
+extern "C" int grid_kv_attend(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_kv_query* query, int32_t* d_status,
+                              void* stream) {
+  return attend("grid_kv_attend", kv, chunk, query, nullptr, 0, d_status, stream);
+}
+
+extern "C" int grid_kv_attend_tree(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_kv_query* query,
+                                   const uint32_t* d_sees, int32_t n_words, int32_t* d_status, void* stream) {
+  if (d_sees && (n_words <= 0 || (uintptr_t)d_sees % 4))
+    return set_error(GRID_E_INVALID_ARG, "grid_kv_attend_tree: bad words");
+  return attend("grid_kv_attend_tree", kv, chunk, query, d_sees, n_words, d_status, stream);
 }

@@ -35,6 +35,7 @@ struct AppendArgs {
   int H, Hk, rot, pairs, n_pos;
   int groups[3];            // up to the last one of the queries, of the keys, of the values
   int splits;               // warps that a token's groups go to
+  const int32_t* depth;     // of the tokens in their trees, or NULL: their order in the row
   int32_t* status;
 };
 
@@ -50,7 +51,9 @@ __global__ void __launch_bounds__(kAppendWarps * 32, D == 128 ? 6 : 8) k_append(
     const int b = ((int)blockIdx.x - token_blocks) * kAppendWarps + warp;
     if (b >= c.B) return;
     int s, n, len;
-    bool ok = row_span(c, b, s, n, len) && (!a.cos || n == 0 || len + n <= a.n_pos);
+    bool ok = row_span(c, b, s, n, len) && (!a.cos || a.depth || n == 0 || len + n <= a.n_pos);
+    if (ok && a.cos && a.depth)
+      for (int i = lane; i < n; i += 32) ok = ok && a.depth[s + i] >= 0 && a.depth[s + i] < a.n_pos - len;
     if (ok && n)
       for (int p = (len >> c.log_page) + lane; p <= (len + n - 1) >> c.log_page; p += 32)
         ok = ok && page_of(c, b, p << c.log_page) >= 0;
@@ -81,12 +84,14 @@ __global__ void __launch_bounds__(kAppendWarps * 32, D == 128 ? 6 : 8) k_append(
   };
   uint4 ahead[kUnroll] = {};
   fetch(split, ahead);
+  const int deep = a.depth ? a.depth[i] : 0;
   const int b = row_of(c, i, lane);
   if (b < 0) return;
   int s, n, len;
   if (!row_span(c, b, s, n, len)) return;
   const int pos = len + i - s;
-  if (a.cos && pos >= a.n_pos) return;
+  const int turn = a.depth ? len + deep : pos;  // whose angles
+  if (a.cos && (deep < 0 || (a.depth ? deep >= a.n_pos - len : pos >= a.n_pos))) return;
   const int page = page_of(c, b, pos);
   if (page < 0) return;
   const int off = pos & ((1 << c.log_page) - 1);
@@ -124,8 +129,8 @@ __global__ void __launch_bounds__(kAppendWarps * 32, D == 128 ? 6 : 8) k_append(
         unpack8<T>(make_uint4(x.x, x.y, y.x, y.y), wt);
       }
       if (turned) {
-        const float4 x = *reinterpret_cast<const float4*>(a.cos + (long long)pos * half + angle);
-        const float4 y = *reinterpret_cast<const float4*>(a.sin + (long long)pos * half + angle);
+        const float4 x = *reinterpret_cast<const float4*>(a.cos + (long long)turn * half + angle);
+        const float4 y = *reinterpret_cast<const float4*>(a.sin + (long long)turn * half + angle);
         c4[0] = x.x, c4[1] = x.y, c4[2] = x.z, c4[3] = x.w;
         s4[0] = y.x, s4[1] = y.y, s4[2] = y.z, s4[3] = y.w;
       }
@@ -176,19 +181,20 @@ __global__ void __launch_bounds__(kAppendWarps * 32, D == 128 ? 6 : 8) k_append(
 
 using namespace grid;
 
-extern "C" int grid_kv_append(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_heads* k, const grid_heads* v,
-                              const grid_heads* q, const grid_heads* q_out, const grid_rotation* rot,
-                              const grid_head_norm* norm, int32_t* d_status, void* stream) {
+static int append(const char* name, const grid_kv* kv, const grid_kv_chunk* chunk, const grid_heads* k, const grid_heads* v,
+                  const grid_heads* q, const grid_heads* q_out, const grid_rotation* rot, const grid_head_norm* norm,
+                  const int32_t* d_depth, int32_t* d_status, void* stream) {
+  auto refuse = [&](int code, const char* why) { return set_error(code, std::string(name) + ": " + why); };
   AppendArgs a = {};
   if (!kv || !d_status || !make_chunk(kv, chunk, a.c) || (chunk->n_tokens && (!heads_ok(k) || !heads_ok(v))) ||
       (q != nullptr) != (q_out != nullptr) || (q && chunk->n_tokens && (!heads_ok(q) || !heads_ok(q_out))))
-    return set_error(GRID_E_INVALID_ARG, "grid_kv_append: bad arguments");
+    return refuse(GRID_E_INVALID_ARG, "bad arguments");
   if (rot && (!rot->d_cos || !rot->d_sin || (uintptr_t)rot->d_cos % 16 || (uintptr_t)rot->d_sin % 16 ||
               rot->n_pos <= 0 || rot->rot <= 0 || rot->rot % 16 || rot->rot > kv->p.head_dim))
-    return set_error(GRID_E_INVALID_ARG, "grid_kv_append: bad rotation (rot is a multiple of 16 up to head_dim)");
+    return refuse(GRID_E_INVALID_ARG, "bad rotation (rot is a multiple of 16 up to head_dim)");
   if (norm && ((uintptr_t)norm->d_q % 16 || (uintptr_t)norm->d_k % 16 || !(norm->eps >= 0.f)))
-    return set_error(GRID_E_INVALID_ARG, "grid_kv_append: bad norm");
-  if (chunk->B > 65535) return set_error(GRID_E_TOO_LARGE, "grid_kv_append: more than 65535 rows");
+    return refuse(GRID_E_INVALID_ARG, "bad norm");
+  if (chunk->B > 65535) return refuse(GRID_E_TOO_LARGE, "more than 65535 rows");
   const grid_kv_pages& p = kv->p;
   auto heads = [&](int kind, const grid_heads* h, int count) {
     if (chunk->n_tokens && h) a.src[kind] = h->d, a.ss[kind][0] = h->token_stride, a.ss[kind][1] = h->head_stride;
@@ -203,12 +209,12 @@ extern "C" int grid_kv_append(const grid_kv* kv, const grid_kv_chunk* chunk, con
   if (rot) a.cos = rot->d_cos, a.sin = rot->d_sin, a.rot = rot->rot, a.pairs = rot->pairs, a.n_pos = rot->n_pos;
   if (norm) a.w[0] = norm->d_q, a.w[1] = norm->d_k, a.eps = norm->eps;
   a.H = p.n_heads, a.Hk = p.n_kv_heads;
-  a.status = d_status;
+  a.status = d_status, a.depth = d_depth;
   // (whole tokens where their warps fill the SMs anyway)
   a.splits = std::max(1, std::min(a.groups[2], 32 * kv->sms / std::max(1, chunk->n_tokens)));
   const long long blocks = ((long long)chunk->n_tokens * a.splits + kAppendWarps - 1) / kAppendWarps;
   const int rows = (chunk->B + kAppendWarps - 1) / kAppendWarps;
-  if (blocks + rows > INT32_MAX) return set_error(GRID_E_TOO_LARGE, "grid_kv_append: too many head vectors in one call");
+  if (blocks + rows > INT32_MAX) return refuse(GRID_E_TOO_LARGE, "too many head vectors in one call");
   auto go = [&](auto kern) {
     return launch_pdl(kern, dim3((unsigned)(blocks + rows)), dim3(kAppendWarps * 32), 0, (cudaStream_t)stream, a, (int)blocks);
   };
@@ -218,4 +224,16 @@ extern "C" int grid_kv_append(const grid_kv* kv, const grid_kv_chunk* chunk, con
     GRID_CUDA(p.head_dim == 64 ? go(k_append<__half, 64>) : go(k_append<__half, 128>));
   GRID_CUDA(cudaGetLastError());
   return GRID_OK;
+}
+
+extern "C" int grid_kv_append(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_heads* k, const grid_heads* v,
+                              const grid_heads* q, const grid_heads* q_out, const grid_rotation* rot,
+                              const grid_head_norm* norm, int32_t* d_status, void* stream) {
+  return append("grid_kv_append", kv, chunk, k, v, q, q_out, rot, norm, nullptr, d_status, stream);
+}
+
+extern "C" int grid_kv_append_tree(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_heads* k, const grid_heads* v,
+                                   const grid_heads* q, const grid_heads* q_out, const grid_rotation* rot,
+                                   const grid_head_norm* norm, const int32_t* d_depth, int32_t* d_status, void* stream) {
+  return append("grid_kv_append_tree", kv, chunk, k, v, q, q_out, rot, norm, d_depth, d_status, stream);
 }

@@ -17,6 +17,7 @@ struct Chunk {  // grid_kv_chunk with the cache's geometry
   const int32_t* start;
   long long table_stride;
   int max_pages, B, N, n_pages, log_page, T;  // T: tokens of every row where start is NULL
+  int max_n;  // the most tokens of a row
 };
 
 // Row b's tokens [a, a + n) and its first position; false where they are not in order.
@@ -25,7 +26,7 @@ __device__ __forceinline__ bool row_span(const Chunk& c, int b, int& a, int& n, 
   const int z = c.start ? c.start[b + 1] : a + c.T;
   len = c.len[b];
   n = z - a;
-  return a >= 0 && z >= a && z <= c.N && len >= 0 && (long long)len + n <= (long long)c.max_pages << c.log_page;
+  return a >= 0 && z >= a && z <= c.N && n <= c.max_n && len >= 0 && (long long)len + n <= (long long)c.max_pages << c.log_page;
 }
 
 // The row of token i, or -1: the last b with start[b] <= i, by a warp (each
@@ -102,6 +103,6 @@ inline bool make_chunk(const grid_kv* kv, const grid_kv_chunk* ch, grid::Chunk& 
       (!ch->d_start && ch->n_tokens % ch->B))
     return false;
   c = grid::Chunk{ch->d_table, ch->d_len, ch->d_start, ch->table_stride, ch->max_pages, ch->B, ch->n_tokens,
-            kv->p.n_pages, kv->log_page, ch->n_tokens / ch->B};
+            kv->p.n_pages, kv->log_page, ch->n_tokens / ch->B, INT32_MAX};
   return true;
 }

@@ -17,9 +17,9 @@ from .build import library_path
 
 GRID_OK = 0
 GRID_ST = {0: "OK", 1: "NONVIABLE", 2: "STACK_OVERFLOW", 3: "TOKEN_NOT_ALLOWED",
-           4: "EMPTY_MASK", 5: "BOUND", 6: "COMPLETE", 7: "PAGES"}
+           4: "EMPTY_MASK", 5: "BOUND", 6: "COMPLETE", 7: "PAGES", 8: "TREE"}
 GRID_ST_OK, GRID_ST_NONVIABLE, GRID_ST_STACK_OVERFLOW, GRID_ST_TOKEN_NOT_ALLOWED = 0, 1, 2, 3
-GRID_ST_EMPTY_MASK, GRID_ST_BOUND, GRID_ST_COMPLETE, GRID_ST_PAGES = 4, 5, 6, 7
+GRID_ST_EMPTY_MASK, GRID_ST_BOUND, GRID_ST_COMPLETE, GRID_ST_PAGES, GRID_ST_TREE = 4, 5, 6, 7, 8
 GRID_DTYPE_F32, GRID_DTYPE_BF16, GRID_DTYPE_F16 = 0, 1, 2
 
 EXPORTED = ["grid_last_error", "grid_compile", "grid_grammar_free", "grid_grammar_info", "grid_grammar_lexicon_trie",
@@ -29,7 +29,9 @@ EXPORTED = ["grid_last_error", "grid_compile", "grid_grammar_free", "grid_gramma
             "grid_reserve", "grid_cache_create", "grid_cache_free", "grid_cache_clear", "grid_cache_stats",
             "grid_masks_cached", "grid_configs_enable_audit", "grid_audit_append", "grid_audit_seal", "grid_audit_head", "grid_audit_verify",
             "grid_audit_genesis", "grid_blake2b", "grid_fingerprint", "grid_apply_mask", "grid_configs_export",
-            "grid_kv_create", "grid_kv_append", "grid_kv_attend", "grid_drafts_create", "grid_draft_verify"]
+            "grid_kv_create", "grid_kv_append", "grid_kv_attend", "grid_drafts_create", "grid_draft_verify",
+            "grid_tree_plan", "grid_kv_append_tree", "grid_kv_attend_tree", "grid_tree_accept", "grid_kv_compact",
+            "grid_pages_create", "grid_pages_update", "grid_kv_copy"]
 
 
 class GridLibraryMissing(RuntimeError):
@@ -121,6 +123,15 @@ def lib():
         "grid_drafts_create": (I32, [I32, I32, I32, ctypes.POINTER(P)]),
         "grid_drafts_free": (None, [P]),
         "grid_draft_verify": (I32, [P, P, P]),
+        "grid_tree_plan": (I32, [P, P, P, I32, P, P]),
+        "grid_kv_append_tree": (I32, [P, P, P, P, P, P, P, P, P, P, P]),
+        "grid_kv_attend_tree": (I32, [P, P, P, P, I32, P, P]),
+        "grid_tree_accept": (I32, [P, P, P, I32, I32, P, P, P, P, P]),
+        "grid_kv_compact": (I32, [P, P, P, P, I32, P, P]),
+        "grid_pages_create": (I32, [I32, I32, ctypes.POINTER(P)]),
+        "grid_pages_free": (None, [P]),
+        "grid_pages_update": (I32, [P, P, P]),
+        "grid_kv_copy": (I32, [P, P, I32, P, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -535,6 +546,13 @@ def grid_configs_export(cfg, row: int, cap: int = 1 << 16):
 # The structures of include/grid.h that calls fill: packed by struct, which takes half the time of ctypes (padding included).
 _HEADS, _CHUNK, _ROTATION, _NORM = struct.Struct("Pqq"), struct.Struct("PqPPiiii"), struct.Struct("PPiiii"), struct.Struct("PPfi")
 _QUERY, _STEP = struct.Struct("PqqPqqPfi"), struct.Struct("PqqPqqPqqPPPPqPiiiiiiPPPP")
+_TREE, _PAGES = struct.Struct("PPii"), struct.Struct("PqPPPPPiiiiPqPPPP")
+
+
+def _dense(x, dtype, *shape):
+    assert x.dtype is dtype and x.is_cuda and x.shape == shape and x.is_contiguous(), \
+        "contiguous %s CUDA tensor %s expected" % (dtype, list(shape))
+    return x.data_ptr()
 
 
 def _heads(x, kv, N, H):
@@ -561,12 +579,13 @@ def _chunk(kv, table, lens, start, status, N):
 
 
 def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None, cos=None, sin=None, pairs=False,
-                   q_norm=None, k_norm=None, eps=1e-6, stream=None):
+                   q_norm=None, k_norm=None, eps=1e-6, depth=None, stream=None):
     """Store a chunk's keys and values in the paged cache ``kv`` (a PagedKV).
     k, v [tokens, kv heads, D] (slices of a projection's output, say); table
     int32 [B, max_pages], lens int32 [B] (tokens cached before the chunk),
     start int32 [B + 1] (None: the same number of tokens per row); q and q_out
-    [tokens, heads, D]; cos, sin float32 [positions, rot / 2]; norm weights [D]."""
+    [tokens, heads, D]; cos, sin float32 [positions, rot / 2]; norm weights [D].
+    depth int32 [tokens]: the chunk is a tree, a token is turned by its depth in it."""
     N = k.shape[0]
     chunk = _chunk(kv, table, lens, start, status, N)
     kh, vh = _HEADS.pack(*_heads(k, kv, N, kv.kv_heads)), _HEADS.pack(*_heads(v, kv, N, kv.kv_heads))
@@ -586,13 +605,18 @@ def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None
             assert w is None or (w.is_cuda and w.dtype is kv.dtype and w.shape == (kv.D,) and w.is_contiguous()), \
                 "norm weights [D] of the cache's type expected"
         norm = _NORM.pack(0 if q_norm is None else q_norm.data_ptr(), 0 if k_norm is None else k_norm.data_ptr(), eps, 0)
-    _check(lib().grid_kv_append(kv.h, chunk, kh, vh, qh, oh, rot, norm, status.data_ptr(), _stream(stream)))
+    if depth is None:
+        _check(lib().grid_kv_append(kv.h, chunk, kh, vh, qh, oh, rot, norm, status.data_ptr(), _stream(stream)))
+    else:
+        _check(lib().grid_kv_append_tree(kv.h, chunk, kh, vh, qh, oh, rot, norm, _dense(depth, kv.i32, N),
+                                         status.data_ptr(), _stream(stream)))
 
 
-def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=None, stream=None):
+def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=None, sees=None, stream=None):
     """Attention of a chunk over the paged cache, after its append (table, lens
     and start as there): q, out [tokens, heads, D], lse float32 [tokens, heads];
-    scale defaults to 1 / sqrt(D)."""
+    scale defaults to 1 / sqrt(D).  sees int32 [tokens, words]: the chunk is a tree,
+    a token sees those of the row's tokens whose bit is set (grid_tree_plan)."""
     N = q.shape[0]
     chunk = _chunk(kv, table, lens, start, status, N)
     if lse is not None:
@@ -600,7 +624,12 @@ def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=
             "float32 lse [tokens, heads] expected"
     query = _QUERY.pack(*_heads(q, kv, N, kv.heads), *_heads(out, kv, N, kv.heads), 0 if lse is None else lse.data_ptr(),
                         kv.D ** -0.5 if scale is None else scale, 0)
-    _check(lib().grid_kv_attend(kv.h, chunk, query, status.data_ptr(), _stream(stream)))
+    if sees is None:
+        _check(lib().grid_kv_attend(kv.h, chunk, query, status.data_ptr(), _stream(stream)))
+        return
+    assert sees.dtype is kv.i32 and sees.is_cuda and sees.is_contiguous() and sees.dim() == 2 and sees.shape[0] == N, \
+        "int32 sees [tokens, words] expected"
+    _check(lib().grid_kv_attend_tree(kv.h, chunk, query, sees.data_ptr(), sees.shape[1], status.data_ptr(), _stream(stream)))
 
 
 class PagedKV:
@@ -626,6 +655,98 @@ class PagedKV:
     def __del__(self):
         if getattr(self, "h", None) and _lib is not None:
             _lib.grid_kv_free(self.h)
+            self.h = None
+
+
+def _tree(parent, start, status, i32):
+    N, B = parent.shape[0], status.shape[0]
+    return _TREE.pack(_dense(parent, i32, N), 0 if start is None else _dense(start, i32, B + 1), B, N), N, B
+
+
+def grid_tree_plan(parent, depth, sees, status, start=None, stream=None):
+    """Depths and visibility of rows of drafted tokens: parent int32 [tokens] (an
+    earlier token of the row, by its index there, or -1), start int32 [B + 1]
+    (None: the same number of tokens per row).  Out: depth int32 [tokens], sees
+    int32 [tokens, words] (words >= a row's tokens / 32), status int32 [B]."""
+    import torch
+    i32 = torch.int32
+    tree, N, B = _tree(parent, start, status, i32)
+    assert sees.dim() == 2, "sees [tokens, words] expected"
+    words = sees.shape[1]
+    _check(lib().grid_tree_plan(tree, _dense(depth, i32, N), _dense(sees, i32, N, words), words, _dense(status, i32, B),
+                                _stream(stream)))
+
+
+def grid_tree_accept(parent, tokens, sampled, path, count, out, status, start=None, eos=-1, stream=None):
+    """The path that the sampled tokens take: parent, tokens (drafted) and sampled
+    int32 [tokens].  Out: path (indices in the row) and out (what was sampled
+    there) int32 [B, most], -1 past the end; count, status int32 [B]."""
+    import torch
+    i32 = torch.int32
+    tree, N, B = _tree(parent, start, status, i32)
+    assert path.dim() == 2, "path [B, most] expected"
+    most = path.shape[1]
+    _check(lib().grid_tree_accept(tree, _dense(tokens, i32, N), _dense(sampled, i32, N), eos, most,
+                                  _dense(path, i32, B, most), _dense(count, i32, B), _dense(out, i32, B, most),
+                                  _dense(status, i32, B), _stream(stream)))
+
+
+def grid_kv_compact(kv, table, lens, path, count, status, n_tokens, start=None, stream=None):
+    """The path's keys and values next to what was cached before the chunk (table,
+    lens, start and n_tokens as in its append; path and count of
+    grid_tree_accept)."""
+    i32 = kv.i32
+    chunk = _chunk(kv, table, lens, start, status, n_tokens)
+    B = lens.shape[0]
+    assert path.dim() == 2, "path [B, most] expected"
+    most = path.shape[1]
+    _check(lib().grid_kv_compact(kv.h, chunk, _dense(path, i32, B, most), _dense(count, i32, B), most, status.data_ptr(),
+                                 _stream(stream)))
+
+
+def grid_pages_update(pages, table, held, want, table_out, held_out, copies, refs, status, parent=None, keep=None,
+                      pinned=None, stream=None):
+    """The next table of a pool's rows: table int32 [A, width], held int32 [A];
+    want, parent (None: itself; -1: begins anew) and keep (None: all) int32 [B];
+    pinned int32 [pages].  Out: table_out int32 [B, width_out], held_out, status
+    int32 [B], copies int32 [3, B] (for grid_kv_copy), refs int32 [pages].
+    ``pages``: a Pages."""
+    i32 = pages.i32
+    A, B = held.shape[0], want.shape[0]
+    for x, n in ((table, A), (table_out, B)):
+        assert x.dtype is i32 and x.is_cuda and x.dim() == 2 and x.shape[0] == n and x.stride(1) == 1, \
+            "int32 CUDA tables [A, width] and [B, width_out] expected, their rows contiguous"
+    assert table.data_ptr() != table_out.data_ptr() and held.data_ptr() != held_out.data_ptr(), \
+        "the new table and lengths need tensors of their own"
+    step = _PAGES.pack(
+        table.data_ptr(), table.stride(0), _dense(held, i32, A), 0 if parent is None else _dense(parent, i32, B),
+        0 if keep is None else _dense(keep, i32, B), _dense(want, i32, B),
+        0 if pinned is None else _dense(pinned, i32, pages.n_pages), A, table.shape[1], B, table_out.shape[1],
+        table_out.data_ptr(), table_out.stride(0), _dense(held_out, i32, B), _dense(copies, i32, 3, B),
+        _dense(refs, i32, pages.n_pages), _dense(status, i32, B))
+    _check(lib().grid_pages_update(pages.h, step, _stream(stream)))
+
+
+def grid_kv_copy(kv, copies, status, stream=None):
+    """Copy pages of a cache: copies int32 [3, n] (from page or -1, to page, tokens
+    from its beginning), status int32 [n]."""
+    n = status.shape[0]
+    _check(lib().grid_kv_copy(kv.h, _dense(copies, kv.i32, 3, n), n, _dense(status, kv.i32, n), _stream(stream)))
+
+
+class Pages:
+    """Scratch for the updates of a pool of n_pages pages of page_size tokens."""
+
+    def __init__(self, n_pages: int, page_size: int):
+        import torch
+        self.i32, self.n_pages = torch.int32, n_pages
+        out = ctypes.c_void_p()
+        _check(lib().grid_pages_create(n_pages, page_size, ctypes.byref(out)))
+        self.h = out
+
+    def __del__(self):
+        if getattr(self, "h", None) and _lib is not None:
+            _lib.grid_pages_free(self.h)
             self.h = None
 
 
