@@ -34,8 +34,9 @@
  * paged cache) and grid_draft_verify (drafted tokens against the masked
  * target distribution).  Where several continuations are drafted at once, the
  * chunk is a tree: grid_tree_plan, grid_kv_append_tree, grid_kv_attend_tree,
- * grid_tree_accept and grid_kv_compact; grid_pages_update and grid_kv_copy hand
- * out, share, fork and take back the pages of the cache.
+ * grid_tree_accept and grid_kv_compact; grid_sample draws from a distribution
+ * cut by top-k, top-p and min-p; grid_pages_update and grid_kv_copy hand out,
+ * share, fork and take back the pages of the cache.
  *
  * Conventions
  *   - Every call returns 0 (GRID_OK) or a negative GRID_E_* code; the message of
@@ -727,6 +728,39 @@ int grid_tree_accept(const grid_tree* tree, const int32_t* d_tokens, const int32
  * a row is left as it was.  Enqueue only. */
 int grid_kv_compact(const grid_kv* kv, const grid_kv_chunk* chunk, const int32_t* d_path, const int32_t* d_count,
                     int32_t max_path, int32_t* d_status, void* stream);
+
+/* ---- sampling from a cut distribution ----
+ * Row b's ids that its mask admits and whose logit is above -inf, ordered by
+ * logit, the largest first, and by id where logits are equal, have p =
+ * softmax(l / T_b).  Kept are the first n of them: n1 = d_top_k[b] (<= 0: all),
+ * n2 the least n whose probabilities sum to d_top_p[b] (>= 1: all; 0 or less: one) times the
+ * sum of the first n1, n3 the number with p >= d_min_p[b] (<= 0: all) times the
+ * largest, and n = max(1, min(n1, n2, n3)).  Drawn is the first largest p_i /
+ * e_i of the kept ids, e the given noise: with e exponential, by their share of
+ * p.  T_b <= 0 (or not a number) keeps the first id; d_logprob[b] is log p of
+ * the drawn token before the cut (T <= 0: of T = 1).  NaN settings other than
+ * T's count as not given.
+ *
+ * NaN logits count as -inf, +inf as the largest finite value of the type; noise
+ * below 2^-126 or not a number leaves its id out of the draw (where nothing is
+ * left: the first id).  A row without ids gets token -1, logprob 0 and GRID_ST_EMPTY_MASK; a
+ * drawn `eos` gives GRID_ST_COMPLETE. */
+typedef struct grid_sample_step {
+  const void* d_logits;       /* dtype (F32 or BF16); B rows of V, logit_stride apart  */
+  int64_t logit_stride;
+  const uint32_t* d_mask;     /* B rows of ceil(V/32) words, mask_stride apart, or NULL */
+  int64_t mask_stride;
+  const float* d_noise;       /* B rows of V, noise_stride apart                       */
+  int64_t noise_stride;
+  const float* d_temperature; /* [B] or NULL: 1                                        */
+  const int32_t* d_top_k;     /* [B] or NULL                                           */
+  const float *d_top_p, *d_min_p; /* [B] or NULL                                       */
+  int32_t dtype, B, V, eos;   /* 1 <= B <= 65535, 1 <= V <= 393216; eos -1: none       */
+  int32_t* d_tokens;          /* out [B]                                               */
+  float* d_logprob;           /* out [B] or NULL                                       */
+  int32_t* d_status;          /* out [B]                                               */
+} grid_sample_step;
+int grid_sample(const grid_sample_step* step, void* stream);
 
 /* ---- the pages of a cache ----
  * What a batch's rows hold of a pool of pages is its table and, per row, how

@@ -31,7 +31,7 @@ EXPORTED = ["grid_last_error", "grid_compile", "grid_grammar_free", "grid_gramma
             "grid_audit_genesis", "grid_blake2b", "grid_fingerprint", "grid_apply_mask", "grid_configs_export",
             "grid_kv_create", "grid_kv_append", "grid_kv_attend", "grid_drafts_create", "grid_draft_verify",
             "grid_tree_plan", "grid_kv_append_tree", "grid_kv_attend_tree", "grid_tree_accept", "grid_kv_compact",
-            "grid_pages_create", "grid_pages_update", "grid_kv_copy"]
+            "grid_sample", "grid_pages_create", "grid_pages_update", "grid_kv_copy"]
 
 
 class GridLibraryMissing(RuntimeError):
@@ -128,6 +128,7 @@ def lib():
         "grid_kv_attend_tree": (I32, [P, P, P, P, I32, P, P]),
         "grid_tree_accept": (I32, [P, P, P, I32, I32, P, P, P, P, P]),
         "grid_kv_compact": (I32, [P, P, P, P, I32, P, P]),
+        "grid_sample": (I32, [P, P]),
         "grid_pages_create": (I32, [I32, I32, ctypes.POINTER(P)]),
         "grid_pages_free": (None, [P]),
         "grid_pages_update": (I32, [P, P, P]),
@@ -546,7 +547,7 @@ def grid_configs_export(cfg, row: int, cap: int = 1 << 16):
 # The structures of include/grid.h that calls fill: packed by struct, which takes half the time of ctypes (padding included).
 _HEADS, _CHUNK, _ROTATION, _NORM = struct.Struct("Pqq"), struct.Struct("PqPPiiii"), struct.Struct("PPiiii"), struct.Struct("PPfi")
 _QUERY, _STEP = struct.Struct("PqqPqqPfi"), struct.Struct("PqqPqqPqqPPPPqPiiiiiiPPPP")
-_TREE, _PAGES = struct.Struct("PPii"), struct.Struct("PqPPPPPiiiiPqPPPP")
+_TREE, _PAGES, _SAMPLE = struct.Struct("PPii"), struct.Struct("PqPPPPPiiiiPqPPPP"), struct.Struct("PqPqPqPPPPiiiiPPP")
 
 
 def _dense(x, dtype, *shape):
@@ -702,6 +703,32 @@ def grid_kv_compact(kv, table, lens, path, count, status, n_tokens, start=None, 
     most = path.shape[1]
     _check(lib().grid_kv_compact(kv.h, chunk, _dense(path, i32, B, most), _dense(count, i32, B), most, status.data_ptr(),
                                  _stream(stream)))
+
+
+def grid_sample(logits, noise, tokens, status, mask=None, temperature=None, top_k=None, top_p=None, min_p=None,
+                logprob=None, eos=-1, stream=None):
+    """Draw one token per row from its distribution cut by top-k, top-p and min-p:
+    logits float32 or bfloat16 [B, V], noise float32 [B, V] (exponential), mask
+    int32 [B, W] (rows of these may be strided); temperature, top_p, min_p float32
+    [B], top_k int32 [B] or None.  Out: tokens, status int32 [B], logprob float32
+    [B] or None."""
+    import torch
+    f32, i32 = torch.float32, torch.int32
+    B, V = logits.shape
+    dt = GRID_DTYPE_F32 if logits.dtype is f32 else GRID_DTYPE_BF16
+    assert dt == GRID_DTYPE_F32 or logits.dtype is torch.bfloat16, "float32 or bfloat16 logits expected"
+
+    def rows(x, dtype, n):
+        assert x.dtype is dtype and x.is_cuda and x.shape == (B, n) and (x.stride(1) == 1 or n == 1), \
+            "%s CUDA tensor [%d, %d] expected, its rows contiguous" % (dtype, B, n)
+        return x.data_ptr(), x.stride(0)
+
+    step = _SAMPLE.pack(
+        *rows(logits, logits.dtype, V), *((0, 0) if mask is None else rows(mask, i32, (V + 31) // 32)), *rows(noise, f32, V),
+        0 if temperature is None else _dense(temperature, f32, B), 0 if top_k is None else _dense(top_k, i32, B),
+        0 if top_p is None else _dense(top_p, f32, B), 0 if min_p is None else _dense(min_p, f32, B), dt, B, V, eos,
+        _dense(tokens, i32, B), 0 if logprob is None else _dense(logprob, f32, B), _dense(status, i32, B))
+    _check(lib().grid_sample(step, _stream(stream)))
 
 
 def grid_pages_update(pages, table, held, want, table_out, held_out, copies, refs, status, parent=None, keep=None,

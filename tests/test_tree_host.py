@@ -1,4 +1,4 @@
-"""What the calls for trees and pages refuse before they launch
+"""What the calls for trees, sampling and pages refuse before they launch
 anything, what they launch, and that a failing CUDA call leaves nothing behind:
 the library on a CUDA runtime without a GPU (no pointer here is dereferenced)."""
 import ctypes
@@ -146,8 +146,36 @@ def test_scratch_of_updates_is_freed_when_a_call_fails(fake):
             assert rt.get("live") == 0, k
 
 
+def sample(**kw):
+    return ctypes.byref(T.SampleStep(**{**dict(d_logits=AT, logit_stride=100, d_mask=AT, mask_stride=4, d_noise=AT, noise_stride=100,
+                                               d_temperature=AT, d_top_k=AT, d_top_p=AT, d_min_p=AT, dtype=G.GRID_DTYPE_F32, B=4, V=100,
+                                               eos=-1, d_tokens=AT, d_logprob=AT, d_status=AT), **kw}))
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(d_logits=None), INVALID), (dict(d_noise=None), INVALID), (dict(d_tokens=None), INVALID), (dict(d_status=None), INVALID),
+    (dict(B=0), INVALID), (dict(V=0), INVALID), (dict(dtype=G.GRID_DTYPE_F16), INVALID), (dict(d_logits=AT + 2), INVALID),
+    (dict(d_mask=AT + 2), INVALID), (dict(d_noise=AT + 1), INVALID), (dict(logit_stride=-1), INVALID), (dict(mask_stride=-4), INVALID),
+    (dict(noise_stride=-1), INVALID), (dict(B=65_536), TOO_LARGE), (dict(V=393_217), TOO_LARGE)])
+def test_a_draw_that_is_refused(fake, bad, code):
+    with fakes.use(fake) as rt:
+        refused(rt, "grid_sample", code, sample(**bad), None)
+        assert G.lib().grid_sample(sample(), None) == 0 and len(rt.launches()) >= 1
+
+
+@pytest.mark.parametrize("dtype", [G.GRID_DTYPE_F32, G.GRID_DTYPE_BF16])
+@pytest.mark.parametrize("B,V", [(1, 1), (3, 4096), (256, 151_937), (65_535, 33), (2, 393_216)])
+def test_a_draw_fits_the_device(fake, dtype, B, V):
+    """Whole rows of blocks, and no more shared memory than a block may have."""
+    with fakes.use(fake) as rt:
+        rt.reset()
+        assert G.lib().grid_sample(sample(B=B, V=V, dtype=dtype), None) == 0
+        for _, g, threads, smem, limit in rt.launches():
+            assert g[0] % B == 0 and g[1] == g[2] == 1 and smem <= limit <= 227 << 10 and threads <= 1024
+
+
 def test_packed_arguments_have_the_layout_of_the_structures():
-    for packed, structure in ((G._TREE, T.Tree), (G._PAGES, T.PagesStep)):
+    for packed, structure in ((G._TREE, T.Tree), (G._PAGES, T.PagesStep), (G._SAMPLE, T.SampleStep)):
         assert packed.size == ctypes.sizeof(structure)
         values = list(range(1, len(structure._fields_) + 1))
         assert bytes(structure(*values)) == packed.pack(*values)
