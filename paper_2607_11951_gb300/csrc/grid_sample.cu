@@ -5,47 +5,60 @@
 // w = 2^((l - m) c), its probability w / Z with Z the sum over the admitted ids.
 // Ids are ordered by one 54-bit number, the logit's bits in the order of integers
 // and then the id's complement, so that what top-k and top-p keep is "order >=
-// X".  X is found by counting: the ids of the present range go into 1,024 bins
-// that keep the order (of the first level by m - l, linearly; of later ones by
-// the order itself), with the number and the weight of each; the bin is found
-// in which the k-th id, or top_p of the weight, is reached; and if it holds few
-// enough ids, these are sorted and X is one of them, else the bin is the next
-// level's range.  Each later level takes ten bits off the order: six at most.
-//
-// Weights are added as integers, in steps of 2^-40 of the largest, so that their
-// sums do not depend on the order of the atomic additions (V ids are off by V
-// 2^-41 of the largest weight at most, less than by the rounding of w itself).
+// X".
 //
 // A cluster of blocks per row holds the row's admitted logits in its shared
 // memory: each logit is read from memory once, noise only where an id is kept.
+// Each block learns what the others found and goes on for itself, so that a
+// step costs one barrier of the cluster.  X is found in up to three steps:
+//   - Ids that cannot be at the cut are left out: below the k-th largest of the
+//     threads' largest logits; or (top-p alone) of less than (1 - top_p) Z / ids,
+//     which together have less than 1 - top_p.
+//   - The others go into 1,024 bins of equal width in m - l, with the number and
+//     the weight of each, and the bin is found in which the k-th id, or top_p of
+//     the weight, is reached.
+//   - That bin's ids are sorted (each counts how many come before it), and X is
+//     one of them.  A bin of more than a list holds, as equal logits make it, is
+//     cut into 512 parts of its range of order instead, and again: nine bits
+//     less each time, six times at most.
+// min-p needs no X: w >= min_p is asked of every id.
+//
+// Sums of weights are integers, so that the order of the atomic additions does not
+// matter: in a bin in steps of 2^-17 or less of its weights (what fits 32 bits if
+// all of a block's ids are in it), elsewhere of 2^-40 of the largest.
 #include <atomic>
 #include <cfloat>
 #include <climits>
 #include <cmath>
+
+#include <cuda_bf16.h>
 
 #include "grid_model.cuh"
 
 namespace grid {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxBlocks = 8;             // of a row: the largest cluster that every device takes
-constexpr int kBins = 1024, kBinBits = 10;
-constexpr int kList = 1024;               // ids that are sorted at once
+constexpr int kBins = 1024, kPer = kBins / kThreads;  // a thread sums up kPer neighbours
+constexpr int kParts = 512, kPartBits = 9;            // of a range of order
+constexpr int kList = 512;                // ids that are sorted at once
+constexpr int kDirect = 256;              // a top_k up to here is looked for without bins
 constexpr int kIdBits = 22;
 constexpr int kMaxIds = 393216;           // 48 Ki fp32 logits for each of eight blocks
-constexpr float kFirstRange = 40.f;       // exponents below m that the first level's bins reach, or to the smallest logit
+constexpr float kFirstRange = 40.f;       // exponents below m that bins reach
 constexpr float kUnit = 1099511627776.f;  // 2^40
+constexpr float kWhole = 8388608.f;       // 2^23: floats from here on are whole numbers
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 using u64 = unsigned long long;
 
 struct SampleArgs {
   grid_sample_step s;
-  int blocks, each;  // blocks of a row, ids of a block (a multiple of 32)
+  int each;  // ids of a block (a multiple of 32)
 };
 
-struct Pick {   // of a draw: the best score, its id and logit; the first id of the largest logit
-  float score, logit;
+struct Pick {   // of a draw: the best score and its id; the first id of the largest logit
+  float score;
   int id, first;
 };
 struct Found {  // the bin that a search ends in, and what lies in the bins before it
@@ -54,33 +67,34 @@ struct Found {  // the bin that a search ends in, and what lies in the bins befo
   u64 weight;
 };
 
-struct Hist {
-  unsigned n[kBins], lo[kBins], hi[kBins];  // ids, and the two halves of their weights
-};
 struct Shared {
   union {
-    Hist hist;
-    u64 list[kList];
+    float tops[kMaxBlocks * kThreads];     // of all threads of the row: their largest logits
+    struct {
+      unsigned n[kBins], w[kBins];         // ids and weights
+    } bins;
+    struct {
+      unsigned n[kParts], lo[kParts], hi[kParts];  // the weights in 64 bits
+    } parts;
   };
-  float top, low, z;           // this block's largest and smallest admitted logit, and its weights
-  unsigned part_n[2];          // of this block's share of the bins: of the first level, of a later one
-  u64 part_w[2];
-  u64 most, least;             // of this block's ids in the present bin
-  unsigned listed;             // block 0: how many ids the list got
-  u64 cut, kept;               // X, and the weight of what it keeps
+  u64 list[2][kList];                      // of one gathering and the next: a block's ids in a part of its own
+  // what every block of the row writes here
+  float top[kMaxBlocks];                   // its largest admitted logit
+  unsigned ids[kMaxBlocks];                // admitted
+  float z[kMaxBlocks];                     // sum of weights
+  unsigned in[2][kMaxBlocks];              // ids in the range that is gathered
+  u64 most[kMaxBlocks], least[kMaxBlocks]; // the first and the last (~) of them
+  Pick pick[kMaxBlocks];                   // (block 0)
+  // of the block alone
   Found found;
-  Pick pick[kMaxBlocks];       // block 0: of every block
-  float zs[kMaxBlocks];
+  u64 target, kept;
+  unsigned staged, at;
   u64 sums[kWarps], sums2[kWarps];
+  float2 warps[kWarps];
   Pick picks[kWarps];
-  float zw[kWarps];
 };
 constexpr int kSharedRoom = (sizeof(Shared) + 127) & ~127;
 
-__device__ __forceinline__ void cluster_sync() {
-  __syncwarp();
-  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ int cluster_rank() {
   int r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -92,19 +106,9 @@ __device__ __forceinline__ uint32_t there(const void* p, int r) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(r));
   return at;
 }
-__device__ __forceinline__ unsigned get(const unsigned& x, int r) {
-  unsigned v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(there(&x, r)) : "memory");
-  return v;
-}
-__device__ __forceinline__ float get(const float& x, int r) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there(&x, r)) : "memory");
-  return v;
-}
-__device__ __forceinline__ u64 get(const u64& x, int r) {
-  u64 v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(there(&x, r)) : "memory");
+__device__ __forceinline__ uint4 get4(const unsigned* x, int r) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(there(x, r)));
   return v;
 }
 __device__ __forceinline__ void put(unsigned& x, unsigned v, int r) {
@@ -120,10 +124,9 @@ __device__ __forceinline__ void put(u64& x, u64 v, int r) {
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(there(&x, r)), "l"(v) : "memory");
 }
 
-__device__ __forceinline__ u64 shfl_xor(u64 x, int o) { return __shfl_xor_sync(~0u, x, o); }
 __device__ __forceinline__ u64 max_warp(u64 x) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) x = max(x, shfl_xor(x, o));
+  for (int o = 16; o; o >>= 1) x = max(x, __shfl_xor_sync(~0u, x, o));
   return x;
 }
 __device__ __forceinline__ float max_warp(float x) {
@@ -137,37 +140,109 @@ __device__ __forceinline__ float sum_warp(float x) {
   return x;
 }
 __device__ __forceinline__ void better(Pick& x, const Pick& y) {
-  if (y.score > x.score || (y.score == x.score && y.id < x.id)) x.score = y.score, x.logit = y.logit, x.id = y.id;
+  if (y.score < x.score || (y.score == x.score && y.id < x.id)) x.score = y.score, x.id = y.id;
   x.first = min(x.first, y.first);
 }
 __device__ __forceinline__ Pick best_warp(Pick x) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
-    const Pick y = {__shfl_xor_sync(~0u, x.score, o), __shfl_xor_sync(~0u, x.logit, o), __shfl_xor_sync(~0u, x.id, o),
-                    __shfl_xor_sync(~0u, x.first, o)};
+    const Pick y = {__shfl_xor_sync(~0u, x.score, o), __shfl_xor_sync(~0u, x.id, o), __shfl_xor_sync(~0u, x.first, o)};
     better(x, y);
   }
   return x;
 }
-
-// A logit as it is kept: NaN as -inf, +inf as the largest finite value of its type, -0 as 0.
-__device__ __forceinline__ float kept_as(float x) { return fminf(fmaxf(x, -INFINITY), FLT_MAX) + 0.f; }
-__device__ __forceinline__ uint16_t kept_as(uint16_t x) {  // bf16
-  if ((x & 0x7FFF) > 0x7F80) return 0xFF80;
-  return x == 0x7F80 ? 0x7F7F : x == 0x8000 ? 0 : x;
+// The sum over the block's threads up to this one, and over all of them.
+template <typename N>
+__device__ __forceinline__ N up_to(N x, u64* sums, N& all) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const N y = __shfl_up_sync(~0u, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();  // (`sums` may still be read from the last time)
+  if (lane == 31) sums[warp] = x;
+  __syncthreads();
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const N y = (N)sums[w];
+    if (w < warp) x += y;
+    all += y;
+  }
+  return x;
 }
+
+// Sixteen bytes of logits: NaN as -inf, +inf as the largest finite value of the type, and -inf where the bit is not set; the
+// largest of them; the values in pairs.
 __device__ __forceinline__ float value(float x) { return x; }
-__device__ __forceinline__ float value(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+__device__ __forceinline__ float value(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }  // bf16
+__device__ __forceinline__ float kept_as(float x) { return fminf(fmaxf(x, -INFINITY), FLT_MAX); }
+__device__ __forceinline__ uint16_t kept_as(uint16_t x) { return (x & 0x7FFF) > 0x7F80 ? 0xFF80 : x == 0x7F80 ? 0x7F7F : x; }
 template <typename T>
-__device__ __forceinline__ T nothing();
+struct Line;
 template <>
-__device__ __forceinline__ float nothing<float>() { return -INFINITY; }
+struct Line<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ float none() { return -INFINITY; }
+  static __device__ __forceinline__ uint4 admit(const uint4& r, unsigned bits) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    uint32_t y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = bits >> e & 1u ? __float_as_uint(kept_as(__uint_as_float(w[e]))) : 0xFF800000u;
+    return make_uint4(y[0], y[1], y[2], y[3]);
+  }
+  static __device__ __forceinline__ float top(const uint4& r) {
+    return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
+  }
+  static __device__ __forceinline__ Two pair(const uint4& r, int e) {
+    return e ? Two{__uint_as_float(r.z), __uint_as_float(r.w)} : Two{__uint_as_float(r.x), __uint_as_float(r.y)};
+  }
+};
 template <>
-__device__ __forceinline__ uint16_t nothing<uint16_t>() { return 0xFF80; }
+struct Line<uint16_t> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ uint16_t none() { return 0xFF80; }
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 v = __hmax2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  static __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 v = __hmin2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  static __device__ __forceinline__ uint4 admit(const uint4& r, unsigned bits) {
+    uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      w[e] = min2(max2(w[e], 0xFF80FF80u), 0x7F7F7F7Fu);
+      if (!(bits >> (2 * e) & 1u)) w[e] = (w[e] & 0xFFFF0000u) | 0xFF80u;
+      if (!(bits >> (2 * e + 1) & 1u)) w[e] = (w[e] & 0xFFFFu) | 0xFF800000u;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ float top(const uint4& r) {
+    const uint32_t x = max2(max2(r.x, r.y), max2(r.z, r.w));
+    return fmaxf(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ Two pair(const uint4& r, int e) {
+    const uint32_t w = e == 0 ? r.x : e == 1 ? r.y : e == 2 ? r.z : r.w;
+    return Two{__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)};
+  }
+};
+// A load where `in` holds, without a branch: as branches, the loads of a loop wait for one another.
+__device__ __forceinline__ void load_if(float& x, const float* p, bool in) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\n@p ld.global.nc.f32 %0, [%1];\n}" : "+f"(x) : "l"(p), "r"((int)in));
+}
+__device__ __forceinline__ void load_if(uint4& x, const void* p, bool in) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %5, 0;\n@p ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n}"
+               : "+r"(x.x), "+r"(x.y), "+r"(x.z), "+r"(x.w)
+               : "l"(p), "r"((int)in));
+}
 
 // The logit's bits in the order of integers, then the id's complement; and back.
 __device__ __forceinline__ u64 order_of(float x, int id) {
-  const unsigned b = __float_as_uint(x);
+  const unsigned b = __float_as_uint(x + 0.f);  // (-0 is 0)
   return (u64)(b ^ ((unsigned)((int)b >> 31) | 0x80000000u)) << kIdBits | (unsigned)((1 << kIdBits) - 1 - id);
 }
 __device__ __forceinline__ float logit_of(u64 o) {
@@ -175,295 +250,574 @@ __device__ __forceinline__ float logit_of(u64 o) {
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 
-// What a row asks for.
+// A row's weights and bins.
 struct Row {
-  float c2;        // 2 log2(e) / T
-  float m, by;     // the largest logit; bins per half of m - l
-  bool first;      // only the first id is kept
+  float c2;     // 2 log2(e) / T
+  float m, by;  // the largest logit; bins per half of m - l
+  float width;  // exponents of a bin
   // half of m - l: of the halves, since the difference of two logits may be past the type
   __device__ __forceinline__ float below(float x) const { return fmaf(0.5f, m, -0.5f * x); }
   __device__ __forceinline__ float weight(float x) const { return exp2_fast(-below(x) * c2); }
-  __device__ __forceinline__ int bin(float x) const { return (int)fminf(below(x) * by, (float)(kBins - 1)); }
+  // The bin, as a whole number in the low bits of a float of 2^23 and more: conversions run at an eighth of an addition's rate.
+  __device__ __forceinline__ float bin_in(float x) const { return fminf(below(x) * by, (float)(kBins - 1)) + kWhole; }
+  static __device__ __forceinline__ int low(float whole) { return __float_as_int(whole) & 0x7FFFFF; }
+  __device__ __forceinline__ int bin(float x) const { return low(bin_in(x)); }
+  __device__ __forceinline__ void reach(float range) {  // bins of halves of m - l up to `range`
+    range = fminf(range, fminf(kFirstRange / c2, FLT_MAX));
+    by = range > 0.f ? fminf(kBins / range, FLT_MAX) : 0.f;
+    width = c2 / by;
+    if (!(width <= 2.f * kFirstRange / kBins)) width = 0.f;  // (no bins, or T past what they can tell apart: as they are)
+  }
+  // A bin's weights are held relative to this, the weight half a bin behind its end: 2^(width/2) to 2^(3 width/2) times it (less in the last bin).
+  __device__ __forceinline__ float share(float x, float bin_in) const {
+    return exp2_fast(fmaf(-below(x), c2, fmaf(bin_in - kWhole, width, width)));
+  }
+  __device__ __forceinline__ float at_end(int bin) const { return exp2_fast(-fmaf((float)bin, width, width)); }
+  // Nothing below this has a half of m - l of up to h: the roundings of both, 2^-23 of h or of a logit, are allowed for.
+  __device__ __forceinline__ float least(float h) const { return m - 2.f * h - 1e-6f * (h + fabsf(m)); }
+  // Nothing above this has one of h or more.
+  __device__ __forceinline__ float most(float h) const { return m - 2.f * h + 1e-6f * (h + fabsf(m)); }
 };
 __device__ __forceinline__ u64 units(float w) { return __float2ull_rn(w * kUnit); }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) k_sample(const SampleArgs a) {
+template <typename T, int blocks>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(const SampleArgs a) {
+  using L = Line<T>;
+  constexpr int N = L::N;
   extern __shared__ __align__(128) uint8_t raw[];
   Shared& sh = *reinterpret_cast<Shared*>(raw);
-  // bins of this block's share, added up over the row's blocks and from the first one of the share on: of the first level, of a later one
-  const int share = kBins / a.blocks;
-  unsigned* const tot_n = reinterpret_cast<unsigned*>(raw + kSharedRoom);
-  u64* const tot_w = reinterpret_cast<u64*>(tot_n + 2 * share);
-  T* const vals = reinterpret_cast<T*>(tot_w + 2 * share);
+  uint4* const lines = reinterpret_cast<uint4*>(raw + kSharedRoom);
   const grid_sample_step& s = a.s;
-  const int b = blockIdx.x / a.blocks, rank = cluster_rank(), blocks = a.blocks;
+  const int b = blockIdx.x / blocks, rank = cluster_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int lo = min(s.V, rank * a.each), n = min(s.V, lo + a.each) - lo;
+  auto sync = [&]() {  // of the row's blocks
+    __syncwarp();
+    if (blocks > 1)
+      asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    else
+      __syncthreads();
+  };
+  if (blocks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   pdl_wait();
-  // ---- the block's logits, admitted ones as they are and the others as -inf
-  Row row;
   const float temp = s.d_temperature ? s.d_temperature[b] : 1.f;
   const int top_k = s.d_top_k ? s.d_top_k[b] : 0;
   const float top_p = s.d_top_p ? s.d_top_p[b] : 1.f, min_p = s.d_min_p ? s.d_min_p[b] : 0.f;
   const bool greedy = !(temp > 0.f);
-  row.first = greedy || top_k == 1 || top_p <= 0.f || min_p > 1.f;
+  const bool first = greedy || top_k == 1 || top_p <= 0.f || min_p > 1.f;  // only the first id is kept
+  Row row;
   row.c2 = fminf((greedy ? 1.f : 1.f / temp) * (2.f * kLog2e), FLT_MAX);
-  float top = -INFINITY, low = INFINITY;
+
+  // ---- the block's logits in lines of 16 bytes as they lie in memory: line v holds the block's ids v N - pad .. + N - 1
+  int pad = 0, count_v = 0;
+  float top = -INFINITY;
+  unsigned ids = 0;
   {
     const T* l = static_cast<const T*>(s.d_logits) + b * s.logit_stride + lo;
     const uint32_t* mask = s.d_mask ? s.d_mask + b * s.mask_stride + (lo >> 5) : nullptr;
-    for (int i = tid; i < n; i += kThreads) {  // (a warp's ids are those of one word: lo is a multiple of 32)
-      T x = nothing<T>();
-      if (!mask || (mask[i >> 5] >> (i & 31) & 1u)) x = kept_as(l[i]);
-      vals[i] = x;
-      const float v = value(x);
-      top = fmaxf(top, v);
-      if (v > -INFINITY) low = fminf(low, v);
+    pad = (int)((uintptr_t)l & 15) / (int)sizeof(T);
+    count_v = n > 0 ? (pad + n + N - 1) / N : 0;
+    constexpr int kAhead = 4;
+    const int inner = n - N;  // a whole line begins at an id of 0 .. inner
+    auto bits_of = [&](int v) {
+      const int i = v * N - pad;
+      if (i < 0 || i > inner) return 0u;
+      if (!mask) return (1u << N) - 1u;
+      const uint32_t* w = mask + (i >> 5);
+      return __funnelshift_r(w[0], (i & 31) > 32 - N ? w[1] : 0u, i & 31) & ((1u << N) - 1u);
+    };
+    unsigned bits[kAhead];
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y) bits[y] = bits_of(tid + y * kThreads);
+    for (int v0 = tid; v0 < count_v; v0 += kAhead * kThreads) {
+      uint4 r[kAhead];
+#pragma unroll
+      for (int y = 0; y < kAhead; ++y) {
+        r[y] = make_uint4(0, 0, 0, 0);
+        load_if(r[y], l + ((long long)(v0 + y * kThreads) * N - pad), bits[y] != 0);
+      }
+      unsigned next[kAhead];
+#pragma unroll
+      for (int y = 0; y < kAhead; ++y) next[y] = bits_of(v0 + (kAhead + y) * kThreads);
+#pragma unroll
+      for (int y = 0; y < kAhead; ++y) {
+        const uint4 x = L::admit(r[y], bits[y]);
+        if (v0 + y * kThreads < count_v) lines[v0 + y * kThreads] = x;
+        top = fmaxf(top, L::top(x));
+        ids += __popc(bits[y]);
+        bits[y] = next[y];
+      }
+    }
+    // lines that are not whole: the first and the last, an id to a thread
+    __syncthreads();
+    if (tid < 2 * N && count_v > 0 && (tid < N || count_v > 1)) {
+      const int v = tid < N ? 0 : count_v - 1, i = v * N + tid % N - pad;
+      if (v * N - pad < 0 || v * N - pad > inner) {
+        T x = L::none();
+        if (i >= 0 && i < n && (!mask || mask[i >> 5] >> (i & 31) & 1u)) {
+          x = kept_as(l[i]);
+          ++ids;
+        }
+        reinterpret_cast<T*>(lines + v)[tid % N] = x;
+        top = fmaxf(top, value(x));
+      }
     }
   }
-  // what every thread has, over the block, to a place of sh
-  auto over_block = [&](float x, float y) {
-    x = max_warp(x), y = max_warp(y);
-    if (lane == 0) sh.sums[warp] = (u64)__float_as_uint(x) << 32 | __float_as_uint(y);
+  // ---- the row's largest logit, all threads' largest, and how many ids are admitted
+  const bool wants_k = !first && top_k > 0;
+  {
+    const float t = max_warp(top);
+    const unsigned c = __reduce_add_sync(~0u, ids);
+    if (lane == 0) sh.warps[warp] = make_float2(t, __uint_as_float(c));
     __syncthreads();
-    const u64 v = sh.sums[lane % kWarps];
-    x = max_warp(__uint_as_float((unsigned)(v >> 32))), y = max_warp(__uint_as_float((unsigned)v));
-    if (tid == 0) sh.top = x, sh.low = y;
-  };
-  over_block(top, -low);
-  cluster_sync();
-  top = max_warp(lane < blocks ? get(sh.top, lane) : -INFINITY);
-  low = -max_warp(lane < blocks ? get(sh.low, lane) : -INFINITY);
-  if (!(top > -INFINITY)) {  // (the same in every block)
+    if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (the others are there)
+    if (wants_k)
+      for (int r = 0; r < blocks; ++r) put(sh.tops[rank * kThreads + tid], top, r);
+    if (tid < blocks) {
+      float x = -INFINITY;
+      unsigned all = 0;
+      for (int w = 0; w < kWarps; ++w) x = fmaxf(x, sh.warps[w].x), all += __float_as_uint(sh.warps[w].y);
+      put(sh.top[rank], x, tid);
+      put(sh.ids[rank], all, tid);
+    }
+    sync();
+  }
+  ids = 0;
+  row.m = -INFINITY;
+  for (int r = 0; r < blocks; ++r) row.m = fmaxf(row.m, sh.top[r]), ids += sh.ids[r];
+  if (!(row.m > -INFINITY)) {  // (the same in every block)
     if (rank == 0 && tid == 0) {
       s.d_tokens[b] = -1;
       if (s.d_logprob) s.d_logprob[b] = 0.f;
       s.d_status[b] = GRID_ST_EMPTY_MASK;
     }
-    cluster_sync();
     return;
   }
-  row.m = top;
+
+  // f(x, i) for the block's ids i whose logit x is admitted and at least `from`
+  auto each = [&](float from, auto f) {
+    from = fmaxf(from, -FLT_MAX);
+    for (int v = tid; v < count_v; v += kThreads) {
+      const uint4 r = lines[v];
+      if (!(L::top(r) >= from)) continue;
+#pragma unroll
+      for (int e = 0; e < N; e += 2) {
+        const Two x = L::pair(r, e / 2);
+        if (x.x >= from) f(x.x, v * N + e - pad);
+        if (x.y >= from) f(x.y, v * N + e + 1 - pad);
+      }
+    }
+  };
+
+  // ---- the sum of the weights
   {
-    const float range = fminf(kFirstRange / row.c2, row.below(low));
-    row.by = range > 0.f ? fminf(kBins / range, FLT_MAX) : 0.f;
+    float z = 0.f;
+    if (row.c2 > 0.f) {
+      Two sum = {0.f, 0.f};
+#pragma unroll 2
+      for (int v = tid; v < count_v; v += kThreads) {
+        const uint4 r = lines[v];
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) {
+          const Two t = mul2(fma2(L::pair(r, e), 0.5f, -0.5f * row.m), Two{row.c2, row.c2});
+          sum = add2(sum, Two{exp2_fast(t.x), exp2_fast(t.y)});
+        }
+      }
+      z = sum.x + sum.y;
+    } else {  // (T is infinite: all finite logits weigh the same)
+      each(-INFINITY, [&](float, int) { z += 1.f; });
+    }
+    z = sum_warp(z);
+    __syncthreads();
+    if (lane == 0) sh.warps[warp].x = z;
+    __syncthreads();
+    if (tid < blocks) {
+      z = 0.f;
+      for (int w = 0; w < kWarps; ++w) z += sh.warps[w].x;
+      put(sh.z[rank], z, tid);
+    }
   }
 
-  // ---- the range of order that is looked at: everything, a bin of the first level, [least, most]
-  const bool by_k = !row.first && top_k > 0 && top_k < s.V, by_p = !row.first && top_p < 1.f;
-  u64 most = ~0ull, least = 0, cut = 0;
-  int first_bin = -1, shift = 0;  // -1: everything
-  auto in_range = [&](float x, int i) {
-    if (first_bin >= 0) return row.bin(x) == first_bin;
-    const u64 o = order_of(x, lo + i);
-    return o >= least && o <= most;
-  };
-  // the range's ids into bins
-  auto count = [&](bool level0, bool counts, bool weights) {
-    for (int i = tid; i < kBins; i += kThreads) sh.hist.n[i] = sh.hist.lo[i] = sh.hist.hi[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += kThreads) {
-      const float x = value(vals[i]);
-      if (!(x > -INFINITY)) continue;
-      int bin;
-      if (level0) {
-        bin = row.bin(x);
-      } else {
-        const u64 o = order_of(x, lo + i);
-        if (o < least || o > most) continue;
-        bin = (int)((most - o) >> shift);
-      }
-      if (counts) atomicAdd(&sh.hist.n[bin], 1u);
-      if (weights) {
-        const u64 w = units(row.weight(x));
-        const unsigned l = (unsigned)w, was = l ? atomicAdd(&sh.hist.lo[bin], l) : 0u;
-        const unsigned h = (unsigned)(w >> 32) + (was + l < was);
-        if (h) atomicAdd(&sh.hist.hi[bin], h);
-      }
-    }
-    cluster_sync();
-    // a thread per bin of the block's share (several where the share is large), then the sums from its first bin on
-    unsigned* const tn = tot_n + (level0 ? 0 : share);
-    u64* const tw = tot_w + (level0 ? 0 : share);
-    unsigned base_n = 0;
-    u64 base_w = 0;
-    for (int j0 = 0; j0 < share; j0 += kThreads) {
-      const int j = j0 + tid;
-      u64 cn = 0, cw = 0;
-      if (j < share)
-        for (int r = 0; r < blocks; ++r) {
-          const int bin = rank * share + j;
-          cn += get(sh.hist.n[bin], r);
-          cw += (u64)get(sh.hist.lo[bin], r) + ((u64)get(sh.hist.hi[bin], r) << 32);
+  // ---- the cut X: ids of order X and more are kept
+  const bool by_k = wants_k && (unsigned)top_k < ids, by_p = !first && top_p < 1.f;
+  u64 cut = 0;
+  if (by_k || by_p) {
+    const Found none = {0, 0u, 0ull};
+    constexpr unsigned room = kList / blocks;  // of a block in a list
+    int turn = 0;                          // which list
+    // The list of all ids in a range, `in`, whose logits lie in from .. to; how many there are (more than kList: no list).
+    auto gather = [&](float from, float to, auto in) {
+      turn ^= 1;
+      u64* list = sh.list[turn];
+      if (tid == 0) sh.staged = 0;
+      __syncthreads();
+      from = fmaxf(from, -FLT_MAX);
+      for (int v = tid; v < count_v; v += kThreads) {
+        const uint4 r = lines[v];
+        if (!(L::top(r) >= from)) continue;
+        unsigned some = 0;
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+          const Two x = L::pair(r, e / 2);
+          some |= (x.x >= from && x.x <= to ? 1u << e : 0u) | (x.y >= from && x.y <= to ? 2u << e : 0u);
         }
-      // inclusive sums over the block's threads
-      for (int o = 1; o < 32; o <<= 1) {
-        const u64 x = __shfl_up_sync(~0u, cn, o), y = __shfl_up_sync(~0u, cw, o);
-        if (lane >= o) cn += x, cw += y;
-      }
-      if (lane == 31) sh.sums[warp] = cn, sh.sums2[warp] = cw;
-      __syncthreads();
-      u64 all_n = 0, all_w = 0;
-      for (int x = 0; x < kWarps; ++x) {
-        if (x < warp) cn += sh.sums[x], cw += sh.sums2[x];
-        all_n += sh.sums[x], all_w += sh.sums2[x];
-      }
-      if (j < share) tn[j] = base_n + (unsigned)cn, tw[j] = base_w + cw;
-      base_n += (unsigned)all_n, base_w += all_w;
-      __syncthreads();
-    }
-    if (tid == 0) sh.part_n[!level0] = base_n, sh.part_w[!level0] = base_w;
-    cluster_sync();
-  };
-  // the bin in which, after `before`, the target is reached
-  auto search = [&](bool level0, bool weights, u64 target, const Found& before) {
-    const unsigned* const tn = tot_n + (level0 ? 0 : share);
-    const u64* const tw = tot_w + (level0 ? 0 : share);
-    unsigned fn = before.count;
-    u64 fw = before.weight;
-    for (int r = 0; r < rank; ++r) fn += get(sh.part_n[!level0], r), fw += get(sh.part_w[!level0], r);
-    for (int j = tid; j < share; j += kThreads) {
-      const unsigned pn = fn + (j ? tn[j - 1] : 0);
-      const u64 pw = fw + (j ? tw[j - 1] : 0);
-      const u64 prev = weights ? pw : pn, now = weights ? fw + tw[j] : fn + tn[j];
-      if (prev < target && now >= target)
-        for (int r = 0; r < blocks; ++r) {
-          put(sh.found.bin, rank * share + j, r);
-          put(sh.found.count, pn, r);
-          put(sh.found.weight, pw, r);
+        for (; some; some &= some - 1) {
+          const int e = __ffs(some) - 1;
+          const float x = value(reinterpret_cast<const T*>(lines + v)[e]);
+          const u64 o = order_of(x, lo + v * N + e - pad);
+          if (*(volatile unsigned*)&sh.staged > room || !in(x, o)) continue;  // (too many already: no need to look further)
+          const unsigned at = atomicAdd(&sh.staged, 1u);
+          if (at < room) list[rank * room + at] = o;
         }
-    }
-    cluster_sync();
-    return sh.found;
-  };
-  // X of a target: the least order that is kept; `kept`: the weight of what it keeps
-  auto find = [&](bool weights, u64 target, bool want_weight, u64& kept) {
-    Found f = search(true, weights, target, Found{0, 0u, 0ull});
-    first_bin = f.bin;
-    for (;;) {
-      // the bin's ids: the first and the last, and a list of them in block 0
-      if (tid == 0) sh.listed = 0;
-      cluster_sync();
-      u64 hi = 0, lo_c = 0;  // (the smallest as the largest complement)
-      for (int i = tid; i < n; i += kThreads) {
-        const float x = value(vals[i]);
-        if (!(x > -INFINITY) || !in_range(x, i)) continue;
-        const u64 o = order_of(x, lo + i);
-        hi = max(hi, o), lo_c = max(lo_c, ~o);
-        unsigned at;
-        asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(at) : "r"(there(&sh.listed, 0)) : "memory");
-        if (at < kList) put(sh.list[at], o, 0);
       }
-      hi = max_warp(hi), lo_c = max_warp(lo_c);
-      if (lane == 0) sh.sums[warp] = hi, sh.sums2[warp] = lo_c;
       __syncthreads();
-      hi = max_warp(sh.sums[lane % kWarps]), lo_c = max_warp(sh.sums2[lane % kWarps]);
-      if (tid == 0) sh.most = hi, sh.least = lo_c;
-      cluster_sync();
-      const unsigned listed = get(sh.listed, 0);
-      most = max_warp(lane < blocks ? get(sh.most, lane) : 0ull);
-      least = ~max_warp(lane < blocks ? get(sh.least, lane) : 0ull);
-      first_bin = -1;
-      if (listed <= kList) {
-        if (rank == 0) {
-          // ---- sorted, the largest first; the sums of their weights
-          int size = 32;
-          while (size < (int)listed) size *= 2;
-          for (int i = listed + tid; i < size; i += kThreads) sh.list[i] = 0;
+      const unsigned mine = sh.staged;
+      if (tid < blocks) put(sh.in[turn][rank], mine, tid);
+      if (mine <= room)
+        for (unsigned x = tid; x < mine * blocks; x += kThreads) {
+          const unsigned r = x % blocks, at = rank * room + x / blocks;
+          if (r != (unsigned)rank) put(list[at], list[at], r);
+        }
+      sync();
+      unsigned all = 0, most = 0;
+      for (int r = 0; r < blocks; ++r) all += sh.in[turn][r], most = max(most, sh.in[turn][r]);
+      return most > room ? kList + 1u : all;
+    };
+    // The list in one piece and sorted: an id's place is the number of those before it.
+    auto sort = [&](unsigned listed) {
+      u64* list = sh.list[turn];
+      u64 mine[kList / kThreads];
+      unsigned place[kList / kThreads] = {};
+#pragma unroll
+      for (int y = 0; y < kList / kThreads; ++y) {
+        unsigned i = tid + y * kThreads, r = 0;
+        while (r + 1 < (unsigned)blocks && i >= sh.in[turn][r]) i -= sh.in[turn][r++];
+        mine[y] = tid + y * kThreads < listed ? list[r * room + i] : 0;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int y = 0; y < kList / kThreads; ++y) list[tid + y * kThreads] = mine[y];
+      __syncthreads();
+#pragma unroll
+      for (int y = 0; y < kList / kThreads; ++y)
+        if (warp * 32 + y * kThreads < listed)
+#pragma unroll 4
+          for (unsigned i = 0; i < listed; i += 2) {  // (zeros past the last)
+            const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(list + i);
+            place[y] += (o.x > mine[y]) + (o.y > mine[y]);
+          }
+      __syncthreads();
+#pragma unroll
+      for (int y = 0; y < kList / kThreads; ++y)
+        if (tid + y * kThreads < listed) list[place[y]] = mine[y];
+      __syncthreads();
+    };
+    // The last id of the sorted list that a target needs, if so much comes before the list (the list's last where roundings
+    // leave the target a little out of reach): its place, and the weight up to it.
+    auto last_of = [&](unsigned listed, bool weights, u64 target, const Found& f) {
+      u64 weight = f.weight;
+      for (unsigned i0 = 0; i0 < listed; i0 += kThreads) {
+        const unsigned i = i0 + tid;
+        const bool some = i < listed;
+        const u64 w = some && by_p ? units(row.weight(logit_of(sh.list[turn][i]))) : 0;
+        u64 all;
+        const u64 upto = up_to(w, sh.sums, all);
+        const u64 was = weights ? weight + upto - w : f.count + (u64)i, now = weights ? weight + upto : f.count + (u64)i + 1;
+        if (some && was < target && (now >= target || i + 1 == listed)) sh.at = i, sh.kept = weight + upto;
+        weight += all;
+      }
+      __syncthreads();
+    };
+    auto target_of = [&](u64 sum) {
+      __syncthreads();
+      if (tid == 0) sh.target = max((u64)ceil((double)top_p * (double)sum), 1ull);
+      __syncthreads();
+      return sh.target;
+    };
+    // The cut from the list: by count, by weight (a target of 0: its share of what is listed, or kept by count), or by both.
+    auto cut_from = [&](unsigned listed, bool k, bool p, u64 target, const Found& f) {
+      sort(listed);
+      if (k || !target) {
+        last_of(listed, false, k ? top_k : f.count + listed, f);
+        listed = sh.at + 1;
+      }
+      if (p) last_of(listed, true, target ? target : target_of(sh.kept), f);
+      return sh.list[turn][sh.at];
+    };
+    // Of the bins kPer tid .. + kPer - 1 of all blocks: the ids and the weight up to and with each.
+    unsigned upto_n[kPer];
+    u64 upto_w[kPer];
+    auto sum_up = [&](const unsigned* n, const unsigned* w, const unsigned* high, float scale, bool counts, bool weights) {
+      u64 low[kPer] = {}, up[kPer] = {};
+      unsigned cn[kPer] = {};
+      const bool in = !high || kPer * tid < kParts;
+#pragma unroll
+      for (int r0 = 0; r0 < blocks; r0 += kMaxBlocks / 2) {  // (four blocks' at once)
+        constexpr int kAt = blocks < kMaxBlocks / 2 ? blocks : kMaxBlocks / 2;
+        uint4 x[kAt] = {}, y[kAt] = {}, z[kAt] = {};
+        if (in && counts)
+#pragma unroll
+          for (int r = 0; r < kAt; ++r) x[r] = get4(n + kPer * tid, r0 + r);
+        if (in && weights)
+#pragma unroll
+          for (int r = 0; r < kAt; ++r) y[r] = get4(w + kPer * tid, r0 + r);
+        if (in && weights && high)
+#pragma unroll
+          for (int r = 0; r < kAt; ++r) z[r] = get4(high + kPer * tid, r0 + r);
+#pragma unroll
+        for (int r = 0; r < kAt; ++r) {
+          cn[0] += x[r].x, cn[1] += x[r].y, cn[2] += x[r].z, cn[3] += x[r].w;
+          low[0] += y[r].x, low[1] += y[r].y, low[2] += y[r].z, low[3] += y[r].w;
+          up[0] += z[r].x, up[1] += z[r].y, up[2] += z[r].z, up[3] += z[r].w;
+        }
+      }
+      unsigned sum_n = 0, all_n;
+      u64 sum_w = 0, all_w;
+#pragma unroll
+      for (int y = 0; y < kPer; ++y) {
+        u64 x = low[y] + (up[y] << 32);
+        if (!high) x = __float2ull_rn((float)x * (row.at_end(kPer * tid + y) * scale));
+        sum_n += cn[y], sum_w += x;
+        upto_n[y] = sum_n, upto_w[y] = sum_w;
+      }
+      const unsigned before_n = up_to(sum_n, sh.sums, all_n) - sum_n;
+      const u64 before_w = up_to(sum_w, sh.sums2, all_w) - sum_w;
+#pragma unroll
+      for (int y = 0; y < kPer; ++y) upto_n[y] += before_n, upto_w[y] += before_w;
+      return Found{0, all_n, all_w};
+    };
+    // The bin in which, after `before`, the target is reached (it is reached in one).
+    auto search = [&](bool weights, u64 target, const Found& f) {
+      __syncthreads();
+      unsigned was_n = __shfl_up_sync(~0u, upto_n[kPer - 1], 1);
+      u64 was_w = __shfl_up_sync(~0u, upto_w[kPer - 1], 1);
+      if (lane == 31) sh.sums[warp] = upto_n[kPer - 1], sh.sums2[warp] = upto_w[kPer - 1];
+      __syncthreads();
+      if (lane == 0) was_n = warp ? (unsigned)sh.sums[warp - 1] : 0u, was_w = warp ? sh.sums2[warp - 1] : 0ull;
+#pragma unroll
+      for (int y = 0; y < kPer; ++y) {
+        const u64 was = weights ? f.weight + was_w : f.count + (u64)was_n;
+        const u64 now = weights ? f.weight + upto_w[y] : f.count + (u64)upto_n[y];
+        if (was < target && now >= target) sh.found = Found{kPer * tid + y, f.count + was_n, f.weight + was_w};
+        was_n = upto_n[y], was_w = upto_w[y];
+      }
+      __syncthreads();
+      return sh.found;
+    };
+    // X of a target among the bins, and the weight up to it.
+    auto find = [&](float from, bool weights, u64 target, u64& kept) {
+      Found f = search(weights, target, none);
+      const int bin = f.bin;
+      // (of equal logits or logits that are nearly so, there may be too many in a bin)
+      float to = INFINITY;
+      if (row.by > 0.f) {
+        // (bins are rounded to the nearest whole number)
+        if (bin < kBins - 1) from = fmaxf(from, row.least((bin + 0.5f) / row.by));
+        if (bin > 0) to = row.most((bin - 0.5f) / row.by);
+      }
+      unsigned listed = gather(from, to, [&](float x, u64) { return row.bin(x) == bin; });
+      if (listed > kList) {
+        u64 most = 0, least = 0;  // (least: as the largest complement)
+        each(from, [&](float x, int i) {
+          const u64 o = order_of(x, lo + i);
+          if (row.bin(x) == bin) most = max(most, o), least = max(least, ~o);
+        });
+        most = max_warp(most), least = max_warp(least);
+        __syncthreads();
+        if (lane == 0) sh.sums[warp] = most, sh.sums2[warp] = least;
+        __syncthreads();
+        for (int w = 0; w < kWarps; ++w) most = max(most, sh.sums[w]), least = max(least, sh.sums2[w]);
+        if (tid < blocks) put(sh.most[rank], most, tid), put(sh.least[rank], least, tid);
+        sync();
+        for (int r = 0; r < blocks; ++r) most = max(most, sh.most[r]), least = max(least, sh.least[r]);
+        least = ~least;
+        unsigned keep_n[kPer];
+        u64 keep_w[kPer];
+#pragma unroll
+        for (int y = 0; y < kPer; ++y) keep_n[y] = upto_n[y], keep_w[y] = upto_w[y];
+        while (listed > kList) {
+          const int shift = max(0, 64 - __clzll((long long)(most - least)) - kPartBits);
+          for (int i = tid; i < kParts; i += kThreads) sh.parts.n[i] = sh.parts.lo[i] = sh.parts.hi[i] = 0;
           __syncthreads();
-          for (int k = 2; k <= size; k *= 2)
-            for (int j = k / 2; j; j /= 2) {
-              for (int x = tid; x < size / 2; x += kThreads) {
-                const int i = 2 * x - (x & (j - 1)), y = i + j;
-                const u64 p = sh.list[i], q = sh.list[y];
-                if ((p < q) == !(i & k)) sh.list[i] = q, sh.list[y] = p;
-              }
-              __syncthreads();
-            }
-          u64 before = f.weight;
-          for (int i0 = 0; i0 < size; i0 += kThreads) {
-            const int i = i0 + tid;
-            const bool some = i < (int)listed;
-            const u64 w = some && (weights || want_weight) ? units(row.weight(logit_of(sh.list[i]))) : 0;
-            u64 pre = w;
-            for (int o = 1; o < 32; o <<= 1) {
-              const u64 x = __shfl_up_sync(~0u, pre, o);
-              if (lane >= o) pre += x;
-            }
-            if (lane == 31) sh.sums[warp] = pre;
-            __syncthreads();
-            u64 all = 0;
-            for (int x = 0; x < kWarps; ++x) {
-              if (x < warp) pre += sh.sums[x];
-              all += sh.sums[x];
-            }
-            // the last one kept: the target is not reached before it, and is with it
-            const u64 prev = weights ? before + pre - w : f.count + (u64)i, now = weights ? before + pre : f.count + (u64)i + 1;
-            if (some && prev < target && now >= target)
-              for (int r = 0; r < blocks; ++r) {
-                put(sh.cut, sh.list[i], r);
-                put(sh.kept, before + pre, r);
-              }
-            before += all;
-            __syncthreads();
+          each(from, [&](float x, int i) {
+            const u64 o = order_of(x, lo + i);
+            if (o < least || o > most) return;
+            const int part = (int)((most - o) >> shift);
+            atomicAdd(&sh.parts.n[part], 1u);
+            if (!by_p) return;
+            const u64 w = units(row.weight(x));
+            const unsigned l = (unsigned)w, was = l ? atomicAdd(&sh.parts.lo[part], l) : 0u;
+            const unsigned h = (unsigned)(w >> 32) + (was + l < was);
+            if (h) atomicAdd(&sh.parts.hi[part], h);
+          });
+          sync();
+          const Found all = sum_up(sh.parts.n, sh.parts.lo, sh.parts.hi, 0.f, true, by_p);
+          // (the bins' weights are rounded otherwise: what they promise may be a little out of reach)
+          f = search(weights, weights ? min(target, f.weight + all.weight) : target, f);
+          most -= (u64)f.bin << shift;
+          if (most - least >> shift) least = most - ((1ull << shift) - 1);
+          const u64 z = most, a = least;
+          listed = gather(logit_of(a), logit_of(z), [&](float, u64 o) { return o >= a && o <= z; });
+        }
+#pragma unroll
+        for (int y = 0; y < kPer; ++y) upto_n[y] = keep_n[y], upto_w[y] = keep_w[y];
+      }
+      const u64 x = cut_from(listed, !weights, weights, target, f);
+      kept = sh.kept;
+      return x;
+    };
+
+    // Ids at or above `from` are looked at.
+    float from = -INFINITY;
+    u64 target = 0;  // of top-p alone
+    bool done = false;
+    if (ids <= room) {  // few ids: all of them sorted
+      done = true;
+    } else if (by_k) {
+      // (the sixteen high bits of the k-th largest are enough)
+      unsigned bits = 0;
+      unsigned mine[blocks];
+#pragma unroll
+      for (int r = 0; r < blocks; ++r) {
+        const float x = sh.tops[r * kThreads + tid];
+        mine[r] = x > -INFINITY ? (unsigned)(order_of(x, 0) >> kIdBits) : 0u;
+      }
+#pragma unroll 1
+      for (int bit = 30; bit >= 16; bit -= 2) {  // (two bits at once: the numbers at or above three borders)
+        unsigned over = 0, most = 0;
+#pragma unroll
+        for (int r = 0; r < blocks; ++r) {
+          over += (mine[r] >= (bits | 1u << bit) ? 1u : 0u) + (mine[r] >= (bits | 2u << bit) ? 1u << 16 : 0u);
+          most += mine[r] >= (bits | 3u << bit);
+        }
+        over = __reduce_add_sync(~0u, over), most = __reduce_add_sync(~0u, most);
+        __syncthreads();
+        if (lane == 0) sh.sums[warp] = (u64)most << 32 | over;
+        __syncthreads();
+        u64 all = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) all += sh.sums[w];
+        const unsigned k = (unsigned)top_k;
+        bits |= ((unsigned)(all >> 32) >= k ? 3u : (unsigned)(all >> 16 & 0xFFFFu) >= k ? 2u : (unsigned)(all & 0xFFFFu) >= k ? 1u : 0u) << bit;
+      }
+      __syncthreads();
+      if (bits) from = logit_of((u64)bits << kIdBits);
+    } else {
+      sync();
+      float z = 0.f;
+      for (int r = 0; r < blocks; ++r) z += sh.z[r];
+      if (row.c2 > 0.f) from = row.least(-log2f(0.99f * (1.f - top_p) * (z / ids)) / row.c2);
+      target = max(__float2ull_ru(top_p * z * kUnit), 1ull);
+    }
+    if (done || (by_k && top_k <= kDirect)) {
+      const unsigned listed = gather(from, INFINITY, [](float, u64) { return true; });
+      done = listed <= kList;
+      if (done) cut = cut_from(listed, by_k, by_p, 0, none);
+    }
+    if (!done) {
+      row.reach(from > -INFINITY ? row.below(from) : INFINITY);
+      for (int i = tid; i < kBins; i += kThreads) sh.bins.n[i] = sh.bins.w[i] = 0;
+      __syncthreads();
+      const float scale = fminf(4.1e9f / a.each, 8e6f);  // (a share is 2^0.04 at most)
+      const float at_least = fmaxf(from, -FLT_MAX);
+      constexpr int kLines = 8 / N;  // eight ids at once, without branches: what one waits for, the others do too
+      for (int v0 = tid; v0 < count_v; v0 += kLines * kThreads) {
+        float x[8];
+        int bin[8];
+        float w[8];
+        bool any = false;
+#pragma unroll
+        for (int y = 0; y < 8; y += 2) {
+          const int v = v0 + y / N * kThreads;
+          const Two t = v < count_v ? L::pair(lines[v], y % N / 2) : Two{-INFINITY, -INFINITY};
+          x[y] = t.x, x[y + 1] = t.y;
+          any = any || fmaxf(t.x, t.y) >= at_least;
+        }
+        if (!any) continue;
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          const float in = row.bin_in(x[y]);
+          bin[y] = Row::low(in);
+          w[y] = by_p ? fmaf(row.share(x[y], in), scale, kWhole) : 0.f;
+        }
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          if (by_k && x[y] >= at_least) atomicAdd(&sh.bins.n[bin[y]], 1u);
+          if (by_p && x[y] >= at_least) atomicAdd(&sh.bins.w[bin[y]], (unsigned)Row::low(w[y]));
+        }
+      }
+      sync();
+      const Found all = sum_up(sh.bins.n, sh.bins.w, nullptr, kUnit / scale, by_k, by_p);
+      u64 kept = all.weight, unused;
+      if (by_k && (unsigned)top_k < all.count) cut = find(from, false, top_k, kept);
+      if (by_p) cut = find(from, true, min(by_k ? target_of(kept) : target, all.weight), unused);
+    }
+  }
+
+  // ---- the draw: the largest w / e is the smallest e 2^((m - l) c)
+  Pick p = {INFINITY, INT_MAX, INT_MAX};
+  {
+    const float last = cut ? logit_of(cut) : -INFINITY;  // the last logit that is kept, and of those ids that have it the last
+    const int last_id = cut ? (1 << kIdBits) - 1 - (int)(cut & ((1u << kIdBits) - 1u)) : INT_MAX;
+    float from = first ? row.m : last;
+    if (!first && min_p > 0.f && row.c2 > 0.f) from = fmaxf(from, row.least(-log2f(min_p) / row.c2));
+    from = fmaxf(from, -FLT_MAX);
+    const bool any_of = cut || min_p > 0.f;  // not all ids of logits from `from` on
+    const float* noise = s.d_noise + b * s.noise_stride + lo;
+    const bool aligned = ((uintptr_t)(noise - pad) & 15) == 0;  // a line's noise is, too
+    constexpr int kLines = 16 / N;  // sixteen ids of a thread at once
+    int best = 0;  // place of the best id, first line's and its number of the sixteen
+    for (int v0 = tid; v0 < count_v; v0 += kLines * kThreads) {
+      uint4 r[kLines], q[4];
+      bool some[kLines];
+#pragma unroll
+      for (int y = 0; y < kLines; ++y) {
+        const int v = v0 + y * kThreads, i = v * N - pad;
+        r[y] = lines[min(v, count_v - 1)];
+        const float t = L::top(r[y]);
+        some[y] = v < count_v && t >= from;
+        if (some[y] && t == row.m) {
+          const T* x = reinterpret_cast<const T*>(lines + v);
+          for (int e = N - 1; e >= 0; --e)
+            if (value(x[e]) == row.m) p.first = min(p.first, lo + i + e);
+        }
+        some[y] = some[y] && !first;
+        const bool whole = aligned && lo + i >= 0 && lo + i + N <= s.V;  // (nothing outside the row is read)
+#pragma unroll
+        for (int e = 0; e < N / 4; ++e) {
+          uint4& o = q[y * (N / 4) + e];
+          o = make_uint4(0x7F800000u, 0x7F800000u, 0x7F800000u, 0x7F800000u);
+          load_if(o, noise + i + 4 * e, some[y] && whole);
+          if (some[y] && !whole) {
+            float n4[4] = {INFINITY, INFINITY, INFINITY, INFINITY};
+#pragma unroll
+            for (int z = 0; z < 4; ++z) load_if(n4[z], noise + i + 4 * e + z, i + 4 * e + z >= 0 && i + 4 * e + z < n);
+            o = make_uint4(__float_as_uint(n4[0]), __float_as_uint(n4[1]), __float_as_uint(n4[2]), __float_as_uint(n4[3]));
           }
         }
-        cluster_sync();
-        kept = sh.kept;
-        return sh.cut;
       }
-      // ---- the next level
-      const int bits = 64 - __clzll((long long)(most - least));
-      shift = max(0, bits - kBinBits);
-      count(false, !weights, weights || want_weight);
-      const Found g = search(false, weights, target, f);
-      most -= (u64)g.bin << shift;
-      if (most - least >> shift) least = most - ((1ull << shift) - 1);
-      f = g;
+#pragma unroll
+      for (int y = 0; y < kLines; ++y) {
+        if (!some[y]) continue;
+#pragma unroll
+        for (int z = 0; z < N; z += 2) {
+          const Two x = L::pair(r[y], z / 2);
+          const Two t = mul2(fma2(x, -0.5f, 0.5f * row.m), Two{row.c2, row.c2});
+          const uint4 o = q[y * (N / 4) + z / 4];
+          const float e0 = __uint_as_float(z % 4 ? o.z : o.x), e1 = __uint_as_float(z % 4 ? o.w : o.y);
+          float s0 = e0 * exp2_fast(t.x), s1 = e1 * exp2_fast(t.y);  // (infinite where the id is not admitted)
+          if (any_of) {
+            const int id = lo + (v0 + y * kThreads) * N + z - pad;
+            const bool in0 = x.x > last || (x.x == last && id <= last_id), in1 = x.y > last || (x.y == last && id + 1 <= last_id);
+            s0 = in0 && !(min_p > 0.f && exp2_fast(-t.x) < min_p) ? s0 : INFINITY;
+            s1 = in1 && !(min_p > 0.f && exp2_fast(-t.y) < min_p) ? s1 : INFINITY;
+          }
+          if (e0 >= FLT_MIN && s0 < p.score) p.score = s0, best = v0 * 16 + y * N + z;
+          if (e1 >= FLT_MIN && s1 < p.score) p.score = s1, best = v0 * 16 + y * N + z + 1;
+        }
+      }
     }
-  };
-
-  // ---- the weights' sum, and the first level's bins
-  float z = 0.f;
-  for (int i = tid; i < n; i += kThreads) {
-    const float x = value(vals[i]);
-    if (x > -INFINITY) z += row.weight(x);  // (-inf has no weight where T is infinite either)
-  }
-  z = sum_warp(z);
-  if (lane == 0) sh.zw[warp] = z;
-  __syncthreads();
-  if (tid == 0) {
-    z = 0.f;
-    for (int x = 0; x < kWarps; ++x) z += sh.zw[x];
-    put(sh.zs[rank], z, 0);
-  }
-  if (by_k || by_p) {
-    count(true, true, by_p);
-    unsigned all_n = 0;
-    u64 all_w = 0;
-    for (int r = 0; r < blocks; ++r) all_n += get(sh.part_n[0], r), all_w += get(sh.part_w[0], r);
-    u64 kept = all_w, unused;
-    if (by_k && (unsigned)top_k < all_n) cut = find(false, top_k, by_p, kept);
-    if (by_p) {
-      const u64 target = (u64)ceil((double)top_p * (double)kept);
-      cut = find(true, min(max(target, 1ull), kept), false, unused);
-    }
-  }
-
-  // ---- the draw
-  Pick p = {0.f, 0.f, INT_MAX, INT_MAX};
-  const float* e = s.d_noise + b * s.noise_stride + lo;
-  for (int i = tid; i < n; i += kThreads) {
-    const float x = value(vals[i]);
-    if (x == row.m) p.first = min(p.first, lo + i);
-    if (row.first || !(x > -INFINITY) || (cut && order_of(x, lo + i) < cut)) continue;
-    const float w = row.weight(x);
-    if (min_p > 0.f && !(w >= min_p)) continue;
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e[i]));
-    const float score = w * r;
-    if (score > p.score && score < INFINITY) p.score = score, p.logit = x, p.id = lo + i;
+    if (p.score < INFINITY) p.id = lo + (best / 16 + best % 16 / N * kThreads) * N + best % N - pad;
   }
   p = best_warp(p);
   if (lane == 0) sh.picks[warp] = p;
@@ -472,19 +826,21 @@ __global__ void __launch_bounds__(kThreads) k_sample(const SampleArgs a) {
     p = best_warp(sh.picks[lane % kWarps]);
     if (lane == 0) {
       put(sh.pick[rank].score, p.score, 0);
-      put(sh.pick[rank].logit, p.logit, 0);
       put(sh.pick[rank].id, p.id, 0);
       put(sh.pick[rank].first, p.first, 0);
+      // (its logit)
+      put(sh.top[rank], p.score < INFINITY ? value(reinterpret_cast<const T*>(lines)[p.id - lo + pad]) : row.m, 0);
     }
   }
-  cluster_sync();
+  sync();
   if (rank == 0 && warp == 0) {
     p = best_warp(sh.pick[lane % blocks]);
-    z = sum_warp(lane < blocks ? sh.zs[lane] : 0.f);
     if (lane == 0) {
-      const bool drawn = p.score > 0.f;
-      const int token = drawn ? p.id : p.first;
-      const float x = drawn ? p.logit : row.m;
+      float z = 0.f, x = row.m;
+      for (int r = 0; r < blocks; ++r) z += sh.z[r];
+      const int token = p.score < INFINITY ? p.id : p.first;
+      for (int r = 0; r < blocks; ++r)
+        if (p.score < INFINITY && sh.pick[r].id == p.id) x = sh.top[r];
       s.d_tokens[b] = token;
       if (s.d_logprob) s.d_logprob[b] = fminf((-row.below(x) * row.c2 - log2f(z)) * kLn2, 0.f);
       s.d_status[b] = token == s.eos ? GRID_ST_COMPLETE : GRID_ST_OK;
@@ -507,26 +863,28 @@ extern "C" int grid_sample(const grid_sample_step* s, void* stream) {
     return set_error(GRID_E_INVALID_ARG, "grid_sample: negative stride or unaligned pointer");
   if (s->B > 65535 || s->V > kMaxIds)
     return set_error(GRID_E_TOO_LARGE, "grid_sample: more than 65535 rows or 393216 ids");
-  SampleArgs a = {*s, 1, 0};
-  while (a.blocks < kMaxBlocks && s->V > 4096 * a.blocks) a.blocks *= 2;
-  a.each = ((s->V + a.blocks - 1) / a.blocks + 31) & ~31;
-  const size_t smem = kSharedRoom + 2 * (size_t)(kBins / a.blocks) * 12 + (size_t)a.each * size;
-  auto go = [&](auto kernel, std::atomic<uint64_t>& ready) {
+  // (blocks by the vocabulary alone: a row's sums do not depend on the batch)
+  int blocks = 1, log = 0;
+  while (blocks < kMaxBlocks && s->V > 4096 * blocks) blocks *= 2, ++log;
+  const SampleArgs a = {*s, ((s->V + blocks - 1) / blocks + 31) & ~31};
+  const size_t smem = kSharedRoom + (size_t)a.each * size + 32;
+  static std::atomic<uint64_t> ready[2][4];  // the devices where a kernel has its room in shared memory
+  auto go = [&](auto kernel) {
+    std::atomic<uint64_t>& done = ready[size == 4][log];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    // (the room for shared memory is set once per device)
-    if (e == cudaSuccess && !(dev < 64 && ready.load() >> dev & 1)) {
+    if (e == cudaSuccess && !(dev < 64 && done.load() >> dev & 1)) {
       e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 << 10);
-      if (e == cudaSuccess && dev < 64) ready.fetch_or(1ull << dev);
+      if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev);
     }
     if (e != cudaSuccess) return e;
-    return launch_cluster(kernel, dim3((unsigned)(s->B * a.blocks)), dim3(kThreads), smem, a.blocks, (cudaStream_t)stream, a);
+    return launch_cluster(kernel, dim3((unsigned)(s->B * blocks)), dim3(kThreads), smem, blocks, (cudaStream_t)stream, a);
   };
-  static std::atomic<uint64_t> ready[2];
-  if (size == 4)
-    GRID_CUDA(go(k_sample<float>, ready[0]));
-  else
-    GRID_CUDA(go(k_sample<uint16_t>, ready[1]));
+  auto launch = [&](auto type) {
+    using T = decltype(type);
+    return blocks == 1 ? go(k_sample<T, 1>) : blocks == 2 ? go(k_sample<T, 2>) : blocks == 4 ? go(k_sample<T, 4>) : go(k_sample<T, 8>);
+  };
+  GRID_CUDA(size == 4 ? launch(0.f) : launch((uint16_t)0));
   GRID_CUDA(cudaGetLastError());
   return GRID_OK;
 }
