@@ -24,7 +24,7 @@
 // min-p needs no X: w >= min_p is asked of every id.
 //
 // Sums of weights are integers, so that the order of the atomic additions does not
-// matter: in a bin in steps of 2^-17 or less of its weights (what fits 32 bits if
+// matter: in a bin in steps of 2^-16 or less of its weights (what fits 32 bits if
 // all of a block's ids are in it), elsewhere of 2^-40 of the largest.
 #include <atomic>
 #include <cfloat>
@@ -79,7 +79,7 @@ struct Shared {
   };
   u64 list[2][kList];                      // of one gathering and the next: a block's ids in a part of its own
   // what every block of the row writes here
-  float top[kMaxBlocks];                   // its largest admitted logit
+  float top[kMaxBlocks], low[kMaxBlocks];  // its largest admitted logit, the smallest of its threads' largest (negative)
   unsigned ids[kMaxBlocks];                // admitted
   float z[kMaxBlocks];                     // sum of weights
   unsigned in[2][kMaxBlocks];              // ids in the range that is gathered
@@ -90,7 +90,7 @@ struct Shared {
   u64 target, kept;
   unsigned staged, at;
   u64 sums[kWarps], sums2[kWarps];
-  float2 warps[kWarps];
+  float3 warps[kWarps];
   Pick picks[kWarps];
 };
 constexpr int kSharedRoom = (sizeof(Shared) + 127) & ~127;
@@ -250,6 +250,8 @@ __device__ __forceinline__ float logit_of(u64 o) {
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 
+__device__ __forceinline__ int id_of(u64 o) { return (1 << kIdBits) - 1 - (int)(o & ((1u << kIdBits) - 1u)); }
+
 // A row's weights and bins.
 struct Row {
   float c2;     // 2 log2(e) / T
@@ -258,21 +260,19 @@ struct Row {
   // half of m - l: of the halves, since the difference of two logits may be past the type
   __device__ __forceinline__ float below(float x) const { return fmaf(0.5f, m, -0.5f * x); }
   __device__ __forceinline__ float weight(float x) const { return exp2_fast(-below(x) * c2); }
-  // The bin, as a whole number in the low bits of a float of 2^23 and more: conversions run at an eighth of an addition's rate.
-  __device__ __forceinline__ float bin_in(float x) const { return fminf(below(x) * by, (float)(kBins - 1)) + kWhole; }
+  // Where it lies among the bins, and the nearest one: a whole number in the low bits of a float of 2^23 and more (conversions
+  // run at an eighth of an addition's rate).
+  __device__ __forceinline__ float place(float x) const { return fminf(below(x) * by, (float)(kBins - 1)); }
   static __device__ __forceinline__ int low(float whole) { return __float_as_int(whole) & 0x7FFFFF; }
-  __device__ __forceinline__ int bin(float x) const { return low(bin_in(x)); }
+  __device__ __forceinline__ int bin(float x) const { return low(place(x) + kWhole); }
   __device__ __forceinline__ void reach(float range) {  // bins of halves of m - l up to `range`
     range = fminf(range, fminf(kFirstRange / c2, FLT_MAX));
     by = range > 0.f ? fminf(kBins / range, FLT_MAX) : 0.f;
     width = c2 / by;
-    if (!(width <= 2.f * kFirstRange / kBins)) width = 0.f;  // (no bins, or T past what they can tell apart: as they are)
+    if (!(by > 0.f)) width = 0.f;  // (all of one logit)
   }
-  // A bin's weights are held relative to this, the weight half a bin behind its end: 2^(width/2) to 2^(3 width/2) times it (less in the last bin).
-  __device__ __forceinline__ float share(float x, float bin_in) const {
-    return exp2_fast(fmaf(-below(x), c2, fmaf(bin_in - kWhole, width, width)));
-  }
-  __device__ __forceinline__ float at_end(int bin) const { return exp2_fast(-fmaf((float)bin, width, width)); }
+  // The weight in a bin's middle.
+  __device__ __forceinline__ float middle(int bin) const { return exp2_fast(-(float)bin * width); }
   // Nothing below this has a half of m - l of up to h: the roundings of both, 2^-23 of h or of a logit, are allowed for.
   __device__ __forceinline__ float least(float h) const { return m - 2.f * h - 1e-6f * (h + fabsf(m)); }
   // Nothing above this has one of h or more.
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
   const bool greedy = !(temp > 0.f);
   const bool first = greedy || top_k == 1 || top_p <= 0.f || min_p > 1.f;  // only the first id is kept
   Row row;
-  row.c2 = fminf((greedy ? 1.f : 1.f / temp) * (2.f * kLog2e), FLT_MAX);
+  row.c2 = fminf((greedy ? 1.f : 1.f / temp) * (2.f * kLog2e), 1e37f);  // (so that 1,024 bins of 40 exponents have a width)
 
   // ---- the block's logits in lines of 16 bytes as they lie in memory: line v holds the block's ids v N - pad .. + N - 1
   int pad = 0, count_v = 0;
@@ -317,35 +317,33 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     const uint32_t* mask = s.d_mask ? s.d_mask + b * s.mask_stride + (lo >> 5) : nullptr;
     pad = (int)((uintptr_t)l & 15) / (int)sizeof(T);
     count_v = n > 0 ? (pad + n + N - 1) / N : 0;
-    constexpr int kAhead = 4;
+    // (the mask's words first, so that no logit waits for its bit: the lists are not in use yet)
+    uint32_t* const words = reinterpret_cast<uint32_t*>(sh.list);
+    static_assert(kMaxIds / kMaxBlocks / 32 < 4 * kList);
+    if (mask) {
+      for (int w = tid; w <= (n + 31) / 32; w += kThreads) words[w] = w < (n + 31) / 32 ? mask[w] : 0u;
+      __syncthreads();
+    }
+    constexpr int kAhead = sizeof(T) == 2 ? 4 : 8;
     const int inner = n - N;  // a whole line begins at an id of 0 .. inner
-    auto bits_of = [&](int v) {
-      const int i = v * N - pad;
-      if (i < 0 || i > inner) return 0u;
-      if (!mask) return (1u << N) - 1u;
-      const uint32_t* w = mask + (i >> 5);
-      return __funnelshift_r(w[0], (i & 31) > 32 - N ? w[1] : 0u, i & 31) & ((1u << N) - 1u);
-    };
-    unsigned bits[kAhead];
-#pragma unroll
-    for (int y = 0; y < kAhead; ++y) bits[y] = bits_of(tid + y * kThreads);
     for (int v0 = tid; v0 < count_v; v0 += kAhead * kThreads) {
       uint4 r[kAhead];
+      unsigned bits[kAhead];
 #pragma unroll
       for (int y = 0; y < kAhead; ++y) {
+        const int i = (v0 + y * kThreads) * N - pad;
+        bits[y] = 0u;
+        if (i >= 0 && i <= inner)
+          bits[y] = mask ? __funnelshift_r(words[i >> 5], words[(i >> 5) + 1], i & 31) & ((1u << N) - 1u) : (1u << N) - 1u;
         r[y] = make_uint4(0, 0, 0, 0);
-        load_if(r[y], l + ((long long)(v0 + y * kThreads) * N - pad), bits[y] != 0);
+        load_if(r[y], l + i, bits[y] != 0);
       }
-      unsigned next[kAhead];
-#pragma unroll
-      for (int y = 0; y < kAhead; ++y) next[y] = bits_of(v0 + (kAhead + y) * kThreads);
 #pragma unroll
       for (int y = 0; y < kAhead; ++y) {
         const uint4 x = L::admit(r[y], bits[y]);
         if (v0 + y * kThreads < count_v) lines[v0 + y * kThreads] = x;
         top = fmaxf(top, L::top(x));
         ids += __popc(bits[y]);
-        bits[y] = next[y];
       }
     }
     // lines that are not whole: the first and the last, an id to a thread
@@ -354,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       const int v = tid < N ? 0 : count_v - 1, i = v * N + tid % N - pad;
       if (v * N - pad < 0 || v * N - pad > inner) {
         T x = L::none();
-        if (i >= 0 && i < n && (!mask || mask[i >> 5] >> (i & 31) & 1u)) {
+        if (i >= 0 && i < n && (!mask || words[i >> 5] >> (i & 31) & 1u)) {
           x = kept_as(l[i]);
           ++ids;
         }
@@ -365,19 +363,24 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
   }
   // ---- the row's largest logit, all threads' largest, and how many ids are admitted
   const bool wants_k = !first && top_k > 0;
+  unsigned* const top_bins = reinterpret_cast<unsigned*>(sh.list[0]);  // (the first list is the other one)
+  static_assert(sizeof(sh.list[0]) >= kBins * sizeof(unsigned));
   {
-    const float t = max_warp(top);
+    const float t = max_warp(top), u = max_warp(top > -INFINITY ? -top : -INFINITY);
     const unsigned c = __reduce_add_sync(~0u, ids);
-    if (lane == 0) sh.warps[warp] = make_float2(t, __uint_as_float(c));
+    if (lane == 0) sh.warps[warp] = make_float3(t, u, __uint_as_float(c));
     __syncthreads();
+    for (int i = tid; i < kBins; i += kThreads) top_bins[i] = 0;
     if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (the others are there)
     if (wants_k)
       for (int r = 0; r < blocks; ++r) put(sh.tops[rank * kThreads + tid], top, r);
     if (tid < blocks) {
-      float x = -INFINITY;
+      float x = -INFINITY, y = -INFINITY;
       unsigned all = 0;
-      for (int w = 0; w < kWarps; ++w) x = fmaxf(x, sh.warps[w].x), all += __float_as_uint(sh.warps[w].y);
+      for (int w = 0; w < kWarps; ++w)
+        x = fmaxf(x, sh.warps[w].x), y = fmaxf(y, sh.warps[w].y), all += __float_as_uint(sh.warps[w].z);
       put(sh.top[rank], x, tid);
+      put(sh.low[rank], y, tid);
       put(sh.ids[rank], all, tid);
     }
     sync();
@@ -437,6 +440,16 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       put(sh.z[rank], z, tid);
     }
   }
+
+  // (min-p by the exponent: the difference comes first, so that it holds at every temperature)
+  const float t_most = min_p > 0.f ? -log2f(min_p) : INFINITY;
+  auto write = [&](int token, float x) {
+    float z = 0.f;
+    for (int r = 0; r < blocks; ++r) z += sh.z[r];
+    s.d_tokens[b] = token;
+    if (s.d_logprob) s.d_logprob[b] = fminf((-row.below(x) * row.c2 - log2f(z)) * kLn2, 0.f);
+    s.d_status[b] = token == s.eos ? GRID_ST_COMPLETE : GRID_ST_OK;
+  };
 
   // ---- the cut X: ids of order X and more are kept
   const bool by_k = wants_k && (unsigned)top_k < ids, by_p = !first && top_p < 1.f;
@@ -547,36 +560,31 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     // Of the bins kPer tid .. + kPer - 1 of all blocks: the ids and the weight up to and with each.
     unsigned upto_n[kPer];
     u64 upto_w[kPer];
-    auto sum_up = [&](const unsigned* n, const unsigned* w, const unsigned* high, float scale, bool counts, bool weights) {
+    auto sum_up = [&](const unsigned* n, const unsigned* w, const unsigned* high, float scale) {
       u64 low[kPer] = {}, up[kPer] = {};
       unsigned cn[kPer] = {};
-      const bool in = !high || kPer * tid < kParts;
+      auto add = [&](const unsigned* of, auto& sums) {
 #pragma unroll
-      for (int r0 = 0; r0 < blocks; r0 += kMaxBlocks / 2) {  // (four blocks' at once)
-        constexpr int kAt = blocks < kMaxBlocks / 2 ? blocks : kMaxBlocks / 2;
-        uint4 x[kAt] = {}, y[kAt] = {}, z[kAt] = {};
-        if (in && counts)
+        for (int r0 = 0; r0 < blocks; r0 += 4) {  // (four blocks' at once)
+          constexpr int kAt = blocks < 4 ? blocks : 4;
+          uint4 x[kAt];
 #pragma unroll
-          for (int r = 0; r < kAt; ++r) x[r] = get4(n + kPer * tid, r0 + r);
-        if (in && weights)
+          for (int r = 0; r < kAt; ++r) x[r] = get4(of + kPer * tid, r0 + r);
 #pragma unroll
-          for (int r = 0; r < kAt; ++r) y[r] = get4(w + kPer * tid, r0 + r);
-        if (in && weights && high)
-#pragma unroll
-          for (int r = 0; r < kAt; ++r) z[r] = get4(high + kPer * tid, r0 + r);
-#pragma unroll
-        for (int r = 0; r < kAt; ++r) {
-          cn[0] += x[r].x, cn[1] += x[r].y, cn[2] += x[r].z, cn[3] += x[r].w;
-          low[0] += y[r].x, low[1] += y[r].y, low[2] += y[r].z, low[3] += y[r].w;
-          up[0] += z[r].x, up[1] += z[r].y, up[2] += z[r].z, up[3] += z[r].w;
+          for (int r = 0; r < kAt; ++r) sums[0] += x[r].x, sums[1] += x[r].y, sums[2] += x[r].z, sums[3] += x[r].w;
         }
+      };
+      if (!high || kPer * tid < kParts) {
+        if (n) add(n, cn);
+        if (w) add(w, low);
+        if (high) add(high, up);
       }
       unsigned sum_n = 0, all_n;
       u64 sum_w = 0, all_w;
 #pragma unroll
       for (int y = 0; y < kPer; ++y) {
         u64 x = low[y] + (up[y] << 32);
-        if (!high) x = __float2ull_rn((float)x * (row.at_end(kPer * tid + y) * scale));
+        if (!high) x = __float2ull_rn((float)x * (row.middle(kPer * tid + y) * scale));
         sum_n += cn[y], sum_w += x;
         upto_n[y] = sum_n, upto_w[y] = sum_w;
       }
@@ -604,6 +612,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       __syncthreads();
       return sh.found;
     };
+    bool ready = false;  // the sums are of the bins
     // X of a target among the bins, and the weight up to it.
     auto find = [&](float from, bool weights, u64 target, u64& kept) {
       Found f = search(weights, target, none);
@@ -631,10 +640,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
         sync();
         for (int r = 0; r < blocks; ++r) most = max(most, sh.most[r]), least = max(least, sh.least[r]);
         least = ~least;
-        unsigned keep_n[kPer];
-        u64 keep_w[kPer];
-#pragma unroll
-        for (int y = 0; y < kPer; ++y) keep_n[y] = upto_n[y], keep_w[y] = upto_w[y];
+        ready = false;
         while (listed > kList) {
           const int shift = max(0, 64 - __clzll((long long)(most - least)) - kPartBits);
           for (int i = tid; i < kParts; i += kThreads) sh.parts.n[i] = sh.parts.lo[i] = sh.parts.hi[i] = 0;
@@ -651,7 +657,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
             if (h) atomicAdd(&sh.parts.hi[part], h);
           });
           sync();
-          const Found all = sum_up(sh.parts.n, sh.parts.lo, sh.parts.hi, 0.f, true, by_p);
+          const Found all = sum_up(sh.parts.n, sh.parts.lo, sh.parts.hi, 0.f);
           // (the bins' weights are rounded otherwise: what they promise may be a little out of reach)
           f = search(weights, weights ? min(target, f.weight + all.weight) : target, f);
           most -= (u64)f.bin << shift;
@@ -659,8 +665,6 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
           const u64 z = most, a = least;
           listed = gather(logit_of(a), logit_of(z), [&](float, u64 o) { return o >= a && o <= z; });
         }
-#pragma unroll
-        for (int y = 0; y < kPer; ++y) upto_n[y] = keep_n[y], upto_w[y] = keep_w[y];
       }
       const u64 x = cut_from(listed, !weights, weights, target, f);
       kept = sh.kept;
@@ -670,38 +674,33 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     // Ids at or above `from` are looked at.
     float from = -INFINITY;
     u64 target = 0;  // of top-p alone
-    bool done = false;
-    if (ids <= room) {  // few ids: all of them sorted
-      done = true;
+    const bool few = ids <= room;  // all of them are sorted
+    if (few) {
+      sync();  // (the sum of the weights)
     } else if (by_k) {
-      // (the sixteen high bits of the k-th largest are enough)
-      unsigned bits = 0;
-      unsigned mine[blocks];
+      // the bin that the k-th largest of the threads' largest lies in
+      float low = -INFINITY;
+      for (int r = 0; r < blocks; ++r) low = fmaxf(low, sh.low[r]);
+      const float range = row.below(-low);
+      row.by = range > 0.f ? fminf(kBins / range, FLT_MAX) : 0.f;
 #pragma unroll
       for (int r = 0; r < blocks; ++r) {
         const float x = sh.tops[r * kThreads + tid];
-        mine[r] = x > -INFINITY ? (unsigned)(order_of(x, 0) >> kIdBits) : 0u;
-      }
-#pragma unroll 1
-      for (int bit = 30; bit >= 16; bit -= 2) {  // (two bits at once: the numbers at or above three borders)
-        unsigned over = 0, most = 0;
-#pragma unroll
-        for (int r = 0; r < blocks; ++r) {
-          over += (mine[r] >= (bits | 1u << bit) ? 1u : 0u) + (mine[r] >= (bits | 2u << bit) ? 1u << 16 : 0u);
-          most += mine[r] >= (bits | 3u << bit);
-        }
-        over = __reduce_add_sync(~0u, over), most = __reduce_add_sync(~0u, most);
-        __syncthreads();
-        if (lane == 0) sh.sums[warp] = (u64)most << 32 | over;
-        __syncthreads();
-        u64 all = 0;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) all += sh.sums[w];
-        const unsigned k = (unsigned)top_k;
-        bits |= ((unsigned)(all >> 32) >= k ? 3u : (unsigned)(all >> 16 & 0xFFFFu) >= k ? 2u : (unsigned)(all & 0xFFFFu) >= k ? 1u : 0u) << bit;
+        if (x > -INFINITY) atomicAdd(&top_bins[row.bin(x)], 1u);
       }
       __syncthreads();
-      if (bits) from = logit_of((u64)bits << kIdBits);
+      const uint4 x = reinterpret_cast<const uint4*>(top_bins)[tid];
+      unsigned all;
+      const unsigned upto = up_to(x.x + x.y + x.z + x.w, sh.sums, all);
+      unsigned at = upto - (x.x + x.y + x.z + x.w);
+      const unsigned one[kPer] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int y = 0; y < kPer; ++y) {
+        if (at < (unsigned)top_k && at + one[y] >= (unsigned)top_k) sh.found.bin = kPer * tid + y;
+        at += one[y];
+      }
+      __syncthreads();
+      if (all >= (unsigned)top_k && row.by > 0.f && sh.found.bin < kBins - 1) from = row.least((sh.found.bin + 0.5f) / row.by);
     } else {
       sync();
       float z = 0.f;
@@ -709,48 +708,105 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       if (row.c2 > 0.f) from = row.least(-log2f(0.99f * (1.f - top_p) * (z / ids)) / row.c2);
       target = max(__float2ull_ru(top_p * z * kUnit), 1ull);
     }
-    if (done || (by_k && top_k <= kDirect)) {
+    if (few || (by_k && top_k <= kDirect)) {
       const unsigned listed = gather(from, INFINITY, [](float, u64) { return true; });
-      done = listed <= kList;
-      if (done) cut = cut_from(listed, by_k, by_p, 0, none);
-    }
-    if (!done) {
-      row.reach(from > -INFINITY ? row.below(from) : INFINITY);
-      for (int i = tid; i < kBins; i += kThreads) sh.bins.n[i] = sh.bins.w[i] = 0;
-      __syncthreads();
-      const float scale = fminf(4.1e9f / a.each, 8e6f);  // (a share is 2^0.04 at most)
-      const float at_least = fmaxf(from, -FLT_MAX);
-      constexpr int kLines = 8 / N;  // eight ids at once, without branches: what one waits for, the others do too
-      for (int v0 = tid; v0 < count_v; v0 += kLines * kThreads) {
-        float x[8];
-        int bin[8];
-        float w[8];
-        bool any = false;
-#pragma unroll
-        for (int y = 0; y < 8; y += 2) {
-          const int v = v0 + y / N * kThreads;
-          const Two t = v < count_v ? L::pair(lines[v], y % N / 2) : Two{-INFINITY, -INFINITY};
-          x[y] = t.x, x[y + 1] = t.y;
-          any = any || fmaxf(t.x, t.y) >= at_least;
+      if (listed <= kList) {  // what is kept is in the list: block 0 draws from it
+        if (rank) return;
+        cut_from(listed, by_k, by_p, 0, none);
+        Pick p = {INFINITY, INT_MAX, 0};
+        for (unsigned i = tid; i <= sh.at; i += kThreads) {
+          const u64 o = sh.list[turn][i];
+          const float x = logit_of(o), t = row.below(x) * row.c2, e = s.d_noise[b * s.noise_stride + id_of(o)];
+          const float score = e * exp2_fast(t);
+          if (e >= FLT_MIN && t <= t_most) better(p, Pick{score, id_of(o), 0});
         }
-        if (!any) continue;
-#pragma unroll
-        for (int y = 0; y < 8; ++y) {
-          const float in = row.bin_in(x[y]);
-          bin[y] = Row::low(in);
-          w[y] = by_p ? fmaf(row.share(x[y], in), scale, kWhole) : 0.f;
+        p = best_warp(p);
+        if (lane == 0) sh.picks[warp] = p;
+        __syncthreads();
+        if (warp == 0) {
+          p = best_warp(sh.picks[lane % kWarps]);
+          const bool drawn = p.score < INFINITY;
+          if (!drawn) p.id = id_of(sh.list[turn][0]);
+          // (the drawn id's logit)
+          float x = row.m;
+          for (unsigned i = lane; drawn && i <= sh.at; i += 32)
+            if (id_of(sh.list[turn][i]) == p.id) x = logit_of(sh.list[turn][i]);
+          x = -max_warp(-x);
+          if (lane == 0) write(p.id, x);
         }
-#pragma unroll
-        for (int y = 0; y < 8; ++y) {
-          if (by_k && x[y] >= at_least) atomicAdd(&sh.bins.n[bin[y]], 1u);
-          if (by_p && x[y] >= at_least) atomicAdd(&sh.bins.w[bin[y]], (unsigned)Row::low(w[y]));
-        }
+        return;
       }
-      sync();
-      const Found all = sum_up(sh.bins.n, sh.bins.w, nullptr, kUnit / scale, by_k, by_p);
-      u64 kept = all.weight, unused;
-      if (by_k && (unsigned)top_k < all.count) cut = find(from, false, top_k, kept);
-      if (by_p) cut = find(from, true, min(by_k ? target_of(kept) : target, all.weight), unused);
+    }
+    row.reach(from > -INFINITY ? row.below(from) : INFINITY);
+    // A weight is held as its share of the one in its bin's middle, 2^(f width) for an id f bins before it, f in -1/2 .. 1/2: a
+    // square in f is within 2^-21 of it (width is 0.08 at most).  So many units make a share of one.
+    const float scale = truncf(fminf(4.1e9f / a.each, 8e6f)), tilt = 0.6931471805599453f * row.width;
+    auto share = [&](float f) {  // (as a whole number)
+      return Row::low(fmaf(f, fmaf(f, 0.5f * tilt * tilt * scale, tilt * scale), scale + kWhole));
+    };
+    Found all;
+    u64 kept = 0;
+    for (int weights = !by_k; weights <= (int)by_p; ++weights) {  // by count, then by weight
+      if (!ready) {
+        for (int i = tid; i < kBins; i += kThreads) sh.bins.n[i] = sh.bins.w[i] = 0;
+        __syncthreads();
+        const float at_least = fmaxf(from, -FLT_MAX);
+        constexpr int kLines = 8 / N;
+        if (by_k && from > -INFINITY) {  // few ids in many lines
+          for (int v = tid; v < count_v; v += kThreads) {
+            const uint4 r = lines[v];
+            if (!(L::top(r) >= at_least)) continue;
+            unsigned some = 0;
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+              const Two x = L::pair(r, e / 2);
+              some |= (x.x >= at_least ? 1u << e : 0u) | (x.y >= at_least ? 2u << e : 0u);
+            }
+            for (; some; some &= some - 1) {
+              const float x = value(reinterpret_cast<const T*>(lines + v)[__ffs(some) - 1]);
+              const float at = row.place(x), in = at + kWhole;
+              atomicAdd(&sh.bins.n[Row::low(in)], 1u);
+              if (by_p) atomicAdd(&sh.bins.w[Row::low(in)], (unsigned)share(in - kWhole - at));
+            }
+          }
+        } else
+        // (eight ids at once, without branches: what one waits for, the others do too)
+        for (int v0 = tid; v0 < count_v; v0 += kLines * kThreads) {
+          float x[8];
+          int bin[8], w[8];
+          bool any = false;
+#pragma unroll
+          for (int y = 0; y < 8; y += 2) {
+            const int v = v0 + y / N * kThreads;
+            const Two t = v < count_v ? L::pair(lines[v], y % N / 2) : Two{-INFINITY, -INFINITY};
+            x[y] = t.x, x[y + 1] = t.y;
+            any = any || fmaxf(t.x, t.y) >= at_least;
+          }
+          if (!any) continue;
+#pragma unroll
+          for (int y = 0; y < 8; y += 2) {
+            Two at = mul2(fma2(Two{x[y], x[y + 1]}, -0.5f, 0.5f * row.m), Two{row.by, row.by});
+            at = Two{fminf(at.x, (float)(kBins - 1)), fminf(at.y, (float)(kBins - 1))};
+            const Two in = add2(at, Two{kWhole, kWhole});
+            const Two f = fma2(at, Two{-1.f, -1.f}, add2(in, Two{-kWhole, -kWhole}));
+            bin[y] = Row::low(in.x), bin[y + 1] = Row::low(in.y);
+            w[y] = share(f.x), w[y + 1] = share(f.y);
+          }
+#pragma unroll
+          for (int y = 0; y < 8; ++y) {
+            if (by_k && x[y] >= at_least) atomicAdd(&sh.bins.n[bin[y]], 1u);
+            if (by_p && x[y] >= at_least) atomicAdd(&sh.bins.w[bin[y]], (unsigned)w[y]);
+          }
+        }
+        sync();
+        all = sum_up(by_k ? sh.bins.n : nullptr, by_p ? sh.bins.w : nullptr, nullptr, kUnit / scale);
+        ready = true;
+        if (!by_k || !weights) kept = all.weight;
+      }
+      if (weights)
+        cut = find(from, true, min(by_k ? target_of(kept) : target, all.weight), kept);
+      else if ((unsigned)top_k < all.count)
+        cut = find(from, false, top_k, kept);
     }
   }
 
@@ -758,11 +814,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
   Pick p = {INFINITY, INT_MAX, INT_MAX};
   {
     const float last = cut ? logit_of(cut) : -INFINITY;  // the last logit that is kept, and of those ids that have it the last
-    const int last_id = cut ? (1 << kIdBits) - 1 - (int)(cut & ((1u << kIdBits) - 1u)) : INT_MAX;
+    const int last_id = cut ? id_of(cut) : INT_MAX;
     float from = first ? row.m : last;
     if (!first && min_p > 0.f && row.c2 > 0.f) from = fmaxf(from, row.least(-log2f(min_p) / row.c2));
     from = fmaxf(from, -FLT_MAX);
-    const bool any_of = cut || min_p > 0.f;  // not all ids of logits from `from` on
     const float* noise = s.d_noise + b * s.noise_stride + lo;
     const bool aligned = ((uintptr_t)(noise - pad) & 15) == 0;  // a line's noise is, too
     constexpr int kLines = 16 / N;  // sixteen ids of a thread at once
@@ -799,26 +854,40 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
 #pragma unroll
       for (int y = 0; y < kLines; ++y) {
         if (!some[y]) continue;
+        // ids of the last logit kept, behind the last one: not kept
+        const int id0 = lo + (v0 + y * kThreads) * N - pad;
+        if (cut && id0 + N - 1 > last_id) {
+          bool tie = false;
+#pragma unroll
+          for (int z = 0; z < N; z += 2) {
+            const Two x = L::pair(r[y], z / 2);
+            tie = tie || x.x == last || x.y == last;
+          }
+          if (tie)
+#pragma unroll
+            for (int z = 0; z < N; ++z) {
+              const Two x = L::pair(r[y], z / 2);
+              if ((z & 1 ? x.y : x.x) == last && id0 + z > last_id) {
+                uint4& o = q[y * (N / 4) + z / 4];
+                (z % 4 == 0 ? o.x : z % 4 == 1 ? o.y : z % 4 == 2 ? o.z : o.w) = 0u;
+              }
+            }
+        }
 #pragma unroll
         for (int z = 0; z < N; z += 2) {
           const Two x = L::pair(r[y], z / 2);
           const Two t = mul2(fma2(x, -0.5f, 0.5f * row.m), Two{row.c2, row.c2});
           const uint4 o = q[y * (N / 4) + z / 4];
           const float e0 = __uint_as_float(z % 4 ? o.z : o.x), e1 = __uint_as_float(z % 4 ? o.w : o.y);
-          float s0 = e0 * exp2_fast(t.x), s1 = e1 * exp2_fast(t.y);  // (infinite where the id is not admitted)
-          if (any_of) {
-            const int id = lo + (v0 + y * kThreads) * N + z - pad;
-            const bool in0 = x.x > last || (x.x == last && id <= last_id), in1 = x.y > last || (x.y == last && id + 1 <= last_id);
-            s0 = in0 && !(min_p > 0.f && exp2_fast(-t.x) < min_p) ? s0 : INFINITY;
-            s1 = in1 && !(min_p > 0.f && exp2_fast(-t.y) < min_p) ? s1 : INFINITY;
-          }
-          if (e0 >= FLT_MIN && s0 < p.score) p.score = s0, best = v0 * 16 + y * N + z;
-          if (e1 >= FLT_MIN && s1 < p.score) p.score = s1, best = v0 * 16 + y * N + z + 1;
+          const float s0 = e0 * exp2_fast(t.x), s1 = e1 * exp2_fast(t.y);  // (infinite where the id is not admitted)
+          if (e0 >= FLT_MIN && x.x >= from && t.x <= t_most && s0 < p.score) p.score = s0, best = v0 * 16 + y * N + z;
+          if (e1 >= FLT_MIN && x.y >= from && t.y <= t_most && s1 < p.score) p.score = s1, best = v0 * 16 + y * N + z + 1;
         }
       }
     }
     if (p.score < INFINITY) p.id = lo + (best / 16 + best % 16 / N * kThreads) * N + best % N - pad;
   }
+  // the block's best of all threads
   p = best_warp(p);
   if (lane == 0) sh.picks[warp] = p;
   __syncthreads();
@@ -836,14 +905,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
   if (rank == 0 && warp == 0) {
     p = best_warp(sh.pick[lane % blocks]);
     if (lane == 0) {
-      float z = 0.f, x = row.m;
-      for (int r = 0; r < blocks; ++r) z += sh.z[r];
-      const int token = p.score < INFINITY ? p.id : p.first;
+      float x = row.m;
       for (int r = 0; r < blocks; ++r)
         if (p.score < INFINITY && sh.pick[r].id == p.id) x = sh.top[r];
-      s.d_tokens[b] = token;
-      if (s.d_logprob) s.d_logprob[b] = fminf((-row.below(x) * row.c2 - log2f(z)) * kLn2, 0.f);
-      s.d_status[b] = token == s.eos ? GRID_ST_COMPLETE : GRID_ST_OK;
+      write(p.score < INFINITY ? p.id : p.first, x);
     }
   }
 }
