@@ -550,31 +550,57 @@ _QUERY, _STEP = struct.Struct("PqqPqqPfi"), struct.Struct("PqqPqqPqqPPPPqPiiiiii
 _TREE, _PAGES, _SAMPLE = struct.Struct("PPii"), struct.Struct("PqPPPPPiiiiPqPPPP"), struct.Struct("PqPqPqPPPPiiiiPPP")
 
 
-def _dense(x, dtype, *shape):
-    assert x.dtype is dtype and x.is_cuda and x.shape == shape and x.is_contiguous(), \
-        "contiguous %s CUDA tensor %s expected" % (dtype, list(shape))
+_int32 = _float32 = _bfloat16 = _current = None
+
+
+def _device():
+    """The current device's number (0.1 us where torch.cuda.current_device() takes 0.3); the caller has a CUDA tensor."""
+    global _int32, _float32, _bfloat16, _current, _raw_stream
+    if _current is None:
+        import torch
+        _stream(None)  # (_raw_stream)
+        _int32, _float32, _bfloat16 = torch.int32, torch.float32, torch.bfloat16
+        _current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _current()
+
+
+def _on(stream, dev):
+    return _raw_stream(dev) if stream is None else _stream(stream)
+
+
+def _ints(x, n, dev):
+    """The address of n int32 values on device dev."""
+    assert x.dtype is _int32 and x.get_device() == dev and x.numel() == n and x.is_contiguous(), \
+        "contiguous int32 tensor of %d values on the current device expected" % n
+    return x.data_ptr()
+
+
+def _floats(x, n, dev):
+    assert x.dtype is _float32 and x.get_device() == dev and x.numel() == n and x.is_contiguous(), \
+        "contiguous float32 tensor of %d values on the current device expected" % n
     return x.data_ptr()
 
 
 def _heads(x, kv, N, H):
     """A [tokens, heads, D] tensor (any strides, D contiguous) as (address, strides)."""
     a, b, c = x.stride()
-    assert x.is_cuda and x.dtype == kv.dtype and x.shape == (N, H, kv.D) and c == 1, \
-        "CUDA tensor [tokens, heads, D] of the cache's type expected, D contiguous"
+    assert x.get_device() == kv.device and x.dtype is kv.dtype and x.shape == (N, H, kv.D) and c == 1, \
+        "tensor [tokens, heads, D] of the cache's type and device expected, D contiguous"
     return x.data_ptr(), a, b
 
 
 def _chunk(kv, table, lens, start, status, N):
-    i32, rows = kv.i32, lens.shape
+    i32, rows, dev = kv.i32, lens.shape, kv.device
     B = rows[0] if rows else 0  # (len() of a tensor takes 0.5 us)
     shape, stride = table.shape, table.stride()
+    assert _device() == dev, "the cache is on another device than the current one"
     assert table.dtype is i32 and lens.dtype is i32 and status.dtype is i32, "int32 table, lens and status expected"
-    assert table.is_cuda and lens.is_cuda and status.is_cuda and len(shape) == 2 and stride[1] == 1, \
-        "table [B, max_pages] on the GPU expected, its rows contiguous"
+    assert table.get_device() == lens.get_device() == status.get_device() == dev and len(shape) == 2 and stride[1] == 1, \
+        "table [B, max_pages] on the cache's device expected, its rows contiguous"
     assert shape[0] == B and rows == status.shape == (B,) and lens.is_contiguous() and status.is_contiguous(), \
         "table [B, max_pages], lens [B] and status [B] expected"
     if start is not None:
-        assert start.dtype is i32 and start.is_cuda and start.is_contiguous() and start.shape == (B + 1,), \
+        assert start.dtype is i32 and start.get_device() == dev and start.is_contiguous() and start.shape == (B + 1,), \
             "int32 start [B + 1] expected"
     return _CHUNK.pack(table.data_ptr(), stride[0], lens.data_ptr(), 0 if start is None else start.data_ptr(), shape[1], B, N, 0)
 
@@ -607,10 +633,10 @@ def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None
                 "norm weights [D] of the cache's type expected"
         norm = _NORM.pack(0 if q_norm is None else q_norm.data_ptr(), 0 if k_norm is None else k_norm.data_ptr(), eps, 0)
     if depth is None:
-        _check(lib().grid_kv_append(kv.h, chunk, kh, vh, qh, oh, rot, norm, status.data_ptr(), _stream(stream)))
+        _check(lib().grid_kv_append(kv.h, chunk, kh, vh, qh, oh, rot, norm, status.data_ptr(), _on(stream, kv.device)))
     else:
-        _check(lib().grid_kv_append_tree(kv.h, chunk, kh, vh, qh, oh, rot, norm, _dense(depth, kv.i32, N),
-                                         status.data_ptr(), _stream(stream)))
+        _check(lib().grid_kv_append_tree(kv.h, chunk, kh, vh, qh, oh, rot, norm, _ints(depth, N, kv.device),
+                                         status.data_ptr(), _on(stream, kv.device)))
 
 
 def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=None, sees=None, stream=None):
@@ -626,11 +652,12 @@ def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=
     query = _QUERY.pack(*_heads(q, kv, N, kv.heads), *_heads(out, kv, N, kv.heads), 0 if lse is None else lse.data_ptr(),
                         kv.D ** -0.5 if scale is None else scale, 0)
     if sees is None:
-        _check(lib().grid_kv_attend(kv.h, chunk, query, status.data_ptr(), _stream(stream)))
+        _check(lib().grid_kv_attend(kv.h, chunk, query, status.data_ptr(), _on(stream, kv.device)))
         return
-    assert sees.dtype is kv.i32 and sees.is_cuda and sees.is_contiguous() and sees.dim() == 2 and sees.shape[0] == N, \
-        "int32 sees [tokens, words] expected"
-    _check(lib().grid_kv_attend_tree(kv.h, chunk, query, sees.data_ptr(), sees.shape[1], status.data_ptr(), _stream(stream)))
+    rows, words = sees.shape
+    assert rows == N, "int32 sees [tokens, words] expected"
+    _check(lib().grid_kv_attend_tree(kv.h, chunk, query, _ints(sees, N * words, kv.device), words, status.data_ptr(),
+                                     _on(stream, kv.device)))
 
 
 class PagedKV:
@@ -646,7 +673,8 @@ class PagedKV:
         dt = {torch.bfloat16: GRID_DTYPE_BF16, torch.float16: GRID_DTYPE_F16}[k_pages.dtype]
         n, page, self.kv_heads, self.D = k_pages.shape
         self.heads, self.dtype, self.pools = heads, k_pages.dtype, (k_pages, v_pages)
-        self.i32, self.f32 = torch.int32, torch.float32
+        self.i32, self.f32, self.device = torch.int32, torch.float32, k_pages.get_device()
+        assert v_pages.get_device() == self.device, "both pools on one device expected"
         p = _KvPages(k_pages.data_ptr(), v_pages.data_ptr(), dt, self.D, heads, self.kv_heads, page, n,
                      k_pages.stride()[:3], v_pages.stride()[:3])
         out = ctypes.c_void_p()
@@ -659,9 +687,9 @@ class PagedKV:
             self.h = None
 
 
-def _tree(parent, start, status, i32):
-    N, B = parent.shape[0], status.shape[0]
-    return _TREE.pack(_dense(parent, i32, N), 0 if start is None else _dense(start, i32, B + 1), B, N), N, B
+def _tree(parent, start, B, dev):
+    N = parent.shape[0]
+    return _TREE.pack(_ints(parent, N, dev), 0 if start is None else _ints(start, B + 1, dev), B, N), N
 
 
 def grid_tree_plan(parent, depth, sees, status, start=None, stream=None):
@@ -669,40 +697,36 @@ def grid_tree_plan(parent, depth, sees, status, start=None, stream=None):
     earlier token of the row, by its index there, or -1), start int32 [B + 1]
     (None: the same number of tokens per row).  Out: depth int32 [tokens], sees
     int32 [tokens, words] (words >= a row's tokens / 32), status int32 [B]."""
-    import torch
-    i32 = torch.int32
-    tree, N, B = _tree(parent, start, status, i32)
-    assert sees.dim() == 2, "sees [tokens, words] expected"
-    words = sees.shape[1]
-    _check(lib().grid_tree_plan(tree, _dense(depth, i32, N), _dense(sees, i32, N, words), words, _dense(status, i32, B),
-                                _stream(stream)))
+    dev, B = _device(), status.shape[0]
+    tree, N = _tree(parent, start, B, dev)
+    rows, words = sees.shape
+    assert rows == N, "sees [tokens, words] expected"
+    _check(lib().grid_tree_plan(tree, _ints(depth, N, dev), _ints(sees, N * words, dev), words, _ints(status, B, dev),
+                                _on(stream, dev)))
 
 
 def grid_tree_accept(parent, tokens, sampled, path, count, out, status, start=None, eos=-1, stream=None):
     """The path that the sampled tokens take: parent, tokens (drafted) and sampled
     int32 [tokens].  Out: path (indices in the row) and out (what was sampled
     there) int32 [B, most], -1 past the end; count, status int32 [B]."""
-    import torch
-    i32 = torch.int32
-    tree, N, B = _tree(parent, start, status, i32)
-    assert path.dim() == 2, "path [B, most] expected"
-    most = path.shape[1]
-    _check(lib().grid_tree_accept(tree, _dense(tokens, i32, N), _dense(sampled, i32, N), eos, most,
-                                  _dense(path, i32, B, most), _dense(count, i32, B), _dense(out, i32, B, most),
-                                  _dense(status, i32, B), _stream(stream)))
+    dev, B = _device(), status.shape[0]
+    tree, N = _tree(parent, start, B, dev)
+    rows, most = path.shape
+    assert rows == B and out.shape == path.shape, "path and out [B, most] expected"
+    _check(lib().grid_tree_accept(tree, _ints(tokens, N, dev), _ints(sampled, N, dev), eos, most, _ints(path, B * most, dev),
+                                  _ints(count, B, dev), _ints(out, B * most, dev), _ints(status, B, dev), _on(stream, dev)))
 
 
 def grid_kv_compact(kv, table, lens, path, count, status, n_tokens, start=None, stream=None):
     """The path's keys and values next to what was cached before the chunk (table,
     lens, start and n_tokens as in its append; path and count of
     grid_tree_accept)."""
-    i32 = kv.i32
-    chunk = _chunk(kv, table, lens, start, status, n_tokens)
+    chunk, dev = _chunk(kv, table, lens, start, status, n_tokens), kv.device
     B = lens.shape[0]
-    assert path.dim() == 2, "path [B, most] expected"
-    most = path.shape[1]
-    _check(lib().grid_kv_compact(kv.h, chunk, _dense(path, i32, B, most), _dense(count, i32, B), most, status.data_ptr(),
-                                 _stream(stream)))
+    rows, most = path.shape
+    assert rows == B, "path [B, most] expected"
+    _check(lib().grid_kv_compact(kv.h, chunk, _ints(path, B * most, dev), _ints(count, B, dev), most, status.data_ptr(),
+                                 _on(stream, dev)))
 
 
 def grid_sample(logits, noise, tokens, status, mask=None, temperature=None, top_k=None, top_p=None, min_p=None,
@@ -712,23 +736,26 @@ def grid_sample(logits, noise, tokens, status, mask=None, temperature=None, top_
     int32 [B, W] (rows of these may be strided); temperature, top_p, min_p float32
     [B], top_k int32 [B] or None.  Out: tokens, status int32 [B], logprob float32
     [B] or None."""
-    import torch
-    f32, i32 = torch.float32, torch.int32
+    dev, dt = _device(), logits.dtype
     B, V = logits.shape
-    dt = GRID_DTYPE_F32 if logits.dtype is f32 else GRID_DTYPE_BF16
-    assert dt == GRID_DTYPE_F32 or logits.dtype is torch.bfloat16, "float32 or bfloat16 logits expected"
-
-    def rows(x, dtype, n):
-        assert x.dtype is dtype and x.is_cuda and x.shape == (B, n) and (x.stride(1) == 1 or n == 1), \
-            "%s CUDA tensor [%d, %d] expected, its rows contiguous" % (dtype, B, n)
-        return x.data_ptr(), x.stride(0)
-
+    assert dt is _float32 or dt is _bfloat16, "float32 or bfloat16 logits expected"
+    by, one = logits.stride()
+    to, two = noise.stride()
+    assert logits.get_device() == noise.get_device() == dev and noise.dtype is _float32 and noise.shape == (B, V) and \
+        (one == two == 1 or V == 1), "logits and float32 noise [B, V] on the current device expected, their rows contiguous"
+    bits = words = 0
+    if mask is not None:
+        words, one = mask.stride()
+        W = (V + 31) // 32
+        assert mask.dtype is _int32 and mask.get_device() == dev and mask.shape == (B, W) and (one == 1 or W == 1), \
+            "int32 mask [B, ceil(V/32)] on the current device expected, its rows contiguous"
+        bits = mask.data_ptr()
     step = _SAMPLE.pack(
-        *rows(logits, logits.dtype, V), *((0, 0) if mask is None else rows(mask, i32, (V + 31) // 32)), *rows(noise, f32, V),
-        0 if temperature is None else _dense(temperature, f32, B), 0 if top_k is None else _dense(top_k, i32, B),
-        0 if top_p is None else _dense(top_p, f32, B), 0 if min_p is None else _dense(min_p, f32, B), dt, B, V, eos,
-        _dense(tokens, i32, B), 0 if logprob is None else _dense(logprob, f32, B), _dense(status, i32, B))
-    _check(lib().grid_sample(step, _stream(stream)))
+        logits.data_ptr(), by, bits, words, noise.data_ptr(), to, 0 if temperature is None else _floats(temperature, B, dev),
+        0 if top_k is None else _ints(top_k, B, dev), 0 if top_p is None else _floats(top_p, B, dev),
+        0 if min_p is None else _floats(min_p, B, dev), GRID_DTYPE_F32 if dt is _float32 else GRID_DTYPE_BF16, B, V, eos,
+        _ints(tokens, B, dev), 0 if logprob is None else _floats(logprob, B, dev), _ints(status, B, dev))
+    _check(lib().grid_sample(step, _on(stream, dev)))
 
 
 def grid_pages_update(pages, table, held, want, table_out, held_out, copies, refs, status, parent=None, keep=None,
@@ -738,27 +765,30 @@ def grid_pages_update(pages, table, held, want, table_out, held_out, copies, ref
     pinned int32 [pages].  Out: table_out int32 [B, width_out], held_out, status
     int32 [B], copies int32 [3, B] (for grid_kv_copy), refs int32 [pages].
     ``pages``: a Pages."""
-    i32 = pages.i32
+    dev, n = pages.device, pages.n_pages
+    assert _device() == dev, "the pages' scratch is on another device than the current one"
     A, B = held.shape[0], want.shape[0]
-    for x, n in ((table, A), (table_out, B)):
-        assert x.dtype is i32 and x.is_cuda and x.dim() == 2 and x.shape[0] == n and x.stride(1) == 1, \
-            "int32 CUDA tables [A, width] and [B, width_out] expected, their rows contiguous"
-    assert table.data_ptr() != table_out.data_ptr() and held.data_ptr() != held_out.data_ptr(), \
-        "the new table and lengths need tensors of their own"
+    (rows, width), (by, one) = table.shape, table.stride()
+    (rows_out, width_out), (by_out, two) = table_out.shape, table_out.stride()
+    at, at_out = table.data_ptr(), table_out.data_ptr()
+    assert table.dtype is table_out.dtype is _int32 and table.get_device() == table_out.get_device() == dev and rows == A and \
+        rows_out == B and (one == 1 or width == 1) and (two == 1 or width_out == 1), \
+        "int32 tables [A, width] and [B, width_out] on the current device expected, their rows contiguous"
+    was, held_at = _ints(held, A, dev), _ints(held_out, B, dev)
+    assert at != at_out and was != held_at, "the new table and lengths need tensors of their own"
     step = _PAGES.pack(
-        table.data_ptr(), table.stride(0), _dense(held, i32, A), 0 if parent is None else _dense(parent, i32, B),
-        0 if keep is None else _dense(keep, i32, B), _dense(want, i32, B),
-        0 if pinned is None else _dense(pinned, i32, pages.n_pages), A, table.shape[1], B, table_out.shape[1],
-        table_out.data_ptr(), table_out.stride(0), _dense(held_out, i32, B), _dense(copies, i32, 3, B),
-        _dense(refs, i32, pages.n_pages), _dense(status, i32, B))
-    _check(lib().grid_pages_update(pages.h, step, _stream(stream)))
+        at, by if A > 1 else width, was, 0 if parent is None else _ints(parent, B, dev), 0 if keep is None else _ints(keep, B, dev),
+        _ints(want, B, dev), 0 if pinned is None else _ints(pinned, n, dev), A, width, B, width_out, at_out,
+        by_out if B > 1 else width_out, held_at, _ints(copies, 3 * B, dev), _ints(refs, n, dev), _ints(status, B, dev))
+    _check(lib().grid_pages_update(pages.h, step, _on(stream, dev)))
 
 
 def grid_kv_copy(kv, copies, status, stream=None):
     """Copy pages of a cache: copies int32 [3, n] (from page or -1, to page, tokens
     from its beginning), status int32 [n]."""
-    n = status.shape[0]
-    _check(lib().grid_kv_copy(kv.h, _dense(copies, kv.i32, 3, n), n, _dense(status, kv.i32, n), _stream(stream)))
+    n, dev = status.shape[0], kv.device
+    assert _device() == dev, "the cache is on another device than the current one"
+    _check(lib().grid_kv_copy(kv.h, _ints(copies, 3 * n, dev), n, _ints(status, n, dev), _on(stream, dev)))
 
 
 class Pages:
@@ -766,7 +796,7 @@ class Pages:
 
     def __init__(self, n_pages: int, page_size: int):
         import torch
-        self.i32, self.n_pages = torch.int32, n_pages
+        self.device, self.n_pages = torch.cuda.current_device() if torch.cuda.is_available() else 0, n_pages
         out = ctypes.c_void_p()
         _check(lib().grid_pages_create(n_pages, page_size, ctypes.byref(out)))
         self.h = out
