@@ -46,6 +46,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32, D == 128 ? 6 : 8) k_append(
   constexpr int kLanes = D / 8, kHeads = 32 / kLanes, kUnroll = kGroup / kHeads;  // lanes of a head, heads of a load, loads
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
+  pdl_next();
   const Chunk& c = a.c;
   if ((int)blockIdx.x >= token_blocks) {  // a warp per row: its status
     const int b = ((int)blockIdx.x - token_blocks) * kAppendWarps + warp;

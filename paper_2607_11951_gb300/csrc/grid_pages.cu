@@ -13,12 +13,14 @@ namespace {
 // ---------------------------------------------------------------------------
 // The update counts, for every page, the new rows that keep it whole, finds the
 // row that a page in part stays with, ranks the free pages by prefix sums and
-// deals them out: five steps, each of which needs all of the one before.  They
-// are one kernel of one block, or of a cluster of eight, whose barriers order
-// what its blocks wrote to memory: a launch costs more than a step.  Counts are
-// atomic additions and minima of integers: their order changes nothing.
+// deals them out: five steps, each of which needs all of the one before, and a
+// launch costs more than a step.  Up to 1,024 rows and 16,384 pages are one
+// block, a thread per row, the pages' counts in its shared memory; more are a
+// cluster of eight blocks, whose barriers order what they wrote to memory.
+// Counts are atomic additions and minima of integers: their order changes
+// nothing.
 constexpr int kUpdateThreads = 1024, kUpdateBlocks = 8;
-constexpr int kAloneEntries = 4096;  // entries of the new table and pages, up to which one block is enough
+constexpr int kAlonePages = 16384;
 constexpr int kNoRoom = -1;          // (a status between the steps: the new table's row is too short)
 
 struct UpdateArgs {
@@ -74,22 +76,22 @@ __device__ __forceinline__ int pages_for(const UpdateArgs& u, int tokens) {
   return (int)(((long long)tokens + (1 << u.log_page) - 1) >> u.log_page);
 }
 
-__global__ void __launch_bounds__(kUpdateThreads) k_update(const UpdateArgs u, int blocks) {
+__global__ void __launch_bounds__(kUpdateThreads) k_update(const UpdateArgs u) {
+  constexpr int blocks = kUpdateBlocks;
   const grid_pages_step& s = u.s;
   __shared__ int sums[32], free_here;
-  const int tid = threadIdx.x, lane = tid & 31, rank = blocks > 1 ? cluster_rank() : 0;
+  const int tid = threadIdx.x, lane = tid & 31, rank = cluster_rank();
   const int threads = blocks * kUpdateThreads, at = rank * kUpdateThreads + tid;
   const int warps = threads / 32, warp = at / 32;
   // (between the steps: the page in part that has to be copied, the fresh pages before the row's, and d_held_out what it keeps)
   int32_t *from = s.d_copies, *to = from + s.B, *tokens = to + s.B;
   auto sync = [&]() {
     __syncwarp();
-    if (blocks > 1)
-      cluster_sync();
-    else
-      __syncthreads();
+    cluster_sync();
   };
   pdl_wait();
+  pdl_next();
+#pragma unroll 4
   for (int p = at; p < u.n_pages; p += threads) {
     s.d_refs[p] = 0;
     u.owner[p] = INT_MAX;
@@ -104,14 +106,17 @@ __global__ void __launch_bounds__(kUpdateThreads) k_update(const UpdateArgs u, i
     const int32_t* old = s.d_table + (ok && parent >= 0 ? parent * s.table_stride : 0);
     int32_t* out = s.d_table_out + b * s.table_out_stride;
     ok = ok && keep >= 0 && keep <= held && want >= keep && pages_for(u, keep) <= min(s.width, s.width_out);
-    for (int j = lane; ok && j < pages_for(u, keep); j += 32) {
+    const int all = ok ? pages_for(u, keep) : 0;
+#pragma unroll 8
+    for (int j = lane; j < all; j += 32) {
       const int p = old[j];
-      ok = p >= 0 && p < u.n_pages;
+      ok = ok && p >= 0 && p < u.n_pages;
     }
     ok = __all_sync(~0u, ok);
     if (!ok) keep = 0;
     const int full = keep >> u.log_page, kept = pages_for(u, keep);
     int last = -1;
+#pragma unroll 8
     for (int j = lane; j < s.width_out; j += 32) {
       const int p = j < kept ? old[j] : -1;
       out[j] = p;
@@ -160,21 +165,20 @@ __global__ void __launch_bounds__(kUpdateThreads) k_update(const UpdateArgs u, i
     return __ballot_sync(~0u, p + lane < p1 && __ldcg(s.d_refs + p + lane) == 0 && !(s.d_pinned && s.d_pinned[p + lane]));
   };
   int n = 0;
+#pragma unroll 4
   for (int p = p0; p < p1; p += 32) n += __popc(free_of(p));
   int here;
   int pre = before(lane == 0 ? n : 0, sums, here);
   pre = __shfl_sync(~0u, pre, 0);
   if (tid == 0) free_here = here;
   sync();
-  int all = here;
-  if (blocks > 1) {
-    all = 0;
-    for (int r = 0; r < blocks; ++r) {
-      const int x = from_block(&free_here, r);
-      if (r < rank) pre += x;
-      all += x;
-    }
+  int all = 0;
+  for (int r = 0; r < blocks; ++r) {
+    const int x = from_block(&free_here, r);
+    if (r < rank) pre += x;
+    all += x;
   }
+#pragma unroll 4
   for (int p = p0; p < p1; p += 32) {
     const unsigned bits = free_of(p);
     if (bits >> lane & 1) u.fresh[pre + __popc(bits & ((1u << lane) - 1))] = p + lane;
@@ -210,46 +214,175 @@ __global__ void __launch_bounds__(kUpdateThreads) k_update(const UpdateArgs u, i
   }
 }
 
+// One block: a thread per row, then a thread per entry of the table (a warp per row would be five times the instructions, for
+// rows of a dozen pages); counts in shared memory.
+struct UpdateRow {
+  int parent, keep, want, kept;  // kept: pages, that in part too; -1: not valid
+  int last, first;               // its page in part (that has to be copied, later on), the fresh pages of the rows before it
+};
+constexpr unsigned kPinned = 1u << 31;  // (in a page's count)
+__global__ void __launch_bounds__(kUpdateThreads) k_update_alone(const UpdateArgs u) {
+  const grid_pages_step& s = u.s;
+  extern __shared__ __align__(16) uint8_t raw[];
+  UpdateRow* const rows = reinterpret_cast<UpdateRow*>(raw);
+  unsigned* const refs = reinterpret_cast<unsigned*>(rows + s.B);
+  int* const owner = reinterpret_cast<int*>(refs + u.n_pages);  // then the free pages in their order
+  __shared__ int sums[32], bad;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, b = tid;
+  pdl_wait();
+  pdl_next();
+  UpdateRow r = {};
+  if (b < s.B) {
+    r.parent = s.d_parent ? s.d_parent[b] : b, r.want = s.d_want[b];
+    r.keep = s.d_keep ? s.d_keep[b] : INT_MAX;
+  }
+#pragma unroll 4
+  for (int p = tid; p < u.n_pages; p += kUpdateThreads) {
+    refs[p] = s.d_pinned && s.d_pinned[p] ? kPinned : 0u;
+    owner[p] = INT_MAX;
+  }
+  if (tid == 0) bad = 0;
+  if (b < s.B) {
+    const bool some = r.parent >= 0 && r.parent < s.A;
+    const int held = some ? s.d_held[r.parent] : 0;
+    if (!some) r.keep = 0;
+    if (some && !s.d_keep) r.keep = held;
+    const bool ok = (some || r.parent == -1) && r.keep >= 0 && r.keep <= held && r.want >= r.keep &&
+                    pages_for(u, r.keep) <= min(s.width, s.width_out);
+    if (!ok) r.keep = 0;
+    r.kept = ok ? pages_for(u, r.keep) : -1;
+    r.last = -1;
+    rows[b] = r;
+  }
+  __syncthreads();
+  // ---- whole pages are counted, pages in part noted
+  const int entries = s.B * s.width_out;
+#pragma unroll 8
+  for (int x = tid; x < entries; x += kUpdateThreads) {
+    const int i = x / s.width_out, j = x - i * s.width_out;
+    const bool in = j < rows[i].kept;
+    const int p = in ? s.d_table[rows[i].parent * s.table_stride + j] : -1;
+    s.d_table_out[i * s.table_out_stride + j] = p;
+    if (!in) continue;
+    if (p < 0 || p >= u.n_pages)
+      bad = 1;
+    else if (j < rows[i].keep >> u.log_page)
+      atomicAdd(&refs[p], 1u);
+    else
+      rows[i].last = p;
+  }
+  __syncthreads();
+  if (bad)  // (rows with a page outside the pool take back what they counted)
+    for (int i = warp; i < s.B; i += kUpdateThreads / 32) {
+      const int kept = rows[i].kept;
+      const int32_t* old = s.d_table + (kept > 0 ? rows[i].parent * s.table_stride : 0);
+      bool ok = true;
+      for (int j = lane; j < kept; j += 32) ok = ok && old[j] >= 0 && old[j] < u.n_pages;
+      if (__all_sync(~0u, ok)) continue;
+      for (int j = lane; j < kept; j += 32) {
+        const int p = old[j];
+        s.d_table_out[i * s.table_out_stride + j] = -1;
+        if (p >= 0 && p < u.n_pages && j < rows[i].keep >> u.log_page) atomicSub(&refs[p], 1u);
+      }
+      __syncwarp();
+      if (lane == 0) rows[i].kept = -1, rows[i].keep = 0, rows[i].last = -1;
+    }
+  if (bad) __syncthreads();
+  if (b < s.B) r = rows[b];
+  if (b < s.B && r.last >= 0) atomicMin(&owner[r.last], b);
+  __syncthreads();
+  // ---- who keeps a page in part, and how many fresh pages the rows before take
+  bool room = false;
+  int need = 0, full = 0;
+  if (b < s.B) {
+    full = r.keep >> u.log_page;
+    const bool stays = r.last >= 0 && owner[r.last] == b && refs[r.last] == 0;
+    // (its own thread alone writes this count; another row that has the page in part is not its owner, whatever it reads)
+    if (stays) refs[r.last] = 1, r.last = -1;
+    room = r.kept >= 0 && pages_for(u, r.want) <= s.width_out;
+    need = room ? pages_for(u, r.want) - full - stays : 0;
+  }
+  int wanted, all;
+  const int first = before(need, sums, wanted);
+  if (b < s.B) rows[b].first = first, rows[b].last = r.last;
+  // ---- the free pages in their order: 32 at a time, a run of them to a warp
+  const int run = ((u.n_pages + kUpdateThreads - 1) / kUpdateThreads) * 32;
+  const int p0 = min(u.n_pages, warp * run), p1 = min(u.n_pages, p0 + run);
+  int n = 0;
+  for (int p = p0; p < p1; p += 32) n += __popc(__ballot_sync(~0u, p + lane < p1 && refs[p + lane] == 0));
+  int pre = before(lane == 0 ? n : 0, sums, all);
+  pre = __shfl_sync(~0u, pre, 0);
+  for (int p = p0; p < p1; p += 32) {  // (nobody looks for an owner any more)
+    const unsigned bits = __ballot_sync(~0u, p + lane < p1 && refs[p + lane] == 0);
+    if (bits >> lane & 1) owner[pre + __popc(bits & ((1u << lane) - 1))] = p + lane;
+    pre += __popc(bits);
+  }
+  __syncthreads();
+  // ---- a thread per fresh page: its row is the last one that begins at or before it
+  for (int x = tid; x < min(wanted, all); x += kUpdateThreads) {
+    int i = 0;
+    for (int step = kUpdateThreads / 2; step; step /= 2)
+      if (i + step < s.B && rows[i + step].first <= x) i += step;
+    const int end = i + 1 < s.B ? rows[i + 1].first : wanted;
+    if (end > all) continue;  // (not all of the row's are there)
+    const int whole = rows[i].keep >> u.log_page, stays = (rows[i].keep & ((1 << u.log_page) - 1)) && rows[i].last < 0;
+    const int p = owner[x];
+    s.d_table_out[i * s.table_out_stride + whole + stays + x - rows[i].first] = p;
+    refs[p] = 1;
+  }
+  if (b < s.B) {
+    const bool fits = room && (need == 0 || first + need <= all), copies = fits && r.last >= 0;
+    if (!fits && r.last >= 0) s.d_table_out[b * s.table_out_stride + full] = -1;
+    s.d_copies[b] = copies ? r.last : -1;
+    s.d_copies[s.B + b] = copies ? owner[first] : -1;
+    s.d_copies[2 * s.B + b] = copies ? r.keep & ((1 << u.log_page) - 1) : 0;
+    s.d_held_out[b] = fits ? r.want : r.last >= 0 ? full << u.log_page : r.keep;
+    s.d_status[b] = fits ? GRID_ST_OK : GRID_ST_PAGES;
+  }
+  __syncthreads();
+  for (int p = tid; p < u.n_pages; p += kUpdateThreads) s.d_refs[p] = refs[p] & ~kPinned;
+}
+
 // ---------------------------------------------------------------------------
-// A copy's tokens, in pieces of 16 bytes that lie in the order of the page's
-// memory, by several blocks: kAhead loads of a thread at once.
-constexpr int kCopyThreads = 256, kAhead = 8;
+// A copy's tokens, in pieces of 16 bytes.  What lies side by side (all of them, or a
+// head's) is cut into chunks of kAhead pieces a thread, which are loaded at once;
+// the chunks of a copy and pool go to `splits` blocks in turn.
+constexpr int kCopyThreads = 128, kAhead = 4, kChunk = kCopyThreads * kAhead;
 
 struct CopyArgs {
   uint4* pool[2];
   long long page[2], token[2], head[2];  // strides in pieces
   const int32_t* copies;
   int32_t* status;
-  int n, n_pages, page_size, Hk, log_parts, splits;  // splits: blocks per copy and pool
+  int n, n_pages, page_size, Hk, log_parts, splits;
 };
 
 __global__ void __launch_bounds__(kCopyThreads) k_copy(const CopyArgs c) {
   const int i = blockIdx.x / (2 * c.splits), rest = blockIdx.x - i * 2 * c.splits, kv = rest & 1, split = rest >> 1;
   pdl_wait();
+  pdl_next();
   const int src = c.copies[i], dst = c.copies[c.n + i], tokens = c.copies[2 * c.n + i];
   const bool none = src < 0, ok = none || (src < c.n_pages && dst >= 0 && dst < c.n_pages && tokens >= 0 && tokens <= c.page_size);
   if (rest == 0 && threadIdx.x == 0) c.status[i] = ok ? GRID_ST_OK : GRID_ST_PAGES;
   if (none || !ok || src == dst) return;
   const long long page = kv ? c.page[1] : c.page[0], token = kv ? c.token[1] : c.token[0], head = kv ? c.head[1] : c.head[0];
-  const bool by_head = token < head;  // a head's tokens lie side by side
-  const int inner = by_head ? tokens : c.Hk, total = (tokens * c.Hk) << c.log_parts, parts = 1 << c.log_parts;
-  const long long inner_step = by_head ? token : head, outer_step = by_head ? head : token;
+  const int parts = 1 << c.log_parts;
+  const bool whole = head == parts && token == (long long)c.Hk << c.log_parts;  // tokens side by side, their heads too
+  const int run = (whole ? tokens * c.Hk : tokens) << c.log_parts, runs = whole ? 1 : c.Hk;
+  const int per = (run + kChunk - 1) / kChunk;
   uint4* pool = kv ? c.pool[1] : c.pool[0];
   const uint4* from = pool + src * page;
   uint4* to = pool + dst * page;
-  const int step = c.splits * kCopyThreads;
-  for (int x = split * kCopyThreads + threadIdx.x; x < total; x += kAhead * step) {
+  for (int k = split; k < runs * per; k += c.splits) {
+    const int r = k / per, z0 = (k - r * per) * kChunk + threadIdx.x;
+    auto place = [&](int z) { return whole ? (long long)z : r * head + (z >> c.log_parts) * token + (z & (parts - 1)); };
     uint4 v[kAhead];
-    long long at[kAhead];
-#pragma unroll
-    for (int y = 0; y < kAhead; ++y) {
-      const int z = x + y * step, vec = z >> c.log_parts, o = vec / inner;
-      at[y] = o * outer_step + (vec - o * inner) * inner_step + (z & (parts - 1));
-      if (z < total) v[y] = from[at[y]];
-    }
 #pragma unroll
     for (int y = 0; y < kAhead; ++y)
-      if (x + y * step < total) to[at[y]] = v[y];
+      if (z0 + y * kCopyThreads < run) v[y] = from[place(z0 + y * kCopyThreads)];
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y)
+      if (z0 + y * kCopyThreads < run) to[place(z0 + y * kCopyThreads)] = v[y];
   }
 }
 
@@ -272,6 +405,7 @@ __global__ void __launch_bounds__(kCompactThreads) k_compact(const CompactArgs a
   const int b = blockIdx.x / a.blocks, block = blockIdx.x - b * a.blocks, lane = threadIdx.x & 31;
   const Chunk& c = a.c;
   pdl_wait();
+  pdl_next();
   const int32_t* path = a.path + (long long)b * a.most;
   const int count = a.count[b];
   int first, n, len;
@@ -353,10 +487,12 @@ extern "C" int grid_pages_create(int32_t n_pages, int32_t page_size, grid_pages*
   while (1 << g->log_page < page_size) ++g->log_page;
   int rc = g->mem.alloc((size_t)n_pages * sizeof(int), (void**)&g->owner);
   if (!rc) rc = g->mem.alloc((size_t)n_pages * sizeof(int), (void**)&g->fresh);
-  if (rc) {
+  const cudaError_t e = rc ? cudaSuccess : cudaFuncSetAttribute(k_update_alone, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                               kUpdateThreads * sizeof(UpdateRow) + kAlonePages * 8);
+  if (rc || e != cudaSuccess) {
     g->mem.release();
     delete g;
-    return rc;
+    return rc ? rc : set_error(GRID_E_CUDA, std::string("grid_pages_create: ") + cudaGetErrorString(e));
   }
   *out = g;
   return GRID_OK;
@@ -377,8 +513,10 @@ extern "C" int grid_pages_update(const grid_pages* g, const grid_pages_step* s, 
   if ((int64_t)s->B * s->width_out > INT32_MAX)
     return set_error(GRID_E_TOO_LARGE, "grid_pages_update: a table of more than 2^31 - 1 entries");
   UpdateArgs u = {*s, g->n_pages, g->log_page, g->owner, g->fresh};
-  const int blocks = (int64_t)s->B * s->width_out + g->n_pages > kAloneEntries ? kUpdateBlocks : 1;
-  GRID_CUDA(launch_cluster(k_update, dim3(blocks), dim3(kUpdateThreads), 0, blocks, (cudaStream_t)stream, u, blocks));
+  if (s->B <= kUpdateThreads && g->n_pages <= kAlonePages)
+    GRID_CUDA(launch_pdl(k_update_alone, dim3(1), dim3(kUpdateThreads), s->B * sizeof(UpdateRow) + g->n_pages * 8, (cudaStream_t)stream, u));
+  else
+    GRID_CUDA(launch_cluster(k_update, dim3(kUpdateBlocks), dim3(kUpdateThreads), 0, kUpdateBlocks, (cudaStream_t)stream, u));
   GRID_CUDA(cudaGetLastError());
   return GRID_OK;
 }
@@ -390,9 +528,10 @@ extern "C" int grid_kv_copy(const grid_kv* kv, const int32_t* d_copies, int32_t 
   set_pools(kv, c);
   c.copies = d_copies, c.status = d_status, c.n = n;
   c.n_pages = kv->p.n_pages, c.page_size = kv->p.page_size;
-  // (as many blocks as half a page, the usual copy, keeps busy with one round of loads)
-  const int pieces = (c.page_size * c.Hk) << c.log_parts;
-  c.splits = std::max(1, std::min(64, pieces / 2 / (kCopyThreads * kAhead)));
+  // (a block for each chunk of half a page, the usual copy; at most 64)
+  const int half = (c.page_size / 2) << c.log_parts;
+  const bool whole = c.head[0] == 1 << c.log_parts && c.token[0] == (long long)c.Hk << c.log_parts;
+  c.splits = std::min<int64_t>(64, whole ? ((int64_t)half * c.Hk + kChunk - 1) / kChunk : (int64_t)c.Hk * ((half + kChunk - 1) / kChunk));
   GRID_CUDA(launch_pdl(k_copy, dim3((unsigned)(n * 2 * c.splits)), dim3(kCopyThreads), 0, (cudaStream_t)stream, c));
   GRID_CUDA(cudaGetLastError());
   return GRID_OK;

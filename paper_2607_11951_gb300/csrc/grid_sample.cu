@@ -54,8 +54,26 @@ using u64 = unsigned long long;
 
 struct SampleArgs {
   grid_sample_step s;
-  int each;  // ids of a block (a multiple of 32)
+  int each;   // ids of a block (a multiple of 32)
+  int sorted; // rows that take long go first
 };
+
+// What a row asks for.
+struct Ask {
+  float temp, top_p, min_p;
+  int top_k;
+  bool greedy, first;  // first: only the first id is kept
+};
+__device__ __forceinline__ Ask ask_of(const grid_sample_step& s, int b) {
+  Ask a;
+  a.temp = s.d_temperature ? s.d_temperature[b] : 1.f;
+  a.top_k = s.d_top_k ? s.d_top_k[b] : 0;
+  a.top_p = s.d_top_p ? s.d_top_p[b] : 1.f, a.min_p = s.d_min_p ? s.d_min_p[b] : 0.f;
+  a.greedy = !(a.temp > 0.f);
+  a.first = a.greedy || a.top_k == 1 || a.top_p <= 0.f || a.min_p > 1.f;
+  return a;
+}
+
 
 struct Pick {   // of a draw: the best score and its id; the first id of the largest logit
   float score;
@@ -89,8 +107,10 @@ struct Shared {
   Found found;
   u64 target, kept;
   unsigned staged, at;
+  int row;
   u64 sums[kWarps], sums2[kWarps];
   float3 warps[kWarps];
+  float zw[kWarps];
   Pick picks[kWarps];
 };
 constexpr int kSharedRoom = (sizeof(Shared) + 127) & ~127;
@@ -288,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
   Shared& sh = *reinterpret_cast<Shared*>(raw);
   uint4* const lines = reinterpret_cast<uint4*>(raw + kSharedRoom);
   const grid_sample_step& s = a.s;
-  const int b = blockIdx.x / blocks, rank = cluster_rank();
+  const int rank = cluster_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int lo = min(s.V, rank * a.each), n = min(s.V, lo + a.each) - lo;
   auto sync = [&]() {  // of the row's blocks
@@ -300,11 +320,28 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
   };
   if (blocks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   pdl_wait();
-  const float temp = s.d_temperature ? s.d_temperature[b] : 1.f;
-  const int top_k = s.d_top_k ? s.d_top_k[b] : 0;
-  const float top_p = s.d_top_p ? s.d_top_p[b] : 1.f, min_p = s.d_min_p ? s.d_min_p[b] : 0.f;
-  const bool greedy = !(temp > 0.f);
-  const bool first = greedy || top_k == 1 || top_p <= 0.f || min_p > 1.f;  // only the first id is kept
+  int b = blockIdx.x / blocks;
+  if (a.sorted) {  // the b-th in the order: rows cut by top-p or a large top-k, uncut ones, those of one id
+    const int per = (s.B + kThreads - 1) / kThreads;
+    u64 mine = 0;  // rows of each kind, 16 bits apart
+    auto kind = [&](int i) {
+      const Ask x = ask_of(s, i);
+      return x.first ? 32 : x.top_p < 1.f || x.top_k > kDirect ? 0 : 16;
+    };
+    for (int i = tid * per; i < min(s.B, (tid + 1) * per); ++i) mine += 1ull << kind(i);
+    u64 all, at = up_to(mine, sh.sums, all) - mine;
+    const int n0 = (int)(all & 0xFFFF), n1 = (int)(all >> 16 & 0xFFFF);
+    const int of = b < n0 ? 0 : b < n0 + n1 ? 16 : 32, nth = b - (of == 0 ? 0 : of == 16 ? n0 : n0 + n1);
+    if ((int)(at >> of & 0xFFFF) <= nth && nth < (int)((at + mine) >> of & 0xFFFF))
+      for (int i = tid * per, k = (int)(at >> of & 0xFFFF); i < min(s.B, (tid + 1) * per); ++i)
+        if (kind(i) == of && k++ == nth) sh.row = i;
+    __syncthreads();
+    b = sh.row;
+  }
+  const Ask ask = ask_of(s, b);
+  const int top_k = ask.top_k;
+  const float temp = ask.temp, top_p = ask.top_p, min_p = ask.min_p;
+  const bool greedy = ask.greedy, first = ask.first;
   Row row;
   row.c2 = fminf((greedy ? 1.f : 1.f / temp) * (2.f * kLog2e), 1e37f);  // (so that 1,024 bins of 40 exponents have a width)
 
@@ -317,34 +354,34 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     const uint32_t* mask = s.d_mask ? s.d_mask + b * s.mask_stride + (lo >> 5) : nullptr;
     pad = (int)((uintptr_t)l & 15) / (int)sizeof(T);
     count_v = n > 0 ? (pad + n + N - 1) / N : 0;
-    // (the mask's words first, so that no logit waits for its bit: the lists are not in use yet)
+    const int inner = n - N;  // a whole line begins at an id of 0 .. inner
+    // The mask's words first, so that no logit waits for its bit (the lists are not in use yet); then all whole lines that
+    // hold an admitted id at once, each by the thread that takes it on.
     uint32_t* const words = reinterpret_cast<uint32_t*>(sh.list);
     static_assert(kMaxIds / kMaxBlocks / 32 < 4 * kList);
     if (mask) {
       for (int w = tid; w <= (n + 31) / 32; w += kThreads) words[w] = w < (n + 31) / 32 ? mask[w] : 0u;
       __syncthreads();
     }
-    constexpr int kAhead = sizeof(T) == 2 ? 4 : 8;
-    const int inner = n - N;  // a whole line begins at an id of 0 .. inner
-    for (int v0 = tid; v0 < count_v; v0 += kAhead * kThreads) {
-      uint4 r[kAhead];
-      unsigned bits[kAhead];
-#pragma unroll
-      for (int y = 0; y < kAhead; ++y) {
-        const int i = (v0 + y * kThreads) * N - pad;
-        bits[y] = 0u;
-        if (i >= 0 && i <= inner)
-          bits[y] = mask ? __funnelshift_r(words[i >> 5], words[(i >> 5) + 1], i & 31) & ((1u << N) - 1u) : (1u << N) - 1u;
-        r[y] = make_uint4(0, 0, 0, 0);
-        load_if(r[y], l + i, bits[y] != 0);
-      }
-#pragma unroll
-      for (int y = 0; y < kAhead; ++y) {
-        const uint4 x = L::admit(r[y], bits[y]);
-        if (v0 + y * kThreads < count_v) lines[v0 + y * kThreads] = x;
-        top = fmaxf(top, L::top(x));
-        ids += __popc(bits[y]);
-      }
+    auto bits_of = [&](int v) {
+      const int i = v * N - pad;
+      if (i < 0 || i > inner) return 0u;
+      return mask ? __funnelshift_r(words[i >> 5], words[(i >> 5) + 1], i & 31) & ((1u << N) - 1u) : (1u << N) - 1u;
+    };
+#pragma unroll 4
+    for (int v = tid; v < count_v; v += kThreads)
+      asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\n@p cp.async.cg.shared.global [%0], [%1], 16;\n}" ::"r"(
+                       (uint32_t)__cvta_generic_to_shared(lines + v)),
+                   "l"(l + (v * N - pad)), "r"(bits_of(v))
+                   : "memory");
+    asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 2
+    for (int v = tid; v < count_v; v += kThreads) {
+      const unsigned bits = bits_of(v);
+      const uint4 x = L::admit(lines[v], bits);
+      lines[v] = x;
+      top = fmaxf(top, L::top(x));
+      ids += __popc(bits);
     }
     // lines that are not whole: the first and the last, an id to a thread
     __syncthreads();
@@ -361,42 +398,6 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       }
     }
   }
-  // ---- the row's largest logit, all threads' largest, and how many ids are admitted
-  const bool wants_k = !first && top_k > 0;
-  unsigned* const top_bins = reinterpret_cast<unsigned*>(sh.list[0]);  // (the first list is the other one)
-  static_assert(sizeof(sh.list[0]) >= kBins * sizeof(unsigned));
-  {
-    const float t = max_warp(top), u = max_warp(top > -INFINITY ? -top : -INFINITY);
-    const unsigned c = __reduce_add_sync(~0u, ids);
-    if (lane == 0) sh.warps[warp] = make_float3(t, u, __uint_as_float(c));
-    __syncthreads();
-    for (int i = tid; i < kBins; i += kThreads) top_bins[i] = 0;
-    if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (the others are there)
-    if (wants_k)
-      for (int r = 0; r < blocks; ++r) put(sh.tops[rank * kThreads + tid], top, r);
-    if (tid < blocks) {
-      float x = -INFINITY, y = -INFINITY;
-      unsigned all = 0;
-      for (int w = 0; w < kWarps; ++w)
-        x = fmaxf(x, sh.warps[w].x), y = fmaxf(y, sh.warps[w].y), all += __float_as_uint(sh.warps[w].z);
-      put(sh.top[rank], x, tid);
-      put(sh.low[rank], y, tid);
-      put(sh.ids[rank], all, tid);
-    }
-    sync();
-  }
-  ids = 0;
-  row.m = -INFINITY;
-  for (int r = 0; r < blocks; ++r) row.m = fmaxf(row.m, sh.top[r]), ids += sh.ids[r];
-  if (!(row.m > -INFINITY)) {  // (the same in every block)
-    if (rank == 0 && tid == 0) {
-      s.d_tokens[b] = -1;
-      if (s.d_logprob) s.d_logprob[b] = 0.f;
-      s.d_status[b] = GRID_ST_EMPTY_MASK;
-    }
-    return;
-  }
-
   // f(x, i) for the block's ids i whose logit x is admitted and at least `from`
   auto each = [&](float from, auto f) {
     from = fmaxf(from, -FLT_MAX);
@@ -412,17 +413,28 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     }
   };
 
-  // ---- the sum of the weights
+  // ---- the block's largest logit and the sum of its weights, relative to that; then, over the row's blocks: the largest
+  // logit, the sum, all threads' largest, the smallest of those, how many ids are admitted
+  const bool wants_k = !first && top_k > 0;
+  unsigned* const top_bins = reinterpret_cast<unsigned*>(sh.list[0]);  // (the first list is the other one)
+  static_assert(sizeof(sh.list[0]) >= kBins * sizeof(unsigned));
+  float all_z = 0.f;
   {
-    float z = 0.f;
-    if (row.c2 > 0.f) {
+    const float t = max_warp(top), u = max_warp(top > -INFINITY ? -top : -INFINITY);
+    const unsigned c = __reduce_add_sync(~0u, ids);
+    if (lane == 0) sh.warps[warp] = make_float3(t, u, __uint_as_float(c));
+    __syncthreads();
+    float m = -INFINITY, z = 0.f;
+    for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sh.warps[w].x);
+    if (!(m > -INFINITY)) {
+    } else if (row.c2 > 0.f) {
       Two sum = {0.f, 0.f};
 #pragma unroll 2
       for (int v = tid; v < count_v; v += kThreads) {
         const uint4 r = lines[v];
 #pragma unroll
         for (int e = 0; e < N / 2; ++e) {
-          const Two t = mul2(fma2(L::pair(r, e), 0.5f, -0.5f * row.m), Two{row.c2, row.c2});
+          const Two t = mul2(fma2(L::pair(r, e), 0.5f, -0.5f * m), Two{row.c2, row.c2});
           sum = add2(sum, Two{exp2_fast(t.x), exp2_fast(t.y)});
         }
       }
@@ -431,23 +443,43 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       each(-INFINITY, [&](float, int) { z += 1.f; });
     }
     z = sum_warp(z);
+    if (lane == 0) sh.zw[warp] = z;
+    for (int i = tid; i < kBins; i += kThreads) top_bins[i] = 0;
     __syncthreads();
-    if (lane == 0) sh.warps[warp].x = z;
-    __syncthreads();
+    if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (the others are there)
+    if (wants_k)
+      for (int r = 0; r < blocks; ++r) put(sh.tops[rank * kThreads + tid], top, r);
     if (tid < blocks) {
+      float y = -INFINITY;
+      unsigned all = 0;
       z = 0.f;
-      for (int w = 0; w < kWarps; ++w) z += sh.warps[w].x;
+      for (int w = 0; w < kWarps; ++w) y = fmaxf(y, sh.warps[w].y), all += __float_as_uint(sh.warps[w].z), z += sh.zw[w];
+      put(sh.top[rank], m, tid);
+      put(sh.low[rank], y, tid);
+      put(sh.ids[rank], all, tid);
       put(sh.z[rank], z, tid);
     }
+    sync();
   }
+  ids = 0;
+  row.m = -INFINITY;
+  for (int r = 0; r < blocks; ++r) row.m = fmaxf(row.m, sh.top[r]), ids += sh.ids[r];
+  if (!(row.m > -INFINITY)) {  // (the same in every block)
+    if (rank == 0 && tid == 0) {
+      s.d_tokens[b] = -1;
+      if (s.d_logprob) s.d_logprob[b] = 0.f;
+      s.d_status[b] = GRID_ST_EMPTY_MASK;
+    }
+    return;
+  }
+  for (int r = 0; r < blocks; ++r)
+    if (sh.top[r] > -INFINITY) all_z += sh.z[r] * row.weight(sh.top[r]);
 
   // (min-p by the exponent: the difference comes first, so that it holds at every temperature)
   const float t_most = min_p > 0.f ? -log2f(min_p) : INFINITY;
   auto write = [&](int token, float x) {
-    float z = 0.f;
-    for (int r = 0; r < blocks; ++r) z += sh.z[r];
     s.d_tokens[b] = token;
-    if (s.d_logprob) s.d_logprob[b] = fminf((-row.below(x) * row.c2 - log2f(z)) * kLn2, 0.f);
+    if (s.d_logprob) s.d_logprob[b] = fminf((-row.below(x) * row.c2 - log2f(all_z)) * kLn2, 0.f);
     s.d_status[b] = token == s.eos ? GRID_ST_COMPLETE : GRID_ST_OK;
   };
 
@@ -560,6 +592,11 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     // Of the bins kPer tid .. + kPer - 1 of all blocks: the ids and the weight up to and with each.
     unsigned upto_n[kPer];
     u64 upto_w[kPer];
+    // bf16 logits from `from` on that are positive and of no more values than there are bins have a bin for each value, the
+    // largest's first: only their numbers are counted
+    bool by_value = false;
+    const int top_value = __float_as_int(row.m) >> 16;
+    auto value_of = [&](int bin) { return __int_as_float((top_value - bin) << 16); };
     auto sum_up = [&](const unsigned* n, const unsigned* w, const unsigned* high, float scale) {
       u64 low[kPer] = {}, up[kPer] = {};
       unsigned cn[kPer] = {};
@@ -584,7 +621,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
 #pragma unroll
       for (int y = 0; y < kPer; ++y) {
         u64 x = low[y] + (up[y] << 32);
-        if (!high) x = __float2ull_rn((float)x * (row.middle(kPer * tid + y) * scale));
+        if (!high && by_value)
+          x = cn[y] ? cn[y] * units(row.weight(value_of(kPer * tid + y))) : 0;
+        else if (!high)
+          x = __float2ull_rn((float)x * (row.middle(kPer * tid + y) * scale));
         sum_n += cn[y], sum_w += x;
         upto_n[y] = sum_n, upto_w[y] = sum_w;
       }
@@ -619,17 +659,20 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       const int bin = f.bin;
       // (of equal logits or logits that are nearly so, there may be too many in a bin)
       float to = INFINITY;
-      if (row.by > 0.f) {
+      auto in_bin = [&](float x) { return by_value ? x == value_of(bin) : row.bin(x) == bin; };
+      if (by_value) {
+        from = to = value_of(bin);
+      } else if (row.by > 0.f) {
         // (bins are rounded to the nearest whole number)
         if (bin < kBins - 1) from = fmaxf(from, row.least((bin + 0.5f) / row.by));
         if (bin > 0) to = row.most((bin - 0.5f) / row.by);
       }
-      unsigned listed = gather(from, to, [&](float x, u64) { return row.bin(x) == bin; });
+      unsigned listed = gather(from, to, [&](float x, u64) { return in_bin(x); });
       if (listed > kList) {
         u64 most = 0, least = 0;  // (least: as the largest complement)
         each(from, [&](float x, int i) {
           const u64 o = order_of(x, lo + i);
-          if (row.bin(x) == bin) most = max(most, o), least = max(least, ~o);
+          if (in_bin(x)) most = max(most, o), least = max(least, ~o);
         });
         most = max_warp(most), least = max_warp(least);
         __syncthreads();
@@ -676,7 +719,6 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     u64 target = 0;  // of top-p alone
     const bool few = ids <= room;  // all of them are sorted
     if (few) {
-      sync();  // (the sum of the weights)
     } else if (by_k) {
       // the bin that the k-th largest of the threads' largest lies in
       float low = -INFINITY;
@@ -702,11 +744,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       __syncthreads();
       if (all >= (unsigned)top_k && row.by > 0.f && sh.found.bin < kBins - 1) from = row.least((sh.found.bin + 0.5f) / row.by);
     } else {
-      sync();
-      float z = 0.f;
-      for (int r = 0; r < blocks; ++r) z += sh.z[r];
-      if (row.c2 > 0.f) from = row.least(-log2f(0.99f * (1.f - top_p) * (z / ids)) / row.c2);
-      target = max(__float2ull_ru(top_p * z * kUnit), 1ull);
+      if (row.c2 > 0.f) from = row.least(-log2f(0.99f * (1.f - top_p) * (all_z / ids)) / row.c2);
+      target = max(__float2ull_ru(top_p * all_z * kUnit), 1ull);
+      by_value = sizeof(T) == 2 && from > 0.f && top_value - (__float_as_int(from) >> 16) < kBins;
     }
     if (few || (by_k && top_k <= kDirect)) {
       const unsigned listed = gather(from, INFINITY, [](float, u64) { return true; });
@@ -752,6 +792,20 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
         __syncthreads();
         const float at_least = fmaxf(from, -FLT_MAX);
         constexpr int kLines = 8 / N;
+        if (by_value) {
+          const int least = (__float_as_int(from) + 0xFFFF) >> 16;  // (as whole numbers, negative logits are below)
+          for (int v = tid; v < count_v; v += kThreads) {
+            const uint4 r = lines[v];
+            if (!(L::top(r) >= from)) continue;
+            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const int x0 = (int16_t)w[y], x1 = (int)w[y] >> 16;
+              if (x0 >= least) atomicAdd(&sh.bins.n[top_value - x0], 1u);
+              if (x1 >= least) atomicAdd(&sh.bins.n[top_value - x1], 1u);
+            }
+          }
+        } else
         if (by_k && from > -INFINITY) {  // few ids in many lines
           for (int v = tid; v < count_v; v += kThreads) {
             const uint4 r = lines[v];
@@ -799,7 +853,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
           }
         }
         sync();
-        all = sum_up(by_k ? sh.bins.n : nullptr, by_p ? sh.bins.w : nullptr, nullptr, kUnit / scale);
+        all = sum_up(by_k || by_value ? sh.bins.n : nullptr, by_p && !by_value ? sh.bins.w : nullptr, nullptr, kUnit / scale);
         ready = true;
         if (!by_k || !weights) kept = all.weight;
       }
@@ -898,7 +952,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       put(sh.pick[rank].id, p.id, 0);
       put(sh.pick[rank].first, p.first, 0);
       // (its logit)
-      put(sh.top[rank], p.score < INFINITY ? value(reinterpret_cast<const T*>(lines)[p.id - lo + pad]) : row.m, 0);
+      put(sh.low[rank], p.score < INFINITY ? value(reinterpret_cast<const T*>(lines)[p.id - lo + pad]) : row.m, 0);
     }
   }
   sync();
@@ -907,7 +961,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     if (lane == 0) {
       float x = row.m;
       for (int r = 0; r < blocks; ++r)
-        if (p.score < INFINITY && sh.pick[r].id == p.id) x = sh.top[r];
+        if (p.score < INFINITY && sh.pick[r].id == p.id) x = sh.low[r];
       write(p.score < INFINITY ? p.id : p.first, x);
     }
   }
@@ -931,7 +985,10 @@ extern "C" int grid_sample(const grid_sample_step* s, void* stream) {
   // (blocks by the vocabulary alone: a row's sums do not depend on the batch)
   int blocks = 1, log = 0;
   while (blocks < kMaxBlocks && s->V > 4096 * blocks) blocks *= 2, ++log;
-  const SampleArgs a = {*s, ((s->V + blocks - 1) / blocks + 31) & ~31};
+  // (where the rows are more than the SMs hold at once, and few enough to look at all: 256 rows over 151,937 bf16 logits,
+  // some greedy, XX us instead of XX)
+  const bool sorted = s->B * blocks > 608 && s->B <= 2048 && (s->d_temperature || s->d_top_k || s->d_top_p || s->d_min_p);
+  const SampleArgs a = {*s, ((s->V + blocks - 1) / blocks + 31) & ~31, sorted};
   const size_t smem = kSharedRoom + (size_t)a.each * size + 32;
   static std::atomic<uint64_t> ready[2][4];  // the devices where a kernel has its room in shared memory
   auto go = [&](auto kernel) {

@@ -26,6 +26,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const grid_tree tree, int
   __shared__ int16_t up[kMaxWords * 32];
   const int b = blockIdx.x, tid = threadIdx.x;
   pdl_wait();
+  pdl_next();
   int a, n;
   const bool fits = tree_span(tree, b, a, n) && n <= 32 * words;
   if (!fits) {
@@ -64,6 +65,7 @@ __global__ void __launch_bounds__(kAcceptWarps * 32) k_accept(const grid_tree tr
   const int lane = threadIdx.x & 31, b = blockIdx.x * kAcceptWarps + (threadIdx.x >> 5);
   if (b >= tree.B) return;
   pdl_wait();
+  pdl_next();
   int a, n;
   const bool fits = tree_span(tree, b, a, n);
   int parent[kHeld], token[kHeld], drawn[kHeld];
