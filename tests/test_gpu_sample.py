@@ -317,3 +317,25 @@ def test_distribution():
     assert float(got[l == -3].sum()) == 0
     chi = ((got - want) ** 2 / want.clamp(min=1e-9))[l > -3].sum()
     assert float(chi) < 24.3, chi  # (one in a thousand)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("B,V,cut", [(400, 5000, "mixed"), (700, 600, "p"), (2049, 40, "mixed"), (1000, 4097, "none")])
+def test_batches_of_more_rows_than_fit_at_once(dt, B, V, cut):
+    """Rows of every kind in any order: each is drawn once, whichever goes first."""
+    Case(B, V, dt, seed=B, cut=cut, greedy=0.3).check()
+
+
+@pytest.mark.parametrize("V", [3000, 151_937])
+def test_bf16_cuts_at_values(V):
+    """Nuclei that end above zero, below it, at it (of either sign) and among equal values."""
+    c = Case(12, V, "bf16", seed=V, cut="p", greedy=0, mask=False)
+    c.T[:] = 1.0
+    c.p[:] = [0.5, 0.9, 0.99, 0.999, 0.9999, 0.3, 0.9, 0.9, 0.9, 0.9, 0.5, 0.5]
+    c.logits[6] = np.round(c.logits[6])
+    c.logits[7] = np.abs(np.round(c.logits[7]))
+    c.logits[8] = -np.abs(c.logits[8])
+    c.logits[9] = np.where(np.arange(V) % 2, -0.0, 0.0)
+    c.logits[10] = np.where(np.arange(V) % 3, np.abs(c.logits[10]), -0.0)
+    c.logits[11, ::2] = 3.0
+    c.check()
