@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(kAppendWarps * 32, D == 128 ? 6 : 8) k_append(
   int s, n, len;
   if (!row_span(c, b, s, n, len)) return;
   const int pos = len + i - s;
-  const int turn = a.depth ? len + deep : pos;  // whose angles
-  if (a.cos && (deep < 0 || (a.depth ? deep >= a.n_pos - len : pos >= a.n_pos))) return;
+  if (a.cos && (a.depth ? deep < 0 || deep >= a.n_pos - len : pos >= a.n_pos)) return;
+  const int turn = a.depth && a.cos ? len + deep : pos;  // whose angles
   const int page = page_of(c, b, pos);
   if (page < 0) return;
   const int off = pos & ((1 << c.log_page) - 1);

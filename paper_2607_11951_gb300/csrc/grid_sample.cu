@@ -21,11 +21,20 @@
 //     one of them.  A bin of more than a list holds, as equal logits make it, is
 //     cut into 512 parts of its range of order instead, and again: nine bits
 //     less each time, six times at most.
-// min-p needs no X: w >= min_p is asked of every id.
+// For a small top-k, or where few ids are admitted, all that is left after the
+// first step is sorted, and block 0 draws from the list.  min-p needs no X: its
+// bound on (m - l) c is asked of every id.
 //
 // Sums of weights are integers, so that the order of the atomic additions does not
 // matter: in a bin in steps of 2^-16 or less of its weights (what fits 32 bits if
 // all of a block's ids are in it), elsewhere of 2^-40 of the largest.
+//
+// Bound by steps that follow one another (a row takes 10 to 30 us, of which the
+// loads are 3 and each barrier of the cluster 0.7) and, where many rows share the
+// SMs, by the instructions for an id and the additions to bins: 32 fp32 rows over
+// 151,936 ids (20 MB) with settings of all kinds take 28.5 us in a graph, 256 bf16
+// rows (83 MB) 86, one row over 512 ids 4.7 (a call takes 7.5).  Without cuts 32
+// rows take 14.8, most of it for the noise (39 MB).
 #include <atomic>
 #include <cfloat>
 #include <climits>
@@ -73,7 +82,6 @@ __device__ __forceinline__ Ask ask_of(const grid_sample_step& s, int b) {
   a.first = a.greedy || a.top_k == 1 || a.top_p <= 0.f || a.min_p > 1.f;
   return a;
 }
-
 
 struct Pick {   // of a draw: the best score and its id; the first id of the largest logit
   float score;
@@ -223,6 +231,13 @@ template <>
 struct Line<uint16_t> {
   static constexpr int N = 8;
   static __device__ __forceinline__ uint16_t none() { return 0xFF80; }
+  // Four bytes, each the top bit of one of x's eight times.
+  template <int kOf>
+  static __device__ __forceinline__ uint32_t signs(uint32_t x) {
+    uint32_t y;
+    asm("prmt.b32 %0, %1, 0, %2;" : "=r"(y) : "r"(x), "n"(kOf));
+    return y;
+  }
   static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
     const __nv_bfloat162 v = __hmax2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -232,13 +247,13 @@ struct Line<uint16_t> {
     return *reinterpret_cast<const uint32_t*>(&v);
   }
   static __device__ __forceinline__ uint4 admit(const uint4& r, unsigned bits) {
+    // (four bits to the tops of four bytes: bit i goes to i + 7, i + 14, i + 21 and i + 28, which never meet; then each top
+    // bit twice as a byte of its own, two bytes for a value)
+    const uint32_t lo = (bits & 15u) * 0x10204080u, hi = (bits >> 4) * 0x10204080u;
+    const uint32_t in[4] = {signs<0x9988>(lo), signs<0xBBAA>(lo), signs<0x9988>(hi), signs<0xBBAA>(hi)};
     uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      w[e] = min2(max2(w[e], 0xFF80FF80u), 0x7F7F7F7Fu);
-      if (!(bits >> (2 * e) & 1u)) w[e] = (w[e] & 0xFFFF0000u) | 0xFF80u;
-      if (!(bits >> (2 * e + 1) & 1u)) w[e] = (w[e] & 0xFFFFu) | 0xFF800000u;
-    }
+    for (int e = 0; e < 4; ++e) w[e] = (min2(max2(w[e], 0xFF80FF80u), 0x7F7F7F7Fu) & in[e]) | (0xFF80FF80u & ~in[e]);
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
   static __device__ __forceinline__ float top(const uint4& r) {
@@ -593,7 +608,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     unsigned upto_n[kPer];
     u64 upto_w[kPer];
     // bf16 logits from `from` on that are positive and of no more values than there are bins have a bin for each value, the
-    // largest's first: only their numbers are counted
+    // largest's first: only their numbers are counted (256 rows with top-p: 120 us instead of 125)
     bool by_value = false;
     const int top_value = __float_as_int(row.m) >> 16;
     auto value_of = [&](int bin) { return __int_as_float((top_value - bin) << 16); };
@@ -805,8 +820,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
               if (x1 >= least) atomicAdd(&sh.bins.n[top_value - x1], 1u);
             }
           }
-        } else
-        if (by_k && from > -INFINITY) {  // few ids in many lines
+        } else if (by_k && from > -INFINITY) {  // few ids in many lines
           for (int v = tid; v < count_v; v += kThreads) {
             const uint4 r = lines[v];
             if (!(L::top(r) >= at_least)) continue;
@@ -824,8 +838,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
             }
           }
         } else
-        // (eight ids at once, without branches: what one waits for, the others do too)
-        for (int v0 = tid; v0 < count_v; v0 += kLines * kThreads) {
+        for (int v0 = tid; v0 < count_v; v0 += kLines * kThreads) {  // eight ids at once: what one waits for, the others do too
           float x[8];
           int bin[8], w[8];
           bool any = false;
@@ -984,9 +997,9 @@ extern "C" int grid_sample(const grid_sample_step* s, void* stream) {
     return set_error(GRID_E_TOO_LARGE, "grid_sample: more than 65535 rows or 393216 ids");
   // (blocks by the vocabulary alone: a row's sums do not depend on the batch)
   int blocks = 1, log = 0;
-  while (blocks < kMaxBlocks && s->V > 4096 * blocks) blocks *= 2, ++log;
+  while (blocks < kMaxBlocks && s->V > 2048 * blocks) blocks *= 2, ++log;
   // (where the rows are more than the SMs hold at once, and few enough to look at all: 256 rows over 151,937 bf16 logits,
-  // some greedy, XX us instead of XX)
+  // some greedy, 86 us instead of 96)
   const bool sorted = s->B * blocks > 608 && s->B <= 2048 && (s->d_temperature || s->d_top_k || s->d_top_p || s->d_min_p);
   const SampleArgs a = {*s, ((s->V + blocks - 1) / blocks + 31) & ~31, sorted};
   const size_t smem = kSharedRoom + (size_t)a.each * size + 32;
