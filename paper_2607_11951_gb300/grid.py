@@ -547,9 +547,11 @@ def grid_configs_export(cfg, row: int, cap: int = 1 << 16):
 # The structures of include/grid.h that calls fill: packed by struct, which takes half the time of ctypes (padding included).
 _HEADS, _CHUNK, _ROTATION, _NORM = struct.Struct("Pqq"), struct.Struct("PqPPiiii"), struct.Struct("PPiiii"), struct.Struct("PPfi")
 _QUERY, _STEP = struct.Struct("PqqPqqPfi"), struct.Struct("PqqPqqPqqPPPPqPiiiiiiPPPP")
+_QUERY_END = struct.Struct("Pfi")  # (after two _HEADS)
 _TREE, _PAGES, _SAMPLE = struct.Struct("PPii"), struct.Struct("PqPPPPPiiiiPqPPPP"), struct.Struct("PqPqPqPPPPiiiiPPP")
 
 
+_pack_heads, _pack_chunk = _HEADS.pack, _CHUNK.pack
 _int32 = _float32 = _bfloat16 = _current = None
 
 
@@ -581,12 +583,12 @@ def _floats(x, n, dev):
     return x.data_ptr()
 
 
-def _heads(x, kv, N, H):
-    """A [tokens, heads, D] tensor (any strides, D contiguous) as (address, strides)."""
+def _heads(x, shape, dtype, dev):
+    """A [tokens, heads, D] tensor (any strides, D contiguous) as grid_heads."""
     a, b, c = x.stride()
-    assert x.get_device() == kv.device and x.dtype is kv.dtype and x.shape == (N, H, kv.D) and c == 1, \
+    assert x.get_device() == dev and x.dtype is dtype and x.shape == shape and c == 1, \
         "tensor [tokens, heads, D] of the cache's type and device expected, D contiguous"
-    return x.data_ptr(), a, b
+    return _pack_heads(x.data_ptr(), a, b)
 
 
 def _chunk(kv, table, lens, start, status, N):
@@ -602,7 +604,7 @@ def _chunk(kv, table, lens, start, status, N):
     if start is not None:
         assert start.dtype is i32 and start.get_device() == dev and start.is_contiguous() and start.shape == (B + 1,), \
             "int32 start [B + 1] expected"
-    return _CHUNK.pack(table.data_ptr(), stride[0], lens.data_ptr(), 0 if start is None else start.data_ptr(), shape[1], B, N, 0)
+    return _pack_chunk(table.data_ptr(), stride[0], lens.data_ptr(), 0 if start is None else start.data_ptr(), shape[1], B, N, 0)
 
 
 def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None, cos=None, sin=None, pairs=False,
@@ -613,24 +615,27 @@ def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None
     start int32 [B + 1] (None: the same number of tokens per row); q and q_out
     [tokens, heads, D]; cos, sin float32 [positions, rot / 2]; norm weights [D].
     depth int32 [tokens]: the chunk is a tree, a token is turned by its depth in it."""
-    N = k.shape[0]
+    N, D, dtype, dev = k.shape[0], kv.D, kv.dtype, kv.device
     chunk = _chunk(kv, table, lens, start, status, N)
-    kh, vh = _HEADS.pack(*_heads(k, kv, N, kv.kv_heads)), _HEADS.pack(*_heads(v, kv, N, kv.kv_heads))
+    shape = (N, kv.kv_heads, D)
+    kh, vh = _heads(k, shape, dtype, dev), _heads(v, shape, dtype, dev)
     qh = oh = rot = norm = None
     assert (q is None) == (q_out is None), "q and q_out go together"
     if q is not None:
-        qh, oh = _HEADS.pack(*_heads(q, kv, N, kv.heads)), _HEADS.pack(*_heads(q_out, kv, N, kv.heads))
+        shape = (N, kv.heads, D)
+        qh = _heads(q, shape, dtype, dev)
+        oh = qh if q_out is q else _heads(q_out, shape, dtype, dev)
     assert (cos is None) == (sin is None), "cos and sin go together"
     if cos is not None:
         shape = cos.shape
-        assert cos.dtype is sin.dtype is kv.f32 and cos.is_cuda and sin.is_cuda and cos.is_contiguous() and \
+        assert cos.dtype is sin.dtype is kv.f32 and cos.get_device() == sin.get_device() == dev and cos.is_contiguous() and \
             sin.is_contiguous() and len(shape) == 2 and shape == sin.shape, \
-            "contiguous float32 CUDA tensors [positions, rot / 2] expected"
+            "contiguous float32 tensors [positions, rot / 2] on the cache's device expected"
         rot = _ROTATION.pack(cos.data_ptr(), sin.data_ptr(), shape[0], 2 * shape[1], pairs, 0)
     if q_norm is not None or k_norm is not None:
         for w in (q_norm, k_norm):
-            assert w is None or (w.is_cuda and w.dtype is kv.dtype and w.shape == (kv.D,) and w.is_contiguous()), \
-                "norm weights [D] of the cache's type expected"
+            assert w is None or (w.get_device() == dev and w.dtype is dtype and w.numel() == D and w.is_contiguous()), \
+                "norm weights [D] of the cache's type and device expected"
         norm = _NORM.pack(0 if q_norm is None else q_norm.data_ptr(), 0 if k_norm is None else k_norm.data_ptr(), eps, 0)
     if depth is None:
         _check(lib().grid_kv_append(kv.h, chunk, kh, vh, qh, oh, rot, norm, status.data_ptr(), _on(stream, kv.device)))
@@ -644,13 +649,14 @@ def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=
     and start as there): q, out [tokens, heads, D], lse float32 [tokens, heads];
     scale defaults to 1 / sqrt(D).  sees int32 [tokens, words]: the chunk is a tree,
     a token sees those of the row's tokens whose bit is set (grid_tree_plan)."""
-    N = q.shape[0]
+    N, dev = q.shape[0], kv.device
     chunk = _chunk(kv, table, lens, start, status, N)
     if lse is not None:
-        assert lse.dtype is kv.f32 and lse.is_cuda and lse.is_contiguous() and lse.shape == (N, kv.heads), \
+        assert lse.dtype is kv.f32 and lse.get_device() == dev and lse.is_contiguous() and lse.shape == (N, kv.heads), \
             "float32 lse [tokens, heads] expected"
-    query = _QUERY.pack(*_heads(q, kv, N, kv.heads), *_heads(out, kv, N, kv.heads), 0 if lse is None else lse.data_ptr(),
-                        kv.D ** -0.5 if scale is None else scale, 0)
+    shape, dtype = (N, kv.heads, kv.D), kv.dtype
+    query = _heads(q, shape, dtype, dev) + _heads(out, shape, dtype, dev) + \
+        _QUERY_END.pack(0 if lse is None else lse.data_ptr(), kv.D ** -0.5 if scale is None else scale, 0)
     if sees is None:
         _check(lib().grid_kv_attend(kv.h, chunk, query, status.data_ptr(), _on(stream, kv.device)))
         return
