@@ -782,6 +782,7 @@ def grid_pages_update(pages, table, held, want, table_out, held_out, copies, ref
         "int32 tables [A, width] and [B, width_out] on the current device expected, their rows contiguous"
     was, held_at = _ints(held, A, dev), _ints(held_out, B, dev)
     assert at != at_out and was != held_at, "the new table and lengths need tensors of their own"
+    assert copies.shape == (3, B), "int32 copies [3, B] expected"
     step = _PAGES.pack(
         at, by if A > 1 else width, was, 0 if parent is None else _ints(parent, B, dev), 0 if keep is None else _ints(keep, B, dev),
         _ints(want, B, dev), 0 if pinned is None else _ints(pinned, n, dev), A, width, B, width_out, at_out,
@@ -794,6 +795,7 @@ def grid_kv_copy(kv, copies, status, stream=None):
     from its beginning), status int32 [n]."""
     n, dev = status.shape[0], kv.device
     assert _device() == dev, "the cache is on another device than the current one"
+    assert copies.shape == (3, n), "int32 copies [3, n] expected"
     _check(lib().grid_kv_copy(kv.h, _ints(copies, 3 * n, dev), n, _ints(status, n, dev), _on(stream, dev)))
 
 
