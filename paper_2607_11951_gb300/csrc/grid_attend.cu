@@ -6,6 +6,10 @@
 // in fp32, P = exp2((S - m) scale log2 e) is rounded to the cache's type for
 // O += P V (tensor cores, fp32), and O and l are rescaled when m grows.
 //
+// A chunk that is a tree of tokens (grid_kv_attend_tree) hides scores by the bits of
+// what each token sees instead of by position, in the tiles that hold tokens of the
+// chunk; all else is the same, and so are the times within 1%.
+//
 // Work.  The query rows of a row b and key head h are its tokens times the
 // H / Hk heads that read h (row = token * group + head), so that a key tile is
 // read once for all of them.  A unit is 256 such rows, or all of them where
@@ -993,8 +997,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++n_o[z];
         }
       if (!ok) break;
-      // A sum of zero: the row sees no key, and gets zeros.  A sum below zero: some key that the rows may read is in no page of the cache (known once all tiles were), and they
-      // get zeros.  A sum that is no number, of a query that is none, gives NaN.
+      // A sum of zero: the row sees no key, and gets zeros.  A sum below zero: some key that the rows may read is in no page of
+      // the cache (known once all tiles were), and they get zeros.  A sum that is no number, of a query that is none, gives NaN.
       if (sh.bad[0][k % kRing] | sh.bad[1][k % kRing]) l = -1.f;
       if (warp_live) {
         tm_after();
