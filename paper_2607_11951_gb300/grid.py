@@ -661,7 +661,7 @@ def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=
         _check(lib().grid_kv_attend(kv.h, chunk, query, status.data_ptr(), _on(stream, kv.device)))
         return
     rows, words = sees.shape
-    assert rows == N, "int32 sees [tokens, words] expected"
+    assert rows == N and words > 0, "int32 sees [tokens, words] expected"
     _check(lib().grid_kv_attend_tree(kv.h, chunk, query, _ints(sees, N * words, kv.device), words, status.data_ptr(),
                                      _on(stream, kv.device)))
 

@@ -283,3 +283,30 @@ def test_forks_read_what_their_parent_wrote():
             # (bf16 probabilities and result: half a step each, of up to sum p |v|; scores off by 64 products' 2^-24 of up to 64 x 16)
             near = (2.0 ** -7 + 2.0 ** -12) * torch.einsum("hj,jhd->hd", x.softmax(1), vs.abs())
             assert bool(((out[last].double() - want).abs() <= near).all())
+
+
+def test_refusals_of_the_binding():
+    import torch
+    from paper_2607_11951_gb300 import grid as G
+    s = State(3, 4, 16, 60, 1)
+    h = G.Pages(s.n_pages, 16)
+    args = {**s.t, **s.out, **s.more}
+    G.grid_pages_update(h, **args)
+    for bad in (dict(table=s.t["table"].long()), dict(table=s.t["table"].cpu()), dict(held=s.t["held"][:2]), dict(want=s.t["want"].float()),
+                dict(table_out=s.out["table_out"][:3]), dict(held_out=s.out["held_out"][:3]), dict(copies=s.out["copies"].T.contiguous()),
+                dict(refs=s.out["refs"][:-1]), dict(status=s.out["status"].cpu()), dict(parent=s.more["parent"][:2]),
+                dict(keep=s.more["keep"].long()), dict(pinned=s.more["pinned"][:-1]),
+                dict(table_out=torch.zeros((7, 4), dtype=torch.int32, device="cuda").T)):
+        with pytest.raises(AssertionError):
+            G.grid_pages_update(h, **{**args, **bad})
+    with pytest.raises(AssertionError):  # (the new table in the old one's place)
+        G.grid_pages_update(h, **{**args, "table": s.out["table_out"], "held": s.out["held_out"], "parent": None, "keep": None})
+    with pytest.raises(G.GridError):  # (more rows than there are to go on)
+        G.grid_pages_update(h, **{**args, "parent": None})
+    with pytest.raises(G.GridError):
+        G.Pages(10, 24)
+    kv = G.PagedKV(*[torch.zeros((4, 16, 1, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)], 1)
+    with pytest.raises(AssertionError):
+        G.grid_kv_copy(kv, s.out["copies"].T.contiguous(), s.out["status"])
+    with pytest.raises(AssertionError):
+        G.grid_kv_copy(kv, s.out["copies"], s.out["status"].cpu())

@@ -437,3 +437,31 @@ def test_a_step_on_another_stream_and_captured():
     s.tokens.fill_(1)
     graphs[0].replay()
     assert same(s.run(), outs[0])
+
+
+def test_refusals_of_the_binding():
+    import torch
+    b = Trees([3, 4], [2, 3], 4, 2, 64, 16)
+    G, i32 = b.G, dict(dtype=torch.int32, device="cuda")
+    depth, sees, st = torch.zeros(5, **i32), torch.zeros((5, 1), **i32), torch.zeros(2, **i32)
+    path, count = torch.zeros((2, 3), **i32), torch.zeros(2, **i32)
+    for call in (lambda: G.grid_kv_attend(b.kv, b.table, b.lens, b.q, b.out, b.status, start=b.start, sees=sees[:4]),
+                 lambda: G.grid_kv_attend(b.kv, b.table, b.lens, b.q, b.out, b.status, start=b.start, sees=sees[:, :0]),
+                 lambda: G.grid_kv_attend(b.kv, b.table, b.lens, b.q, b.out, b.status, start=b.start, sees=sees.long()),
+                 lambda: G.grid_kv_attend(b.kv, b.table, b.lens, b.q, b.out, b.status, start=b.start, sees=sees.cpu()),
+                 lambda: append(b, depth=depth[:4]), lambda: append(b, depth=depth.float()), lambda: append(b, depth=depth.cpu()),
+                 lambda: G.grid_tree_plan(b.parent.cpu(), depth, sees, st, start=b.start),
+                 lambda: G.grid_tree_plan(b.parent, depth[:4], sees, st, start=b.start),
+                 lambda: G.grid_tree_plan(b.parent, depth, sees[:4], st, start=b.start),
+                 lambda: G.grid_tree_plan(b.parent, depth, sees, st, start=b.start[:2]),
+                 lambda: G.grid_tree_accept(b.parent, depth, depth[:3], path, count, path.clone(), st, start=b.start),
+                 lambda: G.grid_tree_accept(b.parent, depth, depth, path, count, path.T.contiguous(), st, start=b.start),
+                 lambda: G.grid_tree_accept(b.parent, depth, depth, path[:1], count, path[:1], st, start=b.start),
+                 lambda: G.grid_kv_compact(b.kv, b.table, b.lens, path[:1], count, b.status, 5, start=b.start),
+                 lambda: G.grid_kv_compact(b.kv, b.table, b.lens, path, count.float(), b.status, 5, start=b.start)):
+        with pytest.raises(AssertionError):
+            call()
+    with pytest.raises(G.GridError):
+        G.grid_tree_plan(b.parent, depth, sees[:, :0].contiguous(), st, start=b.start)
+    with pytest.raises(G.GridError):  # (five tokens of two rows alike)
+        G.grid_tree_plan(b.parent, depth, sees, st)
