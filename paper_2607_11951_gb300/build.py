@@ -1,8 +1,12 @@
 """Build libgrid.so in-tree for sm_103a with nvcc (host C++ and CUDA sources
-compiled in parallel, then linked).  Output: paper_2607_11951_gb300/_build/libgrid.so"""
+compiled in parallel, then linked) and the binding's calls on tensors.  Output:
+paper_2607_11951_gb300/_build/libgrid.so and grid_binding.so"""
+import importlib.util
 import os
+import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -19,6 +23,26 @@ def library_path() -> str:
     return os.path.join(OUT, "libgrid.so")
 
 
+def binding_path() -> str:
+    return os.path.join(OUT, "grid_binding.so")
+
+
+def build_binding() -> None:
+    """The calls on tensors (csrc/grid_python.cpp), against the installed torch."""
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which(NVCC) or "/usr/local/cuda/bin/nvcc")))
+    include = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    libs, tmp = os.path.join(torch, "lib"), binding_path() + ".tmp"
+    cmd = ["g++", "-std=c++17", "-O2", "-fPIC", "-shared"] + ["-I" + i for i in include] + \
+        [os.path.join(CSRC, "grid_python.cpp"), "-o", tmp, "-L" + libs, "-Wl,-rpath," + libs,
+         "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed for grid_python.cpp:\n%s%s" % (r.stdout, r.stderr))
+    os.replace(tmp, binding_path())
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(OUT, exist_ok=True)
 
@@ -33,8 +57,10 @@ def build(verbose: bool = False) -> str:
             sys.stderr.write(r.stderr)
         return obj
 
-    with ThreadPoolExecutor(len(SOURCES)) as ex:
+    with ThreadPoolExecutor(len(SOURCES) + 1) as ex:
+        binding = ex.submit(build_binding)
         objs = list(ex.map(compile_one, SOURCES))
+        binding.result()
     tmp = library_path() + ".tmp"
     cmd = [NVCC, "-shared", "-gencode", "arch=compute_103a,code=sm_103a"] + objs + ["-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -13,7 +13,7 @@ import ctypes
 import os
 import struct
 
-from .build import library_path
+from .build import binding_path, library_path
 
 GRID_OK = 0
 GRID_ST = {0: "OK", 1: "NONVIABLE", 2: "STACK_OVERFLOW", 3: "TOKEN_NOT_ALLOWED",
@@ -544,67 +544,34 @@ def grid_configs_export(cfg, row: int, cap: int = 1 << 16):
 
 
 # ---------------------------------------------------------------------------
-# The structures of include/grid.h that calls fill: packed by struct, which takes half the time of ctypes (padding included).
+# The structures of include/grid.h in struct's notation, padding included: packed by it, which takes half the time of ctypes
+# (_STEP here; the others for callers that fill the structures themselves).
 _HEADS, _CHUNK, _ROTATION, _NORM = struct.Struct("Pqq"), struct.Struct("PqPPiiii"), struct.Struct("PPiiii"), struct.Struct("PPfi")
 _QUERY, _STEP = struct.Struct("PqqPqqPfi"), struct.Struct("PqqPqqPqqPPPPqPiiiiiiPPPP")
-_QUERY_END = struct.Struct("Pfi")  # (after two _HEADS)
-_TREE, _PAGES, _SAMPLE = struct.Struct("PPii"), struct.Struct("PqPPPPPiiiiPqPPPP"), struct.Struct("PqPqPqPPPPiiiiPPP")
+
+# The calls on tensors that follow look at what they are given in compiled code (csrc/grid_python.cpp): a tensor of another
+# type, device, shape or order is an AssertionError.
+_calls = None
+_BOUND = ["grid_kv_append", "grid_kv_append_tree", "grid_kv_attend", "grid_kv_attend_tree", "grid_kv_compact", "grid_kv_copy",
+          "grid_tree_plan", "grid_tree_accept", "grid_sample", "grid_pages_update"]
 
 
-_pack_heads, _pack_chunk = _HEADS.pack, _CHUNK.pack
-_int32 = _float32 = _bfloat16 = _current = None
+def _binding():
+    """The compiled calls, bound to the loaded library."""
+    global _calls
+    if _calls is None:
+        import importlib.util
 
-
-def _device():
-    """The current device's number (0.1 us where torch.cuda.current_device() takes 0.3); the caller has a CUDA tensor."""
-    global _int32, _float32, _bfloat16, _current, _raw_stream
-    if _current is None:
-        import torch
-        _stream(None)  # (_raw_stream)
-        _int32, _float32, _bfloat16 = torch.int32, torch.float32, torch.bfloat16
-        _current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    return _current()
-
-
-def _on(stream, dev):
-    return _raw_stream(dev) if stream is None else _stream(stream)
-
-
-def _ints(x, n, dev):
-    """The address of n int32 values on device dev."""
-    assert x.dtype is _int32 and x.get_device() == dev and x.numel() == n and x.is_contiguous(), \
-        "contiguous int32 tensor of %d values on the current device expected" % n
-    return x.data_ptr()
-
-
-def _floats(x, n, dev):
-    assert x.dtype is _float32 and x.get_device() == dev and x.numel() == n and x.is_contiguous(), \
-        "contiguous float32 tensor of %d values on the current device expected" % n
-    return x.data_ptr()
-
-
-def _heads(x, shape, dtype, dev):
-    """A [tokens, heads, D] tensor (any strides, D contiguous) as grid_heads."""
-    a, b, c = x.stride()
-    assert x.get_device() == dev and x.dtype is dtype and x.shape == shape and c == 1, \
-        "tensor [tokens, heads, D] of the cache's type and device expected, D contiguous"
-    return _pack_heads(x.data_ptr(), a, b)
-
-
-def _chunk(kv, table, lens, start, status, N):
-    i32, rows, dev = kv.i32, lens.shape, kv.device
-    B = rows[0] if rows else 0  # (len() of a tensor takes 0.5 us)
-    shape, stride = table.shape, table.stride()
-    assert _device() == dev, "the cache is on another device than the current one"
-    assert table.dtype is i32 and lens.dtype is i32 and status.dtype is i32, "int32 table, lens and status expected"
-    assert table.get_device() == lens.get_device() == status.get_device() == dev and len(shape) == 2 and stride[1] == 1, \
-        "table [B, max_pages] on the cache's device expected, its rows contiguous"
-    assert shape[0] == B and rows == status.shape == (B,) and lens.is_contiguous() and status.is_contiguous(), \
-        "table [B, max_pages], lens [B] and status [B] expected"
-    if start is not None:
-        assert start.dtype is i32 and start.get_device() == dev and start.is_contiguous() and start.shape == (B + 1,), \
-            "int32 start [B + 1] expected"
-    return _pack_chunk(table.data_ptr(), stride[0], lens.data_ptr(), 0 if start is None else start.data_ptr(), shape[1], B, N, 0)
+        import torch  # noqa: F401  (its libraries, before the module that is linked to them)
+        if not os.path.exists(binding_path()):
+            raise GridLibraryMissing("grid_binding.so not built at %s: run __graft_entry__.build()" % binding_path())
+        L = lib()
+        spec = importlib.util.spec_from_file_location("grid_binding", binding_path())
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.bind(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _BOUND))
+        _calls = module
+    return _calls
 
 
 def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None, cos=None, sin=None, pairs=False,
@@ -615,33 +582,10 @@ def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None
     start int32 [B + 1] (None: the same number of tokens per row); q and q_out
     [tokens, heads, D]; cos, sin float32 [positions, rot / 2]; norm weights [D].
     depth int32 [tokens]: the chunk is a tree, a token is turned by its depth in it."""
-    N, D, dtype, dev = k.shape[0], kv.D, kv.dtype, kv.device
-    chunk = _chunk(kv, table, lens, start, status, N)
-    shape = (N, kv.kv_heads, D)
-    kh, vh = _heads(k, shape, dtype, dev), _heads(v, shape, dtype, dev)
-    qh = oh = rot = norm = None
-    assert (q is None) == (q_out is None), "q and q_out go together"
-    if q is not None:
-        shape = (N, kv.heads, D)
-        qh = _heads(q, shape, dtype, dev)
-        oh = qh if q_out is q else _heads(q_out, shape, dtype, dev)
-    assert (cos is None) == (sin is None), "cos and sin go together"
-    if cos is not None:
-        shape = cos.shape
-        assert cos.dtype is sin.dtype is kv.f32 and cos.get_device() == sin.get_device() == dev and cos.is_contiguous() and \
-            sin.is_contiguous() and len(shape) == 2 and shape == sin.shape, \
-            "contiguous float32 tensors [positions, rot / 2] on the cache's device expected"
-        rot = _ROTATION.pack(cos.data_ptr(), sin.data_ptr(), shape[0], 2 * shape[1], pairs, 0)
-    if q_norm is not None or k_norm is not None:
-        for w in (q_norm, k_norm):
-            assert w is None or (w.get_device() == dev and w.dtype is dtype and w.numel() == D and w.is_contiguous()), \
-                "norm weights [D] of the cache's type and device expected"
-        norm = _NORM.pack(0 if q_norm is None else q_norm.data_ptr(), 0 if k_norm is None else k_norm.data_ptr(), eps, 0)
-    if depth is None:
-        _check(lib().grid_kv_append(kv.h, chunk, kh, vh, qh, oh, rot, norm, status.data_ptr(), _on(stream, kv.device)))
-    else:
-        _check(lib().grid_kv_append_tree(kv.h, chunk, kh, vh, qh, oh, rot, norm, _ints(depth, N, kv.device),
-                                         status.data_ptr(), _on(stream, kv.device)))
+    rc = (_calls or _binding()).kv_append(kv.info, table, lens, k, v, status, start, q, q_out, cos, sin, pairs, q_norm,
+                                          k_norm, eps, depth, stream)
+    if rc:
+        _check(rc)
 
 
 def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=None, sees=None, stream=None):
@@ -649,21 +593,10 @@ def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=
     and start as there): q, out [tokens, heads, D], lse float32 [tokens, heads];
     scale defaults to 1 / sqrt(D).  sees int32 [tokens, words]: the chunk is a tree,
     a token sees those of the row's tokens whose bit is set (grid_tree_plan)."""
-    N, dev = q.shape[0], kv.device
-    chunk = _chunk(kv, table, lens, start, status, N)
-    if lse is not None:
-        assert lse.dtype is kv.f32 and lse.get_device() == dev and lse.is_contiguous() and lse.shape == (N, kv.heads), \
-            "float32 lse [tokens, heads] expected"
-    shape, dtype = (N, kv.heads, kv.D), kv.dtype
-    query = _heads(q, shape, dtype, dev) + _heads(out, shape, dtype, dev) + \
-        _QUERY_END.pack(0 if lse is None else lse.data_ptr(), kv.D ** -0.5 if scale is None else scale, 0)
-    if sees is None:
-        _check(lib().grid_kv_attend(kv.h, chunk, query, status.data_ptr(), _on(stream, kv.device)))
-        return
-    rows, words = sees.shape
-    assert rows == N and words > 0, "int32 sees [tokens, words] expected"
-    _check(lib().grid_kv_attend_tree(kv.h, chunk, query, _ints(sees, N * words, kv.device), words, status.data_ptr(),
-                                     _on(stream, kv.device)))
+    rc = (_calls or _binding()).kv_attend(kv.info, table, lens, q, out, status, lse, start, kv.scale if scale is None else scale,
+                                          sees, stream)
+    if rc:
+        _check(rc)
 
 
 class PagedKV:
@@ -679,13 +612,15 @@ class PagedKV:
         dt = {torch.bfloat16: GRID_DTYPE_BF16, torch.float16: GRID_DTYPE_F16}[k_pages.dtype]
         n, page, self.kv_heads, self.D = k_pages.shape
         self.heads, self.dtype, self.pools = heads, k_pages.dtype, (k_pages, v_pages)
-        self.i32, self.f32, self.device = torch.int32, torch.float32, k_pages.get_device()
+        self.device, self.scale = k_pages.get_device(), self.D ** -0.5
         assert v_pages.get_device() == self.device, "both pools on one device expected"
         p = _KvPages(k_pages.data_ptr(), v_pages.data_ptr(), dt, self.D, heads, self.kv_heads, page, n,
                      k_pages.stride()[:3], v_pages.stride()[:3])
         out = ctypes.c_void_p()
         _check(lib().grid_kv_create(ctypes.byref(p), ctypes.byref(out)))
         self.h = out
+        # (what the compiled calls need to know of it)
+        self.info = struct.pack("Piiiiii", out.value, heads, self.kv_heads, self.D, dt == GRID_DTYPE_F16, self.device, 0)
 
     def __del__(self):
         if getattr(self, "h", None) and _lib is not None:
@@ -693,46 +628,32 @@ class PagedKV:
             self.h = None
 
 
-def _tree(parent, start, B, dev):
-    N = parent.shape[0]
-    return _TREE.pack(_ints(parent, N, dev), 0 if start is None else _ints(start, B + 1, dev), B, N), N
-
-
 def grid_tree_plan(parent, depth, sees, status, start=None, stream=None):
     """Depths and visibility of rows of drafted tokens: parent int32 [tokens] (an
     earlier token of the row, by its index there, or -1), start int32 [B + 1]
     (None: the same number of tokens per row).  Out: depth int32 [tokens], sees
     int32 [tokens, words] (words >= a row's tokens / 32), status int32 [B]."""
-    dev, B = _device(), status.shape[0]
-    tree, N = _tree(parent, start, B, dev)
-    rows, words = sees.shape
-    assert rows == N, "sees [tokens, words] expected"
-    _check(lib().grid_tree_plan(tree, _ints(depth, N, dev), _ints(sees, N * words, dev), words, _ints(status, B, dev),
-                                _on(stream, dev)))
+    rc = (_calls or _binding()).tree_plan(parent, depth, sees, status, start, stream)
+    if rc:
+        _check(rc)
 
 
 def grid_tree_accept(parent, tokens, sampled, path, count, out, status, start=None, eos=-1, stream=None):
     """The path that the sampled tokens take: parent, tokens (drafted) and sampled
     int32 [tokens].  Out: path (indices in the row) and out (what was sampled
     there) int32 [B, most], -1 past the end; count, status int32 [B]."""
-    dev, B = _device(), status.shape[0]
-    tree, N = _tree(parent, start, B, dev)
-    rows, most = path.shape
-    assert rows == B and out.shape == path.shape, "path and out [B, most] expected"
-    _check(lib().grid_tree_accept(tree, _ints(tokens, N, dev), _ints(sampled, N, dev), eos, most, _ints(path, B * most, dev),
-                                  _ints(count, B, dev), _ints(out, B * most, dev), _ints(status, B, dev), _on(stream, dev)))
+    rc = (_calls or _binding()).tree_accept(parent, tokens, sampled, path, count, out, status, start, eos, stream)
+    if rc:
+        _check(rc)
 
 
 def grid_kv_compact(kv, table, lens, path, count, status, n_tokens, start=None, stream=None):
     """The path's keys and values next to what was cached before the chunk (table,
     lens, start and n_tokens as in its append; path and count of
     grid_tree_accept)."""
-    chunk, dev = _chunk(kv, table, lens, start, status, n_tokens), kv.device
-    B = lens.shape[0]
-    rows, most = path.shape
-    assert rows == B, "path [B, most] expected"
-    _check(lib().grid_kv_compact(kv.h, chunk, _ints(path, B * most, dev), _ints(count, B, dev), most, status.data_ptr(),
-                                 _on(stream, dev)))
+    rc = (_calls or _binding()).kv_compact(kv.info, table, lens, path, count, status, n_tokens, start, stream)
+    if rc:
+        _check(rc)
 
 
 def grid_sample(logits, noise, tokens, status, mask=None, temperature=None, top_k=None, top_p=None, min_p=None,
@@ -742,26 +663,9 @@ def grid_sample(logits, noise, tokens, status, mask=None, temperature=None, top_
     int32 [B, W] (rows of these may be strided); temperature, top_p, min_p float32
     [B], top_k int32 [B] or None.  Out: tokens, status int32 [B], logprob float32
     [B] or None."""
-    dev, dt = _device(), logits.dtype
-    B, V = logits.shape
-    assert dt is _float32 or dt is _bfloat16, "float32 or bfloat16 logits expected"
-    by, one = logits.stride()
-    to, two = noise.stride()
-    assert logits.get_device() == noise.get_device() == dev and noise.dtype is _float32 and noise.shape == (B, V) and \
-        (one == two == 1 or V == 1), "logits and float32 noise [B, V] on the current device expected, their rows contiguous"
-    bits = words = 0
-    if mask is not None:
-        words, one = mask.stride()
-        W = (V + 31) // 32
-        assert mask.dtype is _int32 and mask.get_device() == dev and mask.shape == (B, W) and (one == 1 or W == 1), \
-            "int32 mask [B, ceil(V/32)] on the current device expected, its rows contiguous"
-        bits = mask.data_ptr()
-    step = _SAMPLE.pack(
-        logits.data_ptr(), by, bits, words, noise.data_ptr(), to, 0 if temperature is None else _floats(temperature, B, dev),
-        0 if top_k is None else _ints(top_k, B, dev), 0 if top_p is None else _floats(top_p, B, dev),
-        0 if min_p is None else _floats(min_p, B, dev), GRID_DTYPE_F32 if dt is _float32 else GRID_DTYPE_BF16, B, V, eos,
-        _ints(tokens, B, dev), 0 if logprob is None else _floats(logprob, B, dev), _ints(status, B, dev))
-    _check(lib().grid_sample(step, _on(stream, dev)))
+    rc = (_calls or _binding()).sample(logits, noise, tokens, status, mask, temperature, top_k, top_p, min_p, logprob, eos, stream)
+    if rc:
+        _check(rc)
 
 
 def grid_pages_update(pages, table, held, want, table_out, held_out, copies, refs, status, parent=None, keep=None,
@@ -771,32 +675,18 @@ def grid_pages_update(pages, table, held, want, table_out, held_out, copies, ref
     pinned int32 [pages].  Out: table_out int32 [B, width_out], held_out, status
     int32 [B], copies int32 [3, B] (for grid_kv_copy), refs int32 [pages].
     ``pages``: a Pages."""
-    dev, n = pages.device, pages.n_pages
-    assert _device() == dev, "the pages' scratch is on another device than the current one"
-    A, B = held.shape[0], want.shape[0]
-    (rows, width), (by, one) = table.shape, table.stride()
-    (rows_out, width_out), (by_out, two) = table_out.shape, table_out.stride()
-    at, at_out = table.data_ptr(), table_out.data_ptr()
-    assert table.dtype is table_out.dtype is _int32 and table.get_device() == table_out.get_device() == dev and rows == A and \
-        rows_out == B and (one == 1 or width == 1) and (two == 1 or width_out == 1), \
-        "int32 tables [A, width] and [B, width_out] on the current device expected, their rows contiguous"
-    was, held_at = _ints(held, A, dev), _ints(held_out, B, dev)
-    assert at != at_out and was != held_at, "the new table and lengths need tensors of their own"
-    assert copies.shape == (3, B), "int32 copies [3, B] expected"
-    step = _PAGES.pack(
-        at, by if A > 1 else width, was, 0 if parent is None else _ints(parent, B, dev), 0 if keep is None else _ints(keep, B, dev),
-        _ints(want, B, dev), 0 if pinned is None else _ints(pinned, n, dev), A, width, B, width_out, at_out,
-        by_out if B > 1 else width_out, held_at, _ints(copies, 3 * B, dev), _ints(refs, n, dev), _ints(status, B, dev))
-    _check(lib().grid_pages_update(pages.h, step, _on(stream, dev)))
+    rc = (_calls or _binding()).pages_update(pages.at, pages.device, pages.n_pages, table, held, want, table_out, held_out,
+                                             copies, refs, status, parent, keep, pinned, stream)
+    if rc:
+        _check(rc)
 
 
 def grid_kv_copy(kv, copies, status, stream=None):
     """Copy pages of a cache: copies int32 [3, n] (from page or -1, to page, tokens
     from its beginning), status int32 [n]."""
-    n, dev = status.shape[0], kv.device
-    assert _device() == dev, "the cache is on another device than the current one"
-    assert copies.shape == (3, n), "int32 copies [3, n] expected"
-    _check(lib().grid_kv_copy(kv.h, _ints(copies, 3 * n, dev), n, _ints(status, n, dev), _on(stream, dev)))
+    rc = (_calls or _binding()).kv_copy(kv.info, copies, status, stream)
+    if rc:
+        _check(rc)
 
 
 class Pages:
@@ -807,7 +697,7 @@ class Pages:
         self.device, self.n_pages = torch.cuda.current_device() if torch.cuda.is_available() else 0, n_pages
         out = ctypes.c_void_p()
         _check(lib().grid_pages_create(n_pages, page_size, ctypes.byref(out)))
-        self.h = out
+        self.h, self.at = out, out.value
 
     def __del__(self):
         if getattr(self, "h", None) and _lib is not None:

@@ -172,10 +172,3 @@ def test_a_draw_fits_the_device(fake, dtype, B, V):
         assert G.lib().grid_sample(sample(B=B, V=V, dtype=dtype), None) == 0
         for _, g, threads, smem, limit in rt.launches():
             assert g[0] % B == 0 and g[1] == g[2] == 1 and smem <= limit <= 227 << 10 and threads <= 1024
-
-
-def test_packed_arguments_have_the_layout_of_the_structures():
-    for packed, structure in ((G._TREE, T.Tree), (G._PAGES, T.PagesStep), (G._SAMPLE, T.SampleStep)):
-        assert packed.size == ctypes.sizeof(structure)
-        values = list(range(1, len(structure._fields_) + 1))
-        assert bytes(structure(*values)) == packed.pack(*values)
