@@ -212,7 +212,7 @@ static int append(const char* name, const grid_kv* kv, const grid_kv_chunk* chun
   a.H = p.n_heads, a.Hk = p.n_kv_heads;
   a.status = d_status, a.depth = d_depth;
   // (whole tokens where their warps fill the SMs anyway)
-  a.splits = std::max(1, std::min(a.groups[2], 32 * kv->sms / std::max(1, chunk->n_tokens)));
+  a.splits = std::max(1, std::min(a.groups[2], (p.head_dim == 128 ? 24 : 32) * kv->sms / std::max(1, chunk->n_tokens)));
   const long long blocks = ((long long)chunk->n_tokens * a.splits + kAppendWarps - 1) / kAppendWarps;
   const int rows = (chunk->B + kAppendWarps - 1) / kAppendWarps;
   if (blocks + rows > INT32_MAX) return refuse(GRID_E_TOO_LARGE, "too many head vectors in one call");

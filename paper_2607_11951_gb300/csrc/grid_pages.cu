@@ -260,20 +260,35 @@ __global__ void __launch_bounds__(kUpdateThreads) k_update_alone(const UpdateArg
   }
   __syncthreads();
   // ---- whole pages are counted, pages in part noted
-  const int entries = s.B * s.width_out;
-#pragma unroll 8
-  for (int x = tid; x < entries; x += kUpdateThreads) {
-    const int i = x / s.width_out, j = x - i * s.width_out;
-    const bool in = j < rows[i].kept;
-    const int p = in ? s.d_table[rows[i].parent * s.table_stride + j] : -1;
-    s.d_table_out[i * s.table_out_stride + j] = p;
-    if (!in) continue;
-    if (p < 0 || p >= u.n_pages)
-      bad = 1;
-    else if (j < rows[i].keep >> u.log_page)
-      atomicAdd(&refs[p], 1u);
-    else
-      rows[i].last = p;
+  {
+    // (a thread's entries are kUpdateThreads apart: rows and columns by addition, four loads at once)
+    const int w = s.width_out, rows_on = kUpdateThreads / w, on = kUpdateThreads - rows_on * w;
+    int i = tid / w, j = tid - i * w;
+    constexpr int kAtOnce = 4;
+    while (i < s.B) {
+      int at_i[kAtOnce], at_j[kAtOnce], p[kAtOnce];
+#pragma unroll
+      for (int y = 0; y < kAtOnce; ++y) {
+        at_i[y] = i, at_j[y] = j;
+        p[y] = -1;
+        if (i < s.B && j < rows[i].kept) p[y] = s.d_table[rows[i].parent * s.table_stride + j];
+        i += rows_on, j += on;
+        if (j >= w) j -= w, ++i;
+      }
+#pragma unroll
+      for (int y = 0; y < kAtOnce; ++y) {
+        if (at_i[y] >= s.B) break;
+        s.d_table_out[at_i[y] * s.table_out_stride + at_j[y]] = p[y];
+        UpdateRow& row = rows[at_i[y]];
+        if (at_j[y] >= row.kept) continue;
+        if (p[y] < 0 || p[y] >= u.n_pages)
+          bad = 1;
+        else if (at_j[y] < row.keep >> u.log_page)
+          atomicAdd(&refs[p[y]], 1u);
+        else
+          row.last = p[y];
+      }
+    }
   }
   __syncthreads();
   if (bad)  // (rows with a page outside the pool take back what they counted)
