@@ -53,6 +53,7 @@ constexpr int kBins = 1024, kPer = kBins / kThreads;  // a thread sums up kPer n
 constexpr int kParts = 512, kPartBits = 9;            // of a range of order
 constexpr int kList = 512;                // ids that are sorted at once
 constexpr int kDirect = 256;              // a top_k up to here is looked for without bins
+constexpr int kSparse = 2048;             // admitted ids of a block that are taken one by one, if an eighth of all at most
 constexpr int kIdBits = 22;
 constexpr int kMaxIds = 393216;           // 48 Ki fp32 logits for each of eight blocks
 constexpr float kFirstRange = 40.f;       // exponents below m that bins reach
@@ -83,8 +84,8 @@ __device__ __forceinline__ Ask ask_of(const grid_sample_step& s, int b) {
   return a;
 }
 
-struct Pick {   // of a draw: the best score and its id; the first id of the largest logit
-  float score;
+struct Pick {   // of a draw: the best score, its id and logit; the first id of the largest logit
+  float score, logit;
   int id, first;
 };
 struct Found {  // the bin that a search ends in, and what lies in the bins before it
@@ -168,13 +169,14 @@ __device__ __forceinline__ float sum_warp(float x) {
   return x;
 }
 __device__ __forceinline__ void better(Pick& x, const Pick& y) {
-  if (y.score < x.score || (y.score == x.score && y.id < x.id)) x.score = y.score, x.id = y.id;
+  if (y.score < x.score || (y.score == x.score && y.id < x.id)) x.score = y.score, x.logit = y.logit, x.id = y.id;
   x.first = min(x.first, y.first);
 }
 __device__ __forceinline__ Pick best_warp(Pick x) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
-    const Pick y = {__shfl_xor_sync(~0u, x.score, o), __shfl_xor_sync(~0u, x.id, o), __shfl_xor_sync(~0u, x.first, o)};
+    const Pick y = {__shfl_xor_sync(~0u, x.score, o), __shfl_xor_sync(~0u, x.logit, o), __shfl_xor_sync(~0u, x.id, o),
+                    __shfl_xor_sync(~0u, x.first, o)};
     better(x, y);
   }
   return x;
@@ -315,7 +317,7 @@ struct Row {
 };
 __device__ __forceinline__ u64 units(float w) { return __float2ull_rn(w * kUnit); }
 
-template <typename T, int blocks>
+template <typename T, int blocks, bool kMasked>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(const SampleArgs a) {
   using L = Line<T>;
   constexpr int N = L::N;
@@ -361,12 +363,15 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
   row.c2 = fminf((greedy ? 1.f : 1.f / temp) * (2.f * kLog2e), 1e37f);  // (so that 1,024 bins of 40 exponents have a width)
 
   // ---- the block's logits in lines of 16 bytes as they lie in memory: line v holds the block's ids v N - pad .. + N - 1
-  int pad = 0, count_v = 0;
+  // (where few of them are admitted, `taken`: those alone, one after the other, and behind them their places in the block)
+  int pad = 0, count_v = 0, taken = -1;
   float top = -INFINITY;
   unsigned ids = 0;
+  auto places = [&]() { return reinterpret_cast<uint16_t*>(lines + (taken * (int)sizeof(T) + 15) / 16); };
+  auto id_at = [&](int i) { return lo + (taken >= 0 ? (int)places()[i] : i); };
   {
     const T* l = static_cast<const T*>(s.d_logits) + b * s.logit_stride + lo;
-    const uint32_t* mask = s.d_mask ? s.d_mask + b * s.mask_stride + (lo >> 5) : nullptr;
+    const uint32_t* mask = kMasked ? s.d_mask + b * s.mask_stride + (lo >> 5) : nullptr;
     pad = (int)((uintptr_t)l & 15) / (int)sizeof(T);
     count_v = n > 0 ? (pad + n + N - 1) / N : 0;
     const int inner = n - N;  // a whole line begins at an id of 0 .. inner
@@ -375,41 +380,63 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     uint32_t* const words = reinterpret_cast<uint32_t*>(sh.list);
     static_assert(kMaxIds / kMaxBlocks / 32 < 4 * kList);
     if (mask) {
-      for (int w = tid; w <= (n + 31) / 32; w += kThreads) words[w] = w < (n + 31) / 32 ? mask[w] : 0u;
+      const int whole = (n + 31) / 32;
+      for (int w = tid; w <= whole; w += kThreads)
+        words[w] = w < whole ? mask[w] & (32 * w + 32 > n ? (1u << (n - 32 * w)) - 1u : ~0u) : 0u;
       __syncthreads();
-    }
-    auto bits_of = [&](int v) {
-      const int i = v * N - pad;
-      if (i < 0 || i > inner) return 0u;
-      return mask ? __funnelshift_r(words[i >> 5], words[(i >> 5) + 1], i & 31) & ((1u << N) - 1u) : (1u << N) - 1u;
-    };
-#pragma unroll 4
-    for (int v = tid; v < count_v; v += kThreads)
-      asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\n@p cp.async.cg.shared.global [%0], [%1], 16;\n}" ::"r"(
-                       (uint32_t)__cvta_generic_to_shared(lines + v)),
-                   "l"(l + (v * N - pad)), "r"(bits_of(v))
-                   : "memory");
-    asm volatile("cp.async.wait_all;" ::: "memory");
-#pragma unroll 2
-    for (int v = tid; v < count_v; v += kThreads) {
-      const unsigned bits = bits_of(v);
-      const uint4 x = L::admit(lines[v], bits);
-      lines[v] = x;
-      top = fmaxf(top, L::top(x));
-      ids += __popc(bits);
-    }
-    // lines that are not whole: the first and the last, an id to a thread
-    __syncthreads();
-    if (tid < 2 * N && count_v > 0 && (tid < N || count_v > 1)) {
-      const int v = tid < N ? 0 : count_v - 1, i = v * N + tid % N - pad;
-      if (v * N - pad < 0 || v * N - pad > inner) {
-        T x = L::none();
-        if (i >= 0 && i < n && (!mask || words[i >> 5] >> (i & 31) & 1u)) {
-          x = kept_as(l[i]);
-          ++ids;
+      if (blocks > 1) {  // (a block alone is soon through: one row over 512 ids would take 0.5 us more)
+        const int per = (whole + kThreads - 1) / kThreads, w0 = min(whole, tid * per), w1 = min(whole, w0 + per);
+        unsigned mine = 0, all;
+        for (int w = w0; w < w1; ++w) mine += __popc(words[w]);
+        unsigned at = up_to(mine, sh.sums, all) - mine;
+        if (all <= kSparse && all * 8 <= (unsigned)n) {
+          taken = (int)all, pad = 0, count_v = (taken + N - 1) / N;
+          for (int w = w0; w < w1; ++w)
+            for (unsigned bits = words[w]; bits; bits &= bits - 1) places()[at++] = (uint16_t)(32 * w + __ffs(bits) - 1);
+          __syncthreads();
+          for (int i = tid; i < count_v * N; i += kThreads) {
+            T x = L::none();
+            if (i < taken) x = kept_as(l[places()[i]]), ++ids;
+            top = fmaxf(top, value(x));
+            reinterpret_cast<T*>(lines)[i] = x;
+          }
         }
-        reinterpret_cast<T*>(lines + v)[tid % N] = x;
-        top = fmaxf(top, value(x));
+      }
+    }
+    if (taken < 0) {
+      auto bits_of = [&](int v) {
+        const int i = v * N - pad;
+        if (i < 0 || i > inner) return 0u;
+        return mask ? __funnelshift_r(words[i >> 5], words[(i >> 5) + 1], i & 31) & ((1u << N) - 1u) : (1u << N) - 1u;
+      };
+#pragma unroll 4
+      for (int v = tid; v < count_v; v += kThreads)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\n@p cp.async.cg.shared.global [%0], [%1], 16;\n}" ::"r"(
+                         (uint32_t)__cvta_generic_to_shared(lines + v)),
+                     "l"(l + (v * N - pad)), "r"(bits_of(v))
+                     : "memory");
+      asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 2
+      for (int v = tid; v < count_v; v += kThreads) {
+        const unsigned bits = bits_of(v);
+        const uint4 x = L::admit(lines[v], bits);
+        lines[v] = x;
+        top = fmaxf(top, L::top(x));
+        ids += __popc(bits);
+      }
+      // lines that are not whole: the first and the last, an id to a thread
+      __syncthreads();
+      if (tid < 2 * N && count_v > 0 && (tid < N || count_v > 1)) {
+        const int v = tid < N ? 0 : count_v - 1, i = v * N + tid % N - pad;
+        if (v * N - pad < 0 || v * N - pad > inner) {
+          T x = L::none();
+          if (i >= 0 && i < n && (!mask || words[i >> 5] >> (i & 31) & 1u)) {
+            x = kept_as(l[i]);
+            ++ids;
+          }
+          reinterpret_cast<T*>(lines + v)[tid % N] = x;
+          top = fmaxf(top, value(x));
+        }
       }
     }
   }
@@ -524,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
         for (; some; some &= some - 1) {
           const int e = __ffs(some) - 1;
           const float x = value(reinterpret_cast<const T*>(lines + v)[e]);
-          const u64 o = order_of(x, lo + v * N + e - pad);
+          const u64 o = order_of(x, id_at(v * N + e - pad));
           if (*(volatile unsigned*)&sh.staged > room || !in(x, o)) continue;  // (too many already: no need to look further)
           const unsigned at = atomicAdd(&sh.staged, 1u);
           if (at < room) list[rank * room + at] = o;
@@ -686,7 +713,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       if (listed > kList) {
         u64 most = 0, least = 0;  // (least: as the largest complement)
         each(from, [&](float x, int i) {
-          const u64 o = order_of(x, lo + i);
+          const u64 o = order_of(x, id_at(i));
           if (in_bin(x)) most = max(most, o), least = max(least, ~o);
         });
         most = max_warp(most), least = max_warp(least);
@@ -704,7 +731,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
           for (int i = tid; i < kParts; i += kThreads) sh.parts.n[i] = sh.parts.lo[i] = sh.parts.hi[i] = 0;
           __syncthreads();
           each(from, [&](float x, int i) {
-            const u64 o = order_of(x, lo + i);
+            const u64 o = order_of(x, id_at(i));
             if (o < least || o > most) return;
             const int part = (int)((most - o) >> shift);
             atomicAdd(&sh.parts.n[part], 1u);
@@ -768,12 +795,12 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       if (listed <= kList) {  // what is kept is in the list: block 0 draws from it
         if (rank) return;
         cut_from(listed, by_k, by_p, 0, none);
-        Pick p = {INFINITY, INT_MAX, 0};
+        Pick p = {INFINITY, row.m, INT_MAX, 0};
         for (unsigned i = tid; i <= sh.at; i += kThreads) {
           const u64 o = sh.list[turn][i];
           const float x = logit_of(o), t = row.below(x) * row.c2, e = s.d_noise[b * s.noise_stride + id_of(o)];
           const float score = e * exp2_fast(t);
-          if (e >= FLT_MIN && t <= t_most) better(p, Pick{score, id_of(o), 0});
+          if (e >= FLT_MIN && t <= t_most) better(p, Pick{score, x, id_of(o), 0});
         }
         p = best_warp(p);
         if (lane == 0) sh.picks[warp] = p;
@@ -781,13 +808,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
         if (warp == 0) {
           p = best_warp(sh.picks[lane % kWarps]);
           const bool drawn = p.score < INFINITY;
-          if (!drawn) p.id = id_of(sh.list[turn][0]);
-          // (the drawn id's logit)
-          float x = row.m;
-          for (unsigned i = lane; drawn && i <= sh.at; i += 32)
-            if (id_of(sh.list[turn][i]) == p.id) x = logit_of(sh.list[turn][i]);
-          x = -max_warp(-x);
-          if (lane == 0) write(p.id, x);
+          if (lane == 0) write(drawn ? p.id : id_of(sh.list[turn][0]), drawn ? p.logit : row.m);
         }
         return;
       }
@@ -878,7 +899,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
   }
 
   // ---- the draw: the largest w / e is the smallest e 2^((m - l) c)
-  Pick p = {INFINITY, INT_MAX, INT_MAX};
+  Pick p = {INFINITY, row.m, INT_MAX, INT_MAX};
   {
     const float last = cut ? logit_of(cut) : -INFINITY;  // the last logit that is kept, and of those ids that have it the last
     const int last_id = cut ? id_of(cut) : INT_MAX;
@@ -901,10 +922,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
         if (some[y] && t == row.m) {
           const T* x = reinterpret_cast<const T*>(lines + v);
           for (int e = N - 1; e >= 0; --e)
-            if (value(x[e]) == row.m) p.first = min(p.first, lo + i + e);
+            if (value(x[e]) == row.m) p.first = min(p.first, id_at(i + e));
         }
         some[y] = some[y] && !first;
-        const bool whole = aligned && lo + i >= 0 && lo + i + N <= s.V;  // (nothing outside the row is read)
+        const bool whole = taken < 0 && aligned && lo + i >= 0 && lo + i + N <= s.V;  // (nothing outside the row is read)
 #pragma unroll
         for (int e = 0; e < N / 4; ++e) {
           uint4& o = q[y * (N / 4) + e];
@@ -913,7 +934,11 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
           if (some[y] && !whole) {
             float n4[4] = {INFINITY, INFINITY, INFINITY, INFINITY};
 #pragma unroll
-            for (int z = 0; z < 4; ++z) load_if(n4[z], noise + i + 4 * e + z, i + 4 * e + z >= 0 && i + 4 * e + z < n);
+            for (int z = 0; z < 4; ++z) {
+              const int k = i + 4 * e + z;
+              const bool in = k >= 0 && k < (taken >= 0 ? taken : n);
+              load_if(n4[z], noise + (in && taken >= 0 ? (int)places()[k] : k), in);
+            }
             o = make_uint4(__float_as_uint(n4[0]), __float_as_uint(n4[1]), __float_as_uint(n4[2]), __float_as_uint(n4[3]));
           }
         }
@@ -922,8 +947,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       for (int y = 0; y < kLines; ++y) {
         if (!some[y]) continue;
         // ids of the last logit kept, behind the last one: not kept
-        const int id0 = lo + (v0 + y * kThreads) * N - pad;
-        if (cut && id0 + N - 1 > last_id) {
+        const int i0 = (v0 + y * kThreads) * N - pad;
+        if (cut && (taken >= 0 || lo + i0 + N - 1 > last_id)) {
           bool tie = false;
 #pragma unroll
           for (int z = 0; z < N; z += 2) {
@@ -934,7 +959,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
 #pragma unroll
             for (int z = 0; z < N; ++z) {
               const Two x = L::pair(r[y], z / 2);
-              if ((z & 1 ? x.y : x.x) == last && id0 + z > last_id) {
+              if ((z & 1 ? x.y : x.x) == last && id_at(i0 + z) > last_id) {
                 uint4& o = q[y * (N / 4) + z / 4];
                 (z % 4 == 0 ? o.x : z % 4 == 1 ? o.y : z % 4 == 2 ? o.z : o.w) = 0u;
               }
@@ -952,7 +977,11 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
         }
       }
     }
-    if (p.score < INFINITY) p.id = lo + (best / 16 + best % 16 / N * kThreads) * N + best % N - pad;
+    if (p.score < INFINITY) {
+      const int i = (best / 16 + best % 16 / N * kThreads) * N + best % N;
+      p.id = id_at(i - pad);
+      p.logit = value(reinterpret_cast<const T*>(lines)[i]);
+    }
   }
   // the block's best of all threads
   p = best_warp(p);
@@ -964,19 +993,13 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       put(sh.pick[rank].score, p.score, 0);
       put(sh.pick[rank].id, p.id, 0);
       put(sh.pick[rank].first, p.first, 0);
-      // (its logit)
-      put(sh.low[rank], p.score < INFINITY ? value(reinterpret_cast<const T*>(lines)[p.id - lo + pad]) : row.m, 0);
+      put(sh.pick[rank].logit, p.logit, 0);
     }
   }
   sync();
   if (rank == 0 && warp == 0) {
     p = best_warp(sh.pick[lane % blocks]);
-    if (lane == 0) {
-      float x = row.m;
-      for (int r = 0; r < blocks; ++r)
-        if (p.score < INFINITY && sh.pick[r].id == p.id) x = sh.low[r];
-      write(p.score < INFINITY ? p.id : p.first, x);
-    }
+    if (lane == 0) write(p.score < INFINITY ? p.id : p.first, p.score < INFINITY ? p.logit : row.m);
   }
 }
 
@@ -1003,9 +1026,9 @@ extern "C" int grid_sample(const grid_sample_step* s, void* stream) {
   const bool sorted = s->B * blocks > 608 && s->B <= 2048 && (s->d_temperature || s->d_top_k || s->d_top_p || s->d_min_p);
   const SampleArgs a = {*s, ((s->V + blocks - 1) / blocks + 31) & ~31, sorted};
   const size_t smem = kSharedRoom + (size_t)a.each * size + 32;
-  static std::atomic<uint64_t> ready[2][4];  // the devices where a kernel has its room in shared memory
+  static std::atomic<uint64_t> ready[2][2][4];  // the devices where a kernel has its room in shared memory
   auto go = [&](auto kernel) {
-    std::atomic<uint64_t>& done = ready[size == 4][log];
+    std::atomic<uint64_t>& done = ready[size == 4][s->d_mask != nullptr][log];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess && !(dev < 64 && done.load() >> dev & 1)) {
@@ -1015,11 +1038,20 @@ extern "C" int grid_sample(const grid_sample_step* s, void* stream) {
     if (e != cudaSuccess) return e;
     return launch_cluster(kernel, dim3((unsigned)(s->B * blocks)), dim3(kThreads), smem, blocks, (cudaStream_t)stream, a);
   };
-  auto launch = [&](auto type) {
+  auto launch = [&](auto type, auto masked) {
     using T = decltype(type);
-    return blocks == 1 ? go(k_sample<T, 1>) : blocks == 2 ? go(k_sample<T, 2>) : blocks == 4 ? go(k_sample<T, 4>) : go(k_sample<T, 8>);
+    constexpr bool kMasked = decltype(masked)::value;
+    return blocks == 1   ? go(k_sample<T, 1, kMasked>)
+           : blocks == 2 ? go(k_sample<T, 2, kMasked>)
+           : blocks == 4 ? go(k_sample<T, 4, kMasked>)
+                         : go(k_sample<T, 8, kMasked>);
   };
-  GRID_CUDA(size == 4 ? launch(0.f) : launch((uint16_t)0));
+  const std::true_type yes;
+  const std::false_type no;
+  if (size == 4)
+    GRID_CUDA(s->d_mask ? launch(0.f, yes) : launch(0.f, no));
+  else
+    GRID_CUDA(s->d_mask ? launch((uint16_t)0, yes) : launch((uint16_t)0, no));
   GRID_CUDA(cudaGetLastError());
   return GRID_OK;
 }
