@@ -365,7 +365,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
   // ---- the block's logits in lines of 16 bytes as they lie in memory: line v holds the block's ids v N - pad .. + N - 1
   // (where few of them are admitted, `taken`: those alone, one after the other, and behind them their places in the block)
   int pad = 0, count_v = 0, taken = -1;
-  float top = -INFINITY;
+  float top = -INFINITY;  // the thread's largest logit, and the first of its lines that has it
+  int top_v = 0;
   unsigned ids = 0;
   auto places = [&]() { return reinterpret_cast<uint16_t*>(lines + (taken * (int)sizeof(T) + 15) / 16); };
   auto id_at = [&](int i) { return lo + (taken >= 0 ? (int)places()[i] : i); };
@@ -397,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
           for (int i = tid; i < count_v * N; i += kThreads) {
             T x = L::none();
             if (i < taken) x = kept_as(l[places()[i]]), ++ids;
-            top = fmaxf(top, value(x));
+            if (value(x) > top) top = value(x), top_v = i / N;
             reinterpret_cast<T*>(lines)[i] = x;
           }
         }
@@ -421,7 +422,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
         const unsigned bits = bits_of(v);
         const uint4 x = L::admit(lines[v], bits);
         lines[v] = x;
-        top = fmaxf(top, L::top(x));
+        const float t = L::top(x);
+        if (t > top) top = t, top_v = v;
         ids += __popc(bits);
       }
       // lines that are not whole: the first and the last, an id to a thread
@@ -435,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
             ++ids;
           }
           reinterpret_cast<T*>(lines + v)[tid % N] = x;
-          top = fmaxf(top, value(x));
+          if (value(x) > top || (v == 0 && value(x) == top)) top = value(x), top_v = v;
         }
       }
     }
@@ -903,28 +905,26 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
   {
     const float last = cut ? logit_of(cut) : -INFINITY;  // the last logit that is kept, and of those ids that have it the last
     const int last_id = cut ? id_of(cut) : INT_MAX;
-    float from = first ? row.m : last;
-    if (!first && min_p > 0.f && row.c2 > 0.f) from = fmaxf(from, row.least(-log2f(min_p) / row.c2));
+    float from = last;
+    if (min_p > 0.f && row.c2 > 0.f) from = fmaxf(from, row.least(-log2f(min_p) / row.c2));
     from = fmaxf(from, -FLT_MAX);
     const float* noise = s.d_noise + b * s.noise_stride + lo;
     const bool aligned = ((uintptr_t)(noise - pad) & 15) == 0;  // a line's noise is, too
     constexpr int kLines = 16 / N;  // sixteen ids of a thread at once
     int best = 0;  // place of the best id, first line's and its number of the sixteen
-    for (int v0 = tid; v0 < count_v; v0 += kLines * kThreads) {
+    if (top == row.m) {
+      const T* x = reinterpret_cast<const T*>(lines + top_v);
+      for (int e = N - 1; e >= 0; --e)
+        if (value(x[e]) == row.m) p.first = id_at(top_v * N + e - pad);
+    }
+    for (int v0 = tid; v0 < count_v && !first; v0 += kLines * kThreads) {
       uint4 r[kLines], q[4];
       bool some[kLines];
 #pragma unroll
       for (int y = 0; y < kLines; ++y) {
         const int v = v0 + y * kThreads, i = v * N - pad;
         r[y] = lines[min(v, count_v - 1)];
-        const float t = L::top(r[y]);
-        some[y] = v < count_v && t >= from;
-        if (some[y] && t == row.m) {
-          const T* x = reinterpret_cast<const T*>(lines + v);
-          for (int e = N - 1; e >= 0; --e)
-            if (value(x[e]) == row.m) p.first = min(p.first, id_at(i + e));
-        }
-        some[y] = some[y] && !first;
+        some[y] = v < count_v && L::top(r[y]) >= from;
         const bool whole = taken < 0 && aligned && lo + i >= 0 && lo + i + N <= s.V;  // (nothing outside the row is read)
 #pragma unroll
         for (int e = 0; e < N / 4; ++e) {
