@@ -336,6 +336,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       __syncthreads();
   };
   if (blocks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  if (tid == 0) sh.at = 0, sh.found = Found{0, 0u, 0ull};  // (inside the list and the bins, whatever is found)
   pdl_wait();
   int b = blockIdx.x / blocks;
   if (a.sorted) {  // the b-th in the order: rows cut by top-p or a large top-k, uncut ones, those of one id
@@ -746,7 +747,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
           sync();
           const Found all = sum_up(sh.parts.n, sh.parts.lo, sh.parts.hi, 0.f);
           // (the bins' weights are rounded otherwise: what they promise may be a little out of reach)
-          f = search(weights, weights ? min(target, f.weight + all.weight) : target, f);
+          // (of ids that all weigh less than half a unit any may be the last)
+          const bool some = weights && all.weight;
+          f = search(some, some ? min(target, f.weight + all.weight) : weights ? f.count + 1ull : target, f);
           most -= (u64)f.bin << shift;
           if (most - least >> shift) least = most - ((1ull << shift) - 1);
           const u64 z = most, a = least;

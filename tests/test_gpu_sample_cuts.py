@@ -1,0 +1,53 @@
+"""grid_sample where a cut ends exactly where a bound on it lies, and where masks
+differ from block to block."""
+import numpy as np
+import pytest
+
+from tests.test_gpu_sample import Case
+
+pytestmark = pytest.mark.gpu
+
+
+def as_type(x, dt):
+    import torch
+    return torch.from_numpy(x).bfloat16().float().numpy() if dt == "bf16" else x
+
+
+def test_a_tail_of_less_than_a_unit():
+    """A nucleus that, with the roundings of the sums, ends among hundreds of thousands of ids of less than 2^-41 each."""
+    V = 393_216
+    each = V // 8
+    c = Case(2, V, "f32", seed=1, greedy=0, cut="none")
+    tail, ulp = 2.0 ** -41.5, 2.0 ** -23
+    c.logits[:] = np.log(tail)
+    c.logits[:, each::each] = np.log(0.75 * ulp - (each - 1) * tail)  # each block after the first: three quarters of a unit of Z
+    c.logits[:, 0] = 0
+    c.bits[:] = True
+    c.bits[:, 1:each] = False
+    c.T[:] = 1
+    c.p = np.full(2, 1 - 2.0 ** -24, np.float32)
+    c.noise[:] = 1
+    c.check()
+    c = Case(2, V, "f32", seed=1, greedy=0, cut="none")
+    c.logits[:] = np.log(tail)
+    c.logits[:, 0] = 0
+    c.bits = None
+    c.T[:] = 1
+    c.p = np.full(2, 1 - 2.0 ** -24, np.float32)
+    c.check()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [20_000, 151_937])
+@pytest.mark.parametrize("cut", ["none", "k", "p", "min", "mixed"])
+def test_masks_of_some_blocks_sparse_and_some_dense(dt, V, cut):
+    """Blocks that take admitted ids one by one beside others that take whole lines, with few different logits (ties across every
+    cut) and with many."""
+    c = Case(16, V, dt, seed=V + 1, cut=cut)
+    each = ((V + 7) // 8 + 31) & ~31
+    share = c.g.choice([0.0, 0.004, 0.05, 0.12, 0.13, 0.5, 1.0], (16, 8))
+    c.bits = c.g.random((16, V)) < np.repeat(share, each, 1)[:, :V]
+    c.bits[3] = False
+    c.bits[3, c.g.integers(0, V, 5)] = True
+    c.logits[8:] = np.round(c.logits[8:] / 2) * 2 + np.float32(0)
+    c.check()
