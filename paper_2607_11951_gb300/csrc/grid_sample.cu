@@ -894,11 +894,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
         sync();
         all = sum_up(by_k || by_value ? sh.bins.n : nullptr, by_p && !by_value ? sh.bins.w : nullptr, nullptr, kUnit / scale);
         ready = true;
-        if (!by_k || !weights) kept = all.weight;
       }
       if (weights)
         cut = find(from, true, min(by_k ? target_of(kept) : target, all.weight), kept);
-      else if ((unsigned)top_k < all.count)
+      else  // (where `from` leaves no more than top_k ids, too: it is not asked of every id in the draw)
         cut = find(from, false, top_k, kept);
     }
   }

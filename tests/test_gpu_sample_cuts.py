@@ -13,6 +13,27 @@ def as_type(x, dt):
     return torch.from_numpy(x).bfloat16().float().numpy() if dt == "bf16" else x
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("top_p", [1.0, 0.9])
+@pytest.mark.parametrize("k,spread", [(100, False), (200, False), (300, True), (700, True), (2000, True)])
+def test_a_top_k_of_all_that_stand_out(dt, top_p, k, spread):
+    """top_k ids far above the others, each in a line of its own thread (of one of the row's blocks, or of all eight), and noise
+    under which any other id would be drawn if it were not cut."""
+    V = 32_000
+    c = Case(4, V, dt, seed=k, mask=False, greedy=0, cut="none")
+    lines, each = (8 if dt == "bf16" else 4), ((V + 7) // 8 + 31) & ~31
+    j = np.arange(k)
+    out = (j % 8) * each + lines * (j // 8) if spread else lines * j
+    c.logits[:] = as_type(c.g.uniform(-6, -4, (4, V)).astype(np.float32), dt)
+    c.logits[:, out] = as_type(c.g.uniform(9, 10, (4, k)).astype(np.float32), dt)
+    c.T[:] = 1
+    c.k, c.p = np.full(4, k, np.int32), np.full(4, top_p, np.float32)
+    rest = np.ones(V, bool)
+    rest[out] = False
+    c.noise[:, rest] = 1e-12
+    c.check()
+
+
 def test_a_tail_of_less_than_a_unit():
     """A nucleus that, with the roundings of the sums, ends among hundreds of thousands of ids of less than 2^-41 each."""
     V = 393_216
