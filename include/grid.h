@@ -695,7 +695,8 @@ int grid_tree_plan(const grid_tree* tree, int32_t* d_depth, uint32_t* d_sees, in
 /* grid_kv_append of a tree: token i of row b is stored at position d_len[b] + i
  * and turned by the angles of position d_len[b] + d_depth[...] (NULL: of its
  * own position).  A token whose depth is negative, or whose angles are outside
- * the table, is left out, and its row gets GRID_ST_PAGES. */
+ * the table, is left out, and its row gets GRID_ST_PAGES.  Without a rotation
+ * depths are not looked at. */
 int grid_kv_append_tree(const grid_kv* kv, const grid_kv_chunk* chunk, const grid_heads* k, const grid_heads* v,
                         const grid_heads* q, const grid_heads* q_out, const grid_rotation* rot, const grid_head_norm* norm,
                         const int32_t* d_depth, int32_t* d_status, void* stream);

@@ -575,7 +575,7 @@ def _binding():
 
 
 def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None, cos=None, sin=None, pairs=False,
-                   q_norm=None, k_norm=None, eps=1e-6, depth=None, stream=None):
+                   q_norm=None, k_norm=None, eps=1e-6, stream=None, depth=None):
     """Store a chunk's keys and values in the paged cache ``kv`` (a PagedKV).
     k, v [tokens, kv heads, D] (slices of a projection's output, say); table
     int32 [B, max_pages], lens int32 [B] (tokens cached before the chunk),
@@ -588,7 +588,7 @@ def grid_kv_append(kv, table, lens, k, v, status, start=None, q=None, q_out=None
         _check(rc)
 
 
-def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=None, sees=None, stream=None):
+def grid_kv_attend(kv, table, lens, q, out, status, lse=None, start=None, scale=None, stream=None, sees=None):
     """Attention of a chunk over the paged cache, after its append (table, lens
     and start as there): q, out [tokens, heads, D], lse float32 [tokens, heads];
     scale defaults to 1 / sqrt(D).  sees int32 [tokens, words]: the chunk is a tree,

@@ -33,3 +33,14 @@ def test_the_bound_calls_are_the_librarys():
     assert len(set(G._BOUND)) == len(G._BOUND)
     for name in G._BOUND:
         assert name in G.EXPORTED and ctypes.cast(getattr(G.lib(), name), ctypes.c_void_p).value
+
+
+def test_arguments_keep_their_places():
+    """What a caller gave by position before trees came means the same."""
+    import inspect
+
+    from paper_2607_11951_gb300 import grid as G
+    names = lambda f: list(inspect.signature(f).parameters)  # noqa: E731
+    assert names(G.grid_kv_append)[:17] == ["kv", "table", "lens", "k", "v", "status", "start", "q", "q_out", "cos", "sin", "pairs",
+                                            "q_norm", "k_norm", "eps", "stream", "depth"]
+    assert names(G.grid_kv_attend)[:11] == ["kv", "table", "lens", "q", "out", "status", "lse", "start", "scale", "stream", "sees"]
