@@ -17,13 +17,16 @@
 //   - The others go into 1,024 bins of equal width in m - l, with the number and
 //     the weight of each, and the bin is found in which the k-th id, or top_p of
 //     the weight, is reached.
-//   - That bin's ids are sorted (each counts how many come before it), and X is
-//     one of them.  A bin of more than a list holds, as equal logits make it, is
-//     cut into 512 parts of its range of order instead, and again: nine bits
-//     less each time, six times at most.
+//   - That bin's ids are sorted, and X is one of them.  A bin of more than a list
+//     holds, as equal logits make it, is cut into 512 parts of its range of order
+//     instead, and again: nine bits less each time, six times at most.
 // For a small top-k, or where few ids are admitted, all that is left after the
 // first step is sorted, and block 0 draws from the list.  min-p needs no X: its
 // bound on (m - l) c is asked of every id.
+//
+// A block whose mask admits few ids takes those alone, one after the other (one
+// such row over 151,936 ids: 8.2 us instead of 11.2); rows without masks have
+// kernels of their own, which look at no bits.
 //
 // Sums of weights are integers, so that the order of the atomic additions does not
 // matter: in a bin in steps of 2^-16 or less of its weights (what fits 32 bits if
@@ -32,9 +35,9 @@
 // Bound by steps that follow one another (a row takes 10 to 30 us, of which the
 // loads are 3 and each barrier of the cluster 0.7) and, where many rows share the
 // SMs, by the instructions for an id and the additions to bins: 32 fp32 rows over
-// 151,936 ids (20 MB) with settings of all kinds take 28.5 us in a graph, 256 bf16
-// rows (83 MB) 86, one row over 512 ids 4.7 (a call takes 7.5).  Without cuts 32
-// rows take 14.8, most of it for the noise (39 MB).
+// 151,936 ids (20 MB) with settings of all kinds take 27.8 us in a graph, 256 bf16
+// rows (83 MB) 79.5, one row over 512 ids 3.3 (no cut) to 6.7 (top-p).  Without
+// cuts 32 rows take 13.5, most of it for the noise (39 MB).
 #include <atomic>
 #include <cfloat>
 #include <climits>
@@ -52,7 +55,9 @@ constexpr int kMaxBlocks = 8;             // of a row: the largest cluster that 
 constexpr int kBins = 1024, kPer = kBins / kThreads;  // a thread sums up kPer neighbours
 constexpr int kParts = 512, kPartBits = 9;            // of a range of order
 constexpr int kList = 512;                // ids that are sorted at once
-constexpr int kDirect = 256;              // a top_k up to here is looked for without bins
+constexpr int kCounted = 128;             // ids that are sorted by counting (one row of 128: 5.8 us, 6.6 by the network; of 250 7.3, 7.2)
+constexpr unsigned kFew = 128;            // admitted ids that are sorted in any case (one row of 512, top_k 50: 5.0 us, sorted 7.5)
+constexpr int kDirect = 256;              // a top_k up to here is looked for without bins (250, 32 rows over 151,936 ids: 18.0 us, with bins 22.6)
 constexpr int kSparse = 2048;             // admitted ids of a block that are taken one by one, if an eighth of all at most
 constexpr int kIdBits = 22;
 constexpr int kMaxIds = 393216;           // 48 Ki fp32 logits for each of eight blocks
@@ -103,6 +108,7 @@ struct Shared {
     struct {
       unsigned n[kParts], lo[kParts], hi[kParts];  // the weights in 64 bits
     } parts;
+    u64 other[kList];                      // of a list that is sorted
   };
   u64 list[2][kList];                      // of one gathering and the next: a block's ids in a part of its own
   // what every block of the row writes here
@@ -573,33 +579,71 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       for (int r = 0; r < blocks; ++r) all += sh.in[turn][r], most = max(most, sh.in[turn][r]);
       return most > room ? kList + 1u : all;
     };
-    // The list in one piece and sorted: an id's place is the number of those before it.
+    // The list in one piece and sorted.  Up to kCounted ids: an id's place is the number of those before it.  More: by a network
+    // of comparisons, id i of 64 warp + 32 y + lane; partners 32 apart are in one thread, nearer ones in one warp, others meet in
+    // shared memory, in two places by turns (a step costs one barrier; nobody looks at bins now).
     auto sort = [&](unsigned listed) {
       u64* list = sh.list[turn];
-      u64 mine[kList / kThreads];
-      unsigned place[kList / kThreads] = {};
-#pragma unroll
-      for (int y = 0; y < kList / kThreads; ++y) {
-        unsigned i = tid + y * kThreads, r = 0;
+      auto listed_at = [&](unsigned i) {
+        unsigned r = 0;
+        const bool in = i < listed;
         while (r + 1 < (unsigned)blocks && i >= sh.in[turn][r]) i -= sh.in[turn][r++];
-        mine[y] = tid + y * kThreads < listed ? list[r * room + i] : 0;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int y = 0; y < kList / kThreads; ++y) list[tid + y * kThreads] = mine[y];
-      __syncthreads();
-#pragma unroll
-      for (int y = 0; y < kList / kThreads; ++y)
-        if (warp * 32 + y * kThreads < listed)
+        return in ? list[r * room + i] : 0ull;
+      };
+      if (listed <= kCounted) {
+        const u64 mine = tid < kCounted ? listed_at(tid) : 0;
+        __syncthreads();
+        if (tid < kCounted) list[tid] = mine;
+        __syncthreads();
+        unsigned place = 0;
+        if (warp * 32 < listed)
 #pragma unroll 4
           for (unsigned i = 0; i < listed; i += 2) {  // (zeros past the last)
             const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(list + i);
-            place[y] += (o.x > mine[y]) + (o.y > mine[y]);
+            place += (o.x > mine) + (o.y > mine);
           }
-      __syncthreads();
+        __syncthreads();
+        if (tid < listed) list[place] = mine;
+        __syncthreads();
+        return;
+      }
+      unsigned size = 64;
+      while (size < listed) size *= 2;
+      const unsigned i0 = 64 * warp + lane;
+      const bool in = 64 * warp < size;
+      u64 x[2] = {};
+      if (in) x[0] = listed_at(i0), x[1] = listed_at(i0 + 32);
+      bool apart = false;  // where the last values were put
+      for (unsigned k = 2; k <= size; k *= 2) {
+        for (unsigned j = k / 2; j >= 64; j /= 2) {
+          apart = !apart;
+          u64* at = apart ? sh.other : list;
+          if (in) at[i0] = x[0], at[i0 + 32] = x[1];
+          __syncthreads();
+          if (in) {
+            const bool most = ((i0 & k) == 0) == ((i0 & j) == 0);
 #pragma unroll
-      for (int y = 0; y < kList / kThreads; ++y)
-        if (tid + y * kThreads < listed) list[place[y]] = mine[y];
+            for (int y = 0; y < 2; ++y) {
+              const u64 o = at[(i0 ^ j) + 32 * y];
+              x[y] = (o > x[y]) == most ? o : x[y];
+            }
+          }
+        }
+        if (!in) continue;
+        if (k >= 64 && (x[0] > x[1]) != ((i0 & k) == 0)) {
+          const u64 o = x[0];
+          x[0] = x[1], x[1] = o;
+        }
+        for (unsigned j = min(k / 2, 16u); j; j /= 2)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const bool most = (((i0 + 32 * y) & k) == 0) == ((lane & j) == 0);
+            const u64 o = __shfl_xor_sync(~0u, x[y], j);
+            x[y] = (o > x[y]) == most ? o : x[y];
+          }
+      }
+      if (!apart) __syncthreads();
+      if (in) list[i0] = x[0], list[i0 + 32] = x[1];
       __syncthreads();
     };
     // The last id of the sorted list that a target needs, if so much comes before the list (the list's last where roundings
@@ -764,7 +808,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     // Ids at or above `from` are looked at.
     float from = -INFINITY;
     u64 target = 0;  // of top-p alone
-    const bool few = ids <= room;  // all of them are sorted
+    const bool few = ids <= min(room, kFew);  // all of them are sorted
     if (few) {
     } else if (by_k) {
       // the bin that the k-th largest of the threads' largest lies in
