@@ -40,7 +40,7 @@
 // over up to 2,000 (90 MB) 29 us, of which the start and the joins are some 10;
 // one token over 400 takes 9.9.  Bound by the products and the exponentials
 // between them where a chunk is long: a call for 2 x 2,000 tokens over 16,000
-// (605 GF) takes 454 us, 1,330 TFLOP/s (440 back to back in a graph, 1,370); 27
+// (605 GF) takes 439 us, 1,380 TFLOP/s (434 back to back in a graph); 27
 // prompts of up to 2,000 with 64-wide heads, an exponential for every 256
 // operations, 208 us.  The constants' figures below are of 32 + 8 heads of 128
 // (prompts: 14 + 2 of 64) in a graph.

@@ -19,10 +19,10 @@ namespace {
 // cluster of eight blocks, whose barriers order what they wrote to memory.
 // Counts are atomic additions and minima of integers: their order changes
 // nothing.  Bound by the chains of loads, and in one block by its instructions:
-// four rows and 56 pages 4.2 us (as a cluster 9.1), 256 rows of up to 32 of 3,148
-// pages 8.2 (10.9), 30 of up to 1,001 of 10,419 15.2 (20.7), 1,000 of up to 32 of
-// 12,276 19.3 (20.0); 256 of up to 126 of 11,279 would take 13.2 instead of 16.7
-// as a cluster; 256 of up to 1,001 of 87,348 (a cluster) take 34.
+// four rows and 56 pages 3.9 us (as a cluster 9.1), 256 rows of up to 32 of 3,148
+// pages 7.4 (10.9), 30 of up to 1,001 of 10,419 13.2 (20.7), 1,000 of up to 32 of
+// 12,276 17.3 (20.0), 256 of up to 126 of 11,279 14.6 (13.2); 256 of up to 1,001 of
+// 87,348 (a cluster) take 34.
 constexpr int kUpdateThreads = 1024, kUpdateBlocks = 8;
 constexpr int kAlonePages = 16384;
 constexpr int kNoRoom = -1;          // (a status between the steps: the new table's row is too short)

@@ -682,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     unsigned upto_n[kPer];
     u64 upto_w[kPer];
     // bf16 logits from `from` on that are positive and of no more values than there are bins have a bin for each value, the
-    // largest's first: only their numbers are counted (256 rows with top-p: 120 us instead of 125)
+    // largest's first: only their numbers are counted (256 rows with top-p were 120 us instead of 125)
     bool by_value = false;
     const int top_value = __float_as_int(row.m) >> 16;
     auto value_of = [&](int bin) { return __int_as_float((top_value - bin) << 16); };
@@ -1068,7 +1068,7 @@ extern "C" int grid_sample(const grid_sample_step* s, void* stream) {
   int blocks = 1, log = 0;
   while (blocks < kMaxBlocks && s->V > 2048 * blocks) blocks *= 2, ++log;
   // (where the rows are more than the SMs hold at once, and few enough to look at all: 256 rows over 151,937 bf16 logits,
-  // some greedy, 86 us instead of 96)
+  // some greedy, were 86 us instead of 96)
   const bool sorted = s->B * blocks > 608 && s->B <= 2048 && (s->d_temperature || s->d_top_k || s->d_top_p || s->d_min_p);
   const SampleArgs a = {*s, ((s->V + blocks - 1) / blocks + 31) & ~31, sorted};
   const size_t smem = kSharedRoom + (size_t)a.each * size + 32;
