@@ -941,8 +941,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
       }
       if (weights)
         cut = find(from, true, min(by_k ? target_of(kept) : target, all.weight), kept);
-      else  // (where `from` leaves no more than top_k ids, too: it is not asked of every id in the draw)
+      else if ((unsigned)top_k <= all.count)  // (of exactly so many, too: `from` is not asked of every id in the draw)
         cut = find(from, false, top_k, kept);
+      else  // (admitted ids of -inf are counted, but not there)
+        kept = all.weight;
     }
   }
 

@@ -72,3 +72,19 @@ def test_masks_of_some_blocks_sparse_and_some_dense(dt, V, cut):
     c.bits[3, c.g.integers(0, V, 5)] = True
     c.logits[8:] = np.round(c.logits[8:] / 2) * 2 + np.float32(0)
     c.check()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("top_p", [1.0, 0.9])
+@pytest.mark.parametrize("V", [700, 20_000])
+def test_a_top_k_of_more_ids_than_have_a_logit(dt, top_p, V):
+    """More ids admitted than top_k, and fewer of them above -inf: all of those are kept; around that number, the k-th is the last."""
+    c = Case(8, V, dt, seed=V, mask=True, greedy=0, cut="none")
+    c.bits[:] = c.g.random((8, V)) < 0.97
+    c.logits[:, c.g.permutation(V)[:V // 3]] = -np.inf
+    c.logits[:, c.g.permutation(V)[:9]] = np.nan
+    have = (c.bits & (c.logits > -np.inf)).sum(1)
+    c.k = (have + np.array([-2, -1, 0, 1, 2, 60, 100, 150])).astype(np.int32)
+    assert (c.k > 256).all() and (c.k < c.bits.sum(1)).all()
+    c.p = np.full(8, top_p, np.float32)
+    c.check()
