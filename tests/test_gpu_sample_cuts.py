@@ -88,3 +88,49 @@ def test_a_top_k_of_more_ids_than_have_a_logit(dt, top_p, V):
     assert (c.k > 256).all() and (c.k < c.bits.sum(1)).all()
     c.p = np.full(8, top_p, np.float32)
     c.check()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [300, 2048, 2049, 8200, 32_000])
+def test_rows_of_many_shapes(dt, V):
+    """Plateaus, outliers, steps, crowds and next to nothing, at random places or side by side; top_k around the sizes of what
+    stands out, noise under which what is cut would be drawn."""
+    for seed in range(4):
+        c = Case(20, V, dt, seed=V + seed, cut="mixed", greedy=0.05, mask=seed % 2 == 0)
+        each = ((V + 7) // 8 + 31) & ~31
+        for b, l in enumerate(c.logits):
+            g = np.random.default_rng([seed, V, b])
+            m = int(min(V, g.choice([1, 3, 20, 60, 100, 128, 129, 256, 300, 512, 513, 700, 1000, 2000, V])))
+            out = g.permutation(V)[:m] if b % 2 else np.arange(m) * (max(1, V // m) if b % 4 else 1)
+            kind = b % 7
+            if kind == 0:
+                l[:] = g.uniform(-6, -4, V)
+                l[out] = g.uniform(9, 10, m)
+            elif kind == 1:
+                l[:] = -3
+                l[out] = g.choice([2.0, 2.5, 7.0], m)
+            elif kind == 2:
+                l[:] = np.round(l)
+            elif kind == 3:
+                l[:] *= 1e-3
+                l[out] += 1
+            elif kind == 4:
+                l[:] = -np.abs(l) - g.choice([0, 100, 1e4])
+            elif kind == 5:
+                l[:] = g.choice([1e-38, 1e-30, -1e-38, 0.0], V)
+                l[out] = g.choice([0.0, 1e-36, 1.0])
+            if g.random() < 0.3:
+                l[g.integers(0, V, V // 3)] = -np.inf
+            if g.random() < 0.1:
+                l[g.integers(0, V, 3)] = np.nan
+            c.k[b] = g.choice([0, 0, m - 1, m, m + 1, 2 * m, 50, 256, 257, 300])
+            c.p[b] = g.choice([1, 1, 0.9, 0.99, 0.5, 0.999999, 0.3])
+            c.min_p[b] = g.choice([0, 0, 0, 0.1, 1e-4, 0.9])
+            c.T[b] = g.choice([1, 1, 0.7, 1.5, 0.1, 10])
+            if c.bits is not None and g.random() < 0.6:
+                c.bits[b] = g.random(V) < np.repeat(g.choice([0, 0.003, 0.05, 0.12, 0.13, 1], 8), each)[:V]
+            if g.random() < 0.5:
+                order = np.argsort(-np.where(np.isnan(l), -np.inf, l), kind="stable")
+                c.noise[b, order[min(V - 1, max(0, int(c.k[b]))):]] = 1e-20
+        c.logits = as_type(c.logits, dt)
+        c.check()
