@@ -271,6 +271,15 @@ struct HideTree {
   }
 };
 
+// Whether token t of a tree's row sees no key at all: nothing is cached, and no bit up to its own is set.  Asked where a sum of
+// weights is zero, as infinite queries can make it too (which get NaN).
+__device__ __noinline__ bool sees_none(const uint32_t* words, int t, int len) {
+  if (len > 0) return false;
+  for (int w = 0; w < t >> 5; ++w)
+    if (words[w]) return false;
+  return !(words[t >> 5] & ((2u << (t & 31)) - 1u));
+}
+
 // One tile of a row's softmax from nothing: the maximum, base(maximum), then
 // the probabilities, from the last keys to the first: they lie (64-wide heads
 // apart) over the second half of the scores, which is read before.  Returns their
@@ -997,8 +1006,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++n_o[z];
         }
       if (!ok) break;
-      // A sum of zero: the row sees no key, and gets zeros.  A sum below zero: some key that the rows may read is in no page of
-      // the cache (known once all tiles were), and they get zeros.  A sum that is no number, of a query that is none, gives NaN.
+      // A sum below zero: the row sees no key, or some key that the rows may read is in no page of the cache (known once all
+      // tiles were): zeros.  A sum that is no number, of a query that is none, or that is zero (all scores are -inf) gives NaN.
+      if (kTree && whole && l == 0.f && sees_none(g.sees + (long long)(w.a + t) * g.words, t, w.len)) l = -1.f;
       if (sh.bad[0][k % kRing] | sh.bad[1][k % kRing]) l = -1.f;
       if (warp_live) {
         tm_after();
@@ -1021,7 +1031,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int e = 0; e < 16; ++e) y[e] = __uint_as_float(o[e]) * f0;
           }
           if (live && whole) {
-            const uint4 none = {}, a = l <= 0.f ? none : pack8<T>(y), b = l <= 0.f ? none : pack8<T>(y + 8);
+            const uint4 none = {}, a = l < 0.f ? none : pack8<T>(y), b = l < 0.f ? none : pack8<T>(y + 8);
             if (g.sectors) {
               asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + j), "r"(a.x), "r"(a.y), "r"(a.z),
                            "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
@@ -1039,7 +1049,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (live && (p.wide || s == 0)) {
           if (whole) {
-            if (g.lse) g.lse[(long long)(w.a + t) * g.H + head] = l <= 0.f ? -INFINITY : (m - kLift<T> + log2f(l)) * kLn2;
+            if (g.lse) g.lse[(long long)(w.a + t) * g.H + head] = l < 0.f ? -INFINITY : (m - kLift<T> + log2f(l)) * kLn2;
           } else {
             __stcg(g.part_ml + (size_t)slot * 256 + part_row, make_float2(m, l));
           }
@@ -1110,7 +1120,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                   }
                 }
               }
-              bad |= z == 0.f;
+              if (kTree && z == 0.f) bad |= sees_none(g.sees + (long long)(w.a + tok) * g.words, tok, w.len);
               const float by = __frcp_rn(z);
 #pragma unroll
               for (int e = 0; e < kN; ++e) acc[e] = bad ? 0.f : acc[e] * by;
