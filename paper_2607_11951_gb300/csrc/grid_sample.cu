@@ -939,8 +939,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
         all = sum_up(by_k || by_value ? sh.bins.n : nullptr, by_p && !by_value ? sh.bins.w : nullptr, nullptr, kUnit / scale);
         ready = true;
       }
+      // (of the two cuts the one that keeps fewer: the bins' weights are rounded otherwise than those that `kept` was summed
+      // from, so that top-p's share of them can end behind the k-th id)
       if (weights)
-        cut = find(from, true, min(by_k ? target_of(kept) : target, all.weight), kept);
+        cut = max(cut, find(from, true, min(by_k ? target_of(kept) : target, all.weight), kept));
       else if ((unsigned)top_k <= all.count)  // (of exactly so many, too: `from` is not asked of every id in the draw)
         cut = find(from, false, top_k, kept);
       else  // (admitted ids of -inf are counted, but not there)
