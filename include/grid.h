@@ -797,7 +797,8 @@ typedef struct grid_pages_step {
   int32_t A, width, B, width_out;
   int32_t* d_table_out;    /* out: B rows of width_out pages, table_out_stride apart,  */
   int64_t table_out_stride; /* -1 past a row's own; not the old table                  */
-  int32_t* d_held_out;     /* out [B]: d_want where the pages are there; not d_held     */
+  int32_t* d_held_out;     /* out [B]: d_want where the pages are there; may be d_want  */
+                           /* or d_keep, no other output may be an input                */
   int32_t* d_copies;       /* out [3][B]: from page, to page (-1: none), tokens        */
   int32_t* d_refs;         /* out [n_pages]                                            */
   int32_t* d_status;       /* out [B]                                                  */

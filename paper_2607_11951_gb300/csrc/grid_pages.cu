@@ -25,7 +25,6 @@ namespace {
 // 87,348 (a cluster) take 34.
 constexpr int kUpdateThreads = 1024, kUpdateBlocks = 8;
 constexpr int kAlonePages = 16384;
-constexpr int kNoRoom = -1;          // (a status between the steps: the new table's row is too short)
 
 struct UpdateArgs {
   grid_pages_step s;
@@ -87,7 +86,8 @@ __global__ void __launch_bounds__(kUpdateThreads) k_update(const UpdateArgs u) {
   const int tid = threadIdx.x, lane = tid & 31, rank = cluster_rank();
   const int threads = blocks * kUpdateThreads, at = rank * kUpdateThreads + tid;
   const int warps = threads / 32, warp = at / 32;
-  // (between the steps: the page in part that has to be copied, the fresh pages before the row's, and d_held_out what it keeps)
+  // (between the steps: the page in part that has to be copied, the fresh pages before the row's; d_status is what the row keeps,
+  // or ~ that where it is not valid or its row of the new table too short; d_held_out may be d_want and is written last)
   int32_t *from = s.d_copies, *to = from + s.B, *tokens = to + s.B;
   auto sync = [&]() {
     __syncwarp();
@@ -132,10 +132,9 @@ __global__ void __launch_bounds__(kUpdateThreads) k_update(const UpdateArgs u) {
     last = __reduce_max_sync(~0u, last);
     if (lane == 0) {
       const bool room = pages_for(u, want) <= s.width_out;
-      s.d_held_out[b] = keep;
       from[b] = last;
       to[b] = ok && room ? pages_for(u, want) - full : 0;
-      s.d_status[b] = ok && room ? GRID_ST_OK : ok ? kNoRoom : GRID_ST_PAGES;
+      s.d_status[b] = ok && room ? keep : ~keep;
     }
   }
   sync();
@@ -191,10 +190,10 @@ __global__ void __launch_bounds__(kUpdateThreads) k_update(const UpdateArgs u) {
   sync();
   // ---- a warp per row: its fresh pages
   for (int b = warp; b < s.B; b += warps) {
-    const int state = s.d_status[b], keep = s.d_held_out[b], want = s.d_want[b];
+    const int state = s.d_status[b], keep = state >= 0 ? state : ~state, want = s.d_want[b];
     const int copied = __ldcg(from + b), first = __ldcg(to + b), need = __ldcg(tokens + b);
     const int full = keep >> u.log_page, part = keep & ((1 << u.log_page) - 1);
-    const bool fits = state == GRID_ST_OK && (need == 0 || first + need <= all);
+    const bool fits = state >= 0 && (need == 0 || first + need <= all);
     int32_t* out = s.d_table_out + b * s.table_out_stride;
     const int begin = full + (part && copied < 0);
     __syncwarp();
