@@ -804,8 +804,8 @@ typedef struct grid_pages_step {
   int32_t* d_status;       /* out [B]                                                  */
 } grid_pages_step;
 
-/* Scratch for updates over a pool of n_pages pages of page_size tokens (a power
- * of two in 8 .. 1024).  Allocates device memory and synchronizes.  Free with
+/* Scratch for updates over a pool of n_pages pages (2^30 at most) of page_size
+ * tokens (a power of two in 8 .. 1024).  Allocates device memory and synchronizes.  Free with
  * grid_pages_free. */
 int grid_pages_create(int32_t n_pages, int32_t page_size, grid_pages** out);
 void grid_pages_free(grid_pages* p);

@@ -25,6 +25,7 @@ namespace {
 // 87,348 (a cluster) take 34.
 constexpr int kUpdateThreads = 1024, kUpdateBlocks = 8;
 constexpr int kAlonePages = 16384;
+constexpr int kMostPages = 1 << 30;  // (so that an index past the last page by a stride is still one)
 
 struct UpdateArgs {
   grid_pages_step s;
@@ -366,8 +367,10 @@ __global__ void __launch_bounds__(kUpdateThreads) k_update_alone(const UpdateArg
 // head's) is cut into chunks of kAhead pieces a thread, which are loaded at once;
 // the chunks of a copy and pool go to `splits` blocks in turn.  128 copies of some
 // 32 tokens (8 heads of 128, 29 MB moved) take 6.5 us, 4.5 TB/s (256 threads 7.2;
-// two or eight pieces a thread 6.6 to 7.2); three of a few tokens 1.5.
+// two or eight pieces a thread 6.6 to 7.2); three of a few tokens 1.5.  Pieces
+// are counted in 32 bits, up to kMostPieces (16 GB) of a page.
 constexpr int kCopyThreads = 128, kAhead = 4, kChunk = kCopyThreads * kAhead;
+constexpr int64_t kMostPieces = 1 << 30;
 
 struct CopyArgs {
   uint4* pool[2];
@@ -503,6 +506,7 @@ struct grid_pages {
 extern "C" int grid_pages_create(int32_t n_pages, int32_t page_size, grid_pages** out) {
   if (!out || n_pages <= 0 || page_size < 8 || page_size > 1024 || (page_size & (page_size - 1)))
     return set_error(GRID_E_INVALID_ARG, "grid_pages_create: n_pages is positive, page_size a power of two in 8 .. 1024");
+  if (n_pages > kMostPages) return set_error(GRID_E_TOO_LARGE, "grid_pages_create: more than 2^30 pages");
   grid_pages* g = new (std::nothrow) grid_pages;
   if (!g) return set_error(GRID_E_TOO_LARGE, "grid_pages_create: out of host memory");
   g->n_pages = n_pages;
@@ -546,6 +550,8 @@ extern "C" int grid_pages_update(const grid_pages* g, const grid_pages_step* s, 
 extern "C" int grid_kv_copy(const grid_kv* kv, const int32_t* d_copies, int32_t n, int32_t* d_status, void* stream) {
   if (!kv || !d_copies || !d_status || n <= 0) return set_error(GRID_E_INVALID_ARG, "grid_kv_copy: bad arguments");
   if (n > 65535) return set_error(GRID_E_TOO_LARGE, "grid_kv_copy: more than 65535 copies");
+  if ((int64_t)kv->p.n_kv_heads * kv->p.page_size * kv->p.head_dim / 8 > kMostPieces)
+    return set_error(GRID_E_TOO_LARGE, "grid_kv_copy: pages of more than 16 GB of keys");
   CopyArgs c = {};
   set_pools(kv, c);
   c.copies = d_copies, c.status = d_status, c.n = n;
@@ -565,6 +571,8 @@ extern "C" int grid_kv_compact(const grid_kv* kv, const grid_kv_chunk* chunk, co
   if (!kv || !d_path || !d_count || !d_status || max_path <= 0 || !make_chunk(kv, chunk, a.c))
     return set_error(GRID_E_INVALID_ARG, "grid_kv_compact: bad arguments");
   if (chunk->B > 65535) return set_error(GRID_E_TOO_LARGE, "grid_kv_compact: more than 65535 rows");
+  if ((int64_t)2 * kv->p.n_kv_heads * kv->p.head_dim / 8 > kMostPieces)
+    return set_error(GRID_E_TOO_LARGE, "grid_kv_compact: too many heads");
   set_pools(kv, a);
   a.path = d_path, a.count = d_count, a.status = d_status, a.most = max_path;
   a.blocks = ((2 * a.Hk << a.log_parts) + kCompactThreads - 1) / kCompactThreads;
