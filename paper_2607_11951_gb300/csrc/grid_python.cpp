@@ -56,21 +56,26 @@ struct Look {
     if (!t.is_cuda() || t.get_device() != device) return no("a tensor on the current device (the handle's) expected"), nullptr;
     return &t;
   }
-  // n values in one piece; None gives NULL where `some` is false
-  void* dense(PyObject* o, at::ScalarType type, int64_t n, bool some = true) {
+  // A tensor [n], or [n, m] where m is given, in one piece; None gives NULL where `some` is false
+  void* dense(PyObject* o, at::ScalarType type, int64_t n, int64_t m, bool some) {
     if (!ok || (o == Py_None && !some)) return nullptr;
     const at::Tensor* t = tensor(o);
     if (!t) return nullptr;
     if (t->scalar_type() != type) return no(type == at::kInt ? "an int32 tensor expected" : "a tensor of another type expected");
-    if (t->numel() != n || !t->is_contiguous()) {
-      if (ok) PyErr_Format(PyExc_AssertionError, "a contiguous tensor of %lld values expected", (long long)n);
+    if (t->dim() != (m < 0 ? 1 : 2) || t->size(0) != n || (m >= 0 && t->size(1) != m) || !t->is_contiguous()) {
+      if (m < 0)
+        PyErr_Format(PyExc_AssertionError, "a contiguous tensor [%lld] expected", (long long)n);
+      else
+        PyErr_Format(PyExc_AssertionError, "a contiguous tensor [%lld, %lld] expected", (long long)n, (long long)m);
       ok = false;
       return nullptr;
     }
     return t->data_ptr();
   }
-  int32_t* ints(PyObject* o, int64_t n, bool some = true) { return (int32_t*)dense(o, at::kInt, n, some); }
-  float* floats(PyObject* o, int64_t n, bool some = true) { return (float*)dense(o, at::kFloat, n, some); }
+  int32_t* ints(PyObject* o, int64_t n, bool some = true) { return (int32_t*)dense(o, at::kInt, n, -1, some); }
+  float* floats(PyObject* o, int64_t n, bool some = true) { return (float*)dense(o, at::kFloat, n, -1, some); }
+  int32_t* ints2(PyObject* o, int64_t n, int64_t m) { return (int32_t*)dense(o, at::kInt, n, m, true); }
+  float* floats2(PyObject* o, int64_t n, int64_t m, bool some = true) { return (float*)dense(o, at::kFloat, n, m, some); }
   // Rows of n contiguous values; their distance
   void* rows(PyObject* o, at::ScalarType type, int64_t B, int64_t n, int64_t* stride) {
     const at::Tensor* t = tensor(o);
@@ -178,8 +183,7 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t count) {
   if (turned != (a[10] != Py_None)) l.no("cos and sin go together");
   if (turned) {
     const int64_t n = l.size(a[9], 0, 2), half = l.ok ? l.size(a[9], 1, 2) : 0;
-    if (l.ok && (l.size(a[10], 0, 2) != n || l.size(a[10], 1, 2) != half)) l.no("cos and sin of one shape expected");
-    rot.d_cos = l.floats(a[9], n * half), rot.d_sin = l.floats(a[10], n * half);
+    rot.d_cos = l.floats2(a[9], n, half), rot.d_sin = l.floats2(a[10], n, half);
     l.int32(n), l.int32(2 * half);
     rot.n_pos = (int)n, rot.rot = (int)(2 * half);
     const int pairs = PyObject_IsTrue(a[11]);
@@ -189,7 +193,7 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t count) {
   grid_head_norm norm = {};
   if (normed) {
     const at::ScalarType type = c->f16 ? at::kHalf : at::kBFloat16;
-    norm.d_q = l.dense(a[12], type, c->D, false), norm.d_k = l.dense(a[13], type, c->D, false);
+    norm.d_q = l.dense(a[12], type, c->D, -1, false), norm.d_k = l.dense(a[13], type, c->D, -1, false);
     norm.eps = l.number(a[14]);
   }
   const int32_t* depth = l.ints(a[15], N, false);
@@ -210,15 +214,15 @@ PyObject* kv_attend(PyObject*, PyObject* const* a, Py_ssize_t count) {
   if (!c) return nullptr;
   const int64_t N = l.size(a[3], 0, 3);
   const grid_kv_chunk chunk = l.chunk(a[1], a[2], a[7], N);
-  grid_kv_query query = {l.heads(a[3], c, N, c->heads), l.heads(a[4], c, N, c->heads), l.floats(a[6], N * c->heads, false),
+  grid_kv_query query = {l.heads(a[3], c, N, c->heads), l.heads(a[4], c, N, c->heads), l.floats2(a[6], N, c->heads, false),
                          l.number(a[8]), 0};
   int32_t* status = l.ints(a[5], chunk.B);
   const uint32_t* sees = nullptr;
   int64_t words = 0;
   if (a[9] != Py_None) {
     words = l.size(a[9], 1, 2);
-    if (l.ok && (words <= 0 || l.size(a[9], 0, 2) != N)) l.no("sees [tokens, words] expected");
-    sees = (const uint32_t*)l.ints(a[9], N * words);
+    if (words <= 0) l.no("sees [tokens, words] expected");
+    sees = (const uint32_t*)l.ints2(a[9], N, words);
     l.int32(words);
   }
   void* stream = l.stream(a[10]);
@@ -235,8 +239,7 @@ PyObject* kv_compact(PyObject*, PyObject* const* a, Py_ssize_t count) {
   if (!c) return nullptr;
   const grid_kv_chunk chunk = l.chunk(a[1], a[2], a[7], l.whole(a[6]));
   const int64_t most = l.size(a[3], 1, 2);
-  if (l.ok && l.size(a[3], 0, 2) != chunk.B) l.no("path [B, most] expected");
-  const int32_t *path = l.ints(a[3], chunk.B * most), *taken = l.ints(a[4], chunk.B);
+  const int32_t *path = l.ints2(a[3], chunk.B, most), *taken = l.ints(a[4], chunk.B);
   int32_t* status = l.ints(a[5], chunk.B);
   l.int32(most);
   void* stream = l.stream(a[8]);
@@ -251,8 +254,7 @@ PyObject* kv_copy(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const Cache* c = l.cache(a[0]);
   if (!c) return nullptr;
   const int64_t n = l.size(a[2], 0, 1);
-  if (l.ok && (l.size(a[1], 0, 2) != 3 || l.size(a[1], 1, 2) != n)) l.no("copies [3, n] and status [n] expected");
-  const int32_t* copies = l.ints(a[1], 3 * n);
+  const int32_t* copies = l.ints2(a[1], 3, n);
   int32_t* status = l.ints(a[2], n);
   l.int32(n);
   void* stream = l.stream(a[3]);
@@ -268,8 +270,7 @@ PyObject* tree_plan(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const int64_t B = l.size(a[3], 0, 1);
   const grid_tree tree = l.tree(a[0], a[4], B);
   const int64_t words = l.size(a[2], 1, 2);
-  if (l.ok && l.size(a[2], 0, 2) != tree.n_tokens) l.no("sees [tokens, words] expected");
-  int32_t *depth = l.ints(a[1], tree.n_tokens), *sees = l.ints(a[2], tree.n_tokens * words), *status = l.ints(a[3], B);
+  int32_t *depth = l.ints(a[1], tree.n_tokens), *sees = l.ints2(a[2], tree.n_tokens, words), *status = l.ints(a[3], B);
   l.int32(words);
   void* stream = l.stream(a[5]);
   if (!l.ok) return nullptr;
@@ -284,9 +285,8 @@ PyObject* tree_accept(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const int64_t B = l.size(a[6], 0, 1);
   const grid_tree tree = l.tree(a[0], a[7], B);
   const int64_t most = l.size(a[3], 1, 2);
-  if (l.ok && (l.size(a[3], 0, 2) != B || l.size(a[5], 0, 2) != B || l.size(a[5], 1, 2) != most)) l.no("path and out [B, most] expected");
   const int32_t *tokens = l.ints(a[1], tree.n_tokens), *sampled = l.ints(a[2], tree.n_tokens);
-  int32_t *path = l.ints(a[3], B * most), *taken = l.ints(a[4], B), *out = l.ints(a[5], B * most), *status = l.ints(a[6], B);
+  int32_t *path = l.ints2(a[3], B, most), *taken = l.ints(a[4], B), *out = l.ints2(a[5], B, most), *status = l.ints(a[6], B);
   const int eos = l.whole(a[8]);
   l.int32(most);
   void* stream = l.stream(a[9]);
@@ -334,8 +334,7 @@ PyObject* pages_update(PyObject*, PyObject* const* a, Py_ssize_t count) {
   s.d_table_out = (int32_t*)l.rows(a[6], at::kInt, B, width_out, &by_out);
   s.table_stride = A > 1 ? by : width, s.table_out_stride = B > 1 ? by_out : width_out;
   s.d_held = l.ints(a[4], A), s.d_want = l.ints(a[5], B), s.d_held_out = l.ints(a[7], B);
-  if (l.ok && (l.size(a[8], 0, 2) != 3 || l.size(a[8], 1, 2) != B)) l.no("copies [3, B] expected");
-  s.d_copies = l.ints(a[8], 3 * B), s.d_refs = l.ints(a[9], n_pages), s.d_status = l.ints(a[10], B);
+  s.d_copies = l.ints2(a[8], 3, B), s.d_refs = l.ints(a[9], n_pages), s.d_status = l.ints(a[10], B);
   s.d_parent = l.ints(a[11], B, false), s.d_keep = l.ints(a[12], B, false), s.d_pinned = l.ints(a[13], n_pages, false);
   if (l.ok && (s.d_table == s.d_table_out || s.d_held == s.d_held_out)) l.no("the new table and lengths need tensors of their own");
   l.int32(A), l.int32(B), l.int32(width), l.int32(width_out);
