@@ -161,7 +161,21 @@ struct Look {
   }
 };
 
-PyObject* end(const Look& l, int code) { return l.ok ? PyLong_FromLong(code) : nullptr; }
+// The call itself.  Other threads may run meanwhile (the caller's arguments keep the tensors): a launch waits where the
+// stream's queue is full, for a function of the host's that is written in Python, say.
+template <typename F>
+PyObject* go(F call) {
+  struct Others {
+    PyThreadState* mine = PyEval_SaveThread();
+    ~Others() { PyEval_RestoreThread(mine); }
+  };
+  int code;
+  {
+    Others run;
+    code = call();
+  }
+  return PyLong_FromLong(code);
+}
 #define NEEDS(n) \
   if (count != (n)) return PyErr_SetString(PyExc_TypeError, "wrong number of arguments"), nullptr
 
@@ -202,8 +216,11 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const grid_heads *qh = some_q ? &q : nullptr, *oh = some_q ? &out : nullptr;
   const grid_rotation* r = turned ? &rot : nullptr;
   const grid_head_norm* w = normed ? &norm : nullptr;
-  return end(l, a[15] == Py_None ? lib.kv_append(c->kv, &chunk, &k, &v, qh, oh, r, w, status, stream)
-                                 : lib.kv_append_tree(c->kv, &chunk, &k, &v, qh, oh, r, w, depth, status, stream));
+  const bool tree = a[15] != Py_None;
+  return go([&] {
+    return tree ? lib.kv_append_tree(c->kv, &chunk, &k, &v, qh, oh, r, w, depth, status, stream)
+                : lib.kv_append(c->kv, &chunk, &k, &v, qh, oh, r, w, status, stream);
+  });
 }
 
 // kv table lens q out status lse start scale sees stream
@@ -227,8 +244,11 @@ PyObject* kv_attend(PyObject*, PyObject* const* a, Py_ssize_t count) {
   }
   void* stream = l.stream(a[10]);
   if (!l.ok) return nullptr;
-  return end(l, a[9] == Py_None ? lib.kv_attend(c->kv, &chunk, &query, status, stream)
-                                : lib.kv_attend_tree(c->kv, &chunk, &query, sees, (int)words, status, stream));
+  const bool tree = a[9] != Py_None;
+  return go([&] {
+    return tree ? lib.kv_attend_tree(c->kv, &chunk, &query, sees, (int)words, status, stream)
+                : lib.kv_attend(c->kv, &chunk, &query, status, stream);
+  });
 }
 
 // kv table lens path count status n_tokens start stream
@@ -244,7 +264,7 @@ PyObject* kv_compact(PyObject*, PyObject* const* a, Py_ssize_t count) {
   l.int32(most);
   void* stream = l.stream(a[8]);
   if (!l.ok) return nullptr;
-  return end(l, lib.kv_compact(c->kv, &chunk, path, taken, (int)most, status, stream));
+  return go([&] { return lib.kv_compact(c->kv, &chunk, path, taken, (int)most, status, stream); });
 }
 
 // kv copies status stream
@@ -259,7 +279,7 @@ PyObject* kv_copy(PyObject*, PyObject* const* a, Py_ssize_t count) {
   l.int32(n);
   void* stream = l.stream(a[3]);
   if (!l.ok) return nullptr;
-  return end(l, lib.kv_copy(c->kv, copies, (int)n, status, stream));
+  return go([&] { return lib.kv_copy(c->kv, copies, (int)n, status, stream); });
 }
 
 // parent depth sees status start stream
@@ -274,7 +294,7 @@ PyObject* tree_plan(PyObject*, PyObject* const* a, Py_ssize_t count) {
   l.int32(words);
   void* stream = l.stream(a[5]);
   if (!l.ok) return nullptr;
-  return end(l, lib.tree_plan(&tree, depth, (uint32_t*)sees, (int)words, status, stream));
+  return go([&] { return lib.tree_plan(&tree, depth, (uint32_t*)sees, (int)words, status, stream); });
 }
 
 // parent tokens sampled path count out status start eos stream
@@ -291,7 +311,7 @@ PyObject* tree_accept(PyObject*, PyObject* const* a, Py_ssize_t count) {
   l.int32(most);
   void* stream = l.stream(a[9]);
   if (!l.ok) return nullptr;
-  return end(l, lib.tree_accept(&tree, tokens, sampled, eos, (int)most, path, taken, out, status, stream));
+  return go([&] { return lib.tree_accept(&tree, tokens, sampled, eos, (int)most, path, taken, out, status, stream); });
 }
 
 // logits noise tokens status mask temperature top_k top_p min_p logprob eos stream
@@ -315,7 +335,7 @@ PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t count) {
   s.d_tokens = l.ints(a[2], B), s.d_logprob = l.floats(a[9], B, false), s.d_status = l.ints(a[3], B);
   void* stream = l.stream(a[11]);
   if (!l.ok) return nullptr;
-  return end(l, lib.sample(&s, stream));
+  return go([&] { return lib.sample(&s, stream); });
 }
 
 // handle device n_pages table held want table_out held_out copies refs status parent keep pinned stream
@@ -341,7 +361,7 @@ PyObject* pages_update(PyObject*, PyObject* const* a, Py_ssize_t count) {
   s.A = (int)A, s.B = (int)B, s.width = (int)width, s.width_out = (int)width_out;
   void* stream = l.stream(a[14]);
   if (!l.ok) return nullptr;
-  return end(l, lib.pages_update(p, &s, stream));
+  return go([&] { return lib.pages_update(p, &s, stream); });
 }
 
 // The entry points' addresses, in the order of Library.
