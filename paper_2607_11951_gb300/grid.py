@@ -564,7 +564,8 @@ def _binding():
 
         import torch  # noqa: F401  (its libraries, before the module that is linked to them)
         if not os.path.exists(binding_path()):
-            raise GridLibraryMissing("grid_binding.so not built at %s: run __graft_entry__.build()" % binding_path())
+            raise GridLibraryMissing("grid_binding.so not built at %s: run __graft_entry__.build(), which says why if it cannot be" %
+                                     binding_path())
         L = lib()
         spec = importlib.util.spec_from_file_location("grid_binding", binding_path())
         module = importlib.util.module_from_spec(spec)
