@@ -743,9 +743,12 @@ int grid_kv_compact(const grid_kv* kv, const grid_kv_chunk* chunk, const int32_t
  * T's count as not given.
  *
  * NaN logits count as -inf, +inf as the largest finite value of the type; noise
- * below 2^-126 or not a number leaves its id out of the draw (where nothing is
- * left: the first id).  A row without ids gets token -1, logprob 0 and GRID_ST_EMPTY_MASK; a
- * drawn `eos` gives GRID_ST_COMPLETE. */
+ * below 2^-126 or not a number leaves its id out of the draw, and so does a p, or
+ * p / e, of less than 2^-127 of the largest p (where nothing is left: the first
+ * id).  Sums are held to 2^-16 of a nucleus' weight: an id so near the border of
+ * top_p may fall either way (never past top_k).  A row without ids gets token -1,
+ * logprob 0 and GRID_ST_EMPTY_MASK; a drawn `eos` gives GRID_ST_COMPLETE.  Outputs
+ * must not overlap the inputs. */
 typedef struct grid_sample_step {
   const void* d_logits;       /* dtype (F32 or BF16); B rows of V, logit_stride apart  */
   int64_t logit_stride;

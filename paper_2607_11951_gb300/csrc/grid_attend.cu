@@ -8,7 +8,7 @@
 //
 // A chunk that is a tree of tokens (grid_kv_attend_tree) hides scores by the bits of
 // what each token sees instead of by position, in the tiles that hold tokens of the
-// chunk; all else is the same, and so are the times within 1%.
+// chunk; all else is the same, and so are the times within 2%.
 //
 // Work.  The query rows of a row b and key head h are its tokens times the
 // H / Hk heads that read h (row = token * group + head), so that a key tile is

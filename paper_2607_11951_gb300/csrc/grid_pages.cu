@@ -18,11 +18,13 @@ namespace {
 // block, a thread per row, the pages' counts in its shared memory; more are a
 // cluster of eight blocks, whose barriers order what they wrote to memory.
 // Counts are atomic additions and minima of integers: their order changes
-// nothing.  Bound by the chains of loads, and in one block by its instructions:
-// four rows and 56 pages 3.9 us (as a cluster 9.1), 256 rows of up to 32 of 3,148
-// pages 7.4 (10.9), 30 of up to 1,001 of 10,419 13.2 (20.7), 1,000 of up to 32 of
-// 12,276 17.3 (20.0), 256 of up to 126 of 11,279 14.6 (13.2); 256 of up to 1,001 of
-// 87,348 (a cluster) take 34.
+// nothing.  Bound by the chains of loads, in one block by its instructions, and in
+// the cluster by an atomic addition in L2 for each entry of the table, issued by
+// eight SMs: four rows and 56 pages 3.9 us (as a cluster 9.1), 256 rows of up to 32
+// of 3,148 pages 7.4 (10.9), 30 of up to 1,001 of 10,419 13.2 (20.7), 1,000 of up to
+// 32 of 12,276 18.0 (20.0), 256 of up to 126 of 11,279 14.6 (13.2: the table's
+// entries count as well, but the rule goes by what one block has room for); 256 of
+// up to 1,001 of 87,348 (a cluster) take 34 to 48, by how the pages lie.
 constexpr int kUpdateThreads = 1024, kUpdateBlocks = 8;
 constexpr int kAlonePages = 16384;
 constexpr int kMostPages = 1 << 30;  // (so that an index past the last page by a stride is still one)

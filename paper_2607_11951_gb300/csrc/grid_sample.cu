@@ -32,12 +32,17 @@
 // matter: in a bin in steps of 2^-16 or less of its weights (what fits 32 bits if
 // all of a block's ids are in it), elsewhere of 2^-40 of the largest.
 //
-// Bound by steps that follow one another (a row takes 10 to 30 us, of which the
-// loads are 3 and each barrier of the cluster 0.7) and, where many rows share the
-// SMs, by the instructions for an id and the additions to bins: 32 fp32 rows over
-// 151,936 ids (20 MB) with settings of all kinds take 27.8 us in a graph, 256 bf16
-// rows (83 MB) 79.5, one row over 512 ids 3.3 (no cut) to 6.7 (top-p).  Without
-// cuts 32 rows take 13.5, most of it for the noise (39 MB).
+// The end of a nucleus that is found by bins may be off by what rounding a share
+// to 1 / scale gives, 2.3e-6 of the weight before it at 151,936 ids and 6e-6 at
+// 393,216 (the same for all ids of one logit), and by the exponents' roundings.
+// top-k's count is exact, whatever top-p asks for beside it.
+//
+// Bound by steps that follow one another (a row over 151,936 ids takes 9 to 21 us
+// alone, of which the loads are 3 and each barrier of the cluster 0.7) and, where
+// many rows share the SMs, by the instructions for an id and the additions to bins.
+// In a graph: 32 fp32 rows over 151,936 ids (20 MB) with settings of all kinds take
+// 28 us, 256 bf16 rows (83 MB) 72 to 77, one row over 512 ids 3.0 (no cut) to 6.6
+// (top-p).  Without cuts 32 rows take 11.6, most of it for the noise (39 MB).
 #include <atomic>
 #include <cfloat>
 #include <climits>
@@ -864,7 +869,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) k_sample(con
     }
     row.reach(from > -INFINITY ? row.below(from) : INFINITY);
     // A weight is held as its share of the one in its bin's middle, 2^(f width) for an id f bins before it, f in -1/2 .. 1/2: a
-    // square in f is within 2^-21 of it (width is 0.08 at most).  So many units make a share of one.
+    // square in f is within 2^-21 of it (width is 40 / 1,024 at most).  So many units make a share of one.
     const float scale = truncf(fminf(4.1e9f / a.each, 8e6f)), tilt = 0.6931471805599453f * row.width;
     auto share = [&](float f) {  // (as a whole number)
       return Row::low(fmaf(f, fmaf(f, 0.5f * tilt * tilt * scale, tilt * scale), scale + kWhole));
@@ -1071,8 +1076,9 @@ extern "C" int grid_sample(const grid_sample_step* s, void* stream) {
   // (blocks by the vocabulary alone: a row's sums do not depend on the batch)
   int blocks = 1, log = 0;
   while (blocks < kMaxBlocks && s->V > 2048 * blocks) blocks *= 2, ++log;
-  // (where the rows are more than the SMs hold at once, and few enough to look at all: 256 rows over 151,937 bf16 logits,
-  // some greedy, were 86 us instead of 96)
+  // (where four blocks to an SM, as many as of the bf16 kernel fit, do not take all rows at once, and the rows are few enough to
+  // look at all: 256 rows over 151,937 bf16 logits, some greedy, were 86 us instead of 96.  Of the fp32 kernel two fit: 39 to 76
+  // rows over so many ids are more than one wave, too, and keep their own order; 64 with top-p take 53 us)
   const bool sorted = s->B * blocks > 608 && s->B <= 2048 && (s->d_temperature || s->d_top_k || s->d_top_p || s->d_min_p);
   const SampleArgs a = {*s, ((s->V + blocks - 1) / blocks + 31) & ~31, sorted};
   const size_t smem = kSharedRoom + (size_t)a.each * size + 32;

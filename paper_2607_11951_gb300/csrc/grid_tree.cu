@@ -21,7 +21,10 @@ __device__ __forceinline__ bool tree_span(const grid_tree& t, int b, int& a, int
 // the tree in shared memory; the words of a token repeat the walk, so that none
 // waits for another, and stop where the ancestors (in falling order) are below
 // their bits.  Time is the chain of loads: the row's span, its parents, the walk
-// (32 trees of up to 64 tokens: 1.7 us; one of eight 1.3).
+// (32 trees of up to 64 tokens: 1.7 us; one of eight 1.3).  The walks of deep trees
+// are long, and there is one for each word of each token: a chain of 64 tokens
+// takes 3.2 us, of 128 10.5, of 256 62, of 512 446, of 1,024 3,446 (random trees of
+// these sizes 1.6, 2.8, 8.6, 26 and 98).
 __global__ void __launch_bounds__(kPlanThreads) k_plan(const grid_tree tree, int32_t* __restrict__ depth,
                                                        uint32_t* __restrict__ sees, int words, int32_t* __restrict__ status) {
   __shared__ int16_t up[kMaxWords * 32];
